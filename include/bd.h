@@ -47,8 +47,10 @@ typedef enum {
     BD_ERR_NONFINITE = 6,   /* Inf/NaN met by a quantizer (from bd_poll_status)           */
     BD_ERR_TIMEOUT = 7,     /* a bounded device-side wait expired (from bd_poll_status)   */
     BD_ERR_WORKSPACE = 8,   /* workspace missing or too small                             */
-    BD_ERR_SCRATCH_LIMIT = 9 /* bd_linear_noalloc: the problem needs more scratch than the
+    BD_ERR_SCRATCH_LIMIT = 9, /* bd_linear_noalloc: the problem needs more scratch than the
                                 library's built-in buffer holds                             */
+    BD_ERR_INDEX = 10       /* a page, slot, position or row range met on the device lies
+                               outside its bounds (from bd_poll_status)                    */
 } bd_status;
 
 typedef enum { BD_F32 = 0, BD_BF16 = 1, BD_F16 = 2 } bd_dtype;
@@ -313,6 +315,91 @@ bd_status bd_attention(const bd_qtensor *Q, const bd_qtensor *K, const bd_qtenso
                        float scale, void *O, bd_dtype odtype, int64_t ldo, int64_t stride_o,
                        const bd_attention_dump *dump, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Paged KV cache: the same storage rule (keys in 4 bits per token, values in 4-bit chunks of 32 tokens,
+ * the newest values in high precision; appendix "Quantization Dimension", Fig. 9b) for many sequences
+ * that share one pool of pages, as a server keeps them.  All index arrays live on the device, so a step's
+ * calls can be captured into a CUDA graph and replayed while lengths and pages change.
+ *
+ * pool  [pages][kv_heads][page_tokens / 32] records of 35 * head_dim bytes; a record holds 32 tokens of one
+ *       KV head.  head_dim is 64 or 128, page_tokens a multiple of 32.  Parts of a record, in order: key
+ *       codes and value codes (16 * head_dim bytes each), key scales and value scales (head_dim each), key
+ *       ids and value ids (head_dim / 2 each).  Keys are nb = head_dim / 32 tiles of 32 rows (tokens) x 32
+ *       dimensions, values nb tiles of 32 rows (channels) x 32 tokens.  With r = 8 j + g the row and b the
+ *       tile: the 32-bit word t (elements 8 t .. 8 t + 7) is number ((8 b + g) * 4 + t) * 4 + j of the codes,
+ *       the scale byte (e + 127) number (4 g + j) * nb + b of the scales, the id nibble the same number of the
+ *       ids (low nibble first).  Token 8 x + 2 y + z of the chunk is row 8 y + 2 x + z of a key tile; channel
+ *       c is row c % 32 of value tile c / 32.  Elements 0 .. 7 of a word sit in its nibbles 0, 2, 1, 3, 4, 6,
+ *       5, 7 as sign << 3 | index.  No initialisation is needed: what was never written is never used.
+ * tail  [slots][kv_heads][64][head_dim] elements of `dtype`: the values of a sequence's unfinished chunk, and
+ *       of the chunk before it, in the source type; token k is row k % 64.  Keeping both means that a step of
+ *       at most 32 tokens can be repeated, and that up to 32 tokens can be taken back (rejected drafts) by
+ *       calling with the smaller kv_len from then on.
+ *
+ * A step's batch: sequence i has kv_len[i] tokens in the cache, this step's included; its rows of the step are
+ * q_start[i] .. q_start[i + 1] - 1 of the row tensors and belong to its last tokens.  `rows` is the height of
+ * those tensors: rows behind q_start[n] are neither read nor written (padded batches).  max_q and max_kv are host
+ * bounds of the longest sequence's rows and tokens; they size the launches.  Token k of sequence i is in page
+ * page_table[i * ld_table + k / page_tokens]; sequences may share pages that none of them writes.  slot[i] is the
+ * sequence's entry in `tail`.  A sequence may have no row (nothing is done for it).
+ * Errors met on the device (BD_ERR_INDEX from bd_poll_status): a sequence whose numbers contradict the bounds
+ * or whose slot is outside [0, slots) where it is needed is skipped (attention: rows may be left unwritten, and a
+ * chunk without its tail counts as zeros); a page number outside [0, pages) leaves out its tokens: append does not
+ * store them, read gives zeros, attention does not see them. */
+typedef struct {
+    void *pool, *tail;
+    bd_dtype dtype;         /* type of the rows handed in, and of the tail */
+    int64_t pages, slots, kv_heads, page_tokens, head_dim;
+} bd_paged_cache;
+typedef struct {
+    const int32_t *page_table; /* [n][ld_table] */
+    const int32_t *slot;       /* [n]           */
+    const int32_t *kv_len;     /* [n]           */
+    const int32_t *q_start;    /* [n + 1]       */
+    int64_t ld_table, n, rows, max_q, max_kv;
+} bd_paged_batch;
+/* Buffer sizes in bytes. */
+bd_status bd_paged_sizes(const bd_paged_cache *c, size_t *pool_bytes, size_t *tail_bytes);
+/* Stores the step's keys and values: row r, head h at K + r * ldk + h * head_stride_k elements (pointers and strides
+ * 16-byte aligned), V alike.  Keys are quantised at once; values when their chunk is full, then once and for all.
+ * The calls that touch one sequence (its pages, its slot) have to be ordered; a batch names a sequence once. */
+bd_status bd_paged_append(const bd_paged_cache *c, const bd_paged_batch *b, const void *K, const void *V, int64_t ldk,
+                          int64_t head_stride_k, int64_t ldv, int64_t head_stride_v, void *stream);
+/* The values the cache stands for, of each sequence's last tokens (as many as it has rows in the batch), as elements
+ * of the cache's type: exact for fp32 and bf16; fp16 rounds what lies below its normal range. */
+bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *K, void *V, int64_t ldk, int64_t head_stride_k,
+                        int64_t ldv, int64_t head_stride_v, void *stream);
+/* Causal attention of the step's queries over the cache, the step's own tokens included (append them first):
+ *     o_i = sum_j p_ij v_j,   p_i = softmax over the visible j of  s_ij,
+ *     s_ij = scale * q_i . k_j,  or  softcap * tanh(scale * q_i . k_j / softcap)  for softcap > 0,
+ * where the query of token t sees tokens t - window + 1 .. t (window 0: all up to t).  Query head h reads KV head
+ * h / (q_heads / kv_heads).  Q has the cache's type, BD_BF16 or BD_F16 (fp32 caches: BD_ERR_UNSUPPORTED); O is BD_F32 or
+ * that type.  Unlike bd_kvcache_attention, which follows the paper's scope "all", queries and probabilities stay
+ * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  lse (optional, fp32 [rows][q_heads]) receives
+ * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result does not
+ * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.
+ * Accuracy: products exact, fp32 sums; probabilities rounded to 11 bits (8 bits for bf16 in the long-chunk kernel). */
+bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes);
+bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, const void *Q, int64_t q_heads, int64_t ldq,
+                             int64_t head_stride_q, float scale, float softcap, int64_t window, void *O, bd_dtype odtype,
+                             int64_t ldo, int64_t head_stride_o, float *lse, void *workspace, size_t workspace_bytes,
+                             void *stream);
+/* Queries and keys of a step before they are stored and used: per row and head y = x / sqrt(mean(x^2) + eps) * w
+ * (w of the rows' type, [head_dim]; NULL: no normalisation of that operand), then the first `rot` elements are rotated:
+ * pairs (a, b) = (y[i], y[i + rot / 2]), or (y[2 i], y[2 i + 1]) with `interleaved`, become
+ * (a cos - b sin, b cos + a sin) with cos = cos_sin[position * rot + i], sin = cos_sin[position * rot + rot / 2 + i]
+ * (fp32 [positions][rot]).  fp32 arithmetic, one rounding.  head_dim 64 or 128, rot a multiple of 16, at most
+ * head_dim.  Row r, head h of an operand at X + r * ld + h * head_stride elements; outputs may be the inputs.  A row whose
+ * position lies outside [0, positions) is left unwritten (BD_ERR_INDEX from bd_poll_status).  k_heads 0: queries alone. */
+typedef struct {
+    const void *x;
+    void *y;
+    const void *weight;
+    int64_t heads, ldx, head_stride_x, ldy, head_stride_y;
+} bd_rope_operand;
+bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd_dtype dtype, int64_t rows, int64_t head_dim,
+                          const int32_t *position, const float *cos_sin, int64_t positions, int64_t rot, int interleaved,
+                          float eps, void *stream);
+
 /* bd_linear for callers that can neither allocate device memory nor hand in a
  * workspace (the paper has no counterpart; this is a convenience of the library).
  * Think of code that runs where cudaMalloc is off limits: inside a region whose
@@ -369,7 +456,7 @@ bd_status bd_get_formatbook(uint8_t out[16][8]);
 bd_status bd_set_formatbook(const uint8_t in[16][8]);
 
 /* Synchronises `stream`, then returns and clears the device status word:
- * BD_OK, BD_ERR_NONFINITE or BD_ERR_TIMEOUT (or BD_ERR_CUDA). */
+ * BD_OK, BD_ERR_TIMEOUT, BD_ERR_INDEX or BD_ERR_NONFINITE (the first of them that applies; or BD_ERR_CUDA). */
 bd_status bd_poll_status(void *stream);
 
 /* Test hook for the bounded device-side waits (every wait on a barrier inside the kernels gives up

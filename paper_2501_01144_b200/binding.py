@@ -40,6 +40,21 @@ class _CKVCache(ctypes.Structure):
                 ("capacity", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("length", ctypes.c_int64)]
 
 
+class _CPagedCache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("tail", ctypes.c_void_p), ("dtype", ctypes.c_int), ("pages", ctypes.c_int64),
+                ("slots", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+
+
+class _CPagedBatch(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("n", ctypes.c_int64), ("rows", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64)]
+
+
+class _CRopeOperand(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("heads", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("head_stride_x", ctypes.c_int64), ("ldy", ctypes.c_int64), ("head_stride_y", ctypes.c_int64)]
+
+
 def library_path():
     return _LIB_PATH
 
@@ -93,6 +108,13 @@ def load():
     lib.bd_kvcache_pv_batched.argtypes = [kp, i64, vp, i64, i64, i64, vp, ci, i64, i64, vp, sz, vp]
     lib.bd_attention_workspace_size.argtypes = [i64, i64, i64, i64, szp]
     lib.bd_attention.argtypes = [qp, qp, qp, i64, i64, ctypes.c_float, vp, ci, i64, i64, ctypes.POINTER(_CAttentionDump), vp, sz, vp]
+    cp, bp, rp, cf = ctypes.POINTER(_CPagedCache), ctypes.POINTER(_CPagedBatch), ctypes.POINTER(_CRopeOperand), ctypes.c_float
+    lib.bd_paged_sizes.argtypes = [cp, szp, szp]
+    lib.bd_paged_append.argtypes = [cp, bp, vp, vp, i64, i64, i64, i64, vp]
+    lib.bd_paged_read.argtypes = [cp, bp, vp, vp, i64, i64, i64, i64, vp]
+    lib.bd_paged_attention_workspace_size.argtypes = [cp, bp, i64, szp]
+    lib.bd_paged_attention.argtypes = [cp, bp, vp, i64, i64, i64, cf, cf, i64, vp, ci, i64, i64, vp, vp, sz, vp]
+    lib.bd_qk_norm_rope.argtypes = [rp, rp, ci, i64, i64, vp, vp, i64, i64, ci, cf, vp]
     lib.bd_qtensor_sizes_bs.argtypes = [i64, i64, ci, szp, szp, szp]
     lib.bd_quantize_bs.argtypes = [vp, ci, i64, i64, i64, ci, ci, qp, vp]
     lib.bd_export_canonical_bs.argtypes = [qp, ci, vp, vp, vp, vp]
@@ -536,6 +558,185 @@ def kvcache_attention(caches, Qs, scale, out=None, dtype=torch.float32, probs=No
     _check(load().bd_kvcache_attention(arr, n, cq, ctypes.c_float(scale), ctypes.c_void_p(out.data_ptr()), _ydtype(out.dtype), out.stride(1),
                                        out.stride(0), pp, ldp, sp, ctypes.c_void_p(c0._ws.data_ptr()), c0._ws.numel(), _stream(stream)))
     return out
+
+
+def _here(t, what):
+    """The library launches on the current device: a tensor of another one is refused."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} must be on the current CUDA device")
+
+
+def _heads3(x, what, heads, head_dim, dtype):
+    """Pointer, row stride and head stride of [rows, heads, head_dim] with a contiguous last axis."""
+    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.dtype != dtype or (x.stride(2) != 1 and x.numel()):
+        raise ValueError(f"{what} must be [rows, {heads}, {head_dim}] of {dtype} with a contiguous last axis")
+    _here(x, what)
+    ld, hs = x.stride(0), x.stride(1)
+    if x.shape[0] <= 1:                                               # strides of axes of one element mean nothing
+        ld = max(heads * head_dim, ld)
+    return x.data_ptr(), ld, hs if heads > 1 else head_dim
+
+
+class PagedKVCache:
+    """Paged DialectFP4 KV cache shared by many sequences (storage: bd.h).  `pool` uint8 [pages, kv_heads,
+    page_tokens / 32, 35 * head_dim], `tail` [slots, kv_heads, 64, head_dim] of `dtype`.  The caller hands out pages
+    and slots; nothing has to be initialised."""
+
+    def __init__(self, pages, kv_heads, head_dim, slots, page_tokens=64, dtype=torch.bfloat16, device="cuda"):
+        if head_dim not in (64, 128) or page_tokens <= 0 or page_tokens % 32:
+            raise ValueError("head_dim must be 64 or 128, page_tokens a multiple of 32")
+        self._set(torch.empty(pages, kv_heads, page_tokens // 32, 35 * head_dim, dtype=torch.uint8, device=device),
+                  torch.empty(slots, kv_heads, 64, head_dim, dtype=dtype, device=device), page_tokens)
+
+    @classmethod
+    def from_buffers(cls, pool, tail, page_tokens):
+        """A cache over the caller's own buffers (contiguous, shapes as above)."""
+        self = cls.__new__(cls)
+        self._set(pool, tail, page_tokens)
+        return self
+
+    def _set(self, pool, tail, page_tokens):
+        if tail.dim() != 4 or tail.dtype not in _TORCH_DTYPE or tail.shape[2] != 64 or not tail.is_contiguous():
+            raise ValueError("tail must be contiguous [slots, kv_heads, 64, head_dim] of fp32/bf16/fp16")
+        slots, kv_heads, _, d = tail.shape
+        if pool.dtype != torch.uint8 or pool.dim() != 4 or tuple(pool.shape[1:]) != (kv_heads, page_tokens // 32, 35 * d) or not pool.is_contiguous():
+            raise ValueError("pool must be contiguous uint8 [pages, kv_heads, page_tokens / 32, 35 * head_dim]")
+        _here(pool, "pool")
+        _here(tail, "tail")
+        self.pool, self.tail, self.page_tokens = pool, tail, page_tokens
+        self.pages, self.slots, self.kv_heads, self.head_dim, self.dtype = pool.shape[0], slots, kv_heads, d, tail.dtype
+        self._c = _CPagedCache(pool.data_ptr(), tail.data_ptr(), _TORCH_DTYPE[tail.dtype], pool.shape[0], slots, kv_heads, page_tokens, d)
+
+
+class PagedBatch:
+    """One step's sequences (int32 CUDA tensors): page_table [n, width], slots [n], kv_len [n] (this step's tokens
+    included), q_start [n + 1].  max_q: host bound of the rows of one sequence; max_kv: of its tokens (default: what
+    the page table can hold)."""
+
+    def __init__(self, page_table, slots, kv_len, q_start, max_q, max_kv=None):
+        n = kv_len.shape[0]
+        for x in (page_table, slots, kv_len, q_start):
+            if x.dtype != torch.int32 or not x.is_cuda or x.stride(-1) != 1:
+                raise ValueError("the batch's index tensors must be int32 CUDA tensors with a contiguous last axis")
+        if page_table.dim() != 2 or page_table.shape[0] != n or slots.shape != (n,) or kv_len.dim() != 1 or q_start.shape != (n + 1,):
+            raise ValueError("page_table [n, width], slots [n], kv_len [n], q_start [n + 1]")
+        _here(kv_len, "the batch")
+        if len({x.device for x in (page_table, slots, kv_len, q_start)}) > 1:
+            raise ValueError("the batch's tensors must be on one device")
+        self.page_table, self.slots, self.kv_len, self.q_start, self.n = page_table, slots, kv_len, q_start, n
+        self.max_q, self.max_kv, self.width = max_q, max_kv, page_table.shape[1]
+        self._c = _CPagedBatch(page_table.data_ptr(), slots.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(),
+                               max(page_table.stride(0), page_table.shape[1]) if n > 1 else page_table.shape[1], n, 0, 0, 0)
+
+    def _c_for(self, cache, rows):
+        c = self._c
+        held = self.width * cache.page_tokens
+        if self.max_kv is not None and self.max_kv > held:
+            raise ValueError("max_kv exceeds what the page table can hold")
+        c.rows, c.max_q, c.max_kv = rows, min(self.max_q, rows), held if self.max_kv is None else self.max_kv
+        return c
+
+
+def paged_append(cache, batch, k, v, stream=None):
+    """Store the step's keys and values [rows, kv_heads, head_dim] of the cache's type."""
+    kp, ldk, hk = _heads3(k, "keys", cache.kv_heads, cache.head_dim, cache.dtype)
+    vp_, ldv, hv = _heads3(v, "values", cache.kv_heads, cache.head_dim, cache.dtype)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("keys and values must have the same number of rows")
+    if k.shape[0]:
+        cb = batch._c_for(cache, k.shape[0])
+        _check(load().bd_paged_append(ctypes.byref(cache._c), ctypes.byref(cb), kp, vp_, ldk, hk, ldv, hv, _stream(stream)))
+
+
+def paged_read(cache, batch, rows=None, out_k=None, out_v=None, stream=None):
+    """The values the cache stands for of each sequence's last tokens: (keys, values) [rows, kv_heads, head_dim] of the
+    cache's type, laid out by the batch's q_start.  rows: the height of the result when no buffers are given."""
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    if (out_k is None or out_v is None) and rows is None:
+        raise ValueError("give the number of rows or both buffers")
+    out_k = torch.empty(shape, dtype=cache.dtype, device=cache.pool.device) if out_k is None else out_k
+    out_v = torch.empty(shape, dtype=cache.dtype, device=cache.pool.device) if out_v is None else out_v
+    kp, ldk, hk = _heads3(out_k, "out_k", cache.kv_heads, cache.head_dim, cache.dtype)
+    vp_, ldv, hv = _heads3(out_v, "out_v", cache.kv_heads, cache.head_dim, cache.dtype)
+    if out_k.shape[0] != out_v.shape[0]:
+        raise ValueError("the buffers must have the same number of rows")
+    if out_k.shape[0]:
+        cb = batch._c_for(cache, out_k.shape[0])
+        _check(load().bd_paged_read(ctypes.byref(cache._c), ctypes.byref(cb), kp, vp_, ldk, hk, ldv, hv, _stream(stream)))
+    return out_k, out_v
+
+
+def paged_attention_workspace_size(cache, batch, rows, q_heads):
+    b = ctypes.c_size_t()
+    cb = batch._c_for(cache, rows)
+    _check(load().bd_paged_attention_workspace_size(ctypes.byref(cache._c), ctypes.byref(cb), q_heads, ctypes.byref(b)))
+    return b.value
+
+
+def paged_attention(cache, batch, q, scale=None, softcap=0.0, window=0, out=None, dtype=None, lse=None, workspace=None, stream=None):
+    """Causal attention of the step's queries [rows, q_heads, head_dim] (bf16 or fp16, the cache's type) over the paged
+    cache: O [rows, q_heads, head_dim] of q's type or fp32.  softcap > 0: scores softcap * tanh(s / softcap); window > 0:
+    the last `window` tokens.  lse: fp32 [rows, q_heads] that receives the rows' log sums of exponentials."""
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, q_heads, head_dim]")
+    rows, heads, d = q.shape[0], q.shape[1], cache.head_dim
+    if heads <= 0 or heads % cache.kv_heads:
+        raise ValueError("the number of query heads must be a multiple of the number of KV heads")
+    qp, ldq, hq = _heads3(q, "q", heads, d, cache.dtype)
+    if out is None:
+        out = torch.empty(rows, heads, d, dtype=dtype or q.dtype, device=q.device)
+    if out.shape[0] != rows or out.dtype not in _TORCH_DTYPE:
+        raise ValueError("out must have the rows of q")
+    op, ldo, ho = _heads3(out, "out", heads, d, out.dtype)
+    if lse is not None:
+        if lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous fp32 [rows, q_heads]")
+        _here(lse, "lse")
+    if workspace is not None:
+        _here(workspace, "workspace")
+    if not rows:
+        return out
+    cb = batch._c_for(cache, rows)
+    workspace, wptr, wbytes = _ws(workspace, lambda: paged_attention_workspace_size(cache, batch, rows, heads), q.device)
+    _check(load().bd_paged_attention(ctypes.byref(cache._c), ctypes.byref(cb), qp, heads, ldq, hq, d ** -0.5 if scale is None else scale, softcap, window,
+                                     op, _TORCH_DTYPE[out.dtype], ldo, ho, lse.data_ptr() if lse is not None else None, wptr, wbytes, _stream(stream)))
+    return out
+
+
+def qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out_q=None, out_k=None, stream=None):
+    """Per-head normalisation (where a weight [head_dim] is given) and position rotation of queries [rows, heads, head_dim]
+    and keys [rows, kv_heads, head_dim] (k may be None) in one pass.  positions int32 [rows]; cos_sin fp32
+    [positions, rot]: rot / 2 cosines, then rot / 2 sines.  The outputs may be the inputs."""
+    if q.dim() != 3 or q.dtype not in _TORCH_DTYPE:
+        raise ValueError("q must be [rows, heads, head_dim] of fp32/bf16/fp16")
+    rows, d = q.shape[0], q.shape[2]
+    if positions.dtype != torch.int32 or positions.shape != (rows,) or (rows > 1 and positions.stride(0) != 1):
+        raise ValueError("positions must be int32 [rows]")
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+        raise ValueError("cos_sin must be contiguous fp32 [positions, rot]")
+    _here(positions, "positions")
+    _here(cos_sin, "cos_sin")
+    out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
+    if k is not None:
+        out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device) if out_k is None else out_k
+    ops = []
+    for x, y, w, what in ((q, out_q, q_weight, "q"), (k, out_k, k_weight, "k")):
+        if x is None:
+            ops.append(_CRopeOperand(None, None, None, 0, 0, 0, 0, 0))
+            continue
+        if x.dim() != 3 or x.shape[0] != rows or y.dim() != 3 or y.shape != x.shape:
+            raise ValueError(f"{what} and its output must have the rows of q and one shape")
+        xp, ldx, hx = _heads3(x, what, x.shape[1], d, q.dtype)
+        yp, ldy, hy = _heads3(y, "out_" + what, x.shape[1], d, q.dtype)
+        if w is not None:
+            if w.shape != (d,) or w.dtype != q.dtype or not w.is_contiguous():
+                raise ValueError("a weight must be contiguous [head_dim] of the rows' type")
+            _here(w, "weight")
+        ops.append(_CRopeOperand(xp, yp, w.data_ptr() if w is not None else None, x.shape[1], ldx, hx, ldy, hy))
+    if rows:
+        _check(load().bd_qk_norm_rope(ctypes.byref(ops[0]), ctypes.byref(ops[1]), _TORCH_DTYPE[q.dtype], rows, d, positions.data_ptr(), cos_sin.data_ptr(),
+                                      cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0, eps, _stream(stream)))
+    return out_q, out_k
 
 
 NOALLOC_SCRATCH_BYTES = 32 << 20

@@ -268,7 +268,7 @@ constexpr DeviceTables kTables = make_tables(kBook);
 
 // Bits of the device status word (defined in quantize.cuh; the library is one
 // translation unit).  bd_poll_status reads and clears it.
-enum : uint32_t { kStatusNonfinite = 1u, kStatusTimeout = 2u };
+enum : uint32_t { kStatusNonfinite = 1u, kStatusTimeout = 2u, kStatusIndex = 4u };
 
 // Launch helpers shared by the translation units.
 struct QView {                 // a qtensor as kernels see it

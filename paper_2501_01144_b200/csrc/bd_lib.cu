@@ -13,6 +13,8 @@
 #include "blocksize.cuh"
 #include "kvcache.cuh"
 #include "attention.cuh"
+#include "paged.cuh"
+#include "paged_attention.cuh"
 #include "quantize.cuh"
 
 using namespace bd;
@@ -384,6 +386,90 @@ bd_status quantize_bs_dtype(const void *X, bd_dtype dt, int64_t ld, bd_select se
     }
     return launch_result();
 }
+}  // namespace
+
+// ---- paged KV cache: append, read back, attention; position rotation ----
+namespace {
+bd_status check_paged(const bd_paged_cache *c, const bd_paged_batch *b) {
+    if (!c || !c->pool || !c->tail) return BD_ERR_INVALID_ARG;
+    if (c->dtype != BD_F32 && c->dtype != BD_BF16 && c->dtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if (c->pages <= 0 || c->slots <= 0 || c->kv_heads <= 0) return BD_ERR_INVALID_ARG;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->page_tokens <= 0 || c->page_tokens % pg::kChunk) return BD_ERR_SHAPE;
+    if (c->pages > INT32_MAX || c->slots > INT32_MAX || c->page_tokens > INT32_MAX || c->kv_heads > 65535) return BD_ERR_UNSUPPORTED;
+    if (!aligned16(c->pool) || !aligned16(c->tail)) return BD_ERR_ALIGN;
+    if (!b || !b->page_table || !b->slot || !b->kv_len || !b->q_start) return BD_ERR_INVALID_ARG;
+    if (b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0 || b->ld_table <= 0) return BD_ERR_INVALID_ARG;
+    if (b->n > 65535 || b->rows > INT32_MAX || b->max_kv > INT32_MAX - pg::kChunk) return BD_ERR_UNSUPPORTED;
+    if (b->max_q > b->rows || b->max_kv > b->ld_table * c->page_tokens) return BD_ERR_SHAPE;
+    if (((uintptr_t)b->page_table | (uintptr_t)b->slot | (uintptr_t)b->kv_len | (uintptr_t)b->q_start) & 3u) return BD_ERR_ALIGN;
+    return BD_OK;
+}
+pg::Pool pool_of(const bd_paged_cache *c) {
+    return pg::Pool{(uint8_t *)c->pool, c->tail, (int)c->pages, (int)c->slots, (int)c->kv_heads, (int)(c->page_tokens / pg::kChunk),
+                    (int)c->head_dim, elem_bytes(c->dtype)};
+}
+pg::Batch batch_of(const bd_paged_batch *b) {
+    return pg::Batch{b->page_table, b->slot, b->kv_len, b->q_start, b->ld_table, (int)b->n, (int)b->rows, (int)b->max_q, (int)b->max_kv};
+}
+// [rows, heads, d] elements with a row and a head stride: aligned 16-byte pieces, heads and rows that do not overlap
+bd_status check_rows(const void *x, int64_t rows, int64_t heads, int64_t d, int64_t ld, int64_t hs, int esz) {
+    if (!x) return BD_ERR_INVALID_ARG;
+    if (hs < d && heads > 1) return BD_ERR_SHAPE;
+    if (rows > 1 && (hs <= ld ? ld < (heads - 1) * hs + d : hs < (rows - 1) * ld + d || ld < d)) return BD_ERR_SHAPE;
+    if (!aligned16(x) || (ld * esz) % 16 || (hs * esz) % 16) return BD_ERR_ALIGN;
+    return BD_OK;
+}
+unsigned paged_chunks(const bd_paged_batch *b) {                   // chunks that max_q tokens can touch
+    return (unsigned)((std::min(b->max_q, b->max_kv) + pg::kChunk - 2) / pg::kChunk + 1);
+}
+
+// How a call over few rows per KV head is cut: rows per warp tile (8 or 16), tiles, CTAs a sequence is split over.
+struct RowPlan {
+    int wide, tiles, splits;
+};
+RowPlan row_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
+    const int64_t rows = b->max_q * (q_heads / c->kv_heads);
+    RowPlan r;
+    r.wide = rows > 8;
+    r.tiles = (int)((rows + (r.wide ? 15 : 7)) / (r.wide ? 16 : 8));
+    const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), chunks = (b->max_kv + pg::kChunk - 1) / pg::kChunk;
+    const int64_t want = 148 * 4 / ctas, most = (chunks + pg::kRowWarps - 1) / pg::kRowWarps;
+    r.splits = (int)std::max<int64_t>(1, std::min(want, most));
+    return r;
+}
+size_t row_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
+    const RowPlan r = row_plan(c, b, q_heads);
+    return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+}
+template <int DT, int NB, int NT>
+void launch_rows(const pg::Attention &a, dim3 grid, cudaStream_t st) {
+    const size_t smem = pg::RowSmem<NB, NT>::total;
+    if (a.softcap > 0.0f) launch_serialized(pg::attention_rows_kernel<DT, NB, NT, true>, grid, 32 * pg::kRowWarps, smem, st, a);
+    else launch_serialized(pg::attention_rows_kernel<DT, NB, NT, false>, grid, 32 * pg::kRowWarps, smem, st, a);
+}
+template <int DT>
+void launch_rows_dtype(const pg::Attention &a, bool wide, dim3 grid, cudaStream_t st) {
+    if (a.pool.head_dim == 128) wide ? launch_rows<DT, 4, 2>(a, grid, st) : launch_rows<DT, 4, 1>(a, grid, st);
+    else wide ? launch_rows<DT, 2, 2>(a, grid, st) : launch_rows<DT, 2, 1>(a, grid, st);
+}
+template <int DT, int D>
+void launch_rotate(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
+    if (interleaved) launch_serialized(pg::rotate_kernel<DT, D, true>, dim3((unsigned)r.rows), 256, 0, st, r);
+    else launch_serialized(pg::rotate_kernel<DT, D, false>, dim3((unsigned)r.rows), 256, 0, st, r);
+}
+#define BD_PAGED_DISPATCH(kernel, c, grid, st, ...)                                                                              \
+    do {                                                                                                                        \
+        const unsigned threads = (unsigned)(c)->head_dim * 2;                                                                    \
+        if ((c)->head_dim == 128) {                                                                                              \
+            if ((c)->dtype == BD_F32) launch_serialized(kernel<BD_F32, 4>, grid, threads, 0, st, __VA_ARGS__);                   \
+            else if ((c)->dtype == BD_BF16) launch_serialized(kernel<BD_BF16, 4>, grid, threads, 0, st, __VA_ARGS__);            \
+            else launch_serialized(kernel<BD_F16, 4>, grid, threads, 0, st, __VA_ARGS__);                                        \
+        } else {                                                                                                                 \
+            if ((c)->dtype == BD_F32) launch_serialized(kernel<BD_F32, 2>, grid, threads, 0, st, __VA_ARGS__);                   \
+            else if ((c)->dtype == BD_BF16) launch_serialized(kernel<BD_BF16, 2>, grid, threads, 0, st, __VA_ARGS__);            \
+            else launch_serialized(kernel<BD_F16, 2>, grid, threads, 0, st, __VA_ARGS__);                                        \
+        }                                                                                                                        \
+    } while (0)
 }  // namespace
 
 extern "C" {
@@ -1248,6 +1334,127 @@ bd_status bd_attention(const bd_qtensor *Q, const bd_qtensor *K, const bd_qtenso
     return launch_result(kernels);
 }
 
+// ---- paged KV cache: append, read back, attention; position rotation ----
+bd_status bd_paged_sizes(const bd_paged_cache *c, size_t *pool_bytes, size_t *tail_bytes) {
+    if (!c || c->pages <= 0 || c->slots <= 0 || c->kv_heads <= 0) return BD_ERR_INVALID_ARG;
+    if (c->dtype != BD_F32 && c->dtype != BD_BF16 && c->dtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->page_tokens <= 0 || c->page_tokens % pg::kChunk) return BD_ERR_SHAPE;
+    if (pool_bytes) *pool_bytes = (size_t)c->pages * (size_t)c->kv_heads * (size_t)(c->page_tokens / pg::kChunk) * (size_t)pg::record_bytes((int)c->head_dim);
+    if (tail_bytes) *tail_bytes = (size_t)c->slots * (size_t)c->kv_heads * pg::kTailRows * (size_t)c->head_dim * (size_t)elem_bytes(c->dtype);
+    return BD_OK;
+}
+
+bd_status bd_paged_append(const bd_paged_cache *c, const bd_paged_batch *b, const void *K, const void *V, int64_t ldk,
+                          int64_t head_stride_k, int64_t ldv, int64_t head_stride_v, void *stream) {
+    bd_status s = check_paged(c, b);
+    if (s) return s;
+    const int esz = elem_bytes(c->dtype);
+    if ((s = check_rows(K, b->rows, c->kv_heads, c->head_dim, ldk, head_stride_k, esz))) return s;
+    if ((s = check_rows(V, b->rows, c->kv_heads, c->head_dim, ldv, head_stride_v, esz))) return s;
+    if (b->max_q == 0) return BD_OK;
+    const dim3 grid(paged_chunks(b), (unsigned)c->kv_heads, (unsigned)b->n);
+    BD_PAGED_DISPATCH(pg::append_kernel, c, grid, (cudaStream_t)stream, pool_of(c), batch_of(b), (const uint8_t *)K, (const uint8_t *)V, ldk, ldv,
+                      head_stride_k, head_stride_v);
+    return launch_result();
+}
+
+bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *K, void *V, int64_t ldk, int64_t head_stride_k,
+                        int64_t ldv, int64_t head_stride_v, void *stream) {
+    bd_status s = check_paged(c, b);
+    if (s) return s;
+    const int esz = elem_bytes(c->dtype);
+    if ((s = check_rows(K, b->rows, c->kv_heads, c->head_dim, ldk, head_stride_k, esz))) return s;
+    if ((s = check_rows(V, b->rows, c->kv_heads, c->head_dim, ldv, head_stride_v, esz))) return s;
+    if (b->max_q == 0) return BD_OK;
+    const dim3 grid(paged_chunks(b), (unsigned)c->kv_heads, (unsigned)b->n);
+    BD_PAGED_DISPATCH(pg::read_kernel, c, grid, (cudaStream_t)stream, pool_of(c), batch_of(b), (uint8_t *)K, (uint8_t *)V, ldk, ldv,
+                      head_stride_k, head_stride_v);
+    return launch_result();
+}
+
+bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes) {
+    if (!c || !b || !bytes || q_heads <= 0 || c->kv_heads <= 0 || b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0) return BD_ERR_INVALID_ARG;
+    if (q_heads % c->kv_heads || (c->head_dim != 64 && c->head_dim != 128)) return BD_ERR_SHAPE;
+    *bytes = row_workspace(c, b, q_heads);
+    return BD_OK;
+}
+
+bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, const void *Q, int64_t q_heads, int64_t ldq,
+                             int64_t head_stride_q, float scale, float softcap, int64_t window, void *O, bd_dtype odtype,
+                             int64_t ldo, int64_t head_stride_o, float *lse, void *workspace, size_t workspace_bytes,
+                             void *stream) {
+    bd_status s = check_paged(c, b);
+    if (s) return s;
+    if (q_heads <= 0 || window < 0 || !(scale == scale) || !(softcap >= 0.0f) || softcap > 1e30f) return BD_ERR_INVALID_ARG;
+    if (odtype != BD_F32 && odtype != BD_BF16 && odtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if (q_heads % c->kv_heads) return BD_ERR_SHAPE;
+    if (c->dtype == BD_F32 || (odtype != BD_F32 && odtype != c->dtype) || q_heads > 65535) return BD_ERR_UNSUPPORTED;
+    if ((s = check_rows(Q, b->rows, q_heads, c->head_dim, ldq, head_stride_q, 2))) return s;
+    if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
+    if ((uintptr_t)lse & 3u) return BD_ERR_ALIGN;
+    if (b->max_q == 0) return BD_OK;
+    const RowPlan plan = row_plan(c, b, q_heads);
+    const size_t need = row_workspace(c, b, q_heads);
+    if (need && (!workspace || workspace_bytes < need)) return BD_ERR_WORKSPACE;
+    if (need && ((uintptr_t)workspace & 255u)) return BD_ERR_ALIGN;
+    pg::Attention a{};
+    a.pool = pool_of(c);
+    a.batch = batch_of(b);
+    a.q = (const uint8_t *)Q; a.ldq = ldq; a.hsq = head_stride_q;
+    a.o = (uint8_t *)O; a.ldo = ldo; a.hso = head_stride_o;
+    a.lse = lse;
+    a.part = (float *)workspace;
+    a.scale = scale; a.softcap = softcap;
+    a.q_heads = (int)q_heads; a.group = (int)(q_heads / c->kv_heads); a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
+    a.splits = plan.splits; a.row_tiles = plan.tiles; a.odtype = (int)odtype;
+    cudaStream_t st = (cudaStream_t)stream;
+    const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
+    if (c->dtype == BD_BF16) launch_rows_dtype<BD_BF16>(a, plan.wide, grid, st);
+    else launch_rows_dtype<BD_F16>(a, plan.wide, grid, st);
+    int kernels = 1;
+    if (plan.splits > 1) {
+        const dim3 join((unsigned)((b->max_q + 3) / 4), (unsigned)q_heads, (unsigned)b->n);
+        if (c->head_dim == 128) launch_serialized(pg::attention_join_kernel<128>, join, 128, 0, st, a);
+        else launch_serialized(pg::attention_join_kernel<64>, join, 128, 0, st, a);
+        kernels++;
+    }
+    return launch_result(kernels);
+}
+
+bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd_dtype dtype, int64_t rows, int64_t head_dim,
+                          const int32_t *position, const float *cos_sin, int64_t positions, int64_t rot, int interleaved, float eps,
+                          void *stream) {
+    if (!q || !k || !position || !cos_sin || rows < 0 || positions <= 0 || q->heads <= 0 || k->heads < 0 || !(eps >= 0.0f)) return BD_ERR_INVALID_ARG;
+    if (dtype != BD_F32 && dtype != BD_BF16 && dtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if ((head_dim != 64 && head_dim != 128) || rot <= 0 || rot % 16 || rot > head_dim) return BD_ERR_SHAPE;
+    if (rows > INT32_MAX || q->heads + k->heads > 65535) return BD_ERR_UNSUPPORTED;
+    const int esz = elem_bytes(dtype);
+    for (const bd_rope_operand *x : {q, k}) {
+        if (!x->heads) continue;
+        bd_status s = check_rows(x->x, rows, x->heads, head_dim, x->ldx, x->head_stride_x, esz);
+        if (s) return s;
+        if ((s = check_rows(x->y, rows, x->heads, head_dim, x->ldy, x->head_stride_y, esz))) return s;
+        if (!aligned16(x->weight)) return BD_ERR_ALIGN;
+    }
+    if (!aligned16(cos_sin) || ((uintptr_t)position & 3u)) return BD_ERR_ALIGN;
+    if (rows == 0) return BD_OK;
+    pg::Rotation r{(const uint8_t *)q->x, (const uint8_t *)k->x, (uint8_t *)q->y, (uint8_t *)k->y, q->ldx, q->head_stride_x, k->ldx, k->head_stride_x,
+                   q->ldy, q->head_stride_y, k->ldy, k->head_stride_y, q->weight, k->weight, position, cos_sin, positions, (int)rows, (int)q->heads,
+                   (int)k->heads, (int)rot, eps};
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool il = interleaved != 0;
+    if (head_dim == 128) {
+        if (dtype == BD_F32) launch_rotate<BD_F32, 128>(r, il, st);
+        else if (dtype == BD_BF16) launch_rotate<BD_BF16, 128>(r, il, st);
+        else launch_rotate<BD_F16, 128>(r, il, st);
+    } else {
+        if (dtype == BD_F32) launch_rotate<BD_F32, 64>(r, il, st);
+        else if (dtype == BD_BF16) launch_rotate<BD_BF16, 64>(r, il, st);
+        else launch_rotate<BD_F16, 64>(r, il, st);
+    }
+    return launch_result();
+}
+
 bd_status bd_export_canonical(const bd_qtensor *q, uint8_t *codes, uint8_t *ids, uint8_t *scales, void *stream) {
     bd_status s = check_qtensor(q);
     if (s) return s;
@@ -1316,6 +1523,7 @@ bd_status bd_poll_status(void *stream) {
         if (s) return s;
     }
     if (word & kStatusTimeout) return BD_ERR_TIMEOUT;
+    if (word & kStatusIndex) return BD_ERR_INDEX;
     if (word & kStatusNonfinite) return BD_ERR_NONFINITE;
     return BD_OK;
 }
@@ -1342,6 +1550,7 @@ const char *bd_status_string(bd_status s) {
         case BD_ERR_TIMEOUT: return "a bounded device-side wait expired";
         case BD_ERR_WORKSPACE: return "workspace missing or too small";
         case BD_ERR_SCRATCH_LIMIT: return "problem needs more scratch than the built-in no-allocation buffer holds";
+        case BD_ERR_INDEX: return "a page, slot, position or row range lies outside its bounds";
     }
     return "unknown status";
 }

@@ -8,7 +8,7 @@
 
 namespace bd {
 
-// Device status word, read and cleared by bd_poll_status (bits: kStatusNonfinite, kStatusTimeout).
+// Device status word, read and cleared by bd_poll_status (bits: kStatusNonfinite, kStatusTimeout, kStatusIndex).
 __device__ uint32_t g_status_word = 0;
 // Test hooks (bd_debug_fault): a lower poll limit for the bounded waits (0 = the built-in one) and "the code
 // producer of the tensor-core product leaves out its very first stage", which makes a wait run out on purpose.
