@@ -7,6 +7,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libblockdialect.so")
+_PAGED_PATH = os.path.join(_HERE, "_paged.so")
 _SRC = os.path.join(_HERE, "csrc", "bd_lib.cu")
 
 F32, BF16, F16 = 0, 1, 2
@@ -17,6 +18,7 @@ GEMM_AUTO, GEMM_SIMT, GEMM_TCGEN05, GEMM_WARP = 0, 1, 2, 3
 _TORCH_DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 _lib = None
+_paged = None
 
 
 class BdError(RuntimeError):
@@ -61,15 +63,31 @@ def library_path():
 
 def build(verbose=False):
     """Compile the CUDA library in-tree for sm_100a."""
-    srcs = [os.path.join(_HERE, "csrc", f) for f in os.listdir(os.path.join(_HERE, "csrc"))]
+    srcs = [os.path.join(_HERE, "csrc", f) for f in os.listdir(os.path.join(_HERE, "csrc")) if not f.endswith(".cpp")]
     if os.path.exists(_LIB_PATH) and all(os.path.getmtime(_LIB_PATH) >= os.path.getmtime(s) for s in srcs):
+        _build_paged()
         return _LIB_PATH
     cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", "-o", _LIB_PATH, _SRC]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     subprocess.run(cmd, check=True)
+    _build_paged()
     return _LIB_PATH
+
+
+def _build_paged():
+    """Compile the native binding of the paged-cache calls (a CPython module beside the library, linked to it)."""
+    src, header = os.path.join(_HERE, "csrc", "paged_binding.cpp"), os.path.join(os.path.dirname(_HERE), "include", "bd.h")
+    if os.path.exists(_PAGED_PATH) and os.path.getmtime(_PAGED_PATH) >= max(os.path.getmtime(src), os.path.getmtime(header)):
+        return
+    import sysconfig
+    from torch.utils import cpp_extension
+    includes = cpp_extension.include_paths("cuda") + [sysconfig.get_paths()["include"]]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", _PAGED_PATH, src]
+    cmd += [f"-I{i}" for i in includes] + [f"-L{_HERE}", "-l:libblockdialect.so", f"-L{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+    subprocess.run(cmd, check=True)
 
 
 def load():
@@ -137,6 +155,22 @@ def load():
     lib.bd_status_string.restype = ctypes.c_char_p
     _lib = lib
     return lib
+
+
+def _load_paged():
+    """The native binding of the paged-cache calls (once)."""
+    global _paged
+    if _paged is None:
+        load()
+        if not os.path.exists(_PAGED_PATH):
+            raise BdError(-1, f"{_PAGED_PATH} is missing: run __graft_entry__.build() first")
+        import importlib.util
+        spec = importlib.util.spec_from_file_location("_paged", _PAGED_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.set_check(_check)
+        _paged = module
+    return _paged
 
 
 def _check(status):
@@ -560,23 +594,6 @@ def kvcache_attention(caches, Qs, scale, out=None, dtype=torch.float32, probs=No
     return out
 
 
-def _here(t, what):
-    """The library launches on the current device: a tensor of another one is refused."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what} must be on the current CUDA device")
-
-
-def _heads3(x, what, heads, head_dim, dtype):
-    """Pointer, row stride and head stride of [rows, heads, head_dim] with a contiguous last axis."""
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.dtype != dtype or (x.stride(2) != 1 and x.numel()):
-        raise ValueError(f"{what} must be [rows, {heads}, {head_dim}] of {dtype} with a contiguous last axis")
-    _here(x, what)
-    ld, hs = x.stride(0), x.stride(1)
-    if x.shape[0] <= 1:                                               # strides of axes of one element mean nothing
-        ld = max(heads * head_dim, ld)
-    return x.data_ptr(), ld, hs if heads > 1 else head_dim
-
-
 class PagedKVCache:
     """Paged DialectFP4 KV cache shared by many sequences (storage: bd.h).  `pool` uint8 [pages, kv_heads,
     page_tokens / 32, 35 * head_dim], `tail` [slots, kv_heads, 64, head_dim] of `dtype`.  The caller hands out pages
@@ -596,16 +613,14 @@ class PagedKVCache:
         return self
 
     def _set(self, pool, tail, page_tokens):
-        if tail.dim() != 4 or tail.dtype not in _TORCH_DTYPE or tail.shape[2] != 64 or not tail.is_contiguous():
-            raise ValueError("tail must be contiguous [slots, kv_heads, 64, head_dim] of fp32/bf16/fp16")
-        slots, kv_heads, _, d = tail.shape
-        if pool.dtype != torch.uint8 or pool.dim() != 4 or tuple(pool.shape[1:]) != (kv_heads, page_tokens // 32, 35 * d) or not pool.is_contiguous():
-            raise ValueError("pool must be contiguous uint8 [pages, kv_heads, page_tokens / 32, 35 * head_dim]")
-        _here(pool, "pool")
-        _here(tail, "tail")
+        self._c = (_paged or _load_paged()).cache(pool, tail, page_tokens)
         self.pool, self.tail, self.page_tokens = pool, tail, page_tokens
-        self.pages, self.slots, self.kv_heads, self.head_dim, self.dtype = pool.shape[0], slots, kv_heads, d, tail.dtype
-        self._c = _CPagedCache(pool.data_ptr(), tail.data_ptr(), _TORCH_DTYPE[tail.dtype], pool.shape[0], slots, kv_heads, page_tokens, d)
+
+    pages = property(lambda self: self.pool.shape[0])
+    slots = property(lambda self: self.tail.shape[0])
+    kv_heads = property(lambda self: self.tail.shape[1])
+    head_dim = property(lambda self: self.tail.shape[3])
+    dtype = property(lambda self: self.tail.dtype)
 
 
 class PagedBatch:
@@ -614,129 +629,37 @@ class PagedBatch:
     the page table can hold)."""
 
     def __init__(self, page_table, slots, kv_len, q_start, max_q, max_kv=None):
-        n = kv_len.shape[0]
-        for x in (page_table, slots, kv_len, q_start):
-            if x.dtype != torch.int32 or not x.is_cuda or x.stride(-1) != 1:
-                raise ValueError("the batch's index tensors must be int32 CUDA tensors with a contiguous last axis")
-        if page_table.dim() != 2 or page_table.shape[0] != n or slots.shape != (n,) or kv_len.dim() != 1 or q_start.shape != (n + 1,):
-            raise ValueError("page_table [n, width], slots [n], kv_len [n], q_start [n + 1]")
-        _here(kv_len, "the batch")
-        if len({x.device for x in (page_table, slots, kv_len, q_start)}) > 1:
-            raise ValueError("the batch's tensors must be on one device")
-        self.page_table, self.slots, self.kv_len, self.q_start, self.n = page_table, slots, kv_len, q_start, n
-        self.max_q, self.max_kv, self.width = max_q, max_kv, page_table.shape[1]
-        self._c = _CPagedBatch(page_table.data_ptr(), slots.data_ptr(), kv_len.data_ptr(), q_start.data_ptr(),
-                               max(page_table.stride(0), page_table.shape[1]) if n > 1 else page_table.shape[1], n, 0, 0, 0)
-
-    def _c_for(self, cache, rows):
-        c = self._c
-        held = self.width * cache.page_tokens
-        if self.max_kv is not None and self.max_kv > held:
-            raise ValueError("max_kv exceeds what the page table can hold")
-        c.rows, c.max_q, c.max_kv = rows, min(self.max_q, rows), held if self.max_kv is None else self.max_kv
-        return c
+        self._c = (_paged or _load_paged()).batch(page_table, slots, kv_len, q_start, max_q, max_kv)
+        self.page_table, self.slots, self.kv_len, self.q_start, self.max_q, self.max_kv = page_table, slots, kv_len, q_start, max_q, max_kv
 
 
 def paged_append(cache, batch, k, v, stream=None):
     """Store the step's keys and values [rows, kv_heads, head_dim] of the cache's type."""
-    kp, ldk, hk = _heads3(k, "keys", cache.kv_heads, cache.head_dim, cache.dtype)
-    vp_, ldv, hv = _heads3(v, "values", cache.kv_heads, cache.head_dim, cache.dtype)
-    if k.shape[0] != v.shape[0]:
-        raise ValueError("keys and values must have the same number of rows")
-    if k.shape[0]:
-        cb = batch._c_for(cache, k.shape[0])
-        _check(load().bd_paged_append(ctypes.byref(cache._c), ctypes.byref(cb), kp, vp_, ldk, hk, ldv, hv, _stream(stream)))
+    _paged.append(cache._c, batch._c, k, v, stream)
 
 
 def paged_read(cache, batch, rows=None, out_k=None, out_v=None, stream=None):
     """The values the cache stands for of each sequence's last tokens: (keys, values) [rows, kv_heads, head_dim] of the
     cache's type, laid out by the batch's q_start.  rows: the height of the result when no buffers are given."""
-    shape = (rows, cache.kv_heads, cache.head_dim)
-    if (out_k is None or out_v is None) and rows is None:
-        raise ValueError("give the number of rows or both buffers")
-    out_k = torch.empty(shape, dtype=cache.dtype, device=cache.pool.device) if out_k is None else out_k
-    out_v = torch.empty(shape, dtype=cache.dtype, device=cache.pool.device) if out_v is None else out_v
-    kp, ldk, hk = _heads3(out_k, "out_k", cache.kv_heads, cache.head_dim, cache.dtype)
-    vp_, ldv, hv = _heads3(out_v, "out_v", cache.kv_heads, cache.head_dim, cache.dtype)
-    if out_k.shape[0] != out_v.shape[0]:
-        raise ValueError("the buffers must have the same number of rows")
-    if out_k.shape[0]:
-        cb = batch._c_for(cache, out_k.shape[0])
-        _check(load().bd_paged_read(ctypes.byref(cache._c), ctypes.byref(cb), kp, vp_, ldk, hk, ldv, hv, _stream(stream)))
-    return out_k, out_v
+    return _paged.read(cache._c, batch._c, rows, out_k, out_v, stream)
 
 
 def paged_attention_workspace_size(cache, batch, rows, q_heads):
-    b = ctypes.c_size_t()
-    cb = batch._c_for(cache, rows)
-    _check(load().bd_paged_attention_workspace_size(ctypes.byref(cache._c), ctypes.byref(cb), q_heads, ctypes.byref(b)))
-    return b.value
+    return _paged.workspace_size(cache._c, batch._c, rows, q_heads)
 
 
 def paged_attention(cache, batch, q, scale=None, softcap=0.0, window=0, out=None, dtype=None, lse=None, workspace=None, stream=None):
     """Causal attention of the step's queries [rows, q_heads, head_dim] (bf16 or fp16, the cache's type) over the paged
     cache: O [rows, q_heads, head_dim] of q's type or fp32.  softcap > 0: scores softcap * tanh(s / softcap); window > 0:
     the last `window` tokens.  lse: fp32 [rows, q_heads] that receives the rows' log sums of exponentials."""
-    if q.dim() != 3:
-        raise ValueError("q must be [rows, q_heads, head_dim]")
-    rows, heads, d = q.shape[0], q.shape[1], cache.head_dim
-    if heads <= 0 or heads % cache.kv_heads:
-        raise ValueError("the number of query heads must be a multiple of the number of KV heads")
-    qp, ldq, hq = _heads3(q, "q", heads, d, cache.dtype)
-    if out is None:
-        out = torch.empty(rows, heads, d, dtype=dtype or q.dtype, device=q.device)
-    if out.shape[0] != rows or out.dtype not in _TORCH_DTYPE:
-        raise ValueError("out must have the rows of q")
-    op, ldo, ho = _heads3(out, "out", heads, d, out.dtype)
-    if lse is not None:
-        if lse.shape != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("lse must be contiguous fp32 [rows, q_heads]")
-        _here(lse, "lse")
-    if workspace is not None:
-        _here(workspace, "workspace")
-    if not rows:
-        return out
-    cb = batch._c_for(cache, rows)
-    workspace, wptr, wbytes = _ws(workspace, lambda: paged_attention_workspace_size(cache, batch, rows, heads), q.device)
-    _check(load().bd_paged_attention(ctypes.byref(cache._c), ctypes.byref(cb), qp, heads, ldq, hq, d ** -0.5 if scale is None else scale, softcap, window,
-                                     op, _TORCH_DTYPE[out.dtype], ldo, ho, lse.data_ptr() if lse is not None else None, wptr, wbytes, _stream(stream)))
-    return out
+    return _paged.attention(cache._c, batch._c, q, scale, softcap, window, out, dtype, lse, workspace, stream)
 
 
 def qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out_q=None, out_k=None, stream=None):
     """Per-head normalisation (where a weight [head_dim] is given) and position rotation of queries [rows, heads, head_dim]
     and keys [rows, kv_heads, head_dim] (k may be None) in one pass.  positions int32 [rows]; cos_sin fp32
     [positions, rot]: rot / 2 cosines, then rot / 2 sines.  The outputs may be the inputs."""
-    if q.dim() != 3 or q.dtype not in _TORCH_DTYPE:
-        raise ValueError("q must be [rows, heads, head_dim] of fp32/bf16/fp16")
-    rows, d = q.shape[0], q.shape[2]
-    if positions.dtype != torch.int32 or positions.shape != (rows,) or (rows > 1 and positions.stride(0) != 1):
-        raise ValueError("positions must be int32 [rows]")
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
-        raise ValueError("cos_sin must be contiguous fp32 [positions, rot]")
-    _here(positions, "positions")
-    _here(cos_sin, "cos_sin")
-    out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
-    if k is not None:
-        out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device) if out_k is None else out_k
-    ops = []
-    for x, y, w, what in ((q, out_q, q_weight, "q"), (k, out_k, k_weight, "k")):
-        if x is None:
-            ops.append(_CRopeOperand(None, None, None, 0, 0, 0, 0, 0))
-            continue
-        if x.dim() != 3 or x.shape[0] != rows or y.dim() != 3 or y.shape != x.shape:
-            raise ValueError(f"{what} and its output must have the rows of q and one shape")
-        xp, ldx, hx = _heads3(x, what, x.shape[1], d, q.dtype)
-        yp, ldy, hy = _heads3(y, "out_" + what, x.shape[1], d, q.dtype)
-        if w is not None:
-            if w.shape != (d,) or w.dtype != q.dtype or not w.is_contiguous():
-                raise ValueError("a weight must be contiguous [head_dim] of the rows' type")
-            _here(w, "weight")
-        ops.append(_CRopeOperand(xp, yp, w.data_ptr() if w is not None else None, x.shape[1], ldx, hx, ldy, hy))
-    if rows:
-        _check(load().bd_qk_norm_rope(ctypes.byref(ops[0]), ctypes.byref(ops[1]), _TORCH_DTYPE[q.dtype], rows, d, positions.data_ptr(), cos_sin.data_ptr(),
-                                      cos_sin.shape[0], cos_sin.shape[1], 1 if interleaved else 0, eps, _stream(stream)))
-    return out_q, out_k
+    return (_paged or _load_paged()).rope(q, k, positions, cos_sin, q_weight, k_weight, eps, interleaved, out_q, out_k, stream)
 
 
 NOALLOC_SCRATCH_BYTES = 32 << 20
