@@ -377,7 +377,8 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
  * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  lse (optional, fp32 [rows][q_heads]) receives
  * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result does not
  * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.
- * Accuracy: products exact, fp32 sums; probabilities rounded to 11 bits (8 bits for bf16 in the long-chunk kernel). */
+ * Accuracy: products exact, fp32 sums; probabilities rounded to 11 bits, or to the cache's type (bf16: 8 bits) in calls of
+ * more than 16 rows (tokens of a sequence times query heads per KV head). */
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes);
 bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, const void *Q, int64_t q_heads, int64_t ldq,
                              int64_t head_stride_q, float scale, float softcap, int64_t window, void *O, bd_dtype odtype,

@@ -15,6 +15,7 @@
 #include "attention.cuh"
 #include "paged.cuh"
 #include "paged_attention.cuh"
+#include "paged_chunk.cuh"
 #include "quantize.cuh"
 
 using namespace bd;
@@ -425,11 +426,19 @@ unsigned paged_chunks(const bd_paged_batch *b) {                   // chunks tha
 
 // How a call over few rows per KV head is cut: rows per warp tile (8 or 16), tiles, CTAs a sequence is split over.
 struct RowPlan {
+    bool chunk;                       // the tensor-core kernel: tiles of 256 rows
     int wide, tiles, splits;
 };
 RowPlan row_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
     const int64_t rows = b->max_q * (q_heads / c->kv_heads);
-    RowPlan r;
+    RowPlan r{};
+    r.chunk = rows > 16;
+    if (r.chunk) {
+        r.tiles = (int)((rows + 255) / 256);
+        const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), tiles = (b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens;
+        r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(148 / ctas, tiles / 4));
+        return r;
+    }
     r.wide = rows > 8;
     r.tiles = (int)((rows + (r.wide ? 15 : 7)) / (r.wide ? 16 : 8));
     const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), chunks = (b->max_kv + pg::kChunk - 1) / pg::kChunk;
@@ -451,6 +460,27 @@ template <int DT>
 void launch_rows_dtype(const pg::Attention &a, bool wide, dim3 grid, cudaStream_t st) {
     if (a.pool.head_dim == 128) wide ? launch_rows<DT, 4, 2>(a, grid, st) : launch_rows<DT, 4, 1>(a, grid, st);
     else wide ? launch_rows<DT, 2, 2>(a, grid, st) : launch_rows<DT, 2, 1>(a, grid, st);
+}
+template <int DT, int NB, bool CAP>
+bd_status launch_chunk_kernel(const pg::Attention &a, dim3 grid, cudaStream_t st) {
+    constexpr int smem = pg::ChunkSmem<NB>::total;
+    static bool configured[kMaxDevices] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= kMaxDevices) return BD_ERR_UNSUPPORTED;
+    if (!configured[dev]) {
+        const bd_status s = cuda_result(cudaFuncSetAttribute(pg::attention_chunk_kernel<DT, NB, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        if (s) return s;
+        configured[dev] = true;
+    }
+    launch_serialized(pg::attention_chunk_kernel<DT, NB, CAP>, grid, pg::kChunkThreads, smem, st, a);
+    return BD_OK;
+}
+template <int DT>
+bd_status launch_chunk(const pg::Attention &a, dim3 grid, cudaStream_t st) {
+    const bool cap = a.softcap > 0.0f;
+    if (a.pool.head_dim == 128) return cap ? launch_chunk_kernel<DT, 4, true>(a, grid, st) : launch_chunk_kernel<DT, 4, false>(a, grid, st);
+    return cap ? launch_chunk_kernel<DT, 2, true>(a, grid, st) : launch_chunk_kernel<DT, 2, false>(a, grid, st);
 }
 template <int DT, int D>
 void launch_rotate(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
@@ -1409,8 +1439,15 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.splits = plan.splits; a.row_tiles = plan.tiles; a.odtype = (int)odtype;
     cudaStream_t st = (cudaStream_t)stream;
     const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
-    if (c->dtype == BD_BF16) launch_rows_dtype<BD_BF16>(a, plan.wide, grid, st);
-    else launch_rows_dtype<BD_F16>(a, plan.wide, grid, st);
+    a.unit = plan.chunk ? 1.0f : 8388608.0f;
+    if (plan.chunk) {
+        s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);
+        if (s) return s;
+    } else if (c->dtype == BD_BF16) {
+        launch_rows_dtype<BD_BF16>(a, plan.wide, grid, st);
+    } else {
+        launch_rows_dtype<BD_F16>(a, plan.wide, grid, st);
+    }
     int kernels = 1;
     if (plan.splits > 1) {
         const dim3 join((unsigned)((b->max_q + 3) / 4), (unsigned)q_heads, (unsigned)b->n);

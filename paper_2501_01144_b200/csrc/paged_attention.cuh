@@ -36,7 +36,7 @@ struct Attention {
     int64_t ldo, hso;
     float *lse;                       // [rows][q_heads] or null
     float *part;                      // [splits][rows][q_heads][d + 2] (split > 1): output, maximum (log2 units), sum
-    float scale, softcap;
+    float scale, softcap, unit;       // unit: factor of the partial outputs
     int q_heads, group, window, splits, row_tiles, odtype;
 };
 
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const __grid_consta
         for (int x = 0; x < D / 32; x++) o[x] = fmaf(src[k * step + lane + 32 * x], f, o[x]);
     }
 #pragma unroll
-    for (int x = 0; x < D / 32; x++) store_out(p, row, head, lane + 32 * x, l > 0.0f ? o[x] * (8388608.0f / l) : (l == 0.0f ? 0.0f : l));
+    for (int x = 0; x < D / 32; x++) store_out(p, row, head, lane + 32 * x, l > 0.0f ? o[x] * (p.unit / l) : (l == 0.0f ? 0.0f : l));
     if (lane == 0 && p.lse) p.lse[row * p.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
 }
 
