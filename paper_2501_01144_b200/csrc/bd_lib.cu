@@ -401,6 +401,7 @@ bd_status check_paged(const bd_paged_cache *c, const bd_paged_batch *b) {
     if (!b || !b->page_table || !b->slot || !b->kv_len || !b->q_start) return BD_ERR_INVALID_ARG;
     if (b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0 || b->ld_table <= 0) return BD_ERR_INVALID_ARG;
     if (b->n > 65535 || b->rows > INT32_MAX || b->max_kv > INT32_MAX - pg::kChunk) return BD_ERR_UNSUPPORTED;
+    if (b->n * c->kv_heads > INT32_MAX / (b->max_kv / pg::kChunk + 1)) return BD_ERR_UNSUPPORTED;   // chunks are numbered in 32 bits
     if (b->max_q > b->rows || b->max_kv > b->ld_table * c->page_tokens) return BD_ERR_SHAPE;
     if (((uintptr_t)b->page_table | (uintptr_t)b->slot | (uintptr_t)b->kv_len | (uintptr_t)b->q_start) & 3u) return BD_ERR_ALIGN;
     return BD_OK;
@@ -424,14 +425,16 @@ unsigned paged_chunks(const bd_paged_batch *b) {                   // chunks tha
     return (unsigned)((std::min(b->max_q, b->max_kv) + pg::kChunk - 2) / pg::kChunk + 1);
 }
 
-// How a call over few rows per KV head is cut: rows per warp tile (8 or 16), tiles, CTAs a sequence is split over.
-struct RowPlan {
-    bool chunk;                       // the tensor-core kernel: tiles of 256 rows
-    int wide, tiles, splits;
+// Which kernel serves a call and how it is cut.  More than 16 rows per KV head: the tensor-core kernel, whose tiles have 256
+// rows; otherwise the warp-level one with 8 or 16 rows per tile, whose warps share the batch's chunks evenly.
+struct AttentionPlan {
+    bool chunk, wide;
+    int tiles, splits;                // chunk kernel: tiles of 256 rows, CTAs that share a tile's tokens
+    int workers, rounds;              // rows kernel: warps, and the runs each takes at most
 };
-RowPlan row_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
+AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
     const int64_t rows = b->max_q * (q_heads / c->kv_heads);
-    RowPlan r{};
+    AttentionPlan r{};
     r.chunk = rows > 16;
     if (r.chunk) {
         r.tiles = (int)((rows + 255) / 256);
@@ -440,39 +443,53 @@ RowPlan row_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_hea
         return r;
     }
     r.wide = rows > 8;
-    r.tiles = (int)((rows + (r.wide ? 15 : 7)) / (r.wide ? 16 : 8));
-    const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), chunks = (b->max_kv + pg::kChunk - 1) / pg::kChunk;
-    const int64_t want = 148 * 4 / ctas, most = (chunks + pg::kRowWarps - 1) / pg::kRowWarps;
-    r.splits = (int)std::max<int64_t>(1, std::min(want, most));
+    const int warps = pg::row_warps(r.wide ? 2 : 1);
+    const int64_t units = b->n * c->kv_heads * std::max<int64_t>(1, (b->max_kv + pg::kChunk - 1) / pg::kChunk);
+    r.workers = (int)std::min<int64_t>(148 * warps, units);
+    r.rounds = (int)std::min<int64_t>(4, std::max<int64_t>(1, units / ((int64_t)r.workers * pg::kRunUnits)));
     return r;
 }
-size_t row_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
-    const RowPlan r = row_plan(c, b, q_heads);
-    return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+size_t attention_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
+    const AttentionPlan r = attention_plan(c, b, q_heads);
+    if (r.chunk) return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+    const int floats = c->head_dim == 128 ? (r.wide ? pg::part_floats<4, 2>() : pg::part_floats<4, 1>()) : (r.wide ? pg::part_floats<2, 2>() : pg::part_floats<2, 1>());
+    return (size_t)r.workers * (size_t)r.rounds * 2 * (size_t)floats * sizeof(float);
+}
+template <typename Kernel>
+bd_status allow_smem(Kernel kernel, int bytes, bool (&configured)[kMaxDevices]) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= kMaxDevices) return BD_ERR_UNSUPPORTED;
+    if (configured[dev]) return BD_OK;
+    const bd_status s = cuda_result(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    configured[dev] = s == BD_OK;
+    return s;
+}
+template <int DT, int NB, int NT, bool CAP>
+bd_status launch_rows_kernel(const pg::Attention &a, cudaStream_t st) {
+    constexpr int smem = pg::RowSmem<NB, NT>::total, warps = pg::row_warps(NT);
+    static bool configured[kMaxDevices] = {};
+    const bd_status s = allow_smem(pg::attention_rows_kernel<DT, NB, NT, CAP>, smem, configured);
+    if (s) return s;
+    launch_serialized(pg::attention_rows_kernel<DT, NB, NT, CAP>, dim3((unsigned)std::min(148, a.workers)), 32 * warps, smem, st, a);
+    launch_serialized(pg::attention_rows_join_kernel<NB, NT>, dim3((unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 32 * NB, 0, st, a);
+    return BD_OK;
 }
 template <int DT, int NB, int NT>
-void launch_rows(const pg::Attention &a, dim3 grid, cudaStream_t st) {
-    const size_t smem = pg::RowSmem<NB, NT>::total;
-    if (a.softcap > 0.0f) launch_serialized(pg::attention_rows_kernel<DT, NB, NT, true>, grid, 32 * pg::kRowWarps, smem, st, a);
-    else launch_serialized(pg::attention_rows_kernel<DT, NB, NT, false>, grid, 32 * pg::kRowWarps, smem, st, a);
+bd_status launch_rows(const pg::Attention &a, cudaStream_t st) {
+    return a.softcap > 0.0f ? launch_rows_kernel<DT, NB, NT, true>(a, st) : launch_rows_kernel<DT, NB, NT, false>(a, st);
 }
 template <int DT>
-void launch_rows_dtype(const pg::Attention &a, bool wide, dim3 grid, cudaStream_t st) {
-    if (a.pool.head_dim == 128) wide ? launch_rows<DT, 4, 2>(a, grid, st) : launch_rows<DT, 4, 1>(a, grid, st);
-    else wide ? launch_rows<DT, 2, 2>(a, grid, st) : launch_rows<DT, 2, 1>(a, grid, st);
+bd_status launch_rows_dtype(const pg::Attention &a, bool wide, cudaStream_t st) {
+    if (a.pool.head_dim == 128) return wide ? launch_rows<DT, 4, 2>(a, st) : launch_rows<DT, 4, 1>(a, st);
+    return wide ? launch_rows<DT, 2, 2>(a, st) : launch_rows<DT, 2, 1>(a, st);
 }
 template <int DT, int NB, bool CAP>
 bd_status launch_chunk_kernel(const pg::Attention &a, dim3 grid, cudaStream_t st) {
     constexpr int smem = pg::ChunkSmem<NB>::total;
     static bool configured[kMaxDevices] = {};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev < 0 || dev >= kMaxDevices) return BD_ERR_UNSUPPORTED;
-    if (!configured[dev]) {
-        const bd_status s = cuda_result(cudaFuncSetAttribute(pg::attention_chunk_kernel<DT, NB, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        if (s) return s;
-        configured[dev] = true;
-    }
+    const bd_status s = allow_smem(pg::attention_chunk_kernel<DT, NB, CAP>, smem, configured);
+    if (s) return s;
     launch_serialized(pg::attention_chunk_kernel<DT, NB, CAP>, grid, pg::kChunkThreads, smem, st, a);
     return BD_OK;
 }
@@ -1405,7 +1422,7 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes) {
     if (!c || !b || !bytes || q_heads <= 0 || c->kv_heads <= 0 || b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads || (c->head_dim != 64 && c->head_dim != 128)) return BD_ERR_SHAPE;
-    *bytes = row_workspace(c, b, q_heads);
+    *bytes = attention_workspace(c, b, q_heads);
     return BD_OK;
 }
 
@@ -1423,8 +1440,8 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
     if ((uintptr_t)lse & 3u) return BD_ERR_ALIGN;
     if (b->max_q == 0) return BD_OK;
-    const RowPlan plan = row_plan(c, b, q_heads);
-    const size_t need = row_workspace(c, b, q_heads);
+    const AttentionPlan plan = attention_plan(c, b, q_heads);
+    const size_t need = attention_workspace(c, b, q_heads);
     if (need && (!workspace || workspace_bytes < need)) return BD_ERR_WORKSPACE;
     if (need && ((uintptr_t)workspace & 255u)) return BD_ERR_ALIGN;
     pg::Attention a{};
@@ -1436,26 +1453,23 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.part = (float *)workspace;
     a.scale = scale; a.softcap = softcap;
     a.q_heads = (int)q_heads; a.group = (int)(q_heads / c->kv_heads); a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
-    a.splits = plan.splits; a.row_tiles = plan.tiles; a.odtype = (int)odtype;
+    a.odtype = (int)odtype;
+    a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.rounds = plan.rounds;
+    a.k16 = 16u; a.k23 = 1u << 23;
     cudaStream_t st = (cudaStream_t)stream;
-    const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
-    a.unit = plan.chunk ? 1.0f : 8388608.0f;
-    if (plan.chunk) {
-        s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);
-        if (s) return s;
-    } else if (c->dtype == BD_BF16) {
-        launch_rows_dtype<BD_BF16>(a, plan.wide, grid, st);
-    } else {
-        launch_rows_dtype<BD_F16>(a, plan.wide, grid, st);
+    if (!plan.chunk) {
+        s = c->dtype == BD_BF16 ? launch_rows_dtype<BD_BF16>(a, plan.wide, st) : launch_rows_dtype<BD_F16>(a, plan.wide, st);
+        return s ? s : launch_result(2);
     }
-    int kernels = 1;
+    const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
+    s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);
+    if (s) return s;
     if (plan.splits > 1) {
         const dim3 join((unsigned)((b->max_q + 3) / 4), (unsigned)q_heads, (unsigned)b->n);
         if (c->head_dim == 128) launch_serialized(pg::attention_join_kernel<128>, join, 128, 0, st, a);
         else launch_serialized(pg::attention_join_kernel<64>, join, 128, 0, st, a);
-        kernels++;
     }
-    return launch_result(kernels);
+    return launch_result(plan.splits > 1 ? 2 : 1);
 }
 
 bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd_dtype dtype, int64_t rows, int64_t head_dim,

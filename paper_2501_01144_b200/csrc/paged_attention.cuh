@@ -5,19 +5,22 @@
 // with q in bf16 or fp16 as given, k and v the values the cache stands for (the rows of an unfinished value chunk in
 // their source type).  Position kv - t + i sees the tokens up to itself, with a window w the last w of them.
 //
-// A warp takes chunks of 32 tokens one by one.  Both products run on the warp-level fp16 MMA with the cache as the
-// 16-row operand and the queries (or the transposed probabilities) as the 8-column operand, so the few rows of a decode
-// step fill half a tile and nothing of the cache is expanded twice.  A code becomes the fp16 number index-value * 2^-24
-// (a subnormal: the half-unit integer itself in the low byte, the sign on top) without any conversion; the block's
-// power-of-two scale multiplies the fp32 block sum.  bf16 queries are first scaled per row by a power of two into the
-// range of fp16 (exact down to 2^-29 of the row's largest element).  Probabilities are rounded to fp16 (2^-11) for the
-// second product, and their fp32 values are what the row sum adds; the unfinished chunk's values meet probabilities
-// split in two bf16 parts (bf16 caches) or the same fp16 ones (fp16 caches).
-// Every warp keeps its own running maximum, sum and output; the warps of a CTA are joined in shared memory, the CTAs of
-// a split sequence through the workspace by a second kernel, in a fixed order.
-// What bounds it: 140 bytes of cache per token and head (d = 128) against 11 integer instructions per code word and
-// lane, half-rate on this machine: about 5.5 cycles of an SM's integer pipes per token and head, and 5.9 cycles of its
-// share of the memory bandwidth.
+// Work is counted in units of one chunk (32 tokens) of one KV head.  The units of the whole batch, sequence by sequence
+// and head by head, are cut into equal runs, up to four per resident warp, so ragged batches load every SM alike; the warps of
+// an SM take its runs in turn (the schedulers favour some warps: with one fixed share each, the last ones ended alone).
+// A run that covers a head's visible chunks alone writes the result, the others leave (output, maximum, sum) in the workspace,
+// which a second kernel joins in unit order: which warp did a run does not show in the result.  (One CTA per sequence,
+// head and share instead left the SMs 40 % idle on 32 sequences of 1500 to 4113 tokens.)
+// Both products run on the warp-level fp16 MMA with the cache as the 16-row operand and the queries (or the transposed
+// probabilities) as the 8-column operand, so the few rows of a decode step fill half a tile and nothing of the cache is
+// expanded twice.  A code becomes the fp16 number index-value * 2^-24 (a subnormal: the half-unit integer itself in the
+// low byte, the sign on top) without any conversion; the block's power-of-two scale multiplies the fp32 block sum.  bf16
+// queries are first scaled per row by a power of two into the range of fp16 (exact down to 2^-29 of the row's largest
+// element).  Probabilities are rounded to fp16 (2^-11) for the second product, and their fp32 values are what the row sum
+// adds; the unfinished chunk's values meet probabilities split in two bf16 parts (bf16 caches) or the same fp16 ones.
+// What bounds it: the integer (ALU) pipe, which takes two cycles per warp instruction.  A code word costs ten of them, a
+// block two; moves that the multiply-add pipe can do (left shifts) go there.  About 930 cycles of each SM quarter per chunk
+// against 760 for the chunk's 4480 bytes (d = 128) at the measured copy rate.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -35,34 +38,43 @@ struct Attention {
     uint8_t *o;
     int64_t ldo, hso;
     float *lse;                       // [rows][q_heads] or null
-    float *part;                      // [splits][rows][q_heads][d + 2] (split > 1): output, maximum (log2 units), sum
-    float scale, softcap, unit;       // unit: factor of the partial outputs
+    float *part;                      // partial results: of the warps' runs (rows kernel; see Runs), or of the splits
+                                      // [splits][rows][q_heads][d + 2] (chunk kernel): output, maximum (log2 units), sum
+    float scale, softcap;
     int q_heads, group, window, splits, row_tiles, odtype;
+    int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
+    uint32_t k16, k23;                // 2^4 and 2^23: left shifts as multiplications by operands the compiler does not see
 };
 
-constexpr int kRowWarps = 4;
 constexpr int kRowStages = 2;
+constexpr int kRunUnits = 8;          // units that make a further round of runs worth its joins
+__host__ __device__ constexpr int row_warps(int nt) { return nt == 1 ? 16 : 8; }    // warps of a CTA = of an SM, by registers
 
-__device__ __forceinline__ void expand_f16(uint32_t w, uint2 tb, uint32_t (&r)[4]) {
+__device__ __forceinline__ void expand_f16(uint32_t w, uint2 tb, uint32_t k16, uint32_t (&r)[4]) {
     const uint32_t sel = w & 0x77777777u;
     const uint32_t xa = prmt_b32(tb.x, tb.y, sel), xb = prmt_b32(tb.x, tb.y, sel >> 16);
-    const uint32_t odd = w & 0x80808080u, even = (w << 4) & 0x80808080u;   // signs of the odd / even nibbles, one per byte
+    const uint32_t odd = w & 0x80808080u, even = (w * k16) & 0x80808080u;   // signs of the odd / even nibbles, one per byte
     r[0] = prmt_b32(xa, even, 0x5240u);   // nibbles 0, 2 = elements 0, 1
     r[1] = prmt_b32(xa, odd, 0x5341u);    // nibbles 1, 3 = elements 2, 3
     r[2] = prmt_b32(xb, even, 0x7260u);   // nibbles 4, 6 = elements 4, 5
     r[3] = prmt_b32(xb, odd, 0x7361u);    // nibbles 5, 7 = elements 6, 7
 }
+// The same product without an accumulator in front.
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -89,29 +101,130 @@ __device__ __forceinline__ void store_out(const Attention &p, int64_t row, int h
     else *(__half *)o = __float2half_rn(v);
 }
 
+// The chunks a sequence's rows see, and how the batch's units are numbered: sequence by sequence, KV head by KV head,
+// chunk by chunk; a sequence with rows that see nothing counts one (empty) unit per head, so that its zeros are written.
+struct Visible {
+    int begin, end;                   // chunks; end > begin, or equal for the empty unit
+    int units;                        // per head
+};
+__device__ __forceinline__ Visible visible_of(const Sequence &s, int window) {
+    Visible v{0, 0, 0};
+    if (!s.ok || s.t == 0) return v;
+    v.begin = window ? max(0, s.kv - s.t - window + 1) / kChunk : 0;
+    v.end = max((s.kv + kChunk - 1) / kChunk, v.begin);
+    v.units = max(1, v.end - v.begin);
+    return v;
+}
+// Runs: the first `extra` of them have size + 1 units, the others size.  (Unit numbers fit 32 bits: the entry point bounds
+// n * kv_heads * chunks.)
+struct Runs {
+    uint32_t total, count, extra, size;
+    __device__ uint32_t begin(uint32_t w) const { return w * size + min(w, extra); }
+    __device__ uint32_t owner(uint32_t u) const {
+        const uint32_t big = extra * (size + 1u);
+        return u < big ? u / (size + 1u) : extra + (u - big) / size;
+    }
+};
+__device__ __forceinline__ Runs runs_of(uint32_t total, const Attention &p) {
+    const uint32_t most = (uint32_t)p.workers * min((uint32_t)p.rounds, max(1u, total / (uint32_t)(p.workers * kRunUnits)));
+    Runs r{total, min(most, max(1u, total)), 0, 0};
+    r.size = total / r.count;
+    r.extra = total - r.size * r.count;
+    return r;
+}
+// One sequence per lane, 32 at a time.  The first 32 stay in registers, which is the whole batch for most decode steps.
+struct Scan {
+    uint32_t in_front, mine, first;                               // of this lane's sequence among the first 32; the 32's sum
+};
+__device__ __forceinline__ Scan scan_group(const Attention &p, int lane, int b0) {
+    Scan s;
+    s.mine = b0 + lane < p.batch.n ? (uint32_t)visible_of(sequence_of(p.batch, b0 + lane), p.window).units * (uint32_t)p.pool.kv_heads : 0u;
+    uint32_t inc = s.mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    s.in_front = inc - s.mine;
+    s.first = __shfl_sync(0xffffffffu, inc, 31);
+    return s;
+}
+__device__ __forceinline__ uint32_t all_units(const Attention &p, int lane, Scan &s) {
+    s = scan_group(p, lane, 0);
+    uint32_t sum = s.first;
+    for (int b0 = 32; b0 < p.batch.n; b0 += 32) sum += scan_group(p, lane, b0).first;
+    return sum;
+}
+// The sequence that holds unit u, and the units in front of it.
+__device__ __forceinline__ int sequence_at(const Attention &p, int lane, const Scan &first, uint32_t u, uint32_t &before) {
+    Scan s = first;
+    uint32_t sum = 0;
+    int b0 = 0;
+    while (u >= sum + s.first && b0 + 32 < p.batch.n) {
+        sum += s.first;
+        b0 += 32;
+        s = scan_group(p, lane, b0);
+    }
+    const int l = __ffs(__ballot_sync(0xffffffffu, u < sum + s.in_front + s.mine)) - 1;
+    before = sum + __shfl_sync(0xffffffffu, s.in_front, l);
+    return b0 + l;
+}
+// The batch's units, and the units in front of sequence `upto`.
+__device__ __forceinline__ uint32_t units_before(const Attention &p, int lane, int upto, uint32_t &before) {
+    uint32_t sum = 0;
+    before = 0;
+    for (int b0 = 0; b0 < p.batch.n; b0 += 32) {
+        const Scan s = scan_group(p, lane, b0);
+        if (upto >= b0 && upto < b0 + 32) before = sum + __shfl_sync(0xffffffffu, s.in_front, upto - b0);
+        sum += s.first;
+    }
+    return sum;
+}
+// The partial results of run w: slot 2 w for the head that its first unit belongs to, 2 w + 1 for the head of its last unit.
+// Per slot the fragments, 4 floats per lane and step, then maximum and sum per row.
+template <int NB, int NT>
+__device__ __host__ constexpr int part_floats() { return NT * NB * 2 * 128 + 2 * 8 * NT; }
+
 template <int NB, int NT>
 struct RowSmem {
     static constexpr int D = 32 * NB, ROWS = 8 * NT;
-    static constexpr int stage = 35 * D;
-    static constexpr int ring = kRowWarps * kRowStages * stage;
-    static constexpr int joined = kRowWarps * ROWS * (D + 2) * 4;      // takes the ring's place at the end
-    static constexpr int body = ((ring > joined ? ring : joined) + 127) / 128 * 128;
-    static constexpr int table = body, bars = table + 128, words = bars + kRowWarps * kRowStages * 8, total = words + 16;
+    static constexpr int warps = row_warps(NT), stage = 35 * D, ring = warps * kRowStages * stage;
+    static constexpr int table = (ring + 127) / 128 * 128, bars = table + 128, words = bars + warps * kRowStages * 8, total = words + 16;
 };
 
+// Writes one head's rows from the fragments: this lane holds channels 32 b + 8 j + g of rows 8 nt + 2 t4 + i.
+template <int NB, int NT>
+__device__ __forceinline__ void store_rows(const Attention &p, const Sequence &s, int h, int n_rows, const float (&O)[NT][NB][2][4], const float (&m)[NT][2],
+                                           const float (&l)[NT][2], int g, int t4) {
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int r = 8 * nt + 2 * t4 + i;
+            if (r >= n_rows) continue;
+            const int64_t row = s.q0 + r / p.group;
+            const int head = h * p.group + r % p.group;
+            const float lr = l[nt][i], f = lr > 0.0f ? 8388608.0f / lr : (lr == 0.0f ? 0.0f : lr);
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) store_out(p, row, head, 32 * b + 8 * j + g, O[nt][b][j / 2][2 * (j % 2) + i] * f);
+            if (g == 0 && p.lse) p.lse[row * p.q_heads + head] = lr > 0.0f ? (m[nt][i] + log2f(lr)) * 0.6931471805599453f : (lr == 0.0f ? -INFINITY : lr);
+        }
+}
+
 template <int DT, int NB, int NT, bool CAP>
-__global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __grid_constant__ Attention p) {
+__global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(const __grid_constant__ Attention p) {
     using S = RowSmem<NB, NT>;
-    constexpr int D = S::D, ROWS = S::ROWS;
+    constexpr int D = S::D;
     extern __shared__ __align__(128) uint8_t smem[];
-    uint2 *table = (uint2 *)(smem + S::table);
     volatile uint32_t *flags = (volatile uint32_t *)(smem + S::words);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t4 = lane % 4;
-    if (threadIdx.x < 16) table[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
+    if (threadIdx.x < 16) ((uint2 *)(smem + S::table))[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
     if (threadIdx.x == 0) {
-        flags[0] = 0; flags[1] = 1; flags[2] = tc::kSpinLimit;
-        const uint32_t limit = g_debug_spin_limit;
-        if (limit) flags[2] = limit;
+        flags[0] = 0; flags[1] = 1;
+        flags[2] = g_debug_spin_limit ? g_debug_spin_limit : tc::kSpinLimit;
+        flags[3] = S::warps;                                      // the SM's next run: each warp begins with that of its own number
     }
     const uint32_t bar0 = tc::smem_u32(smem + S::bars) + warp * kRowStages * 8;
     if (lane == 0)
@@ -121,149 +234,194 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
     pdl_wait();
     pdl_release();
 
-    const int seq = blockIdx.z, h = blockIdx.y, rt = blockIdx.x % p.row_tiles, split = blockIdx.x / p.row_tiles;
-    const Sequence s = sequence_of(p.batch, seq);
-    if (!s.ok) {
-        if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
-        return;
-    }
-    const int r0 = rt * ROWS, n_rows = s.t * p.group;             // row = token * group + head of the group
-    if (r0 >= n_rows) return;
-    const int row_end = min(r0 + ROWS, n_rows);
-    // chunks that any row of the tile sees, and this split's share of them
-    const int first_pos = s.kv - s.t + r0 / p.group, last_pos = s.kv - s.t + (row_end - 1) / p.group;
-    const int seen_end = max(0, last_pos + 1);
-    const int seen_begin = p.window ? max(0, first_pos - p.window + 1) : 0;
-    const int c_lo = seen_begin / kChunk, c_hi = (seen_end + kChunk - 1) / kChunk;
-    const int per = (max(0, c_hi - c_lo) + p.splits - 1) / p.splits;
-    const int c_begin = c_lo + split * per, c_end = min(c_hi, c_begin + per);
-    const int full = s.kv / kChunk;                               // chunks whose values are stored in 4 bits
+    if (warp * gridDim.x + blockIdx.x >= (uint32_t)(p.workers * p.rounds)) return;
+    Scan first;
+    const uint32_t total = all_units(p, lane, first);
+    const Runs runs = runs_of(total, p);
+    if (blockIdx.x == 0 && warp == 0)                             // sequences with bad numbers have no units: told here
+        for (int b = lane; b < p.batch.n; b += 32)
+            if (!sequence_of(p.batch, b).ok) atomicOr(&g_status_word, kStatusIndex);
+    if (total == 0) return;
+    uint8_t *const ring = smem + warp * kRowStages * S::stage;
+    uint32_t loaded = 0, phase = 0;                               // bits per stage: a record is in flight or there; the barrier's parity
+    const int per_page = p.pool.chunks_per_page;
 
-    // queries: fragments of the 8-column operand, in fp16
-    uint32_t qf[NT][NB][4];
-    float mul[NT][2];                                             // column's factor from block sums to scores
-    int pos[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        const int r = r0 + 8 * nt + g;
-        const bool valid = r < n_rows;
-        const uint8_t *src = p.q + ((int64_t)(s.q0 + r / p.group) * p.ldq + (int64_t)(h * p.group + r % p.group) * p.hsq) * 2;
-        uint4 raw[NB];
-#pragma unroll
-        for (int b = 0; b < NB; b++) raw[b] = valid ? *(const uint4 *)(src + (32 * b + 8 * t4) * 2) : make_uint4(0, 0, 0, 0);
-        float qs = 1.0f;
-        if (DT == BD_BF16) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int b = 0; b < NB; b++) m = absmax_bf16x2(m, absmax_bf16x2(absmax_bf16x2(raw[b].x, raw[b].y), absmax_bf16x2(raw[b].z, raw[b].w)));
-            m = max(m & 0x7fffu, m >> 16 & 0x7fffu);
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            const int ex = min(max((int)(m >> 7), 27), 240);      // biased exponent of the row's largest element
-            const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - ex) << 23);
-            qs = __uint_as_float((uint32_t)(ex - 14) << 23);
-#pragma unroll
-            for (int b = 0; b < NB; b++) {
-                const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    qf[nt][b][i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
-            }
-        } else {
-#pragma unroll
-            for (int b = 0; b < NB; b++) { qf[nt][b][0] = raw[b].x; qf[nt][b][1] = raw[b].y; qf[nt][b][2] = raw[b].z; qf[nt][b][3] = raw[b].w; }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; i++) {                             // this lane's columns 2 t4 + i of the score fragments
-            const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
-            const float k = f * 8388608.0f * p.scale;
-            mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
-            const int rc = r0 + 8 * nt + 2 * t4 + i;
-            pos[nt][i] = rc < n_rows ? s.kv - s.t + rc / p.group : -1;
-        }
-    }
-    float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-#pragma unroll
-        for (int b = 0; b < NB; b++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) O[nt][b][i / 4][i % 4] = 0.0f;
-        m_run[nt][0] = m_run[nt][1] = -INFINITY;
-        l_run[nt][0] = l_run[nt][1] = 0.0f;
-    }
-
-    // the warp's chunks: c_begin + warp, + kRowWarps, ...; a record per stage
-    const int mine = c_begin + warp < c_end ? (c_end - c_begin - warp + kRowWarps - 1) / kRowWarps : 0;
-    uint8_t *ring = smem + warp * kRowStages * S::stage;
-    uint32_t loaded = 0;                                          // bit per stage: the record is in flight or there
-    auto fetch = [&](int i) {
-        const int st = i % kRowStages, c = c_begin + warp + i * kRowWarps;
-        const int64_t off = record_offset(p.pool, p.batch, seq, h, c);
-        if (off < 0) {
+  // run r is the SM r % gridDim's: heads of one sequence spread over the SMs
+  for (uint32_t turn = warp;;) {
+    const uint32_t run = turn * gridDim.x + blockIdx.x;
+    if (run >= runs.count) return;
+    if (lane == 0) turn = atomicAdd((uint32_t *)&flags[3], 1u);
+    turn = __shfl_sync(0xffffffffu, turn, 0);
+    const uint32_t u_begin = runs.begin(run);
+    const int n_units = (int)(runs.begin(run + 1) - u_begin);
+    uint32_t before;
+    // the place in the run that is worked on: sequence, head, chunk
+    int at = sequence_at(p, lane, first, u_begin, before);
+    Visible v = visible_of(sequence_of(p.batch, at), p.window);
+    int h = (int)((u_begin - before) / (uint32_t)v.units);
+    int c = v.begin + (int)(u_begin - before - (uint32_t)(h * v.units));
+    // the place whose record is fetched next, two units ahead; the page numbers come a page early
+    int a_at = at, a_h = h, a_c = c, a_in = 0, a_next = -1, fetched = 0;
+    Visible a_v = v;
+    const uint8_t *a_src = nullptr;                               // nullptr: a page number outside the pool
+    auto page_at = [&](int page) -> const uint8_t * {
+        if (page < 0 || page >= p.pool.pages) {
             if (lane == 0) atomicOr(&g_status_word, kStatusIndex);
-            loaded &= ~(1u << st);
+            return nullptr;
+        }
+        return p.pool.base + (((int64_t)page * p.pool.kv_heads + a_h) * per_page + a_in) * S::stage;
+    };
+    auto enter = [&]() {                                          // a head, from chunk a_c on
+        if (a_c >= a_v.end) { a_src = nullptr; return; }          // (the empty unit)
+        const int32_t *row = p.batch.table + (int64_t)a_at * p.batch.ld_table + a_c / per_page;
+        a_in = a_c % per_page;
+        a_src = page_at(row[0]);
+        a_next = a_c + per_page - a_in < a_v.end ? row[1] : -1;
+    };
+    auto fetch = [&]() {
+        const int st = fetched % kRowStages;
+        loaded = a_src ? loaded | 1u << st : loaded & ~(1u << st);
+        if (a_src && lane == 0) {
+            tc::mbar_expect_tx(bar0 + 8 * st, S::stage);
+            tc::bulk_load(tc::smem_u32(ring + st * S::stage), a_src, S::stage, bar0 + 8 * st);
+        }
+        if (++fetched == n_units) return;
+        if (++a_c < a_v.begin + a_v.units) {
+            if (++a_in < per_page) {
+                if (a_src) a_src += S::stage;
+            } else {
+                a_in = 0;
+                a_src = page_at(a_next);
+                if (a_c + per_page < a_v.end) a_next = p.batch.table[(int64_t)a_at * p.batch.ld_table + a_c / per_page + 1];
+            }
             return;
         }
-        loaded |= 1u << st;
-        if (lane == 0) {
-            tc::mbar_expect_tx(bar0 + 8 * st, S::stage);
-            tc::bulk_load(tc::smem_u32(ring + st * S::stage), p.pool.base + off, S::stage, bar0 + 8 * st);
+        if (++a_h == p.pool.kv_heads) {
+            a_h = 0;
+            do {
+                a_at++;
+                a_v = visible_of(sequence_of(p.batch, a_at), p.window);
+            } while (a_v.units == 0);
         }
+        a_c = a_v.begin;
+        enter();
     };
-    uint32_t phase = 0;                                           // bit per stage
-    for (int i = 0; i < kRowStages && i < mine; i++) fetch(i);
-    for (int i = 0; i < mine; i++) {
-        const int st = i % kRowStages, c = c_begin + warp + i * kRowWarps;
+    enter();
+    for (int i = 0; i < kRowStages && i < n_units; i++) fetch();
+
+    uint32_t qf[NT][NB][4];                                       // queries: fragments of the 8-column operand, in fp16
+    float mul[NT][2];                                             // column's factor from block sums to scores
+    int pos[NT][2];
+    float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
+    Sequence s;
+    int n_rows = 0, first_pos = 0, last_pos = 0, full = 0;
+    bool starts_head = true;                                      // this piece begins at the head's first unit
+    for (int unit = 0; unit < n_units; unit++) {
+        if (unit == 0 || c == v.begin) {
+            // ---- a head begins (or the run does, inside one) ----
+            s = sequence_of(p.batch, at);
+            n_rows = s.t * p.group;
+            first_pos = s.kv - s.t;
+            last_pos = s.kv - 1;
+            full = s.kv / kChunk;
+            starts_head = c == v.begin;
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                const int r = 8 * nt + g;
+                const bool valid = r < n_rows;
+                const uint8_t *src = p.q + ((int64_t)(s.q0 + r / p.group) * p.ldq + (int64_t)(h * p.group + r % p.group) * p.hsq) * 2;
+                uint4 raw[NB];
+#pragma unroll
+                for (int b = 0; b < NB; b++) raw[b] = valid ? *(const uint4 *)(src + (32 * b + 8 * t4) * 2) : make_uint4(0, 0, 0, 0);
+                float qs = 1.0f;
+                if (DT == BD_BF16) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int b = 0; b < NB; b++) m = absmax_bf16x2(m, absmax_bf16x2(absmax_bf16x2(raw[b].x, raw[b].y), absmax_bf16x2(raw[b].z, raw[b].w)));
+                    m = max(m & 0x7fffu, m >> 16 & 0x7fffu);
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                    const int ex = min(max((int)(m >> 7), 27), 240);      // biased exponent of the row's largest element
+                    const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - ex) << 23);
+                    qs = __uint_as_float((uint32_t)(ex - 14) << 23);
+#pragma unroll
+                    for (int b = 0; b < NB; b++) {
+                        const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
+#pragma unroll
+                        for (int i = 0; i < 4; i++) qf[nt][b][i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < NB; b++) { qf[nt][b][0] = raw[b].x; qf[nt][b][1] = raw[b].y; qf[nt][b][2] = raw[b].z; qf[nt][b][3] = raw[b].w; }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
+                    const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
+                    const float k = f * 8388608.0f * p.scale;
+                    mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
+                    const int rc = 8 * nt + 2 * t4 + i;
+                    pos[nt][i] = rc < n_rows ? first_pos + rc / p.group : -1;
+                    m_run[nt][i] = -INFINITY;
+                    l_run[nt][i] = 0.0f;
+                }
+#pragma unroll
+                for (int b = 0; b < NB; b++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) O[nt][b][i / 4][i % 4] = 0.0f;
+            }
+        }
+        const int st = unit % kRowStages;
         const uint8_t *rec = ring + st * S::stage;
-        const bool there = loaded >> st & 1u;
-        if (there) {
-            if (!tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags)) break;
+        if (loaded >> st & 1u) {
+            if (!tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags)) return;   // (status word; this warp's later results stay unwritten)
             phase ^= 1u << st;
             __syncwarp();
-            // ---- scores of 32 tokens ----
-            float sc[NT][2][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                for (int x = 0; x < 8; x++) sc[nt][x / 4][x % 4] = 0.0f;
-            uint32_t scl[4], idw[4];
-            auto load_entries = [&](int64_t scales, int64_t ids) {   // per row j: NB scale bytes, NB id nibbles
+            // scale bytes of the lane's four rows (a word per row, a byte per tile) and 8 * id as bytes, likewise
+            uint32_t scl[4], ide[4];
+            auto load_entries = [&](int64_t scales, int64_t ids) {
                 if (NB == 4) {
                     const uint4 u = *(const uint4 *)(rec + scales + 16 * g);
                     scl[0] = u.x; scl[1] = u.y; scl[2] = u.z; scl[3] = u.w;
                     const uint2 v = *(const uint2 *)(rec + ids + 8 * g);
-                    idw[0] = v.x; idw[1] = v.x >> 16; idw[2] = v.y; idw[3] = v.y >> 16;
+                    ide[0] = v.x * 8u & 0x78787878u;              // even tiles of rows j = 0, 1: bytes 2 j + b / 2
+                    ide[1] = v.x >> 1 & 0x78787878u;              // odd tiles
+                    ide[2] = v.y * 8u & 0x78787878u;
+                    ide[3] = v.y >> 1 & 0x78787878u;
                 } else {
                     const uint2 u = *(const uint2 *)(rec + scales + 8 * g);
                     scl[0] = u.x; scl[1] = u.x >> 16; scl[2] = u.y; scl[3] = u.y >> 16;
                     const uint32_t v = *(const uint32_t *)(rec + ids + 4 * g);
-                    idw[0] = v; idw[1] = v >> 8; idw[2] = v >> 16; idw[3] = v >> 24;
+                    ide[0] = v * 8u & 0x78787878u;                // even tiles of row j: byte j
+                    ide[1] = v >> 1 & 0x78787878u;
                 }
             };
+            auto table_of = [&](int j, int b) {
+                const uint32_t x = NB == 4 ? ide[2 * (j / 2) + b % 2] : ide[b % 2];
+                const int byte = NB == 4 ? 2 * (j % 2) + b / 2 : j;
+                return *(const uint2 *)(smem + S::table + prmt_b32(x, 0u, 0x4440u + byte));
+            };
+            auto factor_of = [&](int j, int b) { return __uint_as_float(prmt_b32(scl[j], 0u, 0x4440u + b) * p.k23); };   // 2^e (scale byte 0: below 2^-126)
+            float sc[NT][2][4];
             load_entries(key_scales(D), key_ids(D));
 #pragma unroll
             for (int b = 0; b < NB; b++) {
                 const uint4 w4 = *(const uint4 *)(rec + b * 512 + lane * 16);
                 const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
                 uint32_t a[4][4];
-                float f[4];
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    expand_f16(w[j], table[idw[j] >> (4 * b) & 15u], a[j]);
-                    f[j] = __uint_as_float((scl[j] >> (8 * b) & 255u) << 23);     // 2^e (scale byte 0: nothing but zeros or 2^-127)
-                }
+                for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), p.k16, a[j]);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                     for (int x = 0; x < 2; x++) {
-                        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], qf[nt][b][0], qf[nt][b][1]);
+                        float acc[4];
+                        mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], qf[nt][b][0], qf[nt][b][1]);
                         mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], qf[nt][b][2], qf[nt][b][3]);
-                        sc[nt][x][0] = fmaf(acc[0], f[2 * x], sc[nt][x][0]);
-                        sc[nt][x][1] = fmaf(acc[1], f[2 * x], sc[nt][x][1]);
-                        sc[nt][x][2] = fmaf(acc[2], f[2 * x + 1], sc[nt][x][2]);
-                        sc[nt][x][3] = fmaf(acc[3], f[2 * x + 1], sc[nt][x][3]);
+                        const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
+                        sc[nt][x][0] = b ? fmaf(acc[0], f0, sc[nt][x][0]) : acc[0] * f0;
+                        sc[nt][x][1] = b ? fmaf(acc[1], f0, sc[nt][x][1]) : acc[1] * f0;
+                        sc[nt][x][2] = b ? fmaf(acc[2], f1, sc[nt][x][2]) : acc[2] * f1;
+                        sc[nt][x][3] = b ? fmaf(acc[3], f1, sc[nt][x][3]) : acc[3] * f1;
                     }
             }
             // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
@@ -277,7 +435,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    float x[4], top = -INFINITY;
+                    float x[4];
 #pragma unroll
                     for (int j = 0; j < 4; j++) {
                         x[j] = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
@@ -286,8 +444,8 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
                             const int tok = tok0 + 2 * j;
                             if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) x[j] = -INFINITY;
                         }
-                        top = fmaxf(top, x[j]);
                     }
+                    float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -324,23 +482,20 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
                     const uint4 w4 = *(const uint4 *)(rec + value_codes(D) + b * 512 + lane * 16);
                     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
                     uint32_t a[4][4];
-                    float f[4];
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        expand_f16(w[j], table[idw[j] >> (4 * b) & 15u], a[j]);
-                        f[j] = __uint_as_float((scl[j] >> (8 * b) & 255u) << 23);
-                    }
+                    for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), p.k16, a[j]);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                         for (int x = 0; x < 2; x++) {
-                            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                            mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
+                            float acc[4];
+                            mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
                             mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
-                            O[nt][b][x][0] = fmaf(acc[0], f[2 * x], O[nt][b][x][0]);
-                            O[nt][b][x][1] = fmaf(acc[1], f[2 * x], O[nt][b][x][1]);
-                            O[nt][b][x][2] = fmaf(acc[2], f[2 * x + 1], O[nt][b][x][2]);
-                            O[nt][b][x][3] = fmaf(acc[3], f[2 * x + 1], O[nt][b][x][3]);
+                            const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
+                            O[nt][b][x][0] = fmaf(acc[0], f0, O[nt][b][x][0]);
+                            O[nt][b][x][1] = fmaf(acc[1], f0, O[nt][b][x][1]);
+                            O[nt][b][x][2] = fmaf(acc[2], f1, O[nt][b][x][2]);
+                            O[nt][b][x][3] = fmaf(acc[3], f1, O[nt][b][x][3]);
                         }
                 }
             } else {
@@ -359,29 +514,26 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
                             pf[nt][j] = transpose8x8(pack_f16(a, b));
                         }
                     }
-                const int slot = p.batch.slot[seq];
+                const int slot = p.batch.slot[at];
                 const bool slot_ok = slot >= 0 && slot < p.pool.slots;
                 if (!slot_ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
                 const uint16_t *tail = (const uint16_t *)p.pool.tail + tail_offset(p.pool, slot_ok ? slot : 0, h, c * kChunk);
                 const int left = slot_ok ? s.kv - c * kChunk : 0;
-#pragma unroll 1
+#pragma unroll
                 for (int b = 0; b < NB; b++) {
                     uint32_t a[4][4];
 #pragma unroll
                     for (int j = 0; j < 4; j++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const int tok = 8 * t4 + 2 * e, ch = 32 * b + 8 * j + g;
-                            const uint32_t x = tok < left ? tail[tok * D + ch] : 0u, y = tok + 1 < left ? tail[(tok + 1) * D + ch] : 0u;
-                            a[j][e] = x | y << 16;
+                        for (int e = 0; e < 4; e++) {             // rows 2 a + i of the 8 x 8 tile: tokens 8 a + 2 e + i
+                            const int tok = 8 * (g / 2) + 2 * e + g % 2;
+                            a[j][e] = transpose8x8(tok < left ? *(const uint32_t *)(tail + tok * D + 32 * b + 8 * j + 2 * t4) : 0u);
                         }
-                    float add[NT][2][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                         for (int x = 0; x < 2; x++) {
-                            float (&acc)[4] = add[nt][x];
-                            acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
+                            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                             if (DT == BD_BF16) {
                                 mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
                                 mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
@@ -391,66 +543,134 @@ __global__ void __launch_bounds__(32 * kRowWarps) attention_rows_kernel(const __
                                 mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
                                 mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
                             }
+#pragma unroll
+                            for (int y = 0; y < 4; y++) O[nt][b][x][y] = fmaf(acc[y], 1.0f / 8388608.0f, O[nt][b][x][y]);
                         }
-#pragma unroll
-                    for (int bb = 0; bb < NB; bb++)              // (b is a run-time index here: registers are picked by comparison)
-                        if (bb == b)
-#pragma unroll
-                            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                for (int x = 0; x < 8; x++) O[nt][bb][x / 4][x % 4] = fmaf(add[nt][x / 4][x % 4], 1.0f / 8388608.0f, O[nt][bb][x / 4][x % 4]);
                 }
             }
         }
         __syncwarp();                                             // every lane is done with the stage
-        if (i + kRowStages < mine) fetch(i + kRowStages);
-    }
-    // ---- join the warps ----
-    __syncthreads();
-    if (flags[0]) return;                                         // a wait ran out (status word): nothing is written
-    float *jo = (float *)smem, *jm = jo + kRowWarps * ROWS * D, *jl = jm + kRowWarps * ROWS;
+        if (fetched < n_units) fetch();
+        const bool ends_head = c + 1 == v.begin + v.units;
+        if (ends_head || unit + 1 == n_units) {
+            // ---- the piece is done: the head's result, or a part of it ----
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++)
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    float &l = l_run[nt][i];
+                    l += __shfl_xor_sync(0xffffffffu, l, 4);
+                    l += __shfl_xor_sync(0xffffffffu, l, 8);
+                    l += __shfl_xor_sync(0xffffffffu, l, 16);
+                }
+            if (starts_head && ends_head) {
+                store_rows<NB, NT>(p, s, h, n_rows, O, m_run, l_run, g, t4);
+            } else {
+                // the piece at the run's start has slot 0; one that begins a head later in the run is the run's last: slot 1
+                const bool at_start = unit <= c - v.begin;
+                float *to = p.part + (int64_t)(2 * run + (at_start ? 0 : 1)) * part_floats<NB, NT>();
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    if (8 * nt + 2 * t4 < n_rows)
+#pragma unroll
+                        for (int b = 0; b < NB; b++)
+#pragma unroll
+                            for (int x = 0; x < 2; x++) *(float4 *)(to + (((nt * NB + b) * 2 + x) * 32 + lane) * 4) = make_float4(O[nt][b][x][0], O[nt][b][x][1], O[nt][b][x][2], O[nt][b][x][3]);
+                    if (g == 0)
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            float *ml = to + NT * NB * 2 * 128 + 2 * (8 * nt + 2 * t4 + i);
+                            ml[0] = m_run[nt][i];
+                            ml[1] = l_run[nt][i];
+                        }
+                }
+            }
+        }
+        if (ends_head && unit + 1 < n_units) {
+            if (++h == p.pool.kv_heads) {
+                h = 0;
+                do {
+                    at++;
+                    v = visible_of(sequence_of(p.batch, at), p.window);
+                } while (v.units == 0);
+            }
+            c = v.begin;
+        } else {
+            c++;
+        }
+    }
+  }
+}
+
+// Joins the parts of heads that several runs share, in unit order.  A warp per sequence, KV head and tile of 32 channels.
+template <int NB, int NT>
+__global__ void __launch_bounds__(32 * NB) attention_rows_join_kernel(const __grid_constant__ Attention p) {
+    const int b = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t4 = lane % 4, h = blockIdx.x, seq = blockIdx.y;
+    pdl_wait();
+    pdl_release();
+    const Sequence s = sequence_of(p.batch, seq);
+    const Visible v = visible_of(s, p.window);
+    if (v.units <= 1) return;                                     // nothing to do, or never shared
+    uint32_t before;
+    const uint32_t total = units_before(p, lane, seq, before);
+    const Runs runs = runs_of(total, p);
+    const uint32_t u0 = before + (uint32_t)(h * v.units), u1 = u0 + (uint32_t)v.units;
+    const int w0 = (int)runs.owner(u0), w1 = (int)runs.owner(u1 - 1);
+    if (w0 == w1) return;
+    const int n_rows = s.t * p.group;
+    constexpr int kAhead = 8;                                     // parts whose loads are in flight together
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        if (8 * nt + 2 * t4 >= n_rows) continue;
+        const int ml = NT * NB * 2 * 128 + 2 * (8 * nt + 2 * t4);
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, O[2][4] = {};
+        for (int w = w0; w <= w1; w += kAhead) {
+            float4 x[kAhead], a[kAhead], c[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                // (a run that is not there repeats the last one, and counts as nothing)
+                const int ww = min(w + k, w1);
+                const float *part = p.part + (int64_t)(2 * ww + (runs.begin(ww) >= u0 ? 0 : 1)) * part_floats<NB, NT>();
+                x[k] = *(const float4 *)(part + ml);
+                a[k] = *(const float4 *)(part + (((nt * NB + b) * 2 + 0) * 32 + lane) * 4);
+                c[k] = *(const float4 *)(part + (((nt * NB + b) * 2 + 1) * 32 + lane) * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                float top = m[i];
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) top = fmaxf(top, i ? x[k].z : x[k].x);
+                const float base = top == -INFINITY ? 0.0f : top, keep = fast_exp2(m[i] - base);
+                m[i] = top;
+                l[i] *= keep;
+#pragma unroll
+                for (int j = 0; j < 4; j++) O[j / 2][2 * (j % 2) + i] *= keep;
+#pragma unroll
+                for (int k = 0; k < kAhead; k++) {
+                    const float f = w + k <= w1 ? fast_exp2((i ? x[k].z : x[k].x) - base) : 0.0f;
+                    l[i] = fmaf(i ? x[k].w : x[k].y, f, l[i]);
+                    O[0][i] = fmaf(i ? a[k].y : a[k].x, f, O[0][i]);
+                    O[0][2 + i] = fmaf(i ? a[k].w : a[k].z, f, O[0][2 + i]);
+                    O[1][i] = fmaf(i ? c[k].y : c[k].x, f, O[1][i]);
+                    O[1][2 + i] = fmaf(i ? c[k].w : c[k].z, f, O[1][2 + i]);
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            float l = l_run[nt][i];
-            l += __shfl_xor_sync(0xffffffffu, l, 4);
-            l += __shfl_xor_sync(0xffffffffu, l, 8);
-            l += __shfl_xor_sync(0xffffffffu, l, 16);
-            const int r = warp * ROWS + 8 * nt + 2 * t4 + i;
-            if (g == 0) { jm[r] = m_run[nt][i]; jl[r] = l; }
+            const int r = 8 * nt + 2 * t4 + i;
+            if (r >= n_rows) continue;
+            const int64_t row = s.q0 + r / p.group;
+            const int head = h * p.group + r % p.group;
+            const float f = l[i] > 0.0f ? 8388608.0f / l[i] : (l[i] == 0.0f ? 0.0f : l[i]);
 #pragma unroll
-            for (int b = 0; b < NB; b++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) jo[r * D + 32 * b + 8 * j + g] = O[nt][b][j / 2][2 * (j % 2) + i];
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < (row_end - r0) * D; i += blockDim.x) {
-        const int r = i / D, ch = i % D;
-        float m = -INFINITY, l = 0.0f, o = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kRowWarps; w++) m = fmaxf(m, jm[w * ROWS + r]);
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int w = 0; w < kRowWarps; w++) {
-            const float f = fast_exp2(jm[w * ROWS + r] - base);
-            l = fmaf(jl[w * ROWS + r], f, l);
-            o = fmaf(jo[(w * ROWS + r) * D + ch], f, o);
-        }
-        const int64_t row = s.q0 + (r0 + r) / p.group;
-        const int head = h * p.group + (r0 + r) % p.group;
-        if (p.splits == 1) {
-            store_out(p, row, head, ch, l > 0.0f ? o * (8388608.0f / l) : (l == 0.0f ? 0.0f : l));
-            if (ch == 0 && p.lse) p.lse[row * p.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
-        } else {
-            float *to = p.part + (((int64_t)split * p.batch.rows + row) * p.q_heads + head) * (D + 2);
-            to[ch] = o;
-            if (ch == 0) { to[D] = m; to[D + 1] = l; }
+            for (int j = 0; j < 4; j++) store_out(p, row, head, 32 * b + 8 * j + g, O[j / 2][2 * (j % 2) + i] * f);
+            if (b == 0 && g == 0 && p.lse) p.lse[row * p.q_heads + head] = l[i] > 0.0f ? (m[i] + log2f(l[i])) * 0.6931471805599453f : (l[i] == 0.0f ? -INFINITY : l[i]);
         }
     }
 }
 
-// Joins the splits of a row, in split order.  A warp per row and head.
+// Joins the splits of a row (chunk kernel), in split order.  A warp per row and head.
 template <int D>
 __global__ void __launch_bounds__(128) attention_join_kernel(const __grid_constant__ Attention p) {
     pdl_wait();
@@ -472,7 +692,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const __grid_consta
         for (int x = 0; x < D / 32; x++) o[x] = fmaf(src[k * step + lane + 32 * x], f, o[x]);
     }
 #pragma unroll
-    for (int x = 0; x < D / 32; x++) store_out(p, row, head, lane + 32 * x, l > 0.0f ? o[x] * (p.unit / l) : (l == 0.0f ? 0.0f : l));
+    for (int x = 0; x < D / 32; x++) store_out(p, row, head, lane + 32 * x, l > 0.0f ? o[x] / l : (l == 0.0f ? 0.0f : l));
     if (lane == 0 && p.lse) p.lse[row * p.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
 }
 
