@@ -449,11 +449,12 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
     r.rounds = (int)std::min<int64_t>(4, std::max<int64_t>(1, units / ((int64_t)r.workers * pg::kRunUnits)));
     return r;
 }
+size_t row_parts_offset(const bd_paged_batch *b) { return ((size_t)(b->n + 1) * sizeof(uint32_t) + 255) / 256 * 256; }   // behind the sequences' unit numbers
 size_t attention_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
     const AttentionPlan r = attention_plan(c, b, q_heads);
     if (r.chunk) return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
     const int floats = c->head_dim == 128 ? (r.wide ? pg::part_floats<4, 2>() : pg::part_floats<4, 1>()) : (r.wide ? pg::part_floats<2, 2>() : pg::part_floats<2, 1>());
-    return (size_t)r.workers * (size_t)r.rounds * 2 * (size_t)floats * sizeof(float);
+    return row_parts_offset(b) + (size_t)r.workers * (size_t)r.rounds * 2 * (size_t)floats * sizeof(float);
 }
 template <typename Kernel>
 bd_status allow_smem(Kernel kernel, int bytes, bool (&configured)[kMaxDevices]) {
@@ -472,7 +473,7 @@ bd_status launch_rows_kernel(const pg::Attention &a, cudaStream_t st) {
     const bd_status s = allow_smem(pg::attention_rows_kernel<DT, NB, NT, CAP>, smem, configured);
     if (s) return s;
     launch_serialized(pg::attention_rows_kernel<DT, NB, NT, CAP>, dim3((unsigned)std::min(148, a.workers)), 32 * warps, smem, st, a);
-    launch_serialized(pg::attention_rows_join_kernel<NB, NT>, dim3((unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 32 * NB, 0, st, a);
+    launch_serialized(pg::attention_rows_join_kernel<NB, NT>, dim3((unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 64 * NB * NT, 0, st, a);
     return BD_OK;
 }
 template <int DT, int NB, int NT>
@@ -1458,6 +1459,10 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.k16 = 16u; a.k23 = 1u << 23;
     cudaStream_t st = (cudaStream_t)stream;
     if (!plan.chunk) {
+        for (int k = 0; k < 4; k++) a.by_runs[k] = make_fast_div((uint32_t)(plan.workers * (k + 1)));
+        a.by_page = make_fast_div((uint32_t)a.pool.chunks_per_page);
+        a.head_of_part = (uint32_t *)workspace;
+        a.part = (float *)((char *)workspace + row_parts_offset(b));
         s = c->dtype == BD_BF16 ? launch_rows_dtype<BD_BF16>(a, plan.wide, st) : launch_rows_dtype<BD_F16>(a, plan.wide, st);
         return s ? s : launch_result(2);
     }

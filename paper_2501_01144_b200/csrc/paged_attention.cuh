@@ -43,6 +43,8 @@ struct Attention {
     float scale, softcap;
     int q_heads, group, window, splits, row_tiles, odtype;
     int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
+    FastDiv by_runs[4], by_page;      // division by workers * (1 .. 4), by the chunks of a page
+    uint32_t *head_of_part;           // rows kernel: [n + 1] units in front of each sequence, then all units
     uint32_t k16, k23;                // 2^4 and 2^23: left shifts as multiplications by operands the compiler does not see
 };
 
@@ -126,9 +128,12 @@ struct Runs {
     }
 };
 __device__ __forceinline__ Runs runs_of(uint32_t total, const Attention &p) {
-    const uint32_t most = (uint32_t)p.workers * min((uint32_t)p.rounds, max(1u, total / (uint32_t)(p.workers * kRunUnits)));
-    Runs r{total, min(most, max(1u, total)), 0, 0};
-    r.size = total / r.count;
+    const uint32_t round = (uint32_t)p.workers * kRunUnits;
+    int k = 1;                                                    // rounds of runs
+    while (k < p.rounds && total >= (uint32_t)(k + 1) * round) k++;
+    if (total <= (uint32_t)p.workers) return Runs{total, total, 0, 1};
+    Runs r{total, (uint32_t)(p.workers * k), 0, 0};
+    r.size = fast_div(total, p.by_runs[k - 1]);
     r.extra = total - r.size * r.count;
     return r;
 }
@@ -168,17 +173,6 @@ __device__ __forceinline__ int sequence_at(const Attention &p, int lane, const S
     const int l = __ffs(__ballot_sync(0xffffffffu, u < sum + s.in_front + s.mine)) - 1;
     before = sum + __shfl_sync(0xffffffffu, s.in_front, l);
     return b0 + l;
-}
-// The batch's units, and the units in front of sequence `upto`.
-__device__ __forceinline__ uint32_t units_before(const Attention &p, int lane, int upto, uint32_t &before) {
-    uint32_t sum = 0;
-    before = 0;
-    for (int b0 = 0; b0 < p.batch.n; b0 += 32) {
-        const Scan s = scan_group(p, lane, b0);
-        if (upto >= b0 && upto < b0 + 32) before = sum + __shfl_sync(0xffffffffu, s.in_front, upto - b0);
-        sum += s.first;
-    }
-    return sum;
 }
 // The partial results of run w: slot 2 w for the head that its first unit belongs to, 2 w + 1 for the head of its last unit.
 // Per slot the fragments, 4 floats per lane and step, then maximum and sum per row.
@@ -241,6 +235,16 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
     if (blockIdx.x == 0 && warp == 0)                             // sequences with bad numbers have no units: told here
         for (int b = lane; b < p.batch.n; b += 32)
             if (!sequence_of(p.batch, b).ok) atomicOr(&g_status_word, kStatusIndex);
+    // the join kernel finds its parts with these
+    if (blockIdx.x == gridDim.x - 1 && warp == 0) {
+        uint32_t sum = 0;
+        for (int b0 = 0; b0 < p.batch.n; b0 += 32) {
+            const Scan sc = b0 ? scan_group(p, lane, b0) : first;
+            if (b0 + lane < p.batch.n) p.head_of_part[b0 + lane] = sum + sc.in_front;
+            sum += sc.first;
+        }
+        if (lane == 0) p.head_of_part[p.batch.n] = sum;
+    }
     if (total == 0) return;
     uint8_t *const ring = smem + warp * kRowStages * S::stage;
     uint32_t loaded = 0, phase = 0;                               // bits per stage: a record is in flight or there; the barrier's parity
@@ -273,8 +277,8 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
     };
     auto enter = [&]() {                                          // a head, from chunk a_c on
         if (a_c >= a_v.end) { a_src = nullptr; return; }          // (the empty unit)
-        const int32_t *row = p.batch.table + (int64_t)a_at * p.batch.ld_table + a_c / per_page;
-        a_in = a_c % per_page;
+        const int32_t *row = p.batch.table + (int64_t)a_at * p.batch.ld_table + fast_div(a_c, p.by_page);
+        a_in = a_c - (int)fast_div(a_c, p.by_page) * per_page;
         a_src = page_at(row[0]);
         a_next = a_c + per_page - a_in < a_v.end ? row[1] : -1;
     };
@@ -292,7 +296,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
             } else {
                 a_in = 0;
                 a_src = page_at(a_next);
-                if (a_c + per_page < a_v.end) a_next = p.batch.table[(int64_t)a_at * p.batch.ld_table + a_c / per_page + 1];
+                if (a_c + per_page < a_v.end) a_next = p.batch.table[(int64_t)a_at * p.batch.ld_table + fast_div(a_c, p.by_page) + 1];
             }
             return;
         }
@@ -602,71 +606,98 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
   }
 }
 
-// Joins the parts of heads that several runs share, in unit order.  A warp per sequence, KV head and tile of 32 channels.
+// Joins the parts of heads that several runs share, in unit order.  A CTA per sequence and KV head; thread = the fragment
+// piece (row group nt, channels b, half x, lane) that it adds up, the rows' weights come from shared memory.
 template <int NB, int NT>
-__global__ void __launch_bounds__(32 * NB) attention_rows_join_kernel(const __grid_constant__ Attention p) {
-    const int b = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t4 = lane % 4, h = blockIdx.x, seq = blockIdx.y;
+__global__ void __launch_bounds__(64 * NB * NT) attention_rows_join_kernel(const __grid_constant__ Attention p) {
+    constexpr int ROWS = 8 * NT, kParts = 64, kAhead = 8, THREADS = 64 * NB * NT;
+    __shared__ float2 ml[kParts][ROWS];                           // maximum and sum, then weight and weighted sum
+    __shared__ float keep[ROWS], top[ROWS], sums[ROWS];
+    const int h = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x % 32, t4 = lane % 4, g = lane / 4;
+    const int piece = threadIdx.x / 32, nt = piece / (2 * NB), b = piece / 2 % NB, x = piece % 2;
     pdl_wait();
     pdl_release();
+    const uint32_t total = p.head_of_part[p.batch.n], before = p.head_of_part[seq];
     const Sequence s = sequence_of(p.batch, seq);
     const Visible v = visible_of(s, p.window);
     if (v.units <= 1) return;                                     // nothing to do, or never shared
-    uint32_t before;
-    const uint32_t total = units_before(p, lane, seq, before);
     const Runs runs = runs_of(total, p);
     const uint32_t u0 = before + (uint32_t)(h * v.units), u1 = u0 + (uint32_t)v.units;
     const int w0 = (int)runs.owner(u0), w1 = (int)runs.owner(u1 - 1);
     if (w0 == w1) return;
-    const int n_rows = s.t * p.group;
-    constexpr int kAhead = 8;                                     // parts whose loads are in flight together
+    const int n_rows = s.t * p.group, first_slot = runs.begin(w0) >= u0 ? 0 : 1;   // (only the first run can begin in front of the head)
+    auto part_of = [&](int w) { return p.part + (int64_t)(2 * w + (w == w0 ? first_slot : 0)) * part_floats<NB, NT>(); };
+    const bool active = 8 * nt + 2 * t4 < n_rows;
+    float O[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int base = w0; base <= w1; base += kParts) {
+        const int n = min(kParts, w1 - base + 1);
+        float4 ahead[kAhead];                                     // the first parts' values, in flight while the weights are made
+        auto load = [&](int k) { return active && k < n ? *(const float4 *)(part_of(base + k) + (piece * 32 + lane) * 4) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
 #pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        if (8 * nt + 2 * t4 >= n_rows) continue;
-        const int ml = NT * NB * 2 * 128 + 2 * (8 * nt + 2 * t4);
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, O[2][4] = {};
-        for (int w = w0; w <= w1; w += kAhead) {
-            float4 x[kAhead], a[kAhead], c[kAhead];
+        for (int k = 0; k < kAhead; k++) ahead[k] = load(k);
+        for (int i = threadIdx.x; i < n * ROWS; i += THREADS) {
+            const int r = i % ROWS;
+            if (r < n_rows) ml[i / ROWS][r] = *(const float2 *)(part_of(base + i / ROWS) + NT * NB * 2 * 128 + 2 * r);
+        }
+        __syncthreads();
+        for (int r = piece; r < n_rows; r += THREADS / 32) {      // a warp per row
+            const float2 a = lane < n ? ml[lane][r] : make_float2(-INFINITY, 0.0f), c = lane + 32 < n ? ml[lane + 32][r] : make_float2(-INFINITY, 0.0f);
+            const float old = base == w0 ? -INFINITY : top[r];
+            float m = fmaxf(fmaxf(a.x, c.x), old);
 #pragma unroll
-            for (int k = 0; k < kAhead; k++) {
-                // (a run that is not there repeats the last one, and counts as nothing)
-                const int ww = min(w + k, w1);
-                const float *part = p.part + (int64_t)(2 * ww + (runs.begin(ww) >= u0 ? 0 : 1)) * part_floats<NB, NT>();
-                x[k] = *(const float4 *)(part + ml);
-                a[k] = *(const float4 *)(part + (((nt * NB + b) * 2 + 0) * 32 + lane) * 4);
-                c[k] = *(const float4 *)(part + (((nt * NB + b) * 2 + 1) * 32 + lane) * 4);
-            }
+            for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            const float zero = m == -INFINITY ? 0.0f : m, fa = fast_exp2(a.x - zero), fc = fast_exp2(c.x - zero);
+            float l = fmaf(a.y, fa, c.y * fc);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                float top = m[i];
-#pragma unroll
-                for (int k = 0; k < kAhead; k++) top = fmaxf(top, i ? x[k].z : x[k].x);
-                const float base = top == -INFINITY ? 0.0f : top, keep = fast_exp2(m[i] - base);
-                m[i] = top;
-                l[i] *= keep;
-#pragma unroll
-                for (int j = 0; j < 4; j++) O[j / 2][2 * (j % 2) + i] *= keep;
-#pragma unroll
-                for (int k = 0; k < kAhead; k++) {
-                    const float f = w + k <= w1 ? fast_exp2((i ? x[k].z : x[k].x) - base) : 0.0f;
-                    l[i] = fmaf(i ? x[k].w : x[k].y, f, l[i]);
-                    O[0][i] = fmaf(i ? a[k].y : a[k].x, f, O[0][i]);
-                    O[0][2 + i] = fmaf(i ? a[k].w : a[k].z, f, O[0][2 + i]);
-                    O[1][i] = fmaf(i ? c[k].y : c[k].x, f, O[1][i]);
-                    O[1][2 + i] = fmaf(i ? c[k].w : c[k].z, f, O[1][2 + i]);
-                }
+            for (int d = 16; d; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+            if (lane < n) ml[lane][r].x = fa;
+            if (lane + 32 < n) ml[lane + 32][r].x = fc;
+            if (lane == 0) {
+                const float k = fast_exp2(old - zero);
+                keep[r] = k;
+                sums[r] = base == w0 ? l : fmaf(sums[r], k, l);
+                top[r] = m;
             }
         }
+        __syncthreads();
+        if (active) {
+            const int r = 8 * nt + 2 * t4;
+            const bool two = r + 1 < n_rows;
+            if (base != w0) {
+                O[0] *= keep[r]; O[2] *= keep[r];
+                if (two) { O[1] *= keep[r + 1]; O[3] *= keep[r + 1]; }
+            }
+            auto add = [&](int k, const float4 &a) {
+                const float f0 = ml[k][r].x, f1 = two ? ml[k][r + 1].x : 0.0f;
+                O[0] = fmaf(a.x, f0, O[0]);
+                O[1] = fmaf(a.y, f1, O[1]);
+                O[2] = fmaf(a.z, f0, O[2]);
+                O[3] = fmaf(a.w, f1, O[3]);
+            };
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int r = 8 * nt + 2 * t4 + i;
-            if (r >= n_rows) continue;
-            const int64_t row = s.q0 + r / p.group;
-            const int head = h * p.group + r % p.group;
-            const float f = l[i] > 0.0f ? 8388608.0f / l[i] : (l[i] == 0.0f ? 0.0f : l[i]);
+            for (int k = 0; k < kAhead; k++)
+                if (k < n) add(k, ahead[k]);
+            for (int k0 = kAhead; k0 < n; k0 += kAhead) {
 #pragma unroll
-            for (int j = 0; j < 4; j++) store_out(p, row, head, 32 * b + 8 * j + g, O[j / 2][2 * (j % 2) + i] * f);
-            if (b == 0 && g == 0 && p.lse) p.lse[row * p.q_heads + head] = l[i] > 0.0f ? (m[i] + log2f(l[i])) * 0.6931471805599453f : (l[i] == 0.0f ? -INFINITY : l[i]);
+                for (int k = 0; k < kAhead; k++) ahead[k] = load(k0 + k);
+#pragma unroll
+                for (int k = 0; k < kAhead; k++)
+                    if (k0 + k < n) add(k0 + k, ahead[k]);
+            }
         }
+        __syncthreads();                                          // (the weights are read; the next round overwrites them)
+    }
+    if (!active) return;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int r = 8 * nt + 2 * t4 + i;
+        if (r >= n_rows) continue;
+        const int64_t row = s.q0 + r / p.group;
+        const int head = h * p.group + r % p.group;
+        const float l = sums[r], f = l > 0.0f ? 8388608.0f / l : (l == 0.0f ? 0.0f : l);
+#pragma unroll
+        for (int j = 0; j < 2; j++) store_out(p, row, head, 32 * b + 16 * x + 8 * j + g, O[2 * j + i] * f);
+        if (b == 0 && x == 0 && g == 0 && p.lse) p.lse[row * p.q_heads + head] = l > 0.0f ? (top[r] + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
     }
 }
 
