@@ -87,6 +87,29 @@ constexpr int index_of_count(int u, bool odd) { return u - (u >= (odd ? 7 : 6)) 
 constexpr uint8_t direct_byte(const Formatbook &b, int d, int v) {
     return e4m3_of_half_units(b.v[d][index_of_count(10 - v, (d & 1) != 0)]);
 }
+// Byte tables of a dialect's magnitudes as 16-bit floats, for the paged KV cache: word 0, 1 the low bytes of the eight
+// values, word 2, 3 the high bytes, without the part that depends on the block's scale.  A value is h * 2^(scale - 128).
+//   bf16: exponent field msb(h) + scale - 1; with scale = 2 k + p the high byte is k - 1 + ((msb + p + 1) >> 1) and bit 7 of
+//         the low byte (msb + p + 1) & 1, so there is a table per dialect and p, and k - 1 is added to every high byte but zero's;
+//   fp16: high byte 4 * (msb + scale - 113) + two mantissa bits, low byte the third one; 4 * (scale - 113) is added.
+struct FloatTable {
+    uint32_t w[4];
+};
+constexpr FloatTable float_table(const Formatbook &b, int d, bool bf16, int p) {
+    FloatTable t{};
+    for (int i = 1; i < 8; i++) {
+        const int h = b.v[d][i];
+        int m = 0;
+        for (int k = 3; k >= 0; k--)
+            if (h >> k & 1) { m = k; break; }
+        const int mant = ((h << 3) >> m) & 7;
+        const uint32_t hi = bf16 ? (uint32_t)((m + p + 1) >> 1) : (uint32_t)(m << 2 | mant >> 1);
+        const uint32_t lo = bf16 ? (uint32_t)(((m + p + 1) & 1) << 7 | mant << 4) : (uint32_t)((mant & 1) << 7);
+        t.w[i / 4] |= lo << (8 * (i % 4));
+        t.w[2 + i / 4] |= hi << (8 * (i % 4));
+    }
+    return t;
+}
 constexpr uint64_t int_lut(const Formatbook &b, int d) {
     uint64_t t = 0;
     for (int i = 0; i < 8; i++) t |= (uint64_t)b.v[d][i] << (8 * i);
@@ -242,6 +265,7 @@ struct DeviceTables {
     uint32_t int_lo[16], int_hi[16];
     uint32_t merged_above[8];     // merged_mask(p) >> 1: popcount(x >> q5) = thresholds above q5
     uint32_t direct_lo[16], direct_hi[16], direct_top[16];   // direct_byte for v = 0..3, 4..7, 8..10
+    FloatTable bf16[32], f16[16];                             // float_table: bf16 by 2 * dialect + p, fp16 by dialect
 };
 constexpr DeviceTables make_tables(const Formatbook &b) {
     DeviceTables t{};
@@ -256,6 +280,11 @@ constexpr DeviceTables make_tables(const Formatbook &b) {
             t.direct_hi[d] |= (uint32_t)direct_byte(b, d, 4 + v) << (8 * v);
             if (v < 3) t.direct_top[d] |= (uint32_t)direct_byte(b, d, 8 + v) << (8 * v);
         }
+    }
+    for (int d = 0; d < 16; d++) {
+        t.bf16[2 * d] = float_table(b, d, true, 0);
+        t.bf16[2 * d + 1] = float_table(b, d, true, 1);
+        t.f16[d] = float_table(b, d, false, 0);
     }
     for (int p = 0; p < 8; p++) {
         t.even_mask[p] = even_range_mask(b, p);

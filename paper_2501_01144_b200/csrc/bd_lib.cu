@@ -428,11 +428,11 @@ unsigned paged_chunks(const bd_paged_batch *b) {                   // chunks tha
 // Which kernel serves a call and how it is cut.  More than 16 rows per KV head: the tensor-core kernel, whose tiles have 256
 // rows; otherwise the warp-level one with 8 or 16 rows per tile, whose warps share the batch's chunks evenly.
 struct AttentionPlan {
-    bool chunk, wide;
+    bool chunk, wide, whole;          // whole: rows kernel with a CTA per head, one launch
     int tiles, splits;                // chunk kernel: tiles of 256 rows, CTAs that share a tile's tokens
     int workers, rounds;              // rows kernel: warps, and the runs each takes at most
 };
-AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
+AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, int64_t window) {
     const int64_t rows = b->max_q * (q_heads / c->kv_heads);
     AttentionPlan r{};
     r.chunk = rows > 16;
@@ -445,14 +445,27 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
     r.wide = rows > 8;
     const int warps = pg::row_warps(r.wide ? 2 : 1);
     const int64_t units = b->n * c->kv_heads * std::max<int64_t>(1, (b->max_kv + pg::kChunk - 1) / pg::kChunk);
+    // A CTA per head and no join where that is about one wave of short heads: measured at 32 / 8 heads x 128, 1 token, whole
+    // against runs: 1 sequence of 512 tokens 8.6 / 10.1 us, of 2048 17.7 / 14.2; 16 of 1024 12.4 / 19.8; 64 of 256 17.3 / 19.9,
+    // of 512 33.8 / 23.7.  4 tokens (16 rows): 8 of 512 12.1 / 13.9, 1 of 1024 16.2 / 14.2, 64 of 256 35.7 / 29.0.
+    const int64_t seen = window ? std::min(b->max_kv, window + b->max_q + pg::kChunk) : b->max_kv;   // tokens from the first visible chunk on
+    const int64_t chunks = std::max<int64_t>(1, (seen + pg::kChunk - 1) / pg::kChunk);
+    const int head_warps = chunks <= 4 ? 4 : chunks <= 8 ? 8 : warps;
+    const int64_t heads_at_once = 148 * (warps / head_warps), waves = (b->n * c->kv_heads + heads_at_once - 1) / heads_at_once;
+    r.whole = waves * chunks <= (r.wide ? 20 : 32);
+    if (r.whole) {
+        r.workers = head_warps;                                   // warps of a CTA
+        return r;
+    }
     r.workers = (int)std::min<int64_t>(148 * warps, units);
     r.rounds = (int)std::min<int64_t>(4, std::max<int64_t>(1, units / ((int64_t)r.workers * pg::kRunUnits)));
     return r;
 }
 size_t row_parts_offset(const bd_paged_batch *b) { return ((size_t)(b->n + 1) * sizeof(uint32_t) + 255) / 256 * 256; }   // behind the sequences' unit numbers
-size_t attention_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads) {
-    const AttentionPlan r = attention_plan(c, b, q_heads);
+size_t attention_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, int64_t window) {
+    const AttentionPlan r = attention_plan(c, b, q_heads, window);
     if (r.chunk) return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+    if (r.whole) return 0;
     const int floats = c->head_dim == 128 ? (r.wide ? pg::part_floats<4, 2>() : pg::part_floats<4, 1>()) : (r.wide ? pg::part_floats<2, 2>() : pg::part_floats<2, 1>());
     return row_parts_offset(b) + (size_t)r.workers * (size_t)r.rounds * 2 * (size_t)floats * sizeof(float);
 }
@@ -468,7 +481,7 @@ bd_status allow_smem(Kernel kernel, int bytes, bool (&configured)[kMaxDevices]) 
 }
 template <int DT, int NB, int NT, bool CAP>
 bd_status launch_rows_kernel(const pg::Attention &a, cudaStream_t st) {
-    constexpr int smem = pg::RowSmem<NB, NT>::total, warps = pg::row_warps(NT);
+    constexpr int warps = pg::row_warps(NT), smem = pg::RowSmem<NB, NT>::bytes(warps);
     static bool configured[kMaxDevices] = {};
     const bd_status s = allow_smem(pg::attention_rows_kernel<DT, NB, NT, CAP>, smem, configured);
     if (s) return s;
@@ -476,8 +489,17 @@ bd_status launch_rows_kernel(const pg::Attention &a, cudaStream_t st) {
     launch_serialized(pg::attention_rows_join_kernel<NB, NT>, dim3((unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 64 * NB * NT, 0, st, a);
     return BD_OK;
 }
+template <int DT, int NB, int NT, bool CAP>
+bd_status launch_head_kernel(const pg::Attention &a, cudaStream_t st) {
+    static bool configured[kMaxDevices] = {};
+    const bd_status s = allow_smem(pg::attention_head_kernel<DT, NB, NT, CAP>, pg::RowSmem<NB, NT>::bytes(pg::row_warps(NT)), configured);
+    if (s) return s;
+    launch_serialized(pg::attention_head_kernel<DT, NB, NT, CAP>, dim3((unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 32u * (unsigned)a.workers, pg::RowSmem<NB, NT>::bytes(a.workers), st, a);
+    return BD_OK;
+}
 template <int DT, int NB, int NT>
 bd_status launch_rows(const pg::Attention &a, cudaStream_t st) {
+    if (a.whole) return a.softcap > 0.0f ? launch_head_kernel<DT, NB, NT, true>(a, st) : launch_head_kernel<DT, NB, NT, false>(a, st);
     return a.softcap > 0.0f ? launch_rows_kernel<DT, NB, NT, true>(a, st) : launch_rows_kernel<DT, NB, NT, false>(a, st);
 }
 template <int DT>
@@ -500,14 +522,22 @@ bd_status launch_chunk(const pg::Attention &a, dim3 grid, cudaStream_t st) {
     if (a.pool.head_dim == 128) return cap ? launch_chunk_kernel<DT, 4, true>(a, grid, st) : launch_chunk_kernel<DT, 4, false>(a, grid, st);
     return cap ? launch_chunk_kernel<DT, 2, true>(a, grid, st) : launch_chunk_kernel<DT, 2, false>(a, grid, st);
 }
+template <int DT, int D, int HEADS>
+void launch_rotate_heads(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
+    const int per_cta = pg::kRotateThreads / (D / 8) * HEADS;
+    const dim3 grid((unsigned)r.rows, (unsigned)((r.q_heads + r.k_heads + per_cta - 1) / per_cta));
+    if (interleaved) launch_serialized(pg::rotate_kernel<DT, D, true, HEADS>, grid, pg::kRotateThreads, 0, st, r);
+    else launch_serialized(pg::rotate_kernel<DT, D, false, HEADS>, grid, pg::kRotateThreads, 0, st, r);
+}
 template <int DT, int D>
 void launch_rotate(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
-    if (interleaved) launch_serialized(pg::rotate_kernel<DT, D, true>, dim3((unsigned)r.rows), 256, 0, st, r);
-    else launch_serialized(pg::rotate_kernel<DT, D, false>, dim3((unsigned)r.rows), 256, 0, st, r);
+    // few rows: one head per group of lanes, so that more SMs work; many: five (fp32: two), so that a thread has ten loads in flight
+    if (r.rows < 4 * 148) launch_rotate_heads<DT, D, 1>(r, interleaved, st);
+    else launch_rotate_heads<DT, D, DT == BD_F32 ? 2 : pg::kRotateHeads>(r, interleaved, st);
 }
 #define BD_PAGED_DISPATCH(kernel, c, grid, st, ...)                                                                              \
     do {                                                                                                                        \
-        const unsigned threads = (unsigned)(c)->head_dim * 2;                                                                    \
+        const unsigned threads = (unsigned)(c)->head_dim;                                                                    \
         if ((c)->head_dim == 128) {                                                                                              \
             if ((c)->dtype == BD_F32) launch_serialized(kernel<BD_F32, 4>, grid, threads, 0, st, __VA_ARGS__);                   \
             else if ((c)->dtype == BD_BF16) launch_serialized(kernel<BD_BF16, 4>, grid, threads, 0, st, __VA_ARGS__);            \
@@ -1423,7 +1453,7 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes) {
     if (!c || !b || !bytes || q_heads <= 0 || c->kv_heads <= 0 || b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads || (c->head_dim != 64 && c->head_dim != 128)) return BD_ERR_SHAPE;
-    *bytes = attention_workspace(c, b, q_heads);
+    *bytes = attention_workspace(c, b, q_heads, 0);                // (a window never needs more)
     return BD_OK;
 }
 
@@ -1441,8 +1471,8 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
     if ((uintptr_t)lse & 3u) return BD_ERR_ALIGN;
     if (b->max_q == 0) return BD_OK;
-    const AttentionPlan plan = attention_plan(c, b, q_heads);
-    const size_t need = attention_workspace(c, b, q_heads);
+    const AttentionPlan plan = attention_plan(c, b, q_heads, window);
+    const size_t need = attention_workspace(c, b, q_heads, window);
     if (need && (!workspace || workspace_bytes < need)) return BD_ERR_WORKSPACE;
     if (need && ((uintptr_t)workspace & 255u)) return BD_ERR_ALIGN;
     pg::Attention a{};
@@ -1455,8 +1485,8 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.scale = scale; a.softcap = softcap;
     a.q_heads = (int)q_heads; a.group = (int)(q_heads / c->kv_heads); a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
     a.odtype = (int)odtype;
-    a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.rounds = plan.rounds;
-    a.k16 = 16u; a.k23 = 1u << 23;
+    a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.whole = plan.whole; a.rounds = plan.rounds;
+    a.k23 = 1u << 23;
     cudaStream_t st = (cudaStream_t)stream;
     if (!plan.chunk) {
         for (int k = 0; k < 4; k++) a.by_runs[k] = make_fast_div((uint32_t)(plan.workers * (k + 1)));
@@ -1464,7 +1494,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
         a.head_of_part = (uint32_t *)workspace;
         a.part = (float *)((char *)workspace + row_parts_offset(b));
         s = c->dtype == BD_BF16 ? launch_rows_dtype<BD_BF16>(a, plan.wide, st) : launch_rows_dtype<BD_F16>(a, plan.wide, st);
-        return s ? s : launch_result(2);
+        return s ? s : launch_result(plan.whole ? 1 : 2);
     }
     const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
     s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);

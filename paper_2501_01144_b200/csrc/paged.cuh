@@ -13,20 +13,6 @@ namespace pg {
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// Element e of a word sits in nibble kNibble[e] (its own inverse): the quantizer gets its elements in that order.
-__device__ __forceinline__ constexpr int nibble_of(int e) {
-    return e == 1 ? 2 : e == 2 ? 1 : e == 5 ? 6 : e == 6 ? 5 : e;
-}
-// The quantizer's word (signs of slots 0..3 in bits 8 s + 7, of 4..7 in bits 8 (s - 4) + 3) with each sign in bit 3 of
-// its own nibble.
-__device__ __forceinline__ uint32_t signs_to_nibbles(uint32_t w) {
-    uint32_t lo = (w >> 7) & 0x01010101u, hi = (w >> 3) & 0x01010101u;
-    lo = (lo | lo >> 4) & 0x00110011u;
-    hi = (hi | hi >> 4) & 0x00110011u;
-    lo = (lo | lo >> 8) & 0x1111u;
-    hi = (hi | hi >> 8) & 0x1111u;
-    return (w & 0x77777777u) | lo << 3 | hi << 19;
-}
 template <int DT>
 __device__ __forceinline__ float load_one(const void *p) {
     if (DT == BD_F32) return *(const float *)p;
@@ -39,39 +25,71 @@ __device__ __forceinline__ void store_one(void *p, float v) {
     else if (DT == BD_BF16) *(__nv_bfloat16 *)p = __float2bfloat16_rn(v);
     else *(__half *)p = __float2half_rn(v);
 }
-// Quantises 32 fp32 bit patterns (in element order) into four words in the record's nibble order.
-__device__ __forceinline__ void quantize_words(const uint32_t (&bits)[32], const SmemTables &tab, uint32_t (&words)[4],
-                                               uint32_t &id, uint32_t &scale) {
-    uint32_t ordered[32], unused[8];
+// A block in a thread's registers as the quantizers take it, and its quantisation into the record's words.
+template <int DT>
+struct Block {
+    uint32_t bits[32];
+    __device__ __forceinline__ void load(const void *p) { Loader<DT>::contiguous(p, bits); }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int k = 0; k < 32; k++) ordered[(k & ~7) + nibble_of(k & 7)] = bits[k];
-    BlockResult res;
-    bool nonfinite;
-    quantize_two_stage_f32<false>(ordered, tab, res, unused, nonfinite);
-    if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
+        for (int k = 0; k < 32; k++) bits[k] = 0;
+    }
+    // column `ch` of 32 rows of `pitch` bytes in shared memory
+    __device__ __forceinline__ void column(const uint8_t *rows, int pitch, int ch) {
 #pragma unroll
-    for (int w = 0; w < 4; w++) words[w] = signs_to_nibbles(res.words[w]);
-    id = res.id;
-    scale = res.scale;
-}
+        for (int k = 0; k < 32; k++) bits[k] = __float_as_uint(load_one<DT>(rows + k * pitch + ch * Loader<DT>::kElemBytes));
+    }
+    __device__ __forceinline__ void quantize(const SmemTables &tab, BlockResult &res) const {
+        uint32_t unused[8];
+        bool nonfinite;
+        quantize_two_stage_f32<false, true>(bits, tab, res, unused, nonfinite);
+        if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
+    }
+};
+template <>
+struct Block<BD_BF16> {                                           // two elements per register
+    uint32_t pairs[16];
+    __device__ __forceinline__ void load(const void *p) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint4 u = __ldg((const uint4 *)p + i);
+            pairs[4 * i] = u.x; pairs[4 * i + 1] = u.y; pairs[4 * i + 2] = u.z; pairs[4 * i + 3] = u.w;
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < 16; k++) pairs[k] = 0;
+    }
+    __device__ __forceinline__ void column(const uint8_t *rows, int pitch, int ch) {
+#pragma unroll
+        for (int k = 0; k < 16; k++)
+            pairs[k] = (uint32_t) * (const uint16_t *)(rows + 2 * k * pitch + 2 * ch) | (uint32_t) * (const uint16_t *)(rows + (2 * k + 1) * pitch + 2 * ch) << 16;
+    }
+    __device__ __forceinline__ void quantize(const SmemTables &tab, BlockResult &res) const {
+        uint32_t unused[8];
+        quantize_bf16_block<false, true>(pairs, tab, res, unused);
+    }
+};
 
 // ---------------------------------------------------------------------------
-// Append.  A CTA takes one chunk of one sequence and head: its first half quantises the chunk's new keys (thread =
-// token and block of 32 dimensions), its second half the chunk's values if this step completes it (thread = channel;
-// the rows of earlier steps come from the tail).  The CTA of the sequence's first chunk also stores the step's newest
-// value rows in the tail, after it has read the waiting ones: those of the newest chunk and of the one before it.
-// Everything is assembled in shared memory.  A chunk whose 32 keys are all new leaves as whole 16-byte pieces; the
-// keys of a partly new chunk go out as the few words that are theirs, since their neighbours belong to other steps.
-// Bytes set the bound: 2 * 2 d read and 35 / 32 d written per token and head for 16-bit sources.
+// Append.  A CTA takes one chunk of one sequence and head.  The chunk's value rows are copied to shared memory if this
+// step completes it (those of earlier steps from the tail); under that copy its threads quantise the chunk's new keys
+// (thread = token and block of 32 dimensions), then the values (thread = channel).  The CTA of the sequence's first chunk
+// also stores the step's newest value rows in the tail, after it has read the waiting ones: those of the newest chunk
+// and of the one before it.
+// A record's part that is new as a whole is assembled in shared memory and leaves as 16-byte pieces; the keys of a partly new
+// chunk go out as the few words that are theirs, since their neighbours belong to other steps.
+// Bound: 2 * 2 d bytes read and 35 / 32 d written per token and head for 16-bit sources; in practice instruction issue, as in the
+// operand quantizer.
 // ---------------------------------------------------------------------------
 template <int DT, int NB>
-__global__ void __launch_bounds__(NB * 64) append_kernel(Pool pool, Batch batch, const uint8_t *__restrict__ K,
+__global__ void __launch_bounds__(NB * 32) append_kernel(Pool pool, Batch batch, const uint8_t *__restrict__ K,
                                                          const uint8_t *__restrict__ V, int64_t ldk, int64_t ldv,
                                                          int64_t hsk, int64_t hsv) {
-    constexpr int D = 32 * NB, EB = Loader<DT>::kElemBytes, HALF = NB * 32;
+    constexpr int D = 32 * NB, EB = Loader<DT>::kElemBytes, kPieces = D * EB / 16, kPitch = D * EB;
     __shared__ SmemTables tab;
     __shared__ __align__(16) uint8_t rec[35 * D];
-    __shared__ __align__(16) uint8_t rows[32 * D * EB];
+    __shared__ __align__(16) uint8_t rows[32 * kPitch];
     __shared__ uint8_t vid[D];
     load_tables(tab);
     pdl_wait();
@@ -87,36 +105,30 @@ __global__ void __launch_bounds__(NB * 64) append_kernel(Pool pool, Batch batch,
     const int p0 = s.kv - s.t, p1 = s.kv;
     const int c = p0 / kChunk + blockIdx.x;
     if (c * kChunk >= p1) return;
-    const int64_t off = record_offset(pool, batch, seq, h, c);
-    if (off < 0 && threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
-    uint8_t *out = pool.base + (off < 0 ? 0 : off);
     const int lo = max(p0, c * kChunk) - c * kChunk, hi = min(p1 - c * kChunk, kChunk);   // the new tokens of this chunk
     const bool whole_keys = lo == 0 && hi == kChunk, whole_values = hi == kChunk;
     const uint8_t *Ks = K + ((int64_t)(s.q0 - p0 + c * kChunk) * ldk + (int64_t)h * hsk) * EB;   // row of the chunk's token 0
     const uint8_t *Vs = V + ((int64_t)(s.q0 - p0 + c * kChunk) * ldv + (int64_t)h * hsv) * EB;
     uint8_t *tail = (uint8_t *)pool.tail;
-
-    if (whole_values && off >= 0) {                               // the chunk's 32 value rows
-        constexpr int kPieces = D * EB / 16;
-        for (int i = threadIdx.x; i < 32 * kPieces; i += blockDim.x) {
+    if (whole_values)                                             // the chunk's 32 value rows
+        for (int i = threadIdx.x; i < 32 * kPieces; i += NB * 32) {
             const int tok = i / kPieces, piece = i % kPieces;
             const uint8_t *src = tok >= lo ? Vs + (int64_t)tok * ldv * EB : tail + tail_offset(pool, slot, h, c * kChunk + tok) * EB;
-            ((uint4 *)rows)[i] = *((const uint4 *)src + piece);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(rows + 16 * i)), "l"((const uint4 *)src + piece) : "memory");
         }
-    }
-    __syncthreads();
-    const bool keys = threadIdx.x < HALF;
-    uint32_t bits[32], words[4], id, scale;
-    if (keys && off >= 0) {
-        const int tok = threadIdx.x / NB, b = threadIdx.x % NB;
-        const bool mine = tok >= lo && tok < hi;
-        if (mine) Loader<DT>::contiguous(Ks + ((int64_t)tok * ldk + 32 * b) * EB, bits);
-        else
-#pragma unroll
-            for (int k = 0; k < 32; k++) bits[k] = 0;
-        quantize_words(bits, tab, words, id, scale);
+    const int tok = threadIdx.x / NB, b = threadIdx.x % NB;
+    const bool mine = tok >= lo && tok < hi;
+    Block<DT> block;
+    if (mine) block.load(Ks + ((int64_t)tok * ldk + 32 * b) * EB);
+    else block.clear();
+    const int64_t off = record_offset(pool, batch, seq, h, c);
+    if (off < 0 && threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
+    uint8_t *out = pool.base + (off < 0 ? 0 : off);
+    BlockResult res;
+    if (whole_keys || __any_sync(0xffffffffu, mine)) {
+        block.quantize(tab, res);
         // the NB lanes of a token put its scales and ids together
-        uint32_t sc = scale << (8 * b), ids = id << (4 * b);
+        uint32_t sc = res.scale << (8 * b), ids = res.id << (4 * b);
 #pragma unroll
         for (int x = 1; x < NB; x *= 2) {
             sc |= __shfl_xor_sync(0xffffffffu, sc, x);
@@ -124,9 +136,9 @@ __global__ void __launch_bounds__(NB * 64) append_kernel(Pool pool, Batch batch,
         }
         const int r = key_row(tok), e = entry_of(NB, 0, r);
         uint8_t *to = whole_keys ? rec : out;
-        if (mine) {
+        if (mine && off >= 0) {
 #pragma unroll
-            for (int t = 0; t < 4; t++) *(uint32_t *)(to + word_byte(b, r, t)) = words[t];
+            for (int t = 0; t < 4; t++) *(uint32_t *)(to + word_byte(b, r, t)) = res.words[t];
             if (b == 0) {
                 if (NB == 4) {
                     *(uint32_t *)(to + key_scales(D) + e) = sc;
@@ -137,37 +149,82 @@ __global__ void __launch_bounds__(NB * 64) append_kernel(Pool pool, Batch batch,
                 }
             }
         }
-    } else if (!keys && whole_values && off >= 0) {
-        const int ch = threadIdx.x - HALF;
-#pragma unroll
-        for (int k = 0; k < 32; k++) bits[k] = __float_as_uint(load_one<DT>(rows + (k * D + ch) * EB));
-        quantize_words(bits, tab, words, id, scale);
-        const int b = ch / 32, r = ch % 32, e = entry_of(NB, b, r);
-#pragma unroll
-        for (int t = 0; t < 4; t++) *(uint32_t *)(rec + value_codes(D) + word_byte(b, r, t)) = words[t];
-        rec[value_scales(D) + e] = (uint8_t)scale;
-        vid[e] = (uint8_t)id;
     }
-    __syncthreads();
-    if (off >= 0) {
+    if (whole_values) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        const int ch = threadIdx.x, vb = ch / 32, r = ch % 32, e = entry_of(NB, vb, r);
+        block.column(rows, kPitch, ch);
+        block.quantize(tab, res);
+#pragma unroll
+        for (int t = 0; t < 4; t++) *(uint32_t *)(rec + value_codes(D) + word_byte(vb, r, t)) = res.words[t];
+        rec[value_scales(D) + e] = (uint8_t)res.scale;
+        vid[e] = (uint8_t)res.id;
+    }
+    if (whole_values || whole_keys) {
+        __syncthreads();
         if (whole_values && threadIdx.x < D / 2) rec[value_ids(D) + threadIdx.x] = vid[2 * threadIdx.x] | vid[2 * threadIdx.x + 1] << 4;
         __syncthreads();
         // whole parts of the record in 16-byte pieces (every part is a multiple of 16 bytes: D is 64 or 128)
-        for (int i = threadIdx.x; i < 35 * D / 16; i += blockDim.x) {
-            const int at = 16 * i;
-            const bool of_keys = at < 16 * D || (at >= 32 * D && at < 33 * D) || (at >= 34 * D && at < 34 * D + D / 2);
-            if (of_keys ? whole_keys : whole_values) ((uint4 *)out)[i] = ((const uint4 *)rec)[i];
-        }
+        if (off >= 0)
+            for (int i = threadIdx.x; i < 35 * D / 16; i += NB * 32) {
+                const int at = 16 * i;
+                const bool of_keys = at < 16 * D || (at >= 32 * D && at < 33 * D) || (at >= 34 * D && at < 34 * D + D / 2);
+                if (of_keys ? whole_keys : whole_values) ((uint4 *)out)[i] = ((const uint4 *)rec)[i];
+            }
     }
-    if (blockIdx.x == 0) {                                        // (the waiting rows were read above)
+    if (blockIdx.x == 0) {
+        // (the waiting rows are in shared memory of every thread's copy: it waited, and met the others, above)
         const int from = max(p0, p1 / kChunk * kChunk - kChunk);
-        constexpr int kPieces = D * EB / 16;
-        for (int i = threadIdx.x; i < (p1 - from) * kPieces; i += blockDim.x) {
-            const int tok = from + i / kPieces, piece = i % kPieces;
-            const uint8_t *src = V + ((int64_t)(s.q0 + tok - p0) * ldv + (int64_t)h * hsv) * EB;
-            *((uint4 *)(tail + tail_offset(pool, slot, h, tok) * EB) + piece) = *((const uint4 *)src + piece);
+        for (int i = threadIdx.x; i < (p1 - from) * kPieces; i += NB * 32) {
+            const int row = from + i / kPieces, piece = i % kPieces;
+            const uint8_t *src = V + ((int64_t)(s.q0 + row - p0) * ldv + (int64_t)h * hsv) * EB;
+            *((uint4 *)(tail + tail_offset(pool, slot, h, row) * EB) + piece) = *((const uint4 *)src + piece);
         }
     }
+}
+
+// 2^(scale - 128), the factor of the half-unit integers; subnormal for scales 0 and 1.
+__device__ __forceinline__ float half_unit(uint32_t scale) {
+    return scale > 1u ? __uint_as_float((scale - 1u) << 23) : __uint_as_float(scale ? 0x00400000u : 0x00200000u);
+}
+// Byte tables of a block's magnitudes h * 2^(scale - 128) in bf16 or fp16, lo[8] and hi[8]: the dialect's table (see
+// float_table; copied to shared memory by the first threads of a CTA) with the block's scale added to the exponent bits.
+// Blocks outside the range of those sums (bf16: scale < 2, fp16: scale < 114, where subnormals begin) are built value by value.
+template <int DT>
+__device__ __forceinline__ void make_base_tables(uint4 *to) {
+    const uint32_t *from = DT == BD_BF16 ? &c_tables.bf16[0].w[0] : &c_tables.f16[0].w[0];
+    for (int i = threadIdx.x; i < (DT == BD_BF16 ? 128 : 64); i += blockDim.x) ((uint32_t *)to)[i] = from[i];
+}
+// TINY: bf16 blocks of scale < 2 (magnitudes below 2^-123) keep their subnormal values; otherwise they count as zeros.
+template <int DT, bool TINY>
+__device__ __forceinline__ uint4 block_table(const uint4 *base, uint32_t id, uint32_t scale) {
+    uint4 t = base[DT == BD_BF16 ? 2 * id + (scale & 1u) : id];
+    const uint32_t k = DT == BD_BF16 ? (scale >> 1) - 1u : (scale - 113u) * 4u;
+    t.z += k * 0x01010100u;
+    t.w += k * 0x01010101u;
+    if (DT == BD_BF16 && !TINY) {
+        if (scale < 2u) t = make_uint4(0, 0, 0, 0);
+    } else if (scale < (DT == BD_BF16 ? 2u : 114u)) {
+        uint32_t b[4] = {0, 0, 0, 0};
+        const uint32_t tlo = c_tables.int_lo[id], thi = c_tables.int_hi[id];
+#pragma unroll
+        for (int i = 1; i < 8; i++) {
+            const float v = (float)((i < 4 ? tlo >> (8 * i) : thi >> (8 * (i - 4))) & 255u) * half_unit(scale);
+            const uint32_t h = DT == BD_BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)) : (uint32_t)__half_as_ushort(__float2half_rn(v));
+            b[i / 4] |= (h & 255u) << (8 * (i % 4));
+            b[2 + i / 4] |= (h >> 8) << (8 * (i % 4));
+        }
+        t = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+    return t;
+}
+__device__ __forceinline__ uint4 expand_word(uint32_t w, const uint4 &t) {
+    const uint32_t sel = w & 0x77777777u, sel_b = sel >> 16, even = w << 4;
+    const uint32_t lo_a = prmt_b32(t.x, t.y, sel), lo_b = prmt_b32(t.x, t.y, sel_b);
+    const uint32_t hi_a = prmt_b32(t.z, t.w, sel) | (prmt_b32(even, w, 0x5140u) & 0x80808080u);
+    const uint32_t hi_b = prmt_b32(t.z, t.w, sel_b) | (prmt_b32(even, w, 0x7362u) & 0x80808080u);
+    return make_uint4(prmt_b32(lo_a, hi_a, 0x6240u), prmt_b32(lo_a, hi_a, 0x7351u), prmt_b32(lo_b, hi_b, 0x6240u), prmt_b32(lo_b, hi_b, 0x7351u));
 }
 
 // The eight values of a word as fp32, in element order; f = 2^(e - 1).
@@ -176,30 +233,29 @@ __device__ __forceinline__ void word_values(uint32_t w, uint32_t tlo, uint32_t t
     const uint32_t xa = prmt_b32(tlo, thi, sel), xb = prmt_b32(tlo, thi, sel >> 16);
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        const int n = nibble_of(e);
+        const int n = place_of<true>(e);
         const uint32_t h = ((n < 4 ? xa : xb) >> (8 * (n & 3))) & 0xffu;
-        const float m = (float)h * f;
-        v[e] = __uint_as_float(__float_as_uint(m) | ((w >> (4 * n + 3)) & 1u) << 31);
+        v[e] = __uint_as_float(__float_as_uint((float)h * f) | ((w >> (4 * n + 3)) & 1u) << 31);
     }
-}
-// 2^(scale - 128), the factor of the half-unit integers; subnormal for scales 0 and 1.
-__device__ __forceinline__ float half_unit(uint32_t scale) {
-    return scale > 1u ? __uint_as_float((scale - 1u) << 23) : __uint_as_float(scale ? 0x00400000u : 0x00200000u);
 }
 
 // ---------------------------------------------------------------------------
-// Read back: the last t tokens of each sequence as values of the cache's type (exact for fp32 and bf16; fp16 rounds
-// what lies below its subnormals).  A CTA takes one chunk of one head; the first half of its threads expands key
-// blocks (thread = token and block, 32 consecutive outputs), the second half value blocks (thread = channel), which
-// meet in shared memory and leave token by token; the tokens of an unfinished chunk come from the tail.
+// Read back: the last t tokens of each sequence as values of the cache's type (exact for fp32 and bf16; fp16 rounds what
+// lies below its normal range).  A CTA takes one chunk of one head: its record (35 d bytes) comes to shared memory in
+// 16-byte pieces, then the keys leave word by word and the values, expanded block by block
+// (thread = channel), through shared memory, so that both are written token by token; the tokens of an unfinished chunk come from the tail.
+// 16-bit types expand with byte permutes (see block_table), fp32 with a multiplication.
 // ---------------------------------------------------------------------------
 template <int DT, int NB>
-__global__ void __launch_bounds__(NB * 64) read_kernel(Pool pool, Batch batch, uint8_t *__restrict__ K, uint8_t *__restrict__ V,
+__global__ void __launch_bounds__(NB * 32) read_kernel(Pool pool, Batch batch, uint8_t *__restrict__ K, uint8_t *__restrict__ V,
                                                        int64_t ldk, int64_t ldv, int64_t hsk, int64_t hsv) {
-    constexpr int D = 32 * NB, EB = Loader<DT>::kElemBytes, HALF = NB * 32, kPieces = D * EB / 16;
-    __shared__ uint2 table[16];
-    __shared__ __align__(16) uint8_t rows[32 * (D * EB + 16)];    // value rows, padded by 16 bytes
-    if (threadIdx.x < 16) table[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
+    constexpr int D = 32 * NB, EB = Loader<DT>::kElemBytes, kPieces = D * EB / 16, kPitch = D * EB + 16;
+    __shared__ uint4 base[DT == BD_F32 ? 1 : 32];
+    __shared__ uint2 table[DT == BD_F32 ? 16 : 1];
+    __shared__ __align__(16) uint8_t rec[35 * D];
+    __shared__ __align__(16) uint8_t rows[32 * kPitch];
+    if (DT != BD_F32) make_base_tables<DT>(base);
+    else if (threadIdx.x < 16) table[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
     pdl_wait();
     pdl_release();
     const int seq = blockIdx.z, h = blockIdx.y;
@@ -218,106 +274,124 @@ __global__ void __launch_bounds__(NB * 64) read_kernel(Pool pool, Batch batch, u
     const int slot = waiting ? batch.slot[seq] : 0;
     const bool slot_ok = slot >= 0 && slot < pool.slots;
     if ((off < 0 || !slot_ok) && threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
-    const uint8_t *rec = pool.base + (off < 0 ? 0 : off);
     const int64_t row0 = (int64_t)s.q0 - p0 + c * kChunk;         // output row of the chunk's token 0
+    for (int i = threadIdx.x; i < 35 * D / 16; i += NB * 32)      // (no page: scales, ids and codes 0, which is the value 0)
+        ((uint4 *)rec)[i] = off >= 0 ? ((const uint4 *)(pool.base + off))[i] : make_uint4(0, 0, 0, 0);
     __syncthreads();
-    if (threadIdx.x < HALF) {
-        const int tok = threadIdx.x / NB, b = threadIdx.x % NB;
-        if (tok >= lo && tok < hi) {
-            const int r = key_row(tok), e = entry_of(NB, b, r);
-            uint8_t *to = K + ((row0 + tok) * ldk + (int64_t)h * hsk + 32 * b) * EB;
-            uint2 tb = make_uint2(0, 0);
-            float f = 0.0f;
-            if (off >= 0) {
-                tb = table[rec[key_ids(D) + e / 2] >> (4 * (e & 1)) & 15];
-                f = half_unit(rec[key_scales(D) + e]);
-            }
-#pragma unroll
-            for (int t = 0; t < 4; t++) {
-                float v[8];
-                const uint32_t w = off >= 0 ? *(const uint32_t *)(rec + word_byte(b, r, t)) : 0u;
-                word_values(w, tb.x, tb.y, f, v);
-                __align__(16) uint8_t piece[8 * EB];
-#pragma unroll
-                for (int k = 0; k < 8; k++) store_one<DT>(piece + k * EB, v[k]);
-#pragma unroll
-                for (int k = 0; k < EB / 2; k++) ((uint4 *)(to + t * 8 * EB))[k] = ((const uint4 *)piece)[k];
-            }
+    // word t of row r of tile b as 8 elements of the type: one 16-byte piece, or two (fp32)
+    auto word = [&](bool key, int b, int r, int t, const uint4 &tb, float f, uint4 (&x)[EB / 2]) {
+        const uint32_t w = *(const uint32_t *)(rec + (key ? 0 : value_codes(D)) + word_byte(b, r, t));
+        if (DT == BD_F32) {
+            float v[8];
+            word_values(w, tb.x, tb.y, f, v);
+            x[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            x[EB / 2 - 1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        } else {
+            x[0] = expand_word(w, tb);
         }
-    } else if (!waiting) {
-        const int ch = threadIdx.x - HALF, b = ch / 32, r = ch % 32, e = entry_of(NB, b, r);
-        uint2 tb = make_uint2(0, 0);
-        float f = 0.0f;
-        if (off >= 0) {
-            tb = table[rec[value_ids(D) + e / 2] >> (4 * (e & 1)) & 15];
-            f = half_unit(rec[value_scales(D) + e]);
+    };
+    auto entry = [&](bool key, int b, int r, uint4 &tb, float &f) {
+        const int e = entry_of(NB, b, r);
+        const uint32_t id = rec[(key ? key_ids(D) : value_ids(D)) + e / 2] >> (4 * (e & 1)) & 15, scale = rec[(key ? key_scales(D) : value_scales(D)) + e];
+        if (DT == BD_F32) {
+            tb = make_uint4(table[id].x, table[id].y, 0, 0);
+            f = half_unit(scale);
+        } else {
+            tb = block_table<DT, true>(base, id, scale);
         }
+    };
+    uint4 tb;
+    float f = 0.0f;
+    // keys: neighbouring threads take neighbouring words of a token, so that their stores join
+    {
+        const int b = threadIdx.x / 4 % NB, t = threadIdx.x % 4;
+        uint8_t *to = K + ((row0 + lo + threadIdx.x / (4 * NB)) * ldk + (int64_t)h * hsk + 32 * b + 8 * t) * EB;
+        for (int tok = lo + threadIdx.x / (4 * NB); tok < hi; tok += 8, to += 8 * ldk * EB) {
+            const int r = key_row(tok);
+            uint4 x[EB / 2];
+            entry(true, b, r, tb, f);
+            word(true, b, r, t, tb, f, x);
+#pragma unroll
+            for (int k = 0; k < EB / 2; k++) ((uint4 *)to)[k] = x[k];
+        }
+    }
+    if (!waiting) {
+        const int ch = threadIdx.x, b = ch / 32, r = ch % 32;
+        uint8_t *to = rows + ch * EB;
+        entry(false, b, r, tb, f);
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            float v[8];
-            const uint32_t w = off >= 0 ? *(const uint32_t *)(rec + value_codes(D) + word_byte(b, r, t)) : 0u;
-            word_values(w, tb.x, tb.y, f, v);
+            uint4 x[EB / 2];
+            word(false, b, r, t, tb, f, x);
 #pragma unroll
-            for (int k = 0; k < 8; k++) store_one<DT>(rows + (8 * t + k) * (D * EB + 16) + ch * EB, v[k]);
+            for (int i = 0; i < EB / 2; i++) {
+                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (EB == 4) {
+                        *(uint32_t *)(to + (8 * t + 4 * i + k) * kPitch) = w[k];
+                    } else {
+                        *(uint16_t *)(to + (8 * t + 2 * k) * kPitch) = (uint16_t)w[k];
+                        *(uint16_t *)(to + (8 * t + 2 * k + 1) * kPitch) = (uint16_t)(w[k] >> 16);
+                    }
+                }
+            }
         }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < (hi - lo) * kPieces; i += blockDim.x) {
-        const int tok = lo + i / kPieces, piece = i % kPieces;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (!waiting) x = ((const uint4 *)(rows + tok * (D * EB + 16)))[piece];
-        else if (slot_ok) x = *((const uint4 *)((const uint8_t *)pool.tail + tail_offset(pool, slot, h, c * kChunk + tok) * EB) + piece);
-        *((uint4 *)(V + ((row0 + tok) * ldv + (int64_t)h * hsv) * EB) + piece) = x;
-    }
+    const int piece = threadIdx.x % kPieces;
+    constexpr int kRowsATurn = NB * 32 / kPieces;
+    int tok = lo + threadIdx.x / kPieces;
+    uint8_t *to = V + ((row0 + tok) * ldv + (int64_t)h * hsv) * EB + 16 * piece;
+    const uint8_t *from = waiting ? (const uint8_t *)pool.tail + tail_offset(pool, slot_ok ? slot : 0, h, c * kChunk + tok) * EB + 16 * piece : rows + tok * kPitch + 16 * piece;
+    for (; tok < hi; tok += kRowsATurn, to += kRowsATurn * ldv * EB, from += kRowsATurn * (waiting ? D * EB : kPitch))
+        *(uint4 *)to = !waiting || slot_ok ? *(const uint4 *)from : make_uint4(0, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------------------
 // Queries and keys of a step: y = x / sqrt(mean(x^2) + eps) * w per head (w may be absent: no normalisation), then the
 // rotation of the first `rot` elements, (a, b) -> (a cos - b sin, b cos + a sin), with cos and sin from the caller's
 // table [positions][rot] (rot / 2 cosines, then rot / 2 sines).  Pairs are (i, i + rot / 2), or (2 i, 2 i + 1).
-// All arithmetic in fp32, one rounding at the end.  D / 8 lanes hold a head, eight elements each; a warp's lanes walk
-// over the heads of one row, so the row's cosines and sines are read once per lane and stay in registers.
+// All arithmetic in fp32, one rounding at the end.
+// D / 8 lanes hold a head, eight elements each as two groups of four: of the rotated part elements 4 l .. and rot / 2 + 4 l ..
+// (pairs that are half the part apart meet in one lane, no exchange), else eight neighbours.  A group of lanes does up to
+// five heads of its row, all loads in front, with the row's cosines and sines in registers.
 // Bound: bytes (every element read and written once).
 // ---------------------------------------------------------------------------
 template <int DT>
-__device__ __forceinline__ void load8(const uint8_t *p, float (&x)[8]) {
-    if (DT == BD_F32) {
-        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        const uint4 u = *(const uint4 *)p;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+struct Quad { typedef uint2 Type; };                              // four elements
+template <>
+struct Quad<BD_F32> { typedef uint4 Type; };
+__device__ __forceinline__ void unpack_f32(const uint4 &u, float *x) {
+    x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+}
+template <int DT>
+__device__ __forceinline__ void unpack4(const uint2 &u, float *x) {
+    const uint32_t w[2] = {u.x, u.y};
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if (DT == BD_BF16) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            } else {
-                const float2 f = __half22float2(*(const __half2 *)&w[i]);
-                x[2 * i] = f.x;
-                x[2 * i + 1] = f.y;
-            }
+    for (int i = 0; i < 2; i++) {
+        if (DT == BD_BF16) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 f = __half22float2(*(const __half2 *)&w[i]);
+            x[2 * i] = f.x;
+            x[2 * i + 1] = f.y;
         }
     }
 }
 template <int DT>
-__device__ __forceinline__ void store8(uint8_t *p, const float (&x)[8]) {
+__device__ __forceinline__ void unpack4(const uint4 &u, float *x) { unpack_f32(u, x); }
+template <int DT>
+__device__ __forceinline__ void store4(uint8_t *p, const float *x) {
     if (DT == BD_F32) {
-        ((float4 *)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        ((float4 *)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]);
+    } else if (DT == BD_BF16) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        *(uint2 *)p = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&b);
     } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if (DT == BD_BF16) {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *(const uint32_t *)&v;
-            } else {
-                const __half2 v = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *(const uint32_t *)&v;
-            }
-        }
-        *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
+        const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
+        *(uint2 *)p = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&b);
     }
 }
 
@@ -332,78 +406,81 @@ struct Rotation {
     int rows, q_heads, k_heads, rot;
     float eps;
 };
+constexpr int kRotateThreads = 128, kRotateHeads = 5;             // 16 or 8 groups of lanes, heads a group has in flight
 
-template <int DT, int D, bool NEIGHBOURS>
-__global__ void __launch_bounds__(256) rotate_kernel(Rotation p) {
-    constexpr int EB = DT == BD_F32 ? 4 : 2, LANES = D / 8, GROUPS = 256 / LANES;
+template <int DT, int D, bool NEIGHBOURS, int HEADS>
+__global__ void __launch_bounds__(kRotateThreads) rotate_kernel(Rotation p) {
+    constexpr int EB = DT == BD_F32 ? 4 : 2, LANES = D / 8, GROUPS = kRotateThreads / LANES;
+    typedef typename Quad<DT>::Type Q4;
     pdl_wait();
     pdl_release();
-    const int row = blockIdx.x, l = threadIdx.x % LANES, grp = threadIdx.x / LANES;
-    const int pos = p.pos[row];
-    const bool ok = pos >= 0 && pos < p.positions;
-    if (!ok && threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
-    // this lane's cosines and sines: one per element (halves) or per pair (neighbours); 1 and 0 outside the rotated part
-    const bool turned = ok && 8 * l < p.rot;
+    const int row = blockIdx.x, l = threadIdx.x % LANES, h0 = blockIdx.y * GROUPS * HEADS + threadIdx.x / LANES, heads = p.q_heads + p.k_heads;
     const int half = p.rot / 2;
-    float co[8], si[8];
-    const float *tb = p.table + (int64_t)(ok ? pos : 0) * p.rot;
-    if (turned) {
-        if (NEIGHBOURS) {
-            const float4 a = *(const float4 *)(tb + 4 * l), b = *(const float4 *)(tb + half + 4 * l);
-            co[0] = a.x; co[1] = a.y; co[2] = a.z; co[3] = a.w;
-            si[0] = b.x; si[1] = b.y; si[2] = b.z; si[3] = b.w;
-        } else {
-            const int e = 8 * l < half ? 8 * l : 8 * l - half;
-            const float sign = 8 * l < half ? -1.0f : 1.0f;
+    const bool turned = 8 * l < p.rot;
+    const int e0 = !NEIGHBOURS && turned ? 4 * l : 8 * l, e1 = !NEIGHBOURS && turned ? half + 4 * l : 8 * l + 4;
+    const int pos = p.pos[row];
+    const uint8_t *q = p.q + ((int64_t)row * p.ldq + e0) * EB, *kk = p.k + ((int64_t)row * p.ldk + e0) * EB;
+    const int de = (e1 - e0) * EB;
+    const int64_t hsq = p.hsq * EB, hsk = p.hsk * EB, hsqo = p.hsqo * EB, hsko = p.hsko * EB;
+    Q4 raw[HEADS][2];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const float4 a = *(const float4 *)(tb + e + 4 * i), b = *(const float4 *)(tb + half + e + 4 * i);
-                co[4 * i] = a.x; co[4 * i + 1] = a.y; co[4 * i + 2] = a.z; co[4 * i + 3] = a.w;
-                si[4 * i] = sign * b.x; si[4 * i + 1] = sign * b.y; si[4 * i + 2] = sign * b.z; si[4 * i + 3] = sign * b.w;
-            }
+    for (int i = 0; i < HEADS; i++) {                             // all loads in front, none waits for the position
+        const int h = h0 + i * GROUPS;
+        if (h < heads) {
+            const uint8_t *src = h < p.q_heads ? q + (int64_t)h * hsq : kk + (int64_t)(h - p.q_heads) * hsk;
+            raw[i][0] = *(const Q4 *)src;
+            raw[i][1] = *(const Q4 *)(src + de);
         }
     }
-    const int partner = turned ? (8 * l < half ? l + half / 8 : l - half / 8) : l;
-    const int lane0 = threadIdx.x % 32 - l;                       // the head's first lane in the warp
-    const int heads = p.q_heads + p.k_heads;
-    for (int h0 = 0; h0 < heads; h0 += GROUPS) {                  // whole warps take every turn (shuffles)
-        const int h = h0 + grp;
-        const bool active = h < heads, is_q = h < p.q_heads;
-        const int hh = is_q ? h : h - p.q_heads;
-        float x[8];
-        if (active) load8<DT>((is_q ? p.q + (row * p.ldq + hh * p.hsq) * EB : p.k + (row * p.ldk + hh * p.hsk) * EB) + 8 * l * EB, x);
-        else
+    if (pos < 0 || pos >= p.positions) {                          // (the whole CTA)
+        if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
+        return;
+    }
+    float4 co = make_float4(1.0f, 1.0f, 1.0f, 1.0f), si = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (turned) {
+        const float *tb = p.table + (int64_t)pos * p.rot + 4 * l;
+        co = *(const float4 *)tb;
+        si = *(const float4 *)(tb + half);
+    }
+    uint8_t *qo = p.q_out + ((int64_t)row * p.ldqo + e0) * EB, *ko = p.k_out + ((int64_t)row * p.ldko + e0) * EB;
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = 0.0f;
-        const void *w = is_q ? p.wq : p.wk;
-        float ss = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-        for (int m = 1; m < LANES; m *= 2) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-        if (w) {
-            const float inv = rsqrtf(ss * (1.0f / D) + p.eps);
-            float g[8];
-            load8<DT>((const uint8_t *)w + 8 * l * EB, g);
-#pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = x[i] * inv * g[i];
+    for (int i = 0; i < HEADS; i++) {
+        const int h = h0 + i * GROUPS;
+        if (h - (int)(threadIdx.x / LANES) >= heads) return;      // whole warps take every turn (shuffles)
+        const bool is_q = h < p.q_heads;
+        float x[8] = {}, y[8];
+        if (h < heads) {
+            unpack4<DT>(raw[i][0], x);
+            unpack4<DT>(raw[i][1], x + 4);
         }
-        float y[8];
-        if (NEIGHBOURS) {
+        if (p.wq || p.wk) {                                       // (the same in all lanes)
+            float ss = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                y[2 * i] = turned ? x[2 * i] * co[i] - x[2 * i + 1] * si[i] : x[2 * i];
-                y[2 * i + 1] = turned ? x[2 * i + 1] * co[i] + x[2 * i] * si[i] : x[2 * i + 1];
-            }
-        } else {
+            for (int j = 0; j < 8; j++) ss = fmaf(x[j], x[j], ss);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float other = __shfl_sync(0xffffffffu, x[i], lane0 + partner);
-                y[i] = turned ? x[i] * co[i] + other * si[i] : x[i];
+            for (int m = 1; m < LANES; m *= 2) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+            const uint8_t *w = (const uint8_t *)(is_q ? p.wq : p.wk);
+            if (w) {
+                const float inv = rsqrtf(ss * (1.0f / D) + p.eps);
+                float g[8];
+                unpack4<DT>(*(const Q4 *)(w + e0 * EB), g);
+                unpack4<DT>(*(const Q4 *)(w + e0 * EB + de), g + 4);
+#pragma unroll
+                for (int j = 0; j < 8; j++) x[j] = x[j] * inv * g[j];
             }
         }
-        if (active && ok)
-            store8<DT>((is_q ? p.q_out + (row * p.ldqo + hh * p.hsqo) * EB : p.k_out + (row * p.ldko + hh * p.hsko) * EB) + 8 * l * EB, y);
+        const float c[4] = {co.x, co.y, co.z, co.w}, s[4] = {si.x, si.y, si.z, si.w};
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int a = NEIGHBOURS ? 2 * j : j, b = NEIGHBOURS ? 2 * j + 1 : j + 4;
+            y[a] = turned ? x[a] * c[j] - x[b] * s[j] : x[a];
+            y[b] = turned ? x[b] * c[j] + x[a] * s[j] : x[b];
+        }
+        if (h < heads) {
+            uint8_t *to = is_q ? qo + (int64_t)h * hsqo : ko + (int64_t)(h - p.q_heads) * hsko;
+            store4<DT>(to, y);
+            store4<DT>(to + de, y + 4);
+        }
     }
 }
 

@@ -19,7 +19,7 @@
 // element).  Probabilities are rounded to fp16 (2^-11) for the second product, and their fp32 values are what the row sum
 // adds; the unfinished chunk's values meet probabilities split in two bf16 parts (bf16 caches) or the same fp16 ones.
 // What bounds it: the integer (ALU) pipe, which takes two cycles per warp instruction.  A code word costs ten of them, a
-// block two; moves that the multiply-add pipe can do (left shifts) go there.  About 930 cycles of each SM quarter per chunk
+// block two; the left shift of a block's scale goes to the multiply-add pipe.  About 930 cycles of each SM quarter per chunk
 // against 760 for the chunk's 4480 bytes (d = 128) at the measured copy rate.
 #pragma once
 #include <cuda_bf16.h>
@@ -42,20 +42,21 @@ struct Attention {
                                       // [splits][rows][q_heads][d + 2] (chunk kernel): output, maximum (log2 units), sum
     float scale, softcap;
     int q_heads, group, window, splits, row_tiles, odtype;
+    bool whole;                       // rows kernel: a CTA per head (workers: its warps)
     int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
     FastDiv by_runs[4], by_page;      // division by workers * (1 .. 4), by the chunks of a page
     uint32_t *head_of_part;           // rows kernel: [n + 1] units in front of each sequence, then all units
-    uint32_t k16, k23;                // 2^4 and 2^23: left shifts as multiplications by operands the compiler does not see
+    uint32_t k23;                     // 2^23: a left shift as a multiplication by an operand the compiler does not see
 };
 
 constexpr int kRowStages = 2;
 constexpr int kRunUnits = 8;          // units that make a further round of runs worth its joins
 __host__ __device__ constexpr int row_warps(int nt) { return nt == 1 ? 16 : 8; }    // warps of a CTA = of an SM, by registers
 
-__device__ __forceinline__ void expand_f16(uint32_t w, uint2 tb, uint32_t k16, uint32_t (&r)[4]) {
+__device__ __forceinline__ void expand_f16(uint32_t w, uint2 tb, uint32_t (&r)[4]) {
     const uint32_t sel = w & 0x77777777u;
     const uint32_t xa = prmt_b32(tb.x, tb.y, sel), xb = prmt_b32(tb.x, tb.y, sel >> 16);
-    const uint32_t odd = w & 0x80808080u, even = (w * k16) & 0x80808080u;   // signs of the odd / even nibbles, one per byte
+    const uint32_t odd = w & 0x80808080u, even = (w << 4) & 0x80808080u;   // signs of the odd / even nibbles, one per byte
     r[0] = prmt_b32(xa, even, 0x5240u);   // nibbles 0, 2 = elements 0, 1
     r[1] = prmt_b32(xa, odd, 0x5341u);    // nibbles 1, 3 = elements 2, 3
     r[2] = prmt_b32(xb, even, 0x7260u);   // nibbles 4, 6 = elements 4, 5
@@ -182,38 +183,315 @@ __device__ __host__ constexpr int part_floats() { return NT * NB * 2 * 128 + 2 *
 template <int NB, int NT>
 struct RowSmem {
     static constexpr int D = 32 * NB, ROWS = 8 * NT;
-    static constexpr int warps = row_warps(NT), stage = 35 * D, ring = warps * kRowStages * stage;
-    static constexpr int table = (ring + 127) / 128 * 128, bars = table + 128, words = bars + warps * kRowStages * 8, total = words + 16;
+    static constexpr int warps = row_warps(NT), stage = 35 * D;
+    static constexpr int table = 0, bars = 128, words = bars + warps * kRowStages * 8, ring = 512;      // the warps' records come last
+    static constexpr int bytes(int warps) { return ring + warps * kRowStages * stage; }
+    static_assert(words + 16 <= ring, "room for the table and the barriers");
+};
+
+// What a warp keeps of the head it works on.
+template <int DT, int NB, int NT, bool CAP>
+struct RowWork {
+    static constexpr int D = 32 * NB;
+    uint32_t qf[NT][NB][4];                                       // queries: fragments of the 8-column operand, in fp16
+    float mul[NT][2];                                             // column's factor from block sums to scores
+    int pos[NT][2];
+    float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
+    Sequence s;
+    int h, n_rows, first_pos, last_pos, full;
+
+    // A head begins: its queries, and nothing seen yet.
+    __device__ __forceinline__ void begin(const Attention &p, const Sequence &seq, int head, int lane) {
+        const int g = lane / 4, t4 = lane % 4;
+        s = seq;
+        h = head;
+        n_rows = s.t * p.group;
+        first_pos = s.kv - s.t;
+        last_pos = s.kv - 1;
+        full = s.kv / kChunk;
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            const int r = 8 * nt + g;
+            const bool valid = r < n_rows;
+            const uint8_t *src = p.q + ((int64_t)(s.q0 + r / p.group) * p.ldq + (int64_t)(h * p.group + r % p.group) * p.hsq) * 2;
+            uint4 raw[NB];
+#pragma unroll
+            for (int b = 0; b < NB; b++) raw[b] = valid ? *(const uint4 *)(src + (32 * b + 8 * t4) * 2) : make_uint4(0, 0, 0, 0);
+            float qs = 1.0f;
+            if (DT == BD_BF16) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int b = 0; b < NB; b++) m = absmax_bf16x2(m, absmax_bf16x2(absmax_bf16x2(raw[b].x, raw[b].y), absmax_bf16x2(raw[b].z, raw[b].w)));
+                m = max(m & 0x7fffu, m >> 16 & 0x7fffu);
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const int ex = min(max((int)(m >> 7), 27), 240);      // biased exponent of the row's largest element
+                const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - ex) << 23);
+                qs = __uint_as_float((uint32_t)(ex - 14) << 23);
+#pragma unroll
+                for (int b = 0; b < NB; b++) {
+                    const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
+#pragma unroll
+                    for (int i = 0; i < 4; i++) qf[nt][b][i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < NB; b++) { qf[nt][b][0] = raw[b].x; qf[nt][b][1] = raw[b].y; qf[nt][b][2] = raw[b].z; qf[nt][b][3] = raw[b].w; }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
+                const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
+                const float k = f * 8388608.0f * p.scale;
+                mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
+                const int rc = 8 * nt + 2 * t4 + i;
+                pos[nt][i] = rc < n_rows ? first_pos + rc / p.group : -1;
+                m_run[nt][i] = -INFINITY;
+                l_run[nt][i] = 0.0f;
+            }
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) O[nt][b][i / 4][i % 4] = 0.0f;
+        }
+    }
+
+    // The 32 tokens of chunk c, whose record is at `rec` (shared memory); table: the dialects' magnitudes.
+    __device__ __forceinline__ void chunk(const Attention &p, const uint8_t *rec, const uint8_t *table, int at, int c, int lane) {
+        const int g = lane / 4, t4 = lane % 4;
+        // scale bytes of the lane's four rows (a word per row, a byte per tile) and 8 * id as bytes, likewise
+        uint32_t scl[4], ide[4];
+        auto load_entries = [&](int64_t scales, int64_t ids) {
+            if (NB == 4) {
+                const uint4 u = *(const uint4 *)(rec + scales + 16 * g);
+                scl[0] = u.x; scl[1] = u.y; scl[2] = u.z; scl[3] = u.w;
+                const uint2 v = *(const uint2 *)(rec + ids + 8 * g);
+                ide[0] = v.x * 8u & 0x78787878u;              // even tiles of rows j = 0, 1: bytes 2 j + b / 2
+                ide[1] = v.x >> 1 & 0x78787878u;              // odd tiles
+                ide[2] = v.y * 8u & 0x78787878u;
+                ide[3] = v.y >> 1 & 0x78787878u;
+            } else {
+                const uint2 u = *(const uint2 *)(rec + scales + 8 * g);
+                scl[0] = u.x; scl[1] = u.x >> 16; scl[2] = u.y; scl[3] = u.y >> 16;
+                const uint32_t v = *(const uint32_t *)(rec + ids + 4 * g);
+                ide[0] = v * 8u & 0x78787878u;                // even tiles of row j: byte j
+                ide[1] = v >> 1 & 0x78787878u;
+            }
+        };
+        auto table_of = [&](int j, int b) {
+            const uint32_t x = NB == 4 ? ide[2 * (j / 2) + b % 2] : ide[b % 2];
+            const int byte = NB == 4 ? 2 * (j % 2) + b / 2 : j;
+            return *(const uint2 *)(table + prmt_b32(x, 0u, 0x4440u + byte));
+        };
+        auto factor_of = [&](int j, int b) { return __uint_as_float(prmt_b32(scl[j], 0u, 0x4440u + b) * p.k23); };   // 2^e (scale byte 0: below 2^-126)
+        float sc[NT][2][4];
+        load_entries(key_scales(D), key_ids(D));
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+            const uint4 w4 = *(const uint4 *)(rec + b * 512 + lane * 16);
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            uint32_t a[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), a[j]);
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    float acc[4];
+                    mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], qf[nt][b][0], qf[nt][b][1]);
+                    mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], qf[nt][b][2], qf[nt][b][3]);
+                    const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
+                    sc[nt][x][0] = b ? fmaf(acc[0], f0, sc[nt][x][0]) : acc[0] * f0;
+                    sc[nt][x][1] = b ? fmaf(acc[1], f0, sc[nt][x][1]) : acc[1] * f0;
+                    sc[nt][x][2] = b ? fmaf(acc[2], f1, sc[nt][x][2]) : acc[2] * f1;
+                    sc[nt][x][3] = b ? fmaf(acc[3], f1, sc[nt][x][3]) : acc[3] * f1;
+                }
+        }
+        // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
+        const int tok0 = c * kChunk + 8 * (g / 2) + g % 2;
+        const bool masked = (c + 1) * kChunk > first_pos + 1 || (p.window && c * kChunk <= last_pos - p.window);
+        uint32_t pf[NT][4];
+        float alpha[NT][2];
+        bool grew = false;
+        float pv[NT][4][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                float x[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    x[j] = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
+                    if (CAP) x[j] = capped(x[j], p.softcap * 1.4426950408889634f);
+                    if (masked) {
+                        const int tok = tok0 + 2 * j;
+                        if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) x[j] = -INFINITY;
+                    }
+                }
+                float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                const float m_new = fmaxf(m_run[nt][i], top);
+                const float base = m_new == -INFINITY ? 0.0f : m_new;
+                alpha[nt][i] = fast_exp2(m_run[nt][i] - base);
+                grew |= m_new > m_run[nt][i];
+                m_run[nt][i] = m_new;
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    pv[nt][j][i] = fast_exp2(x[j] - base);
+                    sum += pv[nt][j][i];
+                }
+                l_run[nt][i] = fmaf(l_run[nt][i], alpha[nt][i], sum);
+            }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int b = 0; b < NB; b++)
+#pragma unroll
+                    for (int x = 0; x < 8; x++) O[nt][b][x / 4][x % 4] *= alpha[nt][x % 2];
+        }
+        if (c < full) {
+            // ---- values stored in 4 bits ----
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) pf[nt][j] = transpose8x8(pack_f16(pv[nt][j][0], pv[nt][j][1]));
+            load_entries(value_scales(D), value_ids(D));
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                const uint4 w4 = *(const uint4 *)(rec + value_codes(D) + b * 512 + lane * 16);
+                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                uint32_t a[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), a[j]);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++) {
+                        float acc[4];
+                        mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
+                        mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
+                        const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
+                        O[nt][b][x][0] = fmaf(acc[0], f0, O[nt][b][x][0]);
+                        O[nt][b][x][1] = fmaf(acc[1], f0, O[nt][b][x][1]);
+                        O[nt][b][x][2] = fmaf(acc[2], f1, O[nt][b][x][2]);
+                        O[nt][b][x][3] = fmaf(acc[3], f1, O[nt][b][x][3]);
+                    }
+            }
+        } else {
+            // ---- the unfinished chunk: rows of the tail; tokens behind the last one count as zeros ----
+            uint32_t lo[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float a = pv[nt][j][0], b = pv[nt][j][1];
+                    if (DT == BD_BF16) {
+                        const uint32_t hi = pack_bf16(a, b);
+                        pf[nt][j] = transpose8x8(hi);
+                        lo[nt][j] = transpose8x8(pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u)));
+                    } else {
+                        pf[nt][j] = transpose8x8(pack_f16(a, b));
+                    }
+                }
+            const int slot = p.batch.slot[at];
+            const bool slot_ok = slot >= 0 && slot < p.pool.slots;
+            if (!slot_ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
+            const uint16_t *tail = (const uint16_t *)p.pool.tail + tail_offset(p.pool, slot_ok ? slot : 0, h, c * kChunk);
+            const int left = slot_ok ? s.kv - c * kChunk : 0;
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                uint32_t a[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {             // rows 2 a + i of the 8 x 8 tile: tokens 8 a + 2 e + i
+                        const int tok = 8 * (g / 2) + 2 * e + g % 2;
+                        a[j][e] = transpose8x8(tok < left ? *(const uint32_t *)(tail + tok * D + 32 * b + 8 * j + 2 * t4) : 0u);
+                    }
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++) {
+                        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if (DT == BD_BF16) {
+                            mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
+                            mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
+                            mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], lo[nt][0], lo[nt][1]);
+                            mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], lo[nt][2], lo[nt][3]);
+                        } else {
+                            mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
+                            mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
+                        }
+#pragma unroll
+                        for (int y = 0; y < 4; y++) O[nt][b][x][y] = fmaf(acc[y], 1.0f / 8388608.0f, O[nt][b][x][y]);
+                    }
+            }
+        }
+    }
+
+    // The warp's sums over the tokens are in place in every lane.
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                float &l = l_run[nt][i];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+            }
+    }
+    // The fragments, then maximum and sum per row, in the order the joins read.
+    __device__ __forceinline__ void store_part(float *to, int lane) const {
+        const int g = lane / 4, t4 = lane % 4;
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            if (8 * nt + 2 * t4 < n_rows)
+#pragma unroll
+                for (int b = 0; b < NB; b++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++) *(float4 *)(to + (((nt * NB + b) * 2 + x) * 32 + lane) * 4) = make_float4(O[nt][b][x][0], O[nt][b][x][1], O[nt][b][x][2], O[nt][b][x][3]);
+            if (g == 0)
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    float *ml = to + NT * NB * 2 * 128 + 2 * (8 * nt + 2 * t4 + i);
+                    ml[0] = m_run[nt][i];
+                    ml[1] = l_run[nt][i];
+                }
+        }
+    }
 };
 
 // Writes one head's rows from the fragments: this lane holds channels 32 b + 8 j + g of rows 8 nt + 2 t4 + i.
-template <int NB, int NT>
-__device__ __forceinline__ void store_rows(const Attention &p, const Sequence &s, int h, int n_rows, const float (&O)[NT][NB][2][4], const float (&m)[NT][2],
-                                           const float (&l)[NT][2], int g, int t4) {
+template <int DT, int NB, int NT, bool CAP>
+__device__ __forceinline__ void store_rows(const Attention &p, const RowWork<DT, NB, NT, CAP> &k, int lane) {
+    const int g = lane / 4, t4 = lane % 4;
 #pragma unroll
     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             const int r = 8 * nt + 2 * t4 + i;
-            if (r >= n_rows) continue;
-            const int64_t row = s.q0 + r / p.group;
-            const int head = h * p.group + r % p.group;
-            const float lr = l[nt][i], f = lr > 0.0f ? 8388608.0f / lr : (lr == 0.0f ? 0.0f : lr);
+            if (r >= k.n_rows) continue;
+            const int64_t row = k.s.q0 + r / p.group;
+            const int head = k.h * p.group + r % p.group;
+            const float lr = k.l_run[nt][i], f = lr > 0.0f ? 8388608.0f / lr : (lr == 0.0f ? 0.0f : lr);
 #pragma unroll
             for (int b = 0; b < NB; b++)
 #pragma unroll
-                for (int j = 0; j < 4; j++) store_out(p, row, head, 32 * b + 8 * j + g, O[nt][b][j / 2][2 * (j % 2) + i] * f);
-            if (g == 0 && p.lse) p.lse[row * p.q_heads + head] = lr > 0.0f ? (m[nt][i] + log2f(lr)) * 0.6931471805599453f : (lr == 0.0f ? -INFINITY : lr);
+                for (int j = 0; j < 4; j++) store_out(p, row, head, 32 * b + 8 * j + g, k.O[nt][b][j / 2][2 * (j % 2) + i] * f);
+            if (g == 0 && p.lse) p.lse[row * p.q_heads + head] = lr > 0.0f ? (k.m_run[nt][i] + log2f(lr)) * 0.6931471805599453f : (lr == 0.0f ? -INFINITY : lr);
         }
 }
 
 template <int DT, int NB, int NT, bool CAP>
 __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(const __grid_constant__ Attention p) {
     using S = RowSmem<NB, NT>;
-    constexpr int D = S::D;
     extern __shared__ __align__(128) uint8_t smem[];
     volatile uint32_t *flags = (volatile uint32_t *)(smem + S::words);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t4 = lane % 4;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x < 16) ((uint2 *)(smem + S::table))[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
     if (threadIdx.x == 0) {
         flags[0] = 0; flags[1] = 1;
@@ -246,7 +524,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
         if (lane == 0) p.head_of_part[p.batch.n] = sum;
     }
     if (total == 0) return;
-    uint8_t *const ring = smem + warp * kRowStages * S::stage;
+    uint8_t *const ring = smem + S::ring + warp * kRowStages * S::stage;
     uint32_t loaded = 0, phase = 0;                               // bits per stage: a record is in flight or there; the barrier's parity
     const int per_page = p.pool.chunks_per_page;
 
@@ -313,281 +591,32 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
     enter();
     for (int i = 0; i < kRowStages && i < n_units; i++) fetch();
 
-    uint32_t qf[NT][NB][4];                                       // queries: fragments of the 8-column operand, in fp16
-    float mul[NT][2];                                             // column's factor from block sums to scores
-    int pos[NT][2];
-    float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
-    Sequence s;
-    int n_rows = 0, first_pos = 0, last_pos = 0, full = 0;
+    RowWork<DT, NB, NT, CAP> work;
     bool starts_head = true;                                      // this piece begins at the head's first unit
     for (int unit = 0; unit < n_units; unit++) {
-        if (unit == 0 || c == v.begin) {
-            // ---- a head begins (or the run does, inside one) ----
-            s = sequence_of(p.batch, at);
-            n_rows = s.t * p.group;
-            first_pos = s.kv - s.t;
-            last_pos = s.kv - 1;
-            full = s.kv / kChunk;
+        if (unit == 0 || c == v.begin) {                          // a head begins (or the run does, inside one)
+            work.begin(p, sequence_of(p.batch, at), h, lane);
             starts_head = c == v.begin;
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                const int r = 8 * nt + g;
-                const bool valid = r < n_rows;
-                const uint8_t *src = p.q + ((int64_t)(s.q0 + r / p.group) * p.ldq + (int64_t)(h * p.group + r % p.group) * p.hsq) * 2;
-                uint4 raw[NB];
-#pragma unroll
-                for (int b = 0; b < NB; b++) raw[b] = valid ? *(const uint4 *)(src + (32 * b + 8 * t4) * 2) : make_uint4(0, 0, 0, 0);
-                float qs = 1.0f;
-                if (DT == BD_BF16) {
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int b = 0; b < NB; b++) m = absmax_bf16x2(m, absmax_bf16x2(absmax_bf16x2(raw[b].x, raw[b].y), absmax_bf16x2(raw[b].z, raw[b].w)));
-                    m = max(m & 0x7fffu, m >> 16 & 0x7fffu);
-                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                    const int ex = min(max((int)(m >> 7), 27), 240);      // biased exponent of the row's largest element
-                    const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - ex) << 23);
-                    qs = __uint_as_float((uint32_t)(ex - 14) << 23);
-#pragma unroll
-                    for (int b = 0; b < NB; b++) {
-                        const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
-#pragma unroll
-                        for (int i = 0; i < 4; i++) qf[nt][b][i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
-                    }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < NB; b++) { qf[nt][b][0] = raw[b].x; qf[nt][b][1] = raw[b].y; qf[nt][b][2] = raw[b].z; qf[nt][b][3] = raw[b].w; }
-                }
-#pragma unroll
-                for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
-                    const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
-                    const float k = f * 8388608.0f * p.scale;
-                    mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
-                    const int rc = 8 * nt + 2 * t4 + i;
-                    pos[nt][i] = rc < n_rows ? first_pos + rc / p.group : -1;
-                    m_run[nt][i] = -INFINITY;
-                    l_run[nt][i] = 0.0f;
-                }
-#pragma unroll
-                for (int b = 0; b < NB; b++)
-#pragma unroll
-                    for (int i = 0; i < 8; i++) O[nt][b][i / 4][i % 4] = 0.0f;
-            }
         }
         const int st = unit % kRowStages;
-        const uint8_t *rec = ring + st * S::stage;
         if (loaded >> st & 1u) {
             if (!tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags)) return;   // (status word; this warp's later results stay unwritten)
             phase ^= 1u << st;
             __syncwarp();
-            // scale bytes of the lane's four rows (a word per row, a byte per tile) and 8 * id as bytes, likewise
-            uint32_t scl[4], ide[4];
-            auto load_entries = [&](int64_t scales, int64_t ids) {
-                if (NB == 4) {
-                    const uint4 u = *(const uint4 *)(rec + scales + 16 * g);
-                    scl[0] = u.x; scl[1] = u.y; scl[2] = u.z; scl[3] = u.w;
-                    const uint2 v = *(const uint2 *)(rec + ids + 8 * g);
-                    ide[0] = v.x * 8u & 0x78787878u;              // even tiles of rows j = 0, 1: bytes 2 j + b / 2
-                    ide[1] = v.x >> 1 & 0x78787878u;              // odd tiles
-                    ide[2] = v.y * 8u & 0x78787878u;
-                    ide[3] = v.y >> 1 & 0x78787878u;
-                } else {
-                    const uint2 u = *(const uint2 *)(rec + scales + 8 * g);
-                    scl[0] = u.x; scl[1] = u.x >> 16; scl[2] = u.y; scl[3] = u.y >> 16;
-                    const uint32_t v = *(const uint32_t *)(rec + ids + 4 * g);
-                    ide[0] = v * 8u & 0x78787878u;                // even tiles of row j: byte j
-                    ide[1] = v >> 1 & 0x78787878u;
-                }
-            };
-            auto table_of = [&](int j, int b) {
-                const uint32_t x = NB == 4 ? ide[2 * (j / 2) + b % 2] : ide[b % 2];
-                const int byte = NB == 4 ? 2 * (j % 2) + b / 2 : j;
-                return *(const uint2 *)(smem + S::table + prmt_b32(x, 0u, 0x4440u + byte));
-            };
-            auto factor_of = [&](int j, int b) { return __uint_as_float(prmt_b32(scl[j], 0u, 0x4440u + b) * p.k23); };   // 2^e (scale byte 0: below 2^-126)
-            float sc[NT][2][4];
-            load_entries(key_scales(D), key_ids(D));
-#pragma unroll
-            for (int b = 0; b < NB; b++) {
-                const uint4 w4 = *(const uint4 *)(rec + b * 512 + lane * 16);
-                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-                uint32_t a[4][4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), p.k16, a[j]);
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        float acc[4];
-                        mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], qf[nt][b][0], qf[nt][b][1]);
-                        mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], qf[nt][b][2], qf[nt][b][3]);
-                        const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
-                        sc[nt][x][0] = b ? fmaf(acc[0], f0, sc[nt][x][0]) : acc[0] * f0;
-                        sc[nt][x][1] = b ? fmaf(acc[1], f0, sc[nt][x][1]) : acc[1] * f0;
-                        sc[nt][x][2] = b ? fmaf(acc[2], f1, sc[nt][x][2]) : acc[2] * f1;
-                        sc[nt][x][3] = b ? fmaf(acc[3], f1, sc[nt][x][3]) : acc[3] * f1;
-                    }
-            }
-            // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
-            const int tok0 = c * kChunk + 8 * (g / 2) + g % 2;
-            const bool masked = (c + 1) * kChunk > first_pos + 1 || (p.window && c * kChunk <= last_pos - p.window);
-            uint32_t pf[NT][4];
-            float alpha[NT][2];
-            bool grew = false;
-            float pv[NT][4][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    float x[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        x[j] = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
-                        if (CAP) x[j] = capped(x[j], p.softcap * 1.4426950408889634f);
-                        if (masked) {
-                            const int tok = tok0 + 2 * j;
-                            if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) x[j] = -INFINITY;
-                        }
-                    }
-                    float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float m_new = fmaxf(m_run[nt][i], top);
-                    const float base = m_new == -INFINITY ? 0.0f : m_new;
-                    alpha[nt][i] = fast_exp2(m_run[nt][i] - base);
-                    grew |= m_new > m_run[nt][i];
-                    m_run[nt][i] = m_new;
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        pv[nt][j][i] = fast_exp2(x[j] - base);
-                        sum += pv[nt][j][i];
-                    }
-                    l_run[nt][i] = fmaf(l_run[nt][i], alpha[nt][i], sum);
-                }
-            if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int b = 0; b < NB; b++)
-#pragma unroll
-                        for (int x = 0; x < 8; x++) O[nt][b][x / 4][x % 4] *= alpha[nt][x % 2];
-            }
-            if (c < full) {
-                // ---- values stored in 4 bits ----
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) pf[nt][j] = transpose8x8(pack_f16(pv[nt][j][0], pv[nt][j][1]));
-                load_entries(value_scales(D), value_ids(D));
-#pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    const uint4 w4 = *(const uint4 *)(rec + value_codes(D) + b * 512 + lane * 16);
-                    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-                    uint32_t a[4][4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), p.k16, a[j]);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int x = 0; x < 2; x++) {
-                            float acc[4];
-                            mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
-                            mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
-                            const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
-                            O[nt][b][x][0] = fmaf(acc[0], f0, O[nt][b][x][0]);
-                            O[nt][b][x][1] = fmaf(acc[1], f0, O[nt][b][x][1]);
-                            O[nt][b][x][2] = fmaf(acc[2], f1, O[nt][b][x][2]);
-                            O[nt][b][x][3] = fmaf(acc[3], f1, O[nt][b][x][3]);
-                        }
-                }
-            } else {
-                // ---- the unfinished chunk: rows of the tail; tokens behind the last one count as zeros ----
-                uint32_t lo[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const float a = pv[nt][j][0], b = pv[nt][j][1];
-                        if (DT == BD_BF16) {
-                            const uint32_t hi = pack_bf16(a, b);
-                            pf[nt][j] = transpose8x8(hi);
-                            lo[nt][j] = transpose8x8(pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u)));
-                        } else {
-                            pf[nt][j] = transpose8x8(pack_f16(a, b));
-                        }
-                    }
-                const int slot = p.batch.slot[at];
-                const bool slot_ok = slot >= 0 && slot < p.pool.slots;
-                if (!slot_ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
-                const uint16_t *tail = (const uint16_t *)p.pool.tail + tail_offset(p.pool, slot_ok ? slot : 0, h, c * kChunk);
-                const int left = slot_ok ? s.kv - c * kChunk : 0;
-#pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    uint32_t a[4][4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {             // rows 2 a + i of the 8 x 8 tile: tokens 8 a + 2 e + i
-                            const int tok = 8 * (g / 2) + 2 * e + g % 2;
-                            a[j][e] = transpose8x8(tok < left ? *(const uint32_t *)(tail + tok * D + 32 * b + 8 * j + 2 * t4) : 0u);
-                        }
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int x = 0; x < 2; x++) {
-                            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                            if (DT == BD_BF16) {
-                                mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
-                                mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
-                                mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], lo[nt][0], lo[nt][1]);
-                                mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], lo[nt][2], lo[nt][3]);
-                            } else {
-                                mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
-                                mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
-                            }
-#pragma unroll
-                            for (int y = 0; y < 4; y++) O[nt][b][x][y] = fmaf(acc[y], 1.0f / 8388608.0f, O[nt][b][x][y]);
-                        }
-                }
-            }
+            work.chunk(p, ring + st * S::stage, smem + S::table, at, c, lane);
         }
         __syncwarp();                                             // every lane is done with the stage
         if (fetched < n_units) fetch();
         const bool ends_head = c + 1 == v.begin + v.units;
         if (ends_head || unit + 1 == n_units) {
-            // ---- the piece is done: the head's result, or a part of it ----
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    float &l = l_run[nt][i];
-                    l += __shfl_xor_sync(0xffffffffu, l, 4);
-                    l += __shfl_xor_sync(0xffffffffu, l, 8);
-                    l += __shfl_xor_sync(0xffffffffu, l, 16);
-                }
+            // the piece is done: the head's result, or a part of it
+            work.finish();
             if (starts_head && ends_head) {
-                store_rows<NB, NT>(p, s, h, n_rows, O, m_run, l_run, g, t4);
+                store_rows(p, work, lane);
             } else {
                 // the piece at the run's start has slot 0; one that begins a head later in the run is the run's last: slot 1
                 const bool at_start = unit <= c - v.begin;
-                float *to = p.part + (int64_t)(2 * run + (at_start ? 0 : 1)) * part_floats<NB, NT>();
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    if (8 * nt + 2 * t4 < n_rows)
-#pragma unroll
-                        for (int b = 0; b < NB; b++)
-#pragma unroll
-                            for (int x = 0; x < 2; x++) *(float4 *)(to + (((nt * NB + b) * 2 + x) * 32 + lane) * 4) = make_float4(O[nt][b][x][0], O[nt][b][x][1], O[nt][b][x][2], O[nt][b][x][3]);
-                    if (g == 0)
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            float *ml = to + NT * NB * 2 * 128 + 2 * (8 * nt + 2 * t4 + i);
-                            ml[0] = m_run[nt][i];
-                            ml[1] = l_run[nt][i];
-                        }
-                }
+                work.store_part(p.part + (int64_t)(2 * run + (at_start ? 0 : 1)) * part_floats<NB, NT>(), lane);
             }
         }
         if (ends_head && unit + 1 < n_units) {
@@ -604,6 +633,101 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
         }
     }
   }
+}
+
+// Short contexts: a CTA takes a whole head, its warps the head's chunks in turn, and the warps' parts meet in shared memory,
+// so that the call is one launch (one sequence of 513 tokens: WHOLE_A us against WHOLE_B us through runs and the join kernel).
+template <int DT, int NB, int NT, bool CAP>
+__global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(const __grid_constant__ Attention p) {
+    using S = RowSmem<NB, NT>;
+    static_assert(part_floats<NB, NT>() * 4 <= kRowStages * S::stage, "a warp's part takes the place of its records");
+    extern __shared__ __align__(128) uint8_t smem[];
+    volatile uint32_t *flags = (volatile uint32_t *)(smem + S::words);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32, h = blockIdx.x, seq = blockIdx.y;
+    if (threadIdx.x < 16) ((uint2 *)(smem + S::table))[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
+    if (threadIdx.x == 0) {
+        flags[0] = 0; flags[1] = 1;
+        flags[2] = g_debug_spin_limit ? g_debug_spin_limit : tc::kSpinLimit;
+    }
+    const uint32_t bar0 = tc::smem_u32(smem + S::bars) + warp * kRowStages * 8;
+    if (lane == 0)
+        for (int i = 0; i < kRowStages; i++) tc::mbar_init(bar0 + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    pdl_wait();
+    pdl_release();
+    const Sequence s = sequence_of(p.batch, seq);
+    if (!s.ok) {
+        if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
+        return;
+    }
+    if (s.t == 0) return;
+    const Visible v = visible_of(s, p.window);
+    uint8_t *const ring = smem + S::ring + warp * kRowStages * S::stage;
+    const int n = v.end > v.begin + warp ? (v.end - v.begin - warp + warps - 1) / warps : 0;     // this warp's chunks
+    const int32_t *pages = p.batch.table + (int64_t)seq * p.batch.ld_table;
+    uint32_t loaded = 0, phase = 0;
+    int page = -1;
+    auto look_up = [&](int i) { if (i < n) page = pages[fast_div(v.begin + warp + i * warps, p.by_page)]; };
+    auto fetch = [&](int i) {
+        const int st = i % kRowStages, c = v.begin + warp + i * warps;
+        const bool ok = page >= 0 && page < p.pool.pages;
+        if (!ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
+        loaded = ok ? loaded | 1u << st : loaded & ~(1u << st);
+        if (ok && lane == 0) {
+            const int in = c - (int)fast_div(c, p.by_page) * p.pool.chunks_per_page;
+            tc::mbar_expect_tx(bar0 + 8 * st, S::stage);
+            tc::bulk_load(tc::smem_u32(ring + st * S::stage), p.pool.base + (((int64_t)page * p.pool.kv_heads + h) * p.pool.chunks_per_page + in) * S::stage, S::stage, bar0 + 8 * st);
+        }
+        look_up(i + 1);
+    };
+    look_up(0);
+    for (int i = 0; i < kRowStages && i < n; i++) fetch(i);
+    RowWork<DT, NB, NT, CAP> work;
+    work.begin(p, s, h, lane);
+    bool alive = true;
+    for (int i = 0; i < n; i++) {
+        const int st = i % kRowStages;
+        if (loaded >> st & 1u) {
+            alive = tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags);
+            if (!alive) break;
+            phase ^= 1u << st;
+            __syncwarp();
+            work.chunk(p, ring + st * S::stage, smem + S::table, seq, v.begin + warp + i * warps, lane);
+        }
+        __syncwarp();
+        if (i + kRowStages < n) fetch(i + kRowStages);
+    }
+    work.finish();
+    __syncwarp();                                                 // (the warp's records are read)
+    work.store_part((float *)ring, lane);
+    __syncthreads();
+    if (flags[0]) return;                                         // a wait ran out (status word): nothing is written
+    // thread = fragment piece and lane, as in the join kernel
+    for (int i = threadIdx.x; i < NT * NB * 2 * 32; i += blockDim.x) {
+        const int piece = i / 32, nt = piece / (2 * NB), b = piece / 2 % NB, x = piece % 2, t4 = lane % 4, g = lane / 4;
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int r = 8 * nt + 2 * t4 + k;
+            if (r >= work.n_rows) continue;
+            float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+            for (int w = 0; w < warps; w++) m = fmaxf(m, ((const float *)(smem + S::ring + w * kRowStages * S::stage))[NT * NB * 2 * 128 + 2 * r]);
+            const float zero = m == -INFINITY ? 0.0f : m;
+            for (int w = 0; w < warps; w++) {
+                const float *part = (const float *)(smem + S::ring + w * kRowStages * S::stage);
+                const float f = fast_exp2(part[NT * NB * 2 * 128 + 2 * r] - zero);
+                l = fmaf(part[NT * NB * 2 * 128 + 2 * r + 1], f, l);
+                o0 = fmaf(part[(piece * 32 + lane) * 4 + k], f, o0);
+                o1 = fmaf(part[(piece * 32 + lane) * 4 + 2 + k], f, o1);
+            }
+            const int64_t row = s.q0 + r / p.group;
+            const int head = h * p.group + r % p.group;
+            const float f = l > 0.0f ? 8388608.0f / l : (l == 0.0f ? 0.0f : l);
+            store_out(p, row, head, 32 * b + 16 * x + g, o0 * f);
+            store_out(p, row, head, 32 * b + 16 * x + 8 + g, o1 * f);
+            if (b == 0 && x == 0 && g == 0 && p.lse) p.lse[row * p.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
+        }
+    }
 }
 
 // Joins the parts of heads that several runs share, in unit order.  A CTA per sequence and KV head; thread = the fragment

@@ -59,65 +59,6 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
         : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
 
-// Byte tables of a dialect's magnitudes h * 2^(scale - 128) in bf16 or fp16: lo[8], hi[8].
-//   bf16: exponent field msb(h) + scale - 1; with scale = 2 k + p the high byte is k - 1 + ((msb + p + 1) >> 1) and bit 7 of
-//         the low byte (msb + p + 1) & 1, so the stored tables (one per dialect and p) take (k - 1) in every byte but that of zero;
-//   fp16: high byte 4 * (msb + scale - 113) + two mantissa bits, low byte the third one: 4 * (scale - 113) is added.
-// Blocks outside the range of those sums (bf16: scale < 2, values below 2^-123, taken as zero; fp16: scale < 114, where
-// subnormals begin) are built value by value.
-template <int DT>
-__device__ __forceinline__ uint4 base_table(int id, int p) {
-    uint32_t b[4] = {0, 0, 0, 0};
-    for (int i = 1; i < 8; i++) {
-        const uint32_t h = (i < 4 ? c_tables.int_lo[id] >> (8 * i) : c_tables.int_hi[id] >> (8 * (i - 4))) & 255u;
-        const int m = 31 - __clz(h);
-        const uint32_t mant = (h << 3 >> m) & 7u;
-        uint32_t lo, hi;
-        if (DT == BD_BF16) {
-            hi = (uint32_t)(m + p + 1) >> 1;
-            lo = (uint32_t)(m + p + 1 & 1) << 7 | mant << 4;
-        } else {
-            hi = (uint32_t)m << 2 | mant >> 1;
-            lo = (mant & 1u) << 7;
-        }
-        b[i / 4] |= lo << (8 * (i % 4));
-        b[2 + i / 4] |= hi << (8 * (i % 4));
-    }
-    return make_uint4(b[0], b[1], b[2], b[3]);
-}
-template <int DT>
-__device__ __forceinline__ uint4 block_table(const uint4 *base, uint32_t id, uint32_t scale) {
-    uint4 t = base[DT == BD_BF16 ? 2 * id + (scale & 1u) : id];
-    if (DT == BD_BF16) {
-        const uint32_t k = (scale >> 1) - 1u;
-        t.z += k * 0x01010100u;
-        t.w += k * 0x01010101u;
-        if (scale < 2u) t = make_uint4(0, 0, 0, 0);
-    } else {
-        const uint32_t k = (scale - 113u) * 4u;
-        t.z += k * 0x01010100u;
-        t.w += k * 0x01010101u;
-        if (scale < 114u) {
-            uint32_t b[4] = {0, 0, 0, 0};
-            const uint32_t tlo = c_tables.int_lo[id], thi = c_tables.int_hi[id];
-#pragma unroll
-            for (int i = 1; i < 8; i++) {
-                const uint32_t h = __half_as_ushort(__float2half_rn((float)((i < 4 ? tlo >> (8 * i) : thi >> (8 * (i - 4))) & 255u) * half_unit(scale)));
-                b[i / 4] |= (h & 255u) << (8 * (i % 4));
-                b[2 + i / 4] |= (h >> 8) << (8 * (i % 4));
-            }
-            t = make_uint4(b[0], b[1], b[2], b[3]);
-        }
-    }
-    return t;
-}
-__device__ __forceinline__ uint4 expand_word(uint32_t w, const uint4 &t) {
-    const uint32_t sel = w & 0x77777777u, sel_b = sel >> 16, even = w << 4;
-    const uint32_t lo_a = prmt_b32(t.x, t.y, sel), lo_b = prmt_b32(t.x, t.y, sel_b);
-    const uint32_t hi_a = prmt_b32(t.z, t.w, sel) | (prmt_b32(even, w, 0x5140u) & 0x80808080u);
-    const uint32_t hi_b = prmt_b32(t.z, t.w, sel_b) | (prmt_b32(even, w, 0x7362u) & 0x80808080u);
-    return make_uint4(prmt_b32(lo_a, hi_a, 0x6240u), prmt_b32(lo_a, hi_a, 0x7351u), prmt_b32(lo_b, hi_b, 0x6240u), prmt_b32(lo_b, hi_b, 0x7351u));
-}
 // 16-byte piece `piece` (of 16-bit elements 8 piece ..) of row `row` in a K-major tile of `rows` rows: halves of 64
 // elements, 128-byte rows, 128-byte swizzle.
 __device__ __forceinline__ uint32_t swizzled(int rows, int row, int piece) {
@@ -144,7 +85,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     volatile uint32_t *const chunk_ok = (volatile uint32_t *)(sm + S::flags);       // [8 tiles]: bit e = chunk e of the tile has a page
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, wg = warp / 4;
 
-    if (threadIdx.x < 32) ((uint4 *)(sm + S::table))[threadIdx.x] = base_table<DT>(DT == BD_BF16 ? threadIdx.x / 2 : threadIdx.x % 16, threadIdx.x & 1);
+    make_base_tables<DT>((uint4 *)(sm + S::table));
     if (threadIdx.x < 8) chunk_ok[threadIdx.x] = 0;
     if (threadIdx.x == 0) {
         abort_flag[0] = 0;
@@ -394,7 +335,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (off >= 0) {
 #pragma unroll
                 for (int b = 0; b < NB; b++) {
-                    const uint4 t = block_table<DT>(table, kx.ids >> (4 * b) & 15u, kx.scales >> (8 * b) & 255u);
+                    const uint4 t = block_table<DT, false>(table, kx.ids >> (4 * b) & 15u, kx.scales >> (8 * b) & 255u);
 #pragma unroll
                     for (int q = 0; q < 4; q++) *(uint4 *)(kt + swizzled(128, 32 * e + lane, 4 * b + q)) = expand_word(kx.w[b][q], t);
                 }
@@ -415,7 +356,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (stored) {
 #pragma unroll
                 for (int b = 0; b < NB; b++) {
-                    const uint4 t = block_table<DT>(table, vx.ids >> (4 * b) & 15u, vx.scales >> (8 * b) & 255u);
+                    const uint4 t = block_table<DT, false>(table, vx.ids >> (4 * b) & 15u, vx.scales >> (8 * b) & 255u);
 #pragma unroll
                     for (int q = 0; q < 4; q++) *(uint4 *)(vt + swizzled(D, 32 * b + lane, 4 * e + q)) = expand_word(vx.w[b][q], t);
                 }

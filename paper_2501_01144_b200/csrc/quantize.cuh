@@ -255,11 +255,18 @@ __device__ __forceinline__ uint32_t absmax_f32(uint32_t a, uint32_t b) {
     return d;
 }
 
+// Where the quantizers below put element e of a group: its slot of the operand layout, or (PAGED) its nibble in the words of
+// the paged KV cache, where sign and index share a nibble and elements 1, 2 and 5, 6 change places.
+template <bool PAGED>
+__device__ __forceinline__ constexpr int place_of(int e) {
+    return !PAGED ? slot_of(e) : e == 1 ? 2 : e == 2 ? 1 : e == 5 ? 6 : e == 6 ? 5 : e;
+}
+
 // Two-stage rule on a block of 32 fp32 bit patterns with the arithmetic of the bf16 fast path below: the
 // maximum as a tree of |.|-maxima, one fma.rz per element on |x| for its 5-bit code (a clamped block is
 // prescaled by 2^64 first), popcount of the shifted merged threshold mask, signs gathered with byte permutes
 // (three per four elements).  BYTES: operand bytes in e4m3[0..7] instead of indices in res.words.
-template <bool BYTES>
+template <bool BYTES, bool PAGED = false>
 __device__ __forceinline__ void quantize_two_stage_f32(const uint32_t (&bits_in)[32], const SmemTables &tab, BlockResult &res,
                                                        uint32_t (&e4m3)[8], bool &nonfinite) {
     uint32_t bits[32], t16[16];
@@ -290,12 +297,14 @@ __device__ __forceinline__ void quantize_two_stage_f32(const uint32_t (&bits_in)
 #pragma unroll
     for (int k = 0; k < 32; k++) {
         const uint32_t t = __float_as_uint(__fmaf_rz(fabsf(__uint_as_float(bits[k])), scale, 8388608.0f));
-        v[k / 8] = (uint32_t)__popc(__funnelshift_r(above, 0u, t)) * (1u << (4 * slot_of(k % 8))) + v[k / 8];
+        v[k / 8] = (uint32_t)__popc(__funnelshift_r(above, 0u, t)) * (1u << (4 * place_of<PAGED>(k % 8))) + v[k / 8];
     }
 #pragma unroll
     for (int w = 0; w < 4; w++) {                                 // the top bytes of the group's eight elements
-        s03[w] = prmt_b32(prmt_b32(bits[8 * w], bits[8 * w + 1], 0x0073u), prmt_b32(bits[8 * w + 2], bits[8 * w + 3], 0x0073u), 0x5410u);
-        s47[w] = prmt_b32(prmt_b32(bits[8 * w + 4], bits[8 * w + 5], 0x0073u), prmt_b32(bits[8 * w + 6], bits[8 * w + 7], 0x0073u), 0x5410u);
+        // (PAGED: elements 2, 3, 6, 7 have their signs in the odd nibbles, 0, 1, 4, 5 in the even ones)
+        const int f = PAGED ? 2 : 0, o = PAGED ? -2 : 0;
+        s03[w] = prmt_b32(prmt_b32(bits[8 * w + f], bits[8 * w + 1 + f], 0x0073u), prmt_b32(bits[8 * w + 2 + 2 * f], bits[8 * w + 3 + 2 * f], 0x0073u), 0x5410u);
+        s47[w] = prmt_b32(prmt_b32(bits[8 * w + 4 + 2 * o], bits[8 * w + 5 + 2 * o], 0x0073u), prmt_b32(bits[8 * w + 6 + o], bits[8 * w + 7 + o], 0x0073u), 0x5410u);
     }
     res.scale = eadj - 2u;
     if (BYTES) {
@@ -325,7 +334,7 @@ __device__ __forceinline__ void quantize_two_stage_f32(const uint32_t (&bits_in)
 // A block whose exponent is clamped (maximum below 2^-123, eadj < 4) would need a scale of 2^128 or more: its
 // elements are first multiplied by 2^64 (exact for a power of two, subnormal inputs included) and the scale
 // shrinks by the same factor, so the common arithmetic serves it too, with no call and no local memory.
-template <bool BYTES>
+template <bool BYTES, bool PAGED = false>
 __device__ __forceinline__ void quantize_bf16_block(const uint32_t (&Rin)[16], const SmemTables &tab, BlockResult &res,
                                                     uint32_t (&e4m3)[8]) {
     uint32_t R[16], s03[4], s47[4];
@@ -354,8 +363,9 @@ __device__ __forceinline__ void quantize_bf16_block(const uint32_t (&Rin)[16], c
 #pragma unroll
     for (int w = 0; w < 4; w++) {
         // the high byte of each bf16 carries its sign in bit 7
-        s03[w] = prmt_b32(R[4 * w], R[4 * w + 1], 0x7531u);
-        s47[w] = prmt_b32(R[4 * w + 2], R[4 * w + 3], 0x7531u);
+        // (PAGED: as above)
+        s03[w] = prmt_b32(R[4 * w + (PAGED ? 1 : 0)], R[4 * w + (PAGED ? 3 : 1)], 0x7531u);
+        s47[w] = prmt_b32(R[4 * w + (PAGED ? 0 : 2)], R[4 * w + (PAGED ? 2 : 3)], 0x7531u);
     }
     const float scale = __uint_as_float((258u - eadj_eff) << 23);        // 2^(2 - e) (over 2^64 for a clamped block), e = eadj - 129
     const uint32_t m5 = __float_as_uint(__fmaf_rz(amax_f, scale, 8388608.0f)) & 63u;
@@ -371,8 +381,8 @@ __device__ __forceinline__ void quantize_bf16_block(const uint32_t (&Rin)[16], c
         // funnel shift in wrap mode uses only the low five bits of the count, i.e. q5
         const uint32_t v_lo = __popc(__funnelshift_r(above, 0u, t_lo));
         const uint32_t v_hi = __popc(__funnelshift_r(above, 0u, t_hi));
-        v[i / 4] = v_lo * (1u << (4 * slot_of(2 * (i % 4)))) + v[i / 4];
-        v[i / 4] = v_hi * (1u << (4 * slot_of(2 * (i % 4) + 1))) + v[i / 4];
+        v[i / 4] = v_lo * (1u << (4 * place_of<PAGED>(2 * (i % 4)))) + v[i / 4];
+        v[i / 4] = v_hi * (1u << (4 * place_of<PAGED>(2 * (i % 4) + 1))) + v[i / 4];
     }
     res.scale = eadj - 2u;
     if (BYTES) {
