@@ -430,6 +430,7 @@ unsigned paged_chunks(const bd_paged_batch *b) {                   // chunks tha
 struct AttentionPlan {
     bool chunk, wide, whole;          // whole: rows kernel with a CTA per head, one launch
     int tiles, splits;                // chunk kernel: tiles of 256 rows, CTAs that share a tile's tokens
+    size_t images;                    // bytes of the tiles expanded in front, 0: every CTA expands its own
     int workers, rounds;              // rows kernel: warps, and the runs each takes at most
 };
 AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, int64_t window) {
@@ -440,6 +441,8 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
         r.tiles = (int)((rows + 255) / 256);
         const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), tiles = (b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens;
         r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(148 / ctas, tiles / 4));
+        const size_t images = (size_t)b->n * (size_t)c->kv_heads * (size_t)tiles * (size_t)(2 * 128 * c->head_dim * 2);
+        if (r.tiles >= 4 && images <= ((size_t)1 << 30)) r.images = images;
         return r;
     }
     r.wide = rows > 8;
@@ -464,7 +467,10 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
 size_t row_parts_offset(const bd_paged_batch *b) { return ((size_t)(b->n + 1) * sizeof(uint32_t) + 255) / 256 * 256; }   // behind the sequences' unit numbers
 size_t attention_workspace(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, int64_t window) {
     const AttentionPlan r = attention_plan(c, b, q_heads, window);
-    if (r.chunk) return r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+    if (r.chunk) {
+        const size_t parts = r.splits > 1 ? (size_t)r.splits * (size_t)b->rows * (size_t)q_heads * (size_t)(c->head_dim + 2) * sizeof(float) : 0;
+        return r.images ? align256(parts) + r.images + r.images / (size_t)(2 * 128 * c->head_dim * 2) * sizeof(uint32_t) : parts;
+    }
     if (r.whole) return 0;
     const int floats = c->head_dim == 128 ? (r.wide ? pg::part_floats<4, 2>() : pg::part_floats<4, 1>()) : (r.wide ? pg::part_floats<2, 2>() : pg::part_floats<2, 1>());
     return row_parts_offset(b) + (size_t)r.workers * (size_t)r.rounds * 2 * (size_t)floats * sizeof(float);
@@ -507,20 +513,24 @@ bd_status launch_rows_dtype(const pg::Attention &a, bool wide, cudaStream_t st) 
     if (a.pool.head_dim == 128) return wide ? launch_rows<DT, 4, 2>(a, st) : launch_rows<DT, 4, 1>(a, st);
     return wide ? launch_rows<DT, 2, 2>(a, st) : launch_rows<DT, 2, 1>(a, st);
 }
-template <int DT, int NB, bool CAP>
+template <int DT, int NB, bool CAP, bool IMAGES>
 bd_status launch_chunk_kernel(const pg::Attention &a, dim3 grid, cudaStream_t st) {
     constexpr int smem = pg::ChunkSmem<NB>::total;
     static bool configured[kMaxDevices] = {};
-    const bd_status s = allow_smem(pg::attention_chunk_kernel<DT, NB, CAP>, smem, configured);
+    const bd_status s = allow_smem(pg::attention_chunk_kernel<DT, NB, CAP, IMAGES>, smem, configured);
     if (s) return s;
-    launch_serialized(pg::attention_chunk_kernel<DT, NB, CAP>, grid, pg::kChunkThreads, smem, st, a);
+    if (IMAGES) launch_serialized(pg::expand_kernel<DT, NB>, dim3((unsigned)a.image_tiles, (unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 256, 0, st, a);
+    launch_serialized(pg::attention_chunk_kernel<DT, NB, CAP, IMAGES>, grid, pg::kChunkThreads, smem, st, a);
     return BD_OK;
+}
+template <int DT, int NB>
+bd_status launch_chunk_dim(const pg::Attention &a, dim3 grid, cudaStream_t st) {
+    if (a.softcap > 0.0f) return a.images ? launch_chunk_kernel<DT, NB, true, true>(a, grid, st) : launch_chunk_kernel<DT, NB, true, false>(a, grid, st);
+    return a.images ? launch_chunk_kernel<DT, NB, false, true>(a, grid, st) : launch_chunk_kernel<DT, NB, false, false>(a, grid, st);
 }
 template <int DT>
 bd_status launch_chunk(const pg::Attention &a, dim3 grid, cudaStream_t st) {
-    const bool cap = a.softcap > 0.0f;
-    if (a.pool.head_dim == 128) return cap ? launch_chunk_kernel<DT, 4, true>(a, grid, st) : launch_chunk_kernel<DT, 4, false>(a, grid, st);
-    return cap ? launch_chunk_kernel<DT, 2, true>(a, grid, st) : launch_chunk_kernel<DT, 2, false>(a, grid, st);
+    return a.pool.head_dim == 128 ? launch_chunk_dim<DT, 4>(a, grid, st) : launch_chunk_dim<DT, 2>(a, grid, st);
 }
 template <int DT, int D, int HEADS>
 void launch_rotate_heads(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
@@ -1466,6 +1476,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     if (q_heads <= 0 || window < 0 || !(scale == scale) || !(softcap >= 0.0f) || softcap > 1e30f) return BD_ERR_INVALID_ARG;
     if (odtype != BD_F32 && odtype != BD_BF16 && odtype != BD_F16) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads) return BD_ERR_SHAPE;
+    if (b->max_q * (q_heads / c->kv_heads) > 65535ll * 256) return BD_ERR_UNSUPPORTED;
     if (c->dtype == BD_F32 || (odtype != BD_F32 && odtype != c->dtype) || q_heads > 65535) return BD_ERR_UNSUPPORTED;
     if ((s = check_rows(Q, b->rows, q_heads, c->head_dim, ldq, head_stride_q, 2))) return s;
     if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
@@ -1496,7 +1507,13 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
         s = c->dtype == BD_BF16 ? launch_rows_dtype<BD_BF16>(a, plan.wide, st) : launch_rows_dtype<BD_F16>(a, plan.wide, st);
         return s ? s : launch_result(plan.whole ? 1 : 2);
     }
-    const dim3 grid((unsigned)(plan.splits * plan.tiles), (unsigned)c->kv_heads, (unsigned)b->n);
+    if (plan.images) {
+        const size_t parts = attention_workspace(c, b, q_heads, window) - plan.images - plan.images / (size_t)(2 * 128 * c->head_dim * 2) * sizeof(uint32_t);
+        a.images = (uint8_t *)workspace + parts;
+        a.image_ok = (uint32_t *)(a.images + plan.images);
+        a.image_tiles = (int)((b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens);
+    }
+    const dim3 grid((unsigned)(plan.splits * c->kv_heads), (unsigned)plan.tiles, (unsigned)b->n);
     s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);
     if (s) return s;
     if (plan.splits > 1) {
@@ -1504,7 +1521,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
         if (c->head_dim == 128) launch_serialized(pg::attention_join_kernel<128>, join, 128, 0, st, a);
         else launch_serialized(pg::attention_join_kernel<64>, join, 128, 0, st, a);
     }
-    return launch_result(plan.splits > 1 ? 2 : 1);
+    return launch_result((plan.splits > 1 ? 2 : 1) + (plan.images ? 1 : 0));
 }
 
 bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd_dtype dtype, int64_t rows, int64_t head_dim,

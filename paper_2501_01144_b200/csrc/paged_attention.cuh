@@ -45,6 +45,9 @@ struct Attention {
     bool whole;                       // rows kernel: a CTA per head (workers: its warps)
     int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
     FastDiv by_runs[4], by_page;      // division by workers * (1 .. 4), by the chunks of a page
+    uint8_t *images;                  // chunk kernel: expanded tiles (null: expanded by every CTA), [n][kv_heads][image_tiles]
+    uint32_t *image_ok;
+    int image_tiles;
     uint32_t *head_of_part;           // rows kernel: [n + 1] units in front of each sequence, then all units
     uint32_t k23;                     // 2^23: a left shift as a multiplication by an operand the compiler does not see
 };

@@ -14,6 +14,8 @@
 // exponent bits; a code word becomes eight values with byte permutes alone.  Keys keep the record's row order in the
 // tile, which only permutes the columns of S; P is written in token order.
 // P is rounded to the cache's type (8 or 11 bits): the MMA takes both operands of one type.
+// When many CTAs read the same tokens (IMAGES), a kernel in front expands every tile once into the workspace, in the layout it
+// has in shared memory, and one thread copies the tiles with bulk copies: the softmax then has the SM's issue slots for itself.
 // All waits are bounded; a wait that runs out raises the abort word, every role drains and nothing is written.
 #pragma once
 #include "gemm_tc.cuh"
@@ -22,7 +24,7 @@
 namespace bd {
 namespace pg {
 
-constexpr int kChunkThreads = 512;            // launched with 128 registers a thread = 4 warpgroups x 128; split 184 + 184 + 96 + 48
+constexpr int kChunkThreads = 512;            // launched with 128 registers a thread = 4 warpgroups x 128; split 184 + 184 + 96 + 48, or 208 + 208 + 48 + 48
 constexpr int kTileTokens = 128;
 
 template <int NB>
@@ -72,7 +74,92 @@ struct Lane {
     uint32_t scales, ids;
 };
 
-template <int DT, int NB, bool CAP>
+// A tile's values of the chunk that is not in 4 bits: rows of the tail as columns (`left` of them, zeros behind).
+template <int NB>
+__device__ __forceinline__ void tail_columns(const uint16_t *src, int left, uint8_t *vt, int e, int lane) {
+    constexpr int D = 32 * NB;
+#pragma unroll 1
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int k = 8 * q + 2 * i;
+                const uint32_t x = k < left ? src[k * D + 32 * b + lane] : 0u, y = k + 1 < left ? src[(k + 1) * D + 32 * b + lane] : 0u;
+                w[i] = x | y << 16;
+            }
+            *(uint4 *)(vt + swizzled(D, 32 * b + lane, 4 * e + q)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+}
+template <int NB>
+__device__ __forceinline__ void load_lane(const Pool &pool, int64_t off, bool values, int lane, Lane<NB> &x) {
+    constexpr int D = 32 * NB;
+    const int entry = entry_of(NB, 0, lane);
+    const uint8_t *rec = pool.base + off;
+    const uint8_t *codes = rec + (values ? value_codes(D) : 0), *sc = rec + (values ? value_scales(D) : key_scales(D)) + entry,
+                  *id = rec + (values ? value_ids(D) : key_ids(D)) + entry / 2;
+    x.scales = NB == 4 ? *(const uint32_t *)sc : *(const uint16_t *)sc;
+    x.ids = NB == 4 ? *(const uint16_t *)id : *id;
+#pragma unroll
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int t = 0; t < 4; t++) x.w[b][t] = *(const uint32_t *)(codes + word_byte(b, lane, t));
+}
+// Chunk e of a tile from a lane's registers: keys in rows 32 e + lane, values (columns 32 e ..) in rows 32 b + lane.
+template <int DT, int NB>
+__device__ __forceinline__ void expand_lane(const uint4 *table, const Lane<NB> &x, bool values, uint8_t *tile, int e, int lane) {
+    constexpr int D = 32 * NB;
+#pragma unroll
+    for (int b = 0; b < NB; b++) {
+        const uint4 t = block_table<DT, false>(table, x.ids >> (4 * b) & 15u, x.scales >> (8 * b) & 255u);
+#pragma unroll
+        for (int q = 0; q < 4; q++)
+            *(uint4 *)(tile + (values ? swizzled(D, 32 * b + lane, 4 * e + q) : swizzled(128, 32 * e + lane, 4 * b + q))) = expand_word(x.w[b][q], t);
+    }
+}
+
+// Expanded tiles: per sequence, KV head and tile of 128 tokens the key image and the value image, and a word that says which
+// of its four chunks have a page.
+__device__ __forceinline__ int64_t image_index(const Attention &p, int seq, int h, int tile) { return ((int64_t)seq * p.pool.kv_heads + h) * p.image_tiles + tile; }
+
+template <int DT, int NB>
+__global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ Attention p) {
+    constexpr int D = 32 * NB, kImage = 128 * D * 2;
+    __shared__ uint4 table[32];
+    make_base_tables<DT>(table);
+    pdl_wait();
+    pdl_release();
+    __syncthreads();
+    const int tile = blockIdx.x, h = blockIdx.y, seq = blockIdx.z, warp = threadIdx.x / 32, e = warp % 4, lane = threadIdx.x % 32;
+    const bool values = warp >= 4;
+    const Sequence s = sequence_of(p.batch, seq);
+    if (!s.ok || s.t == 0) return;
+    if (tile * kTileTokens >= s.kv || (p.window && (tile + 1) * kTileTokens <= s.kv - s.t - p.window + 1)) return;   // nobody sees it
+    const int c = 4 * tile + e, full = s.kv / kChunk, n_chunks = (s.kv + kChunk - 1) / kChunk;
+    const int64_t off = c < n_chunks ? record_offset(p.pool, p.batch, seq, h, c) : -1, at = image_index(p, seq, h, tile);
+    uint8_t *image = p.images + at * (2 * kImage) + (values ? kImage : 0);
+    if (off < 0 && c < n_chunks && lane == 0) atomicOr(&g_status_word, kStatusIndex);
+    __shared__ uint32_t ok;
+    if (threadIdx.x == 0) ok = 0;
+    __syncthreads();
+    if (!values && off >= 0 && lane == 0) atomicOr(&ok, 1u << e);
+    if (off >= 0 && (!values || c < full)) {
+        Lane<NB> x;
+        load_lane<NB>(p.pool, off, values, lane, x);
+        expand_lane<DT, NB>(table, x, values, image, e, lane);
+    } else if (values) {
+        const int slot = p.batch.slot[seq];
+        const bool tail = c == full && c < n_chunks && off >= 0, slot_ok = slot >= 0 && slot < p.pool.slots;
+        if (tail && !slot_ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
+        const int left = tail && slot_ok ? s.kv - c * kChunk : 0;
+        tail_columns<NB>((const uint16_t *)p.pool.tail + tail_offset(p.pool, left ? slot : 0, h, c * kChunk), left, image, e, lane);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) p.image_ok[at] = ok;
+}
+
+template <int DT, int NB, bool CAP, bool IMAGES>
 __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const __grid_constant__ Attention p) {
     using S = ChunkSmem<NB>;
     constexpr int D = S::D;
@@ -99,9 +186,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(s_full + 8 * i, 1);
             tc::mbar_init(p_full + 8 * i, 4);
-            tc::mbar_init(k_full + 8 * i, 4);
+            tc::mbar_init(k_full + 8 * i, IMAGES ? 1 : 4);
             tc::mbar_init(k_empty + 8 * i, 1);
-            tc::mbar_init(v_full + 8 * i, 4);
+            tc::mbar_init(v_full + 8 * i, IMAGES ? 1 : 4);
             tc::mbar_init(v_empty + 8 * i, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -109,7 +196,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     pdl_wait();                                                   // (before the first decision that depends on the batch's numbers)
     pdl_release();
 
-    const int seq = blockIdx.z, h = blockIdx.y, split = blockIdx.x % p.splits, pair = p.row_tiles - 1 - blockIdx.x / p.splits;   // longest rows first
+    // longest rows first, all heads of them
+    const int seq = blockIdx.z, split = blockIdx.x % p.splits, h = blockIdx.x / p.splits, pair = p.row_tiles - 1 - (int)blockIdx.y;
     const Sequence s = sequence_of(p.batch, seq);
     if (!s.ok) {
         if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
@@ -136,7 +224,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     constexpr uint32_t kFmt = DT == BD_BF16 ? 1u : 0u;
 
     if (wg < 2) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        if (IMAGES) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         // ---- softmax of tile wg; thread = row = tensor-memory lane ----
         const int quad = warp % 4, row = 128 * wg + 32 * quad + lane, r = r0 + row;
         {                                                         // queries of this tile into shared memory
@@ -295,11 +384,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             }
         }
     } else if (wg == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-        // ---- expansion: warp e takes chunk e of every tile; lane = row of the record's tiles ----
+        if (IMAGES) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         const int e = warp % 4, full = s.kv / kChunk, n_chunks = (s.kv + kChunk - 1) / kChunk;
+        bool alive = true;
+        if (IMAGES) {
+            // ---- bulk copies of the expanded tiles, by one thread ----
+            if (e == 0 && lane == 0) {
+                const uint8_t *src = p.images + image_index(p, seq, h, t_begin) * (2 * S::kv_tile);
+                const uint32_t *ok = p.image_ok + image_index(p, seq, h, t_begin);
+                for (int j = 0; j < n_tiles && alive; j++, src += 2 * S::kv_tile) {
+                    const int st = j & 1;
+                    const uint32_t parity = (uint32_t)(j >> 1 & 1) ^ 1u;
+                    const uint32_t there = ok[j];
+                    alive = tc::mbar_wait(k_empty + 8 * st, parity, abort_flag);
+                    if (!alive) break;
+                    chunk_ok[j & 7] = there;
+                    tc::mbar_expect_tx(k_full + 8 * st, S::kv_tile);
+                    tc::bulk_load(base + S::k + st * S::kv_tile, src, S::kv_tile, k_full + 8 * st);
+                    alive = tc::mbar_wait(v_empty + 8 * st, parity, abort_flag);
+                    if (!alive) break;
+                    tc::mbar_expect_tx(v_full + 8 * st, S::kv_tile);
+                    tc::bulk_load(base + S::v + st * S::kv_tile, src + S::kv_tile, S::kv_tile, v_full + 8 * st);
+                }
+            }
+            __syncwarp();
+        } else {
+        // ---- expansion: warp e takes chunk e of every tile; lane = row of the record's tiles ----
         const uint4 *table = (const uint4 *)(sm + S::table);
-        const int entry = entry_of(NB, 0, lane);
         auto place = [&](int j) -> int64_t {                      // the chunk's record, -1: none
             const int c = 4 * (t_begin + j) + e;
             if (c >= n_chunks) return -1;
@@ -307,39 +419,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (off < 0 && lane == 0) atomicOr(&g_status_word, kStatusIndex);
             return off;
         };
-        auto load = [&](int64_t off, bool values, Lane<NB> &x) {
-            if (off < 0) return;
-            const uint8_t *rec = p.pool.base + off;
-            const uint8_t *codes = rec + (values ? value_codes(D) : 0), *sc = rec + (values ? value_scales(D) : key_scales(D)) + entry,
-                          *id = rec + (values ? value_ids(D) : key_ids(D)) + entry / 2;
-            x.scales = NB == 4 ? *(const uint32_t *)sc : *(const uint16_t *)sc;
-            x.ids = NB == 4 ? *(const uint16_t *)id : *id;
-#pragma unroll
-            for (int b = 0; b < NB; b++)
-#pragma unroll
-                for (int t = 0; t < 4; t++) x.w[b][t] = *(const uint32_t *)(codes + word_byte(b, lane, t));
-        };
-        bool alive = true;
         Lane<NB> kx, vx;
         int64_t off = n_tiles > 0 ? place(0) : -1;
-        load(off, false, kx);
+        if (off >= 0) load_lane<NB>(p.pool, off, false, lane, kx);
         for (int j = 0; j < n_tiles && alive; j++) {
             const int st = j & 1;
             const uint32_t parity = (uint32_t)(j >> 1 & 1) ^ 1u;
             const int c = 4 * (t_begin + j) + e;
             const bool stored = c < full && off >= 0;
-            if (stored) load(off, true, vx);
+            if (stored) load_lane<NB>(p.pool, off, true, lane, vx);
             alive = tc::mbar_wait(k_empty + 8 * st, parity, abort_flag);
             if (!alive) break;
-            uint8_t *kt = sm + S::k + st * S::kv_tile;
-            if (off >= 0) {
-#pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    const uint4 t = block_table<DT, false>(table, kx.ids >> (4 * b) & 15u, kx.scales >> (8 * b) & 255u);
-#pragma unroll
-                    for (int q = 0; q < 4; q++) *(uint4 *)(kt + swizzled(128, 32 * e + lane, 4 * b + q)) = expand_word(kx.w[b][q], t);
-                }
-            }
+            if (off >= 0) expand_lane<DT, NB>(table, kx, false, sm + S::k + st * S::kv_tile, e, lane);
             // tile j + 8 reuses this flag: eight tiles on, every reader of tile j is done (two tiles in shared memory, one in S)
             if (lane == 0) {
                 if (off >= 0) atomicOr((uint32_t *)&chunk_ok[j & 7], 1u << e);
@@ -349,42 +440,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_local(k_full + 8 * st);
             const int64_t next = j + 1 < n_tiles ? place(j + 1) : -1;
-            load(next, false, kx);
+            if (next >= 0) load_lane<NB>(p.pool, next, false, lane, kx);
             alive = tc::mbar_wait(v_empty + 8 * st, parity, abort_flag);
             if (!alive) break;
             uint8_t *vt = sm + S::v + st * S::kv_tile;
             if (stored) {
-#pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    const uint4 t = block_table<DT, false>(table, vx.ids >> (4 * b) & 15u, vx.scales >> (8 * b) & 255u);
-#pragma unroll
-                    for (int q = 0; q < 4; q++) *(uint4 *)(vt + swizzled(D, 32 * b + lane, 4 * e + q)) = expand_word(vx.w[b][q], t);
-                }
+                expand_lane<DT, NB>(table, vx, true, vt, e, lane);
             } else {
                 // the unfinished chunk from the tail; nothing (zeros) behind it and where there is no page
                 const int slot = p.batch.slot[seq];
                 const bool tail = c == full && c < n_chunks && off >= 0, slot_ok = slot >= 0 && slot < p.pool.slots;
                 if (tail && !slot_ok && lane == 0) atomicOr(&g_status_word, kStatusIndex);
                 const int left = tail && slot_ok ? s.kv - c * kChunk : 0;
-                const uint16_t *src = (const uint16_t *)p.pool.tail + tail_offset(p.pool, left ? slot : 0, h, c * kChunk);
-#pragma unroll 1
-                for (int b = 0; b < NB; b++)
-#pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const int k = 8 * q + 2 * i;
-                            const uint32_t x = k < left ? src[k * D + 32 * b + lane] : 0u, y = k + 1 < left ? src[(k + 1) * D + 32 * b + lane] : 0u;
-                            w[i] = x | y << 16;
-                        }
-                        *(uint4 *)(vt + swizzled(D, 32 * b + lane, 4 * e + q)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
+                tail_columns<NB>((const uint16_t *)p.pool.tail + tail_offset(p.pool, left ? slot : 0, h, c * kChunk), left, vt, e, lane);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_local(v_full + 8 * st);
             off = next;
+        }
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
