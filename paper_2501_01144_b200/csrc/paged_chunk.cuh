@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const sm = smem_raw + (base - tc::smem_u32(smem_raw));
     const uint32_t bars = base + S::bars;
-    const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, k_full = bars + 40, k_empty = bars + 56, v_full = bars + 72, v_empty = bars + 88, drained = bars + 104;
+    const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, k_full = bars + 40, k_empty = bars + 56, v_full = bars + 72, v_empty = bars + 88, p_half = bars + 104, drained = bars + 120;
     volatile uint32_t *const words = (volatile uint32_t *)(sm + S::words), *const abort_flag = words + 1;
     volatile uint32_t *const chunk_ok = (volatile uint32_t *)(sm + S::flags);       // [8 tiles]: bit e = chunk e of the tile has a page
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, wg = warp / 4;
@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(s_full + 8 * i, 1);
             tc::mbar_init(p_full + 8 * i, 4);
+            tc::mbar_init(p_half + 8 * i, 4);
             tc::mbar_init(k_full + 8 * i, IMAGES ? 1 : 4);
             tc::mbar_init(k_empty + 8 * i, 1);
             tc::mbar_init(v_full + 8 * i, IMAGES ? 1 : 4);
@@ -328,12 +329,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                         out[4 * (n % 8 / 2) + n / 8] = DT == BD_BF16 ? pack_bf16(a, b) : pack_f16(a, b);
                     }
                     tcgen05_st_x16(t_s + 16 * c, out);
+                    if (c % 2) {                                  // half of P is there
+                        tc::tcgen05_wait_st();
+                        tc::tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive_local((c == 1 ? p_half : p_full) + 8 * wg);
+                    }
                 }
                 l += l0 + l1;
-                tc::tcgen05_wait_st();
-                tc::tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive_local(p_full + 8 * wg);
             }
             // ---- the tile's result ----
             if (n_tiles > 0 && alive) alive = tc::mbar_wait(s_full + 8 * wg, n_tiles & 1, abort_flag);
@@ -478,10 +481,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                 }
                 __syncwarp();
             };
-            auto values = [&](int t, int st, bool first) {
+            auto values = [&](int t, int st, bool first, int half) {
                 if (tc::elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < kTileTokens / 16; k++) {
+                    for (int i = 0; i < kTileTokens / 32; i++) {
+                        const int k = half * (kTileTokens / 32) + i;
                         const uint32_t at = (uint32_t)(k / 4) * (uint32_t)(D * 128 >> 4) + 2u * (uint32_t)(k % 4);
                         mma_f16_ts(tmem + 256u + 128u * t, tmem + 128u * t + 8u * k, tc::desc_join(lo_v + (uint32_t)st * (S::kv_tile >> 4) + at, hi), idesc_o, !(first && k == 0));
                     }
@@ -506,10 +510,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                 const bool more = j + 1 < n_tiles;
                 alive = tc::mbar_wait(v_full + 8 * st, j >> 1 & 1, abort_flag, 0);
                 for (int t = 0; t < n_q && alive; t++) {
+                    alive = tc::mbar_wait(p_half + 8 * t, j & 1, abort_flag, 0);
+                    if (!alive) break;
+                    tc::tcgen05_fence_after();
+                    values(t, st, j == 0, 0);
                     alive = tc::mbar_wait(p_full + 8 * t, j & 1, abort_flag, 0);
                     if (!alive) break;
                     tc::tcgen05_fence_after();
-                    values(t, st, j == 0);
+                    values(t, st, false, 1);
                     if (more) {
                         if (t == 0) alive = tc::mbar_wait(k_full + 8 * nx, (j + 1) >> 1 & 1, abort_flag, 0);
                         if (!alive) break;
