@@ -285,39 +285,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                         }
                     }
                 }
-                float top[4];
-#pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    top[c] = __uint_as_float(x[c][0]);
-#pragma unroll
-                    for (int n = 1; n < 32; n++) top[c] = fmaxf(top[c], __uint_as_float(x[c][n]));
-                }
+                // The exponentials of the first half start from the maximum of the tiles before; under them the tile's own
+                // maximum is found, and only if a row's has grown by more than 2^8 are they done again (and O rescaled).
                 const float k = CAP ? 1.0f : mul;
-                const float m_new = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;       // (k > 0: a scale of zero counts as 1e-37)
-                const bool none = !(m_new > -INFINITY);
-                bool grew = !none && m_new > m + 8.0f;            // m = -inf: the first visible token
-                if (__any_sync(0xffffffffu, grew)) {
-                    const float alpha = grew ? fast_exp2(m - m_new) : 1.0f;
-                    if (grew) m = m_new;
-                    l *= alpha;
-                    if (j > 0) {                                  // S(j) complete implies that the products up to j - 1 are
-#pragma unroll
-                        for (int c = 0; c < D / 32; c++) {
-                            uint32_t o[32];
-                            tc::tcgen05_ld_32x32b_x32(t_o + 32 * c, o);
-                            tc::tcgen05_wait_ld();
-#pragma unroll
-                            for (int n = 0; n < 32; n++) o[n] = __float_as_uint(__uint_as_float(o[n]) * alpha);
-                            tcgen05_st_x16(t_o + 32 * c, o);
-                            tcgen05_st_x16(t_o + 32 * c + 16, o + 16);
-                        }
-                    }
-                }
-                const float sub = m == -INFINITY ? 0.0f : -m;
                 float l0 = 0.0f, l1 = 0.0f;
-#pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    uint32_t out[16];
+                uint32_t out[2][16];
+                auto exponentials = [&](int c, float sub, uint32_t (&to)[16]) {
 #pragma unroll
                     for (int n = 0; n < 32; n += 2) {
                         float a = __uint_as_float(x[c][n]), b = __uint_as_float(x[c][n + 1]);
@@ -326,15 +299,53 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                         b = fast_exp2(b);
                         add2(l0, l1, a, b);
                         // columns n, n + 1 are tokens 8 x + 2 y + {0, 1} with n = 8 y + 2 x: pair 4 x + y in token order
-                        out[4 * (n % 8 / 2) + n / 8] = DT == BD_BF16 ? pack_bf16(a, b) : pack_f16(a, b);
+                        to[4 * (n % 8 / 2) + n / 8] = DT == BD_BF16 ? pack_bf16(a, b) : pack_f16(a, b);
                     }
-                    tcgen05_st_x16(t_s + 16 * c, out);
-                    if (c % 2) {                                  // half of P is there
-                        tc::tcgen05_wait_st();
-                        tc::tcgen05_fence_before();
-                        __syncwarp();
-                        if (lane == 0) tc::mbar_arrive_local((c == 1 ? p_half : p_full) + 8 * wg);
+                };
+                float sub = m == -INFINITY ? 0.0f : -m;
+                exponentials(0, sub, out[0]);
+                exponentials(1, sub, out[1]);
+                float top[4];
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    top[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+                    for (int n = 1; n < 32; n++) top[c] = fmaxf(top[c], __uint_as_float(x[c][n]));
+                }
+                const float m_new = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;       // (k > 0: a scale of zero counts as 1e-37)
+                const bool grew = m_new > m + 8.0f;               // m = -inf: the first visible token; m_new = -inf: none
+                if (__any_sync(0xffffffffu, grew)) {
+                    const float alpha = grew ? fast_exp2(m - m_new) : 1.0f;
+                    if (grew) m = m_new;
+                    l *= alpha;
+                    if (j > 0) {                                  // S(j) complete implies that the products up to j - 1 are
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; c++) {
+                            uint32_t o[16];
+                            tc::tcgen05_ld_32x32b_x16(t_o + 16 * c, o);
+                            tc::tcgen05_wait_ld();
+#pragma unroll
+                            for (int n = 0; n < 16; n++) o[n] = __float_as_uint(__uint_as_float(o[n]) * alpha);
+                            tcgen05_st_x16(t_o + 16 * c, o);
+                        }
                     }
+                    sub = m == -INFINITY ? 0.0f : -m;
+                    l0 = l1 = 0.0f;
+                    exponentials(0, sub, out[0]);
+                    exponentials(1, sub, out[1]);
+                }
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    if (half) {
+                        exponentials(2, sub, out[0]);
+                        exponentials(3, sub, out[1]);
+                    }
+                    tcgen05_st_x16(t_s + 32 * half, out[0]);
+                    tcgen05_st_x16(t_s + 32 * half + 16, out[1]);
+                    tc::tcgen05_wait_st();
+                    tc::tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive_local((half ? p_full : p_half) + 8 * wg);
                 }
                 l += l0 + l1;
             }
