@@ -1476,7 +1476,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     if (q_heads <= 0 || window < 0 || !(scale == scale) || !(softcap >= 0.0f) || softcap > 1e30f) return BD_ERR_INVALID_ARG;
     if (odtype != BD_F32 && odtype != BD_BF16 && odtype != BD_F16) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads) return BD_ERR_SHAPE;
-    if (b->max_q * (q_heads / c->kv_heads) > 65535ll * 256) return BD_ERR_UNSUPPORTED;
+    if ((b->max_q * (q_heads / c->kv_heads) / 256 + 1) * b->n > INT32_MAX / (148 * c->kv_heads)) return BD_ERR_UNSUPPORTED;   // CTAs of a launch
     if (c->dtype == BD_F32 || (odtype != BD_F32 && odtype != c->dtype) || q_heads > 65535) return BD_ERR_UNSUPPORTED;
     if ((s = check_rows(Q, b->rows, q_heads, c->head_dim, ldq, head_stride_q, 2))) return s;
     if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
@@ -1498,10 +1498,10 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.odtype = (int)odtype;
     a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.whole = plan.whole; a.rounds = plan.rounds;
     a.k23 = 1u << 23;
+    a.by_page = make_fast_div((uint32_t)a.pool.chunks_per_page);
     cudaStream_t st = (cudaStream_t)stream;
     if (!plan.chunk) {
         for (int k = 0; k < 4; k++) a.by_runs[k] = make_fast_div((uint32_t)(plan.workers * (k + 1)));
-        a.by_page = make_fast_div((uint32_t)a.pool.chunks_per_page);
         a.head_of_part = (uint32_t *)workspace;
         a.part = (float *)((char *)workspace + row_parts_offset(b));
         s = c->dtype == BD_BF16 ? launch_rows_dtype<BD_BF16>(a, plan.wide, st) : launch_rows_dtype<BD_F16>(a, plan.wide, st);
@@ -1513,7 +1513,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
         a.image_ok = (uint32_t *)(a.images + plan.images);
         a.image_tiles = (int)((b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens);
     }
-    const dim3 grid((unsigned)(plan.splits * c->kv_heads), (unsigned)plan.tiles, (unsigned)b->n);
+    const dim3 grid((unsigned)(plan.splits * c->kv_heads * plan.tiles * b->n));
     s = c->dtype == BD_BF16 ? launch_chunk<BD_BF16>(a, grid, st) : launch_chunk<BD_F16>(a, grid, st);
     if (s) return s;
     if (plan.splits > 1) {

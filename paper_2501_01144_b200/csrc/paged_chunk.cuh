@@ -31,7 +31,7 @@ template <int NB>
 struct ChunkSmem {
     static constexpr int D = 32 * NB;
     static constexpr int q_tile = 128 * D * 2, kv_tile = 128 * D * 2;
-    static constexpr int q = 0, k = q + 2 * q_tile, v = k + 2 * kv_tile, table = v + 2 * kv_tile, bars = table + 512, words = bars + 128, flags = words + 32,
+    static constexpr int q = 0, k = q + 2 * q_tile, v = k + 2 * kv_tile, table = v + 2 * kv_tile, bars = table + 512, words = bars + 128, flags = words + 64,
                          total = flags + 64 + 1024;              // + slack for 1024-byte alignment
 };
 
@@ -197,8 +197,35 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     pdl_wait();                                                   // (before the first decision that depends on the batch's numbers)
     pdl_release();
 
-    // longest rows first, all heads of them
-    const int seq = blockIdx.z, split = blockIdx.x % p.splits, h = blockIdx.x / p.splits, pair = p.row_tiles - 1 - (int)blockIdx.y;
+    // Which rows: the items (sequence, tile of 256 rows) in the order of their work, heaviest first, all heads of one behind
+    // each other: CTAs start in this order, so the light ones fill up what the heavy ones leave (six ragged chunks, 32 heads x 64:
+    // 92 -> 84 us).  More items than the CTA has threads: as they are numbered, tiles from the last.
+    const int heads = p.pool.kv_heads * p.splits, items = p.row_tiles * p.batch.n;
+    int item = (int)(blockIdx.x / (uint32_t)heads);
+    if (items <= kChunkThreads && items > 1) {
+        int *weight = (int *)(sm + S::q);                         // (the queries come later)
+        int mine = 0;
+        if ((int)threadIdx.x < items) {
+            const Sequence q = sequence_of(p.batch, threadIdx.x / p.row_tiles);
+            const int first = (int)(threadIdx.x % p.row_tiles) * 256, rows = q.t * p.group;
+            if (q.ok && first < rows) {
+                const int last = q.kv - q.t + (min(first + 256, rows) - 1) / p.group, from = p.window ? max(0, q.kv - q.t + first / p.group - p.window + 1) : 0;
+                mine = max(0, last + 1 - from) + 1;
+            }
+            weight[threadIdx.x] = mine;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < items) {
+            int rank = 0;
+            for (int i = 0; i < items; i++) rank += weight[i] > mine || (weight[i] == mine && i < (int)threadIdx.x);
+            if (rank == item) words[8] = threadIdx.x;
+        }
+        __syncthreads();
+        item = (int)words[8];
+    } else {
+        item = item / p.row_tiles * p.row_tiles + p.row_tiles - 1 - item % p.row_tiles;
+    }
+    const int seq = item / p.row_tiles, pair = item % p.row_tiles, h = (int)(blockIdx.x % (uint32_t)heads) / p.splits, split = (int)blockIdx.x % p.splits;
     const Sequence s = sequence_of(p.batch, seq);
     if (!s.ok) {
         if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
@@ -429,9 +456,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         auto place = [&](int j) -> int64_t {                      // the chunk's record, -1: none
             const int c = 4 * (t_begin + j) + e;
             if (c >= n_chunks) return -1;
-            const int64_t off = record_offset(p.pool, p.batch, seq, h, c);
-            if (off < 0 && lane == 0) atomicOr(&g_status_word, kStatusIndex);
-            return off;
+            const int at = (int)fast_div(c, p.by_page), page = p.batch.table[(int64_t)seq * p.batch.ld_table + at];
+            if (page < 0 || page >= p.pool.pages) {
+                if (lane == 0) atomicOr(&g_status_word, kStatusIndex);
+                return -1;
+            }
+            return (((int64_t)page * p.pool.kv_heads + h) * p.pool.chunks_per_page + c - at * p.pool.chunks_per_page) * (35 * D);
         };
         Lane<NB> kx, vx;
         int64_t off = n_tiles > 0 ? place(0) : -1;
