@@ -454,7 +454,7 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
     const int64_t seen = window ? std::min(b->max_kv, window + b->max_q + pg::kChunk) : b->max_kv;   // tokens from the first visible chunk on
     const int64_t chunks = std::max<int64_t>(1, (seen + pg::kChunk - 1) / pg::kChunk);
     const int head_warps = chunks <= 4 ? 4 : chunks <= 8 ? 8 : warps;
-    const int64_t heads_at_once = 148 * (warps / head_warps), waves = (b->n * c->kv_heads + heads_at_once - 1) / heads_at_once;
+    const int64_t heads_at_once = 148 * (warps / std::min(warps, head_warps)), waves = (b->n * c->kv_heads + heads_at_once - 1) / heads_at_once;
     r.whole = waves * chunks <= (r.wide ? 20 : 32);
     if (r.whole) {
         r.workers = head_warps;                                   // warps of a CTA

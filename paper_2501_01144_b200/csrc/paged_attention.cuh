@@ -54,7 +54,7 @@ struct Attention {
 
 constexpr int kRowStages = 2;
 constexpr int kRunUnits = 8;          // units that make a further round of runs worth its joins
-__host__ __device__ constexpr int row_warps(int nt) { return nt == 1 ? 16 : 8; }    // warps of a CTA = of an SM, by registers
+__host__ __device__ constexpr int row_warps(int nt) { return nt == 1 ? 16 : 12; }    // warps of a CTA = of an SM, by registers
 
 __device__ __forceinline__ void expand_f16(uint32_t w, uint2 tb, uint32_t (&r)[4]) {
     const uint32_t sel = w & 0x77777777u;
@@ -188,7 +188,9 @@ struct RowSmem {
     static constexpr int D = 32 * NB, ROWS = 8 * NT;
     static constexpr int warps = row_warps(NT), stage = 35 * D;
     static constexpr int table = 0, bars = 128, words = bars + warps * kRowStages * 8, ring = 512;      // the warps' records come last
-    static constexpr int bytes(int warps) { return ring + warps * kRowStages * stage; }
+    // per warp: its records, then its queries' fragments
+    static constexpr int queries = kRowStages * stage, per_warp = (queries + NT * NB * 512 + 127) / 128 * 128;
+    static constexpr int bytes(int warps) { return ring + warps * per_warp; }
     static_assert(words + 16 <= ring, "room for the table and the barriers");
 };
 
@@ -196,7 +198,7 @@ struct RowSmem {
 template <int DT, int NB, int NT, bool CAP>
 struct RowWork {
     static constexpr int D = 32 * NB;
-    uint32_t qf[NT][NB][4];                                       // queries: fragments of the 8-column operand, in fp16
+    uint4 *qf;                                                    // queries: fragments of the 8-column operand in fp16, [NT][NB][32 lanes] (shared memory)
     float mul[NT][2];                                             // column's factor from block sums to scores
     int pos[NT][2];
     float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
@@ -204,10 +206,11 @@ struct RowWork {
     int h, n_rows, first_pos, last_pos, full;
 
     // A head begins: its queries, and nothing seen yet.
-    __device__ __forceinline__ void begin(const Attention &p, const Sequence &seq, int head, int lane) {
+    __device__ __forceinline__ void begin(const Attention &p, const Sequence &seq, int head, uint4 *fragments, int lane) {
         const int g = lane / 4, t4 = lane % 4;
         s = seq;
         h = head;
+        qf = fragments + lane;
         n_rows = s.t * p.group;
         first_pos = s.kv - s.t;
         last_pos = s.kv - 1;
@@ -234,12 +237,14 @@ struct RowWork {
 #pragma unroll
                 for (int b = 0; b < NB; b++) {
                     const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
+                    uint32_t f[4];
 #pragma unroll
-                    for (int i = 0; i < 4; i++) qf[nt][b][i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+                    for (int i = 0; i < 4; i++) f[i] = pack_f16(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+                    qf[(nt * NB + b) * 32] = make_uint4(f[0], f[1], f[2], f[3]);
                 }
             } else {
 #pragma unroll
-                for (int b = 0; b < NB; b++) { qf[nt][b][0] = raw[b].x; qf[nt][b][1] = raw[b].y; qf[nt][b][2] = raw[b].z; qf[nt][b][3] = raw[b].w; }
+                for (int b = 0; b < NB; b++) qf[(nt * NB + b) * 32] = raw[b];
             }
 #pragma unroll
             for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
@@ -296,18 +301,20 @@ struct RowWork {
 #pragma unroll
             for (int j = 0; j < 4; j++) expand_f16(w[j], table_of(j, b), a[j]);
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++)
+            for (int nt = 0; nt < NT; nt++) {
+                const uint4 q = qf[(nt * NB + b) * 32];          // (this lane wrote it)
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
                     float acc[4];
-                    mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], qf[nt][b][0], qf[nt][b][1]);
-                    mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], qf[nt][b][2], qf[nt][b][3]);
+                    mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], q.x, q.y);
+                    mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], q.z, q.w);
                     const float f0 = factor_of(2 * x, b), f1 = factor_of(2 * x + 1, b);
                     sc[nt][x][0] = b ? fmaf(acc[0], f0, sc[nt][x][0]) : acc[0] * f0;
                     sc[nt][x][1] = b ? fmaf(acc[1], f0, sc[nt][x][1]) : acc[1] * f0;
                     sc[nt][x][2] = b ? fmaf(acc[2], f1, sc[nt][x][2]) : acc[2] * f1;
                     sc[nt][x][3] = b ? fmaf(acc[3], f1, sc[nt][x][3]) : acc[3] * f1;
                 }
+            }
         }
         // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
         const int tok0 = c * kChunk + 8 * (g / 2) + g % 2;
@@ -527,7 +534,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
         if (lane == 0) p.head_of_part[p.batch.n] = sum;
     }
     if (total == 0) return;
-    uint8_t *const ring = smem + S::ring + warp * kRowStages * S::stage;
+    uint8_t *const ring = smem + S::ring + warp * S::per_warp;
     uint32_t loaded = 0, phase = 0;                               // bits per stage: a record is in flight or there; the barrier's parity
     const int per_page = p.pool.chunks_per_page;
 
@@ -598,7 +605,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
     bool starts_head = true;                                      // this piece begins at the head's first unit
     for (int unit = 0; unit < n_units; unit++) {
         if (unit == 0 || c == v.begin) {                          // a head begins (or the run does, inside one)
-            work.begin(p, sequence_of(p.batch, at), h, lane);
+            work.begin(p, sequence_of(p.batch, at), h, (uint4 *)(ring + S::queries), lane);
             starts_head = c == v.begin;
         }
         const int st = unit % kRowStages;
@@ -643,7 +650,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
 template <int DT, int NB, int NT, bool CAP>
 __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(const __grid_constant__ Attention p) {
     using S = RowSmem<NB, NT>;
-    static_assert(part_floats<NB, NT>() * 4 <= kRowStages * S::stage, "a warp's part takes the place of its records");
+    static_assert(part_floats<NB, NT>() * 4 <= S::per_warp, "a warp's part takes the place of its records");
     extern __shared__ __align__(128) uint8_t smem[];
     volatile uint32_t *flags = (volatile uint32_t *)(smem + S::words);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32, h = blockIdx.x, seq = blockIdx.y;
@@ -666,7 +673,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
     }
     if (s.t == 0) return;
     const Visible v = visible_of(s, p.window);
-    uint8_t *const ring = smem + S::ring + warp * kRowStages * S::stage;
+    uint8_t *const ring = smem + S::ring + warp * S::per_warp;
     const int n = v.end > v.begin + warp ? (v.end - v.begin - warp + warps - 1) / warps : 0;     // this warp's chunks
     const int32_t *pages = p.batch.table + (int64_t)seq * p.batch.ld_table;
     uint32_t loaded = 0, phase = 0;
@@ -687,7 +694,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
     look_up(0);
     for (int i = 0; i < kRowStages && i < n; i++) fetch(i);
     RowWork<DT, NB, NT, CAP> work;
-    work.begin(p, s, h, lane);
+    work.begin(p, s, h, (uint4 *)(ring + S::queries), lane);
     bool alive = true;
     for (int i = 0; i < n; i++) {
         const int st = i % kRowStages;
@@ -714,10 +721,10 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
             const int r = 8 * nt + 2 * t4 + k;
             if (r >= work.n_rows) continue;
             float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-            for (int w = 0; w < warps; w++) m = fmaxf(m, ((const float *)(smem + S::ring + w * kRowStages * S::stage))[NT * NB * 2 * 128 + 2 * r]);
+            for (int w = 0; w < warps; w++) m = fmaxf(m, ((const float *)(smem + S::ring + w * S::per_warp))[NT * NB * 2 * 128 + 2 * r]);
             const float zero = m == -INFINITY ? 0.0f : m;
             for (int w = 0; w < warps; w++) {
-                const float *part = (const float *)(smem + S::ring + w * kRowStages * S::stage);
+                const float *part = (const float *)(smem + S::ring + w * S::per_warp);
                 const float f = fast_exp2(part[NT * NB * 2 * 128 + 2 * r] - zero);
                 l = fmaf(part[NT * NB * 2 * 128 + 2 * r + 1], f, l);
                 o0 = fmaf(part[(piece * 32 + lane) * 4 + k], f, o0);

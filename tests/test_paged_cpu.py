@@ -155,7 +155,7 @@ def test_bad_attention_calls_are_refused(kw, status):
     lib = bd.load()
     a = dict(q_heads=4, scale=0.1, softcap=0.0, window=0, odtype=bd.BF16, ldo=512, lse=None, ws=0x100000, wbytes=1 << 40, dtype=bd.BF16)
     a.update(kw)
-    cc, bb = cache(dtype=a["dtype"]), batch()
+    cc, bb = cache(dtype=a["dtype"]), batch(ld_table=100, max_kv=6400)      # long enough to be shared out: a workspace is needed
     assert lib.bd_paged_attention(ctypes.byref(cc), ctypes.byref(bb), 0x8000, a["q_heads"], 512, 128, a["scale"], a["softcap"], a["window"], 0x9000, a["odtype"],
                                   a["ldo"], 128, a["lse"], a["ws"], a["wbytes"], None) == status
 
