@@ -1499,6 +1499,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.whole = plan.whole; a.rounds = plan.rounds;
     a.k23 = 1u << 23;
     a.by_page = make_fast_div((uint32_t)a.pool.chunks_per_page);
+    a.by_group = make_fast_div((uint32_t)a.group);
     cudaStream_t st = (cudaStream_t)stream;
     if (!plan.chunk) {
         for (int k = 0; k < 4; k++) a.by_runs[k] = make_fast_div((uint32_t)(plan.workers * (k + 1)));

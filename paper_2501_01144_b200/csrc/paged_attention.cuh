@@ -44,7 +44,8 @@ struct Attention {
     int q_heads, group, window, splits, row_tiles, odtype;
     bool whole;                       // rows kernel: a CTA per head (workers: its warps)
     int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
-    FastDiv by_runs[4], by_page;      // division by workers * (1 .. 4), by the chunks of a page
+    FastDiv by_runs[4], by_page, by_group;      // division by workers * (1 .. 4), by the chunks of a page, by `group`
+    __device__ __forceinline__ int token(int row) const { return (int)fast_div((uint32_t)row, by_group); }     // of the sequence's rows
     uint8_t *images;                  // chunk kernel: expanded tiles (null: expanded by every CTA), [n][kv_heads][image_tiles]
     uint32_t *image_ok;
     int image_tiles;
@@ -219,7 +220,7 @@ struct RowWork {
         for (int nt = 0; nt < NT; nt++) {
             const int r = 8 * nt + g;
             const bool valid = r < n_rows;
-            const uint8_t *src = p.q + ((int64_t)(s.q0 + r / p.group) * p.ldq + (int64_t)(h * p.group + r % p.group) * p.hsq) * 2;
+            const uint8_t *src = p.q + ((int64_t)(s.q0 + p.token(r)) * p.ldq + (int64_t)(h * p.group + (r - p.token(r) * p.group)) * p.hsq) * 2;
             uint4 raw[NB];
 #pragma unroll
             for (int b = 0; b < NB; b++) raw[b] = valid ? *(const uint4 *)(src + (32 * b + 8 * t4) * 2) : make_uint4(0, 0, 0, 0);
@@ -252,7 +253,7 @@ struct RowWork {
                 const float k = f * 8388608.0f * p.scale;
                 mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
                 const int rc = 8 * nt + 2 * t4 + i;
-                pos[nt][i] = rc < n_rows ? first_pos + rc / p.group : -1;
+                pos[nt][i] = rc < n_rows ? first_pos + p.token(rc) : -1;
                 m_run[nt][i] = -INFINITY;
                 l_run[nt][i] = 0.0f;
             }
@@ -485,8 +486,8 @@ __device__ __forceinline__ void store_rows(const Attention &p, const RowWork<DT,
         for (int i = 0; i < 2; i++) {
             const int r = 8 * nt + 2 * t4 + i;
             if (r >= k.n_rows) continue;
-            const int64_t row = k.s.q0 + r / p.group;
-            const int head = k.h * p.group + r % p.group;
+            const int64_t row = k.s.q0 + p.token(r);
+            const int head = k.h * p.group + (r - p.token(r) * p.group);
             const float lr = k.l_run[nt][i], f = lr > 0.0f ? 8388608.0f / lr : (lr == 0.0f ? 0.0f : lr);
 #pragma unroll
             for (int b = 0; b < NB; b++)
@@ -730,8 +731,8 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
                 o0 = fmaf(part[(piece * 32 + lane) * 4 + k], f, o0);
                 o1 = fmaf(part[(piece * 32 + lane) * 4 + 2 + k], f, o1);
             }
-            const int64_t row = s.q0 + r / p.group;
-            const int head = h * p.group + r % p.group;
+            const int64_t row = s.q0 + p.token(r);
+            const int head = h * p.group + (r - p.token(r) * p.group);
             const float f = l > 0.0f ? 8388608.0f / l : (l == 0.0f ? 0.0f : l);
             store_out(p, row, head, 32 * b + 16 * x + g, o0 * f);
             store_out(p, row, head, 32 * b + 16 * x + 8 + g, o1 * f);
@@ -826,8 +827,8 @@ __global__ void __launch_bounds__(64 * NB * NT) attention_rows_join_kernel(const
     for (int i = 0; i < 2; i++) {
         const int r = 8 * nt + 2 * t4 + i;
         if (r >= n_rows) continue;
-        const int64_t row = s.q0 + r / p.group;
-        const int head = h * p.group + r % p.group;
+        const int64_t row = s.q0 + p.token(r);
+        const int head = h * p.group + (r - p.token(r) * p.group);
         const float l = sums[r], f = l > 0.0f ? 8388608.0f / l : (l == 0.0f ? 0.0f : l);
 #pragma unroll
         for (int j = 0; j < 2; j++) store_out(p, row, head, 32 * b + 16 * x + 8 * j + g, O[2 * j + i] * f);

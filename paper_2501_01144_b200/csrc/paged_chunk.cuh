@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             const Sequence q = sequence_of(p.batch, threadIdx.x / p.row_tiles);
             const int first = (int)(threadIdx.x % p.row_tiles) * 256, rows = q.t * p.group;
             if (q.ok && first < rows) {
-                const int last = q.kv - q.t + (min(first + 256, rows) - 1) / p.group, from = p.window ? max(0, q.kv - q.t + first / p.group - p.window + 1) : 0;
+                const int last = q.kv - q.t + p.token(min(first + 256, rows) - 1), from = p.window ? max(0, q.kv - q.t + p.token(first) - p.window + 1) : 0;
                 mine = max(0, last + 1 - from) + 1;
             }
             weight[threadIdx.x] = mine;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     const int r0 = pair * 256, n_rows = s.t * p.group;
     if (r0 >= n_rows) return;
     const int row_end = min(r0 + 256, n_rows), n_q = row_end - r0 > 128 ? 2 : 1;
-    const int first_pos = s.kv - s.t + r0 / p.group, last_pos = s.kv - s.t + (row_end - 1) / p.group;
+    const int first_pos = s.kv - s.t + p.token(r0), last_pos = s.kv - s.t + p.token(row_end - 1);
     const int seen_end = max(0, last_pos + 1), seen_begin = p.window ? max(0, first_pos - p.window + 1) : 0;
     const int t_lo = seen_begin / kTileTokens, t_hi = (seen_end + kTileTokens - 1) / kTileTokens;
     const int per = (max(0, t_hi - t_lo) + p.splits - 1) / p.splits;
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                 const int qr = i / kPieces, piece = i % kPieces, rr = r0 + 128 * wg + qr;
                 uint4 x = make_uint4(0, 0, 0, 0);
                 if (rr < n_rows) {
-                    x = *(const uint4 *)(p.q + ((int64_t)(s.q0 + rr / p.group) * p.ldq + (int64_t)(h * p.group + rr % p.group) * p.hsq + 8 * piece) * 2);
+                    x = *(const uint4 *)(p.q + ((int64_t)(s.q0 + p.token(rr)) * p.ldq + (int64_t)(h * p.group + (rr - p.token(rr) * p.group)) * p.hsq + 8 * piece) * 2);
                     x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
                 }
                 *(uint4 *)(sm + S::q + wg * S::q_tile + swizzled(128, qr, piece)) = x;
@@ -275,13 +275,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (lane == 0) tc::mbar_arrive_local(q_full);
         }
         if (wg < n_q) {
-            const int pos = r < n_rows ? s.kv - s.t + r / p.group : -1;
+            const int pos = r < n_rows ? s.kv - s.t + p.token(r) : -1;
             const float mul = fmaxf(fabsf(p.scale), 1e-37f) * (CAP ? 2.0f * 1.4426950408889634f / p.softcap : 1.4426950408889634f);
             const float cap2 = p.softcap * 1.4426950408889634f;
             const uint32_t t_s = tmem + 128u * wg + ((uint32_t)(32 * quad) << 16), t_o = tmem + 256u + 128u * wg + ((uint32_t)(32 * quad) << 16);
             // positions of the warp's 32 rows: the tiles that need a mask
-            const int w_first = s.kv - s.t + (r0 + 128 * wg + 32 * quad) / p.group;
-            const int w_last = s.kv - s.t + min(r0 + 128 * wg + 32 * quad + 31, n_rows - 1) / p.group;
+            const int w_first = s.kv - s.t + p.token(r0 + 128 * wg + 32 * quad);
+            const int w_last = s.kv - s.t + p.token(min(r0 + 128 * wg + 32 * quad + 31, n_rows - 1));
             float m = -INFINITY, l = 0.0f;
             bool alive = true;
             for (int j = 0; j < n_tiles && alive; j++) {
@@ -380,8 +380,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (n_tiles > 0 && alive) alive = tc::mbar_wait(s_full + 8 * wg, n_tiles & 1, abort_flag);
             tc::tcgen05_fence_after();
             if (alive) {
-                const int64_t out_row = s.q0 + r / p.group;
-                const int head = h * p.group + r % p.group;
+                const int64_t out_row = s.q0 + p.token(r);
+                const int head = h * p.group + (r - p.token(r) * p.group);
                 const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
                 float *part = p.splits > 1 ? p.part + (((int64_t)split * p.batch.rows + out_row) * p.q_heads + head) * (D + 2) : nullptr;
 #pragma unroll
