@@ -545,19 +545,24 @@ void launch_rotate(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
     if (r.rows < 4 * 148) launch_rotate_heads<DT, D, 1>(r, interleaved, st);
     else launch_rotate_heads<DT, D, DT == BD_F32 ? 2 : pg::kRotateHeads>(r, interleaved, st);
 }
-#define BD_PAGED_DISPATCH(kernel, c, grid, st, ...)                                                                              \
-    do {                                                                                                                        \
-        const unsigned threads = (unsigned)(c)->head_dim;                                                                    \
-        if ((c)->head_dim == 128) {                                                                                              \
-            if ((c)->dtype == BD_F32) launch_serialized(kernel<BD_F32, 4>, grid, threads, 0, st, __VA_ARGS__);                   \
-            else if ((c)->dtype == BD_BF16) launch_serialized(kernel<BD_BF16, 4>, grid, threads, 0, st, __VA_ARGS__);            \
-            else launch_serialized(kernel<BD_F16, 4>, grid, threads, 0, st, __VA_ARGS__);                                        \
-        } else {                                                                                                                 \
-            if ((c)->dtype == BD_F32) launch_serialized(kernel<BD_F32, 2>, grid, threads, 0, st, __VA_ARGS__);                   \
-            else if ((c)->dtype == BD_BF16) launch_serialized(kernel<BD_BF16, 2>, grid, threads, 0, st, __VA_ARGS__);            \
-            else launch_serialized(kernel<BD_F16, 2>, grid, threads, 0, st, __VA_ARGS__);                                        \
-        }                                                                                                                        \
-    } while (0)
+template <int NB>
+void launch_append(const bd_paged_cache *c, const bd_paged_batch *b, dim3 grid, const void *K, const void *V, int64_t ldk, int64_t ldv, int64_t hsk, int64_t hsv, cudaStream_t st) {
+    const pg::Pool p = pool_of(c);
+    const pg::Batch q = batch_of(b);
+    const uint8_t *k = (const uint8_t *)K, *v = (const uint8_t *)V;
+    if (c->dtype == BD_F32) launch_serialized(pg::append_kernel<BD_F32, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+    else if (c->dtype == BD_BF16) launch_serialized(pg::append_kernel<BD_BF16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+    else launch_serialized(pg::append_kernel<BD_F16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+}
+template <int NB>
+void launch_read(const bd_paged_cache *c, const bd_paged_batch *b, dim3 grid, void *K, void *V, int64_t ldk, int64_t ldv, int64_t hsk, int64_t hsv, cudaStream_t st) {
+    const pg::Pool p = pool_of(c);
+    const pg::Batch q = batch_of(b);
+    uint8_t *k = (uint8_t *)K, *v = (uint8_t *)V;
+    if (c->dtype == BD_F32) launch_serialized(pg::read_f32_kernel<NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+    else if (c->dtype == BD_BF16) launch_serialized(pg::read_kernel<BD_BF16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+    else launch_serialized(pg::read_kernel<BD_F16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
+}
 }  // namespace
 
 extern "C" {
@@ -1441,8 +1446,8 @@ bd_status bd_paged_append(const bd_paged_cache *c, const bd_paged_batch *b, cons
     if ((s = check_rows(V, b->rows, c->kv_heads, c->head_dim, ldv, head_stride_v, esz))) return s;
     if (b->max_q == 0) return BD_OK;
     const dim3 grid(paged_chunks(b), (unsigned)c->kv_heads, (unsigned)b->n);
-    BD_PAGED_DISPATCH(pg::append_kernel, c, grid, (cudaStream_t)stream, pool_of(c), batch_of(b), (const uint8_t *)K, (const uint8_t *)V, ldk, ldv,
-                      head_stride_k, head_stride_v);
+    if (c->head_dim == 128) launch_append<4>(c, b, grid, K, V, ldk, ldv, head_stride_k, head_stride_v, (cudaStream_t)stream);
+    else launch_append<2>(c, b, grid, K, V, ldk, ldv, head_stride_k, head_stride_v, (cudaStream_t)stream);
     return launch_result();
 }
 
@@ -1455,8 +1460,8 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
     if ((s = check_rows(V, b->rows, c->kv_heads, c->head_dim, ldv, head_stride_v, esz))) return s;
     if (b->max_q == 0) return BD_OK;
     const dim3 grid(paged_chunks(b), (unsigned)c->kv_heads, (unsigned)b->n);
-    BD_PAGED_DISPATCH(pg::read_kernel, c, grid, (cudaStream_t)stream, pool_of(c), batch_of(b), (uint8_t *)K, (uint8_t *)V, ldk, ldv,
-                      head_stride_k, head_stride_v);
+    if (c->head_dim == 128) launch_read<4>(c, b, grid, K, V, ldk, ldv, head_stride_k, head_stride_v, (cudaStream_t)stream);
+    else launch_read<2>(c, b, grid, K, V, ldk, ldv, head_stride_k, head_stride_v, (cudaStream_t)stream);
     return launch_result();
 }
 

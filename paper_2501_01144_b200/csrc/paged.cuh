@@ -241,21 +241,109 @@ __device__ __forceinline__ void word_values(uint32_t w, uint32_t tlo, uint32_t t
 
 // ---------------------------------------------------------------------------
 // Read back: the last t tokens of each sequence as values of the cache's type (exact for fp32 and bf16; fp16 rounds what
-// lies below its normal range).  A CTA takes one chunk of one head: its record (35 d bytes) comes to shared memory in
-// 16-byte pieces, then the keys leave word by word and the values, expanded block by block
-// (thread = channel), through shared memory, so that both are written token by token; the tokens of an unfinished chunk come from the tail.
-// 16-bit types expand with byte permutes (see block_table), fp32 with a multiplication.
+// lies below its normal range).  A CTA takes one chunk of one head, warp b its tile b of keys and of values; lane 4 g + t reads
+// the words t of the rows g, 8 + g, 16 + g, 24 + g as one 16-byte piece of each.
+// 16-bit types: a word becomes eight values with byte permutes (see block_table).  A key word is then 16 consecutive bytes of
+// a token's result; the value words of a warp are eight tokens of a channel each, which stmatrix turns around on the way to
+// shared memory (pieces exchanged within a row so that its eight rows meet different banks), from where whole tokens leave.
+// fp32 (read_f32_kernel): the record comes to shared memory, values are multiplied out element by element.
+// The tokens of an unfinished chunk come from the tail.
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ int turned_piece(int token, int piece) { return piece ^ ((token >> 3) << 1 | (token & 1)); }
+
 template <int DT, int NB>
 __global__ void __launch_bounds__(NB * 32) read_kernel(Pool pool, Batch batch, uint8_t *__restrict__ K, uint8_t *__restrict__ V,
                                                        int64_t ldk, int64_t ldv, int64_t hsk, int64_t hsv) {
-    constexpr int D = 32 * NB, EB = Loader<DT>::kElemBytes, kPieces = D * EB / 16, kPitch = D * EB + 16;
-    __shared__ uint4 base[DT == BD_F32 ? 1 : 32];
-    __shared__ uint2 table[DT == BD_F32 ? 16 : 1];
+    constexpr int D = 32 * NB, kPieces = D / 8;
+    __shared__ uint4 base[32];
+    __shared__ __align__(16) uint8_t rows[32 * D * 2];
+    make_base_tables<DT>(base);
+    pdl_wait();
+    pdl_release();
+    const int seq = blockIdx.z, h = blockIdx.y, b = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const Sequence s = sequence_of(batch, seq);
+    if (!s.ok || s.t > s.kv) {
+        if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
+        return;
+    }
+    if (s.t == 0) return;
+    const int p0 = s.kv - s.t, p1 = s.kv;
+    const int c = p0 / kChunk + blockIdx.x;
+    if (c * kChunk >= p1) return;
+    const int lo = max(p0, c * kChunk) - c * kChunk, hi = min(p1 - c * kChunk, kChunk);
+    const bool waiting = (c + 1) * kChunk > p1;                   // the unfinished chunk: its values are in the tail
+    const int64_t off = record_offset(pool, batch, seq, h, c);
+    const int slot = waiting ? batch.slot[seq] : 0;
+    const bool slot_ok = slot >= 0 && slot < pool.slots;
+    if ((off < 0 || !slot_ok) && threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
+    const int64_t row0 = (int64_t)s.q0 - p0 + c * kChunk;         // output row of the chunk's token 0
+    struct Tile {
+        uint4 w;
+        uint32_t scale, id;                                       // a byte and a nibble per row
+    };
+    auto fetch = [&](bool key) {                                  // (no page: scales, ids and codes 0, which is the value 0)
+        Tile x{make_uint4(0, 0, 0, 0), 0, 0};
+        if (off >= 0) {
+            const uint8_t *rec = pool.base + off;
+            x.w = *(const uint4 *)(rec + (key ? 0 : value_codes(D)) + 512 * b + 16 * lane);
+            const uint8_t *sc = rec + (key ? key_scales(D) : value_scales(D)) + 4 * NB * g + b, *id = rec + (key ? key_ids(D) : value_ids(D)) + (4 * NB * g + b) / 2;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                x.scale |= (uint32_t)sc[NB * j] << (8 * j);
+                x.id |= (uint32_t)(id[NB / 2 * j] >> (4 * (b & 1)) & 15) << (4 * j);
+            }
+        }
+        return x;
+    };
+    const Tile key = fetch(true);
+    Tile value = {};
+    if (!waiting) value = fetch(false);
+    __syncthreads();
+    auto expand = [&](const Tile &x, int j) {
+        const uint32_t w = j == 0 ? x.w.x : j == 1 ? x.w.y : j == 2 ? x.w.z : x.w.w;
+        return expand_word(w, block_table<DT, true>(base, x.id >> (4 * j) & 15u, x.scale >> (8 * j) & 255u));
+    };
+    {
+        uint8_t *to = K + (row0 * ldk + (int64_t)h * hsk + 32 * b + 8 * t) * 2;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint4 x = expand(key, j);
+            const int tok = key_token(8 * j + g);
+            if (tok >= lo && tok < hi) *(uint4 *)(to + tok * ldk * 2) = x;
+        }
+    }
+    if (!waiting) {
+        // matrix p of four: eight channels x the tokens 8 a + 2 p + i; this lane addresses the row i' of matrix lane / 8
+        const int tok = 8 * (lane % 8 / 2) + 2 * (lane / 8) + lane % 2;
+        const uint32_t row = (uint32_t)__cvta_generic_to_shared(rows) + tok * D * 2;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint4 x = expand(value, j);
+            asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                         ::"r"(row + 16 * turned_piece(tok, 4 * b + j)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        }
+        __syncthreads();
+    }
+    const int piece = threadIdx.x % kPieces;
+    constexpr int kRowsATurn = NB * 32 / kPieces;
+    const uint8_t *from = (const uint8_t *)pool.tail + (tail_offset(pool, slot_ok ? slot : 0, h, c * kChunk) + 8 * piece) * 2;
+    uint8_t *to = V + (row0 * ldv + (int64_t)h * hsv + 8 * piece) * 2;
+    for (int tok = lo + threadIdx.x / kPieces; tok < hi; tok += kRowsATurn) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (!waiting) x = ((const uint4 *)rows)[tok * kPieces + turned_piece(tok, piece)];
+        else if (slot_ok) x = *(const uint4 *)(from + tok * D * 2);
+        *(uint4 *)(to + tok * ldv * 2) = x;
+    }
+}
+
+template <int NB>
+__global__ void __launch_bounds__(NB * 32) read_f32_kernel(Pool pool, Batch batch, uint8_t *__restrict__ K, uint8_t *__restrict__ V,
+                                                       int64_t ldk, int64_t ldv, int64_t hsk, int64_t hsv) {
+    constexpr int D = 32 * NB, EB = 4, kPieces = D * EB / 16, kPitch = D * EB + 16;
+    __shared__ uint2 table[16];
     __shared__ __align__(16) uint8_t rec[35 * D];
     __shared__ __align__(16) uint8_t rows[32 * kPitch];
-    if (DT != BD_F32) make_base_tables<DT>(base);
-    else if (threadIdx.x < 16) table[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
+    if (threadIdx.x < 16) table[threadIdx.x] = make_uint2(c_tables.int_lo[threadIdx.x], c_tables.int_hi[threadIdx.x]);
     pdl_wait();
     pdl_release();
     const int seq = blockIdx.z, h = blockIdx.y;
@@ -278,41 +366,27 @@ __global__ void __launch_bounds__(NB * 32) read_kernel(Pool pool, Batch batch, u
     for (int i = threadIdx.x; i < 35 * D / 16; i += NB * 32)      // (no page: scales, ids and codes 0, which is the value 0)
         ((uint4 *)rec)[i] = off >= 0 ? ((const uint4 *)(pool.base + off))[i] : make_uint4(0, 0, 0, 0);
     __syncthreads();
-    // word t of row r of tile b as 8 elements of the type: one 16-byte piece, or two (fp32)
-    auto word = [&](bool key, int b, int r, int t, const uint4 &tb, float f, uint4 (&x)[EB / 2]) {
-        const uint32_t w = *(const uint32_t *)(rec + (key ? 0 : value_codes(D)) + word_byte(b, r, t));
-        if (DT == BD_F32) {
-            float v[8];
-            word_values(w, tb.x, tb.y, f, v);
-            x[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-            x[EB / 2 - 1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
-        } else {
-            x[0] = expand_word(w, tb);
-        }
+    // word t of row r of tile b
+    auto word = [&](bool key, int b, int r, int t, const uint2 &tb, float f, float (&v)[8]) {
+        word_values(*(const uint32_t *)(rec + (key ? 0 : value_codes(D)) + word_byte(b, r, t)), tb.x, tb.y, f, v);
     };
-    auto entry = [&](bool key, int b, int r, uint4 &tb, float &f) {
+    auto entry = [&](bool key, int b, int r, uint2 &tb, float &f) {
         const int e = entry_of(NB, b, r);
-        const uint32_t id = rec[(key ? key_ids(D) : value_ids(D)) + e / 2] >> (4 * (e & 1)) & 15, scale = rec[(key ? key_scales(D) : value_scales(D)) + e];
-        if (DT == BD_F32) {
-            tb = make_uint4(table[id].x, table[id].y, 0, 0);
-            f = half_unit(scale);
-        } else {
-            tb = block_table<DT, true>(base, id, scale);
-        }
+        tb = table[rec[(key ? key_ids(D) : value_ids(D)) + e / 2] >> (4 * (e & 1)) & 15];
+        f = half_unit(rec[(key ? key_scales(D) : value_scales(D)) + e]);
     };
-    uint4 tb;
-    float f = 0.0f;
+    uint2 tb;
+    float f = 0.0f, v[8];
     // keys: neighbouring threads take neighbouring words of a token, so that their stores join
     {
         const int b = threadIdx.x / 4 % NB, t = threadIdx.x % 4;
         uint8_t *to = K + ((row0 + lo + threadIdx.x / (4 * NB)) * ldk + (int64_t)h * hsk + 32 * b + 8 * t) * EB;
         for (int tok = lo + threadIdx.x / (4 * NB); tok < hi; tok += 8, to += 8 * ldk * EB) {
             const int r = key_row(tok);
-            uint4 x[EB / 2];
             entry(true, b, r, tb, f);
-            word(true, b, r, t, tb, f, x);
-#pragma unroll
-            for (int k = 0; k < EB / 2; k++) ((uint4 *)to)[k] = x[k];
+            word(true, b, r, t, tb, f, v);
+            ((float4 *)to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            ((float4 *)to)[1] = make_float4(v[4], v[5], v[6], v[7]);
         }
     }
     if (!waiting) {
@@ -321,21 +395,9 @@ __global__ void __launch_bounds__(NB * 32) read_kernel(Pool pool, Batch batch, u
         entry(false, b, r, tb, f);
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            uint4 x[EB / 2];
-            word(false, b, r, t, tb, f, x);
+            word(false, b, r, t, tb, f, v);
 #pragma unroll
-            for (int i = 0; i < EB / 2; i++) {
-                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    if (EB == 4) {
-                        *(uint32_t *)(to + (8 * t + 4 * i + k) * kPitch) = w[k];
-                    } else {
-                        *(uint16_t *)(to + (8 * t + 2 * k) * kPitch) = (uint16_t)w[k];
-                        *(uint16_t *)(to + (8 * t + 2 * k + 1) * kPitch) = (uint16_t)(w[k] >> 16);
-                    }
-                }
-            }
+            for (int k = 0; k < 8; k++) *(float *)(to + (8 * t + k) * kPitch) = v[k];
         }
         __syncthreads();
     }
