@@ -439,10 +439,23 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
     r.chunk = rows > 16;
     if (r.chunk) {
         r.tiles = (int)((rows + 255) / 256);
-        const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles), tiles = (b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens;
-        r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(148 / ctas, tiles / 4));
-        const size_t images = (size_t)b->n * (size_t)c->kv_heads * (size_t)tiles * (size_t)(2 * 128 * c->head_dim * 2);
-        if (r.tiles >= 4 && images <= ((size_t)1 << 30)) r.images = images;
+        const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles);
+        const int64_t seen = window ? std::min(b->max_kv, window + b->max_q + pg::kTileTokens) : b->max_kv, tiles = std::max<int64_t>(1, (seen + pg::kTileTokens - 1) / pg::kTileTokens);
+        // CTAs that share a tile's tokens, where the batch alone does not fill the SMs: the time of a CTA's tiles (2.6 us each at
+        // d = 128, 1.65 at 64) against the join's (12 us and its traffic).  Measured, 32 / 8 heads x 128, alone against split:
+        // 32 new of 1024 tokens 23.4 / 22.3 us (2), 256 of 1024 28.5 / 33.5 (2), 256 of 4096 83.5 / 44.9 (4), 32 of 16384 268 / 38 (18).
+        double best = 0;
+        for (int64_t k = 1; k <= std::max<int64_t>(1, std::min<int64_t>(148 / ctas, tiles)); k++) {
+            const double join = k > 1 ? 12.0 + 2.0 * (double)k * (double)b->rows * (double)q_heads * (double)(c->head_dim + 2) * 4.0 / 4e6 : 0.0;
+            const double us = (double)((tiles + k - 1) / k) * (c->head_dim == 128 ? 2.6 : 1.65) + join;
+            if (k == 1 || us < best) { best = us; r.splits = (int)k; }
+        }
+        if (window) r.splits = std::min(r.splits, attention_plan(c, b, q_heads, 0).splits);       // the workspace is asked for without a window
+        // Tiles expanded once in front pay when many CTAs read each: 32 / 8 heads x 128, expanded by every CTA against in front:
+        // 4096 new of 16384 tokens 1059 / 809 us, 512 of 16384 182 / 170, 768 of 4096 86 / 79, 256 of 16384 103 / 114, 2048 of 2048 57 / 65,
+        // 4096 of 4096 with 32 KV heads 194 / 205.  d = 64 (half the expansion per exponential): 4096 of 8192 358 / 376, never better.
+        const size_t images = (size_t)b->n * (size_t)c->kv_heads * (size_t)((b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens) * (size_t)(2 * 128 * c->head_dim * 2);
+        if (c->head_dim == 128 && r.tiles >= 8 && seen >= 4096 && b->max_kv >= 2 * b->max_q && images <= ((size_t)1 << 30)) r.images = images;
         return r;
     }
     r.wide = rows > 8;
@@ -519,18 +532,16 @@ bd_status launch_chunk_kernel(const pg::Attention &a, dim3 grid, cudaStream_t st
     static bool configured[kMaxDevices] = {};
     const bd_status s = allow_smem(pg::attention_chunk_kernel<DT, NB, CAP, IMAGES>, smem, configured);
     if (s) return s;
-    if (IMAGES) launch_serialized(pg::expand_kernel<DT, NB>, dim3((unsigned)a.image_tiles, (unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 256, 0, st, a);
+    if constexpr (IMAGES) launch_serialized(pg::expand_kernel<DT, NB>, dim3((unsigned)a.image_tiles, (unsigned)a.pool.kv_heads, (unsigned)a.batch.n), 256, 0, st, a);
     launch_serialized(pg::attention_chunk_kernel<DT, NB, CAP, IMAGES>, grid, pg::kChunkThreads, smem, st, a);
     return BD_OK;
 }
-template <int DT, int NB>
-bd_status launch_chunk_dim(const pg::Attention &a, dim3 grid, cudaStream_t st) {
-    if (a.softcap > 0.0f) return a.images ? launch_chunk_kernel<DT, NB, true, true>(a, grid, st) : launch_chunk_kernel<DT, NB, true, false>(a, grid, st);
-    return a.images ? launch_chunk_kernel<DT, NB, false, true>(a, grid, st) : launch_chunk_kernel<DT, NB, false, false>(a, grid, st);
-}
 template <int DT>
 bd_status launch_chunk(const pg::Attention &a, dim3 grid, cudaStream_t st) {
-    return a.pool.head_dim == 128 ? launch_chunk_dim<DT, 4>(a, grid, st) : launch_chunk_dim<DT, 2>(a, grid, st);
+    const bool cap = a.softcap > 0.0f;
+    if (a.images) return cap ? launch_chunk_kernel<DT, 4, true, true>(a, grid, st) : launch_chunk_kernel<DT, 4, false, true>(a, grid, st);
+    if (a.pool.head_dim == 128) return cap ? launch_chunk_kernel<DT, 4, true, false>(a, grid, st) : launch_chunk_kernel<DT, 4, false, false>(a, grid, st);
+    return cap ? launch_chunk_kernel<DT, 2, true, false>(a, grid, st) : launch_chunk_kernel<DT, 2, false, false>(a, grid, st);
 }
 template <int DT, int D, int HEADS>
 void launch_rotate_heads(const pg::Rotation &r, bool interleaved, cudaStream_t st) {
