@@ -188,7 +188,8 @@ def check_attention(w, new, heads, out_dtype=torch.float32, softcap=0.0, window=
             ds = (128 + 8) * 2.0 ** -24 * scale * qk + 2.0 ** -20 * (softcap or 0.0) + 2.0 ** -22 * (np.abs(np.where(np.isinf(rl), 0, rl))[..., None] + 1)
             # probabilities: half a step of their 16-bit form, 2^-22 of the exponential, an absolute 2^-25 below fp16's normal range; sums over the tokens in fp32
             rel = p_half_step + 2 * ds + 2.0 ** -21 + s.length * 2.0 ** -24
-            bound = rel * pv + 2.0 ** -25 * vv + HALF_STEP[out_dtype] * np.abs(ro) + 2.0 ** -24 * (out_dtype == torch.float16)
+            # (calls of more than 16 rows on fp16 caches hold the values in fp16: half a step of its subnormals, 2^-25, each)
+            bound = rel * pv + 2.0 ** -25 * vv + 2.0 ** -25 * (w.kind == torch.float16) + HALF_STEP[out_dtype] * np.abs(ro) + 2.0 ** -24 * (out_dtype == torch.float16)
             err = np.abs(o[at:at + t] - ro)
             assert (err <= bound).all(), f"max error / bound {np.nanmax(err / np.maximum(bound, 1e-300))}, t {t} of {s.length}"
             seen = np.isfinite(rl)
@@ -227,9 +228,105 @@ def test_chunks_of_prompts(kind, d):
 
 def test_long_context_is_split_and_joined():
     w = World(1, 1, 128, 128, torch.bfloat16, seed=30, max_tokens=9000)
-    w.step([8990])
+    w.step([8920])
     check_attention(w, [1], 4)
     check_attention(w, [2], 1, window=4000)
+    check_attention(w, [5], 4)                                      # 20 rows: the tensor-core kernel, its tokens shared by CTAs
+    check_attention(w, [33], 4, window=3000, softcap=15.0)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("softcap,window", [(0.0, 0), (12.0, 4050)])
+def test_many_rows_over_a_long_context(kind, softcap, window):
+    """Tiles expanded in front (2048 rows and 4096 tokens or more, head_dim 128), with an unfinished chunk."""
+    w = World(2, 1, 128, 64, kind, seed=36, max_tokens=4300)
+    w.step([3990, 3])
+    assert bd.paged_attention_workspace_size(w.cache, w.batch([256, 1]), 257, 8) > (1 << 20)
+    check_attention(w, [256, 40], 8, softcap=softcap, window=window)
+    # a page number outside the pool: its tokens are not seen, by this kernel or the one for few rows
+    bits, _ = queries(w.rng, 257, 8, 128, kind)
+    q, table = to_device(bits, kind), w.table.clone()
+    table[0, 20] = -7
+    many = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([4246, 43]), i32([0, 256, 257]), 256), q, softcap=softcap, window=window, dtype=torch.float32)
+    few = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([4246, 43]), i32([0, 2, 3]), 2), torch.cat([q[254:256], q[256:]]), softcap=softcap, window=window, dtype=torch.float32)
+    with pytest.raises(bd.BdError):
+        bd.poll_status()
+    assert (many[254:] - few).abs().max() <= 2 * (HALF_STEP[kind] + 2.0 ** -11) * w.cache.head_dim ** 0.5 * 4 and torch.isfinite(many).all()
+
+
+@pytest.mark.parametrize("heads,most", [(4, 1), (8, 4), (16, 4)])
+def test_many_ragged_sequences_share_the_warps(heads, most):
+    """More sequences than a scan's 32 lanes, lengths from nothing to two pages of chunks: runs that cross heads and sequences."""
+    n = 75
+    w = World(n, 2, 64, 96, torch.bfloat16, seed=37, max_tokens=1500)
+    old = [0 if i % 7 == 3 else 1 + (i * 37) % 120 for i in range(n)]
+    old[5], old[60], old[74] = 1400, 1111, 900
+    w.step(old)
+    new = [0 if i % 5 == 1 else 1 + i % most for i in range(n)]
+    if most * heads // 2 <= 16:                                     # (more rows: the tensor-core kernel, no need to share)
+        assert bd.paged_attention_workspace_size(w.cache, w.batch(new), sum(new), heads) > 0
+    check_attention(w, new, heads)
+    check_attention(w, new[::-1], heads, window=500)
+
+
+def test_more_row_tiles_than_a_cta_orders():
+    n = 530
+    w = World(n, 1, 64, 32, torch.bfloat16, seed=38, max_tokens=64)
+    w.step([i % 9 for i in range(n)])
+    check_attention(w, [5 if i % 11 == 0 else i % 3 for i in range(n)], 4)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("scale", [2.0 ** -120, 2.0 ** -20, 2.0 ** -11, 2.0 ** 8])
+def test_magnitudes_at_the_ends_of_the_types(kind, scale):
+    if kind == torch.float16 and scale < 2.0 ** -20:
+        pytest.skip("below fp16's range")
+    w = World(1, 2, 128, 32, kind, seed=39, max_tokens=128)
+    k, v = source_rows(w.rng, 75, 2, 128, torch.float32)
+    conv = {torch.float32: lambda x: x, torch.bfloat16: inputs.to_bf16_bits, torch.float16: inputs.to_f16_bits}[kind]
+    k, v = conv((k * scale).astype(np.float32)), conv((v * scale).astype(np.float32))
+    w.seqs[0].append(k, v)
+    bd.paged_append(w.cache, w.batch([75]), to_device(k, kind), to_device(v, kind))
+    check_read(w)
+    if kind != torch.float32 and scale > 2.0 ** -100:
+        w.kind = kind
+        check = dict(scale=128 ** -0.5 / scale)
+        check_attention(w, [1], 4, **check)
+        check_attention(w, [40], 4, **check)
+
+
+def test_a_pool_beyond_32_bits():
+    """Pages whose records lie more than 2^32 bytes into the pool."""
+    hk, d, page = 8, 128, 64
+    pages = (1 << 32) // (hk * 2 * 35 * d) + 60
+    w = World.__new__(World)
+    w.rng, w.n, w.kv_heads, w.d, w.page, w.kind = np.random.default_rng(41), 1, hk, d, page, torch.bfloat16
+    w.table = i32([[pages - 1 - 3 * i for i in range(12)]])
+    w.slots = i32([2])
+    w.cache = bd.PagedKVCache(pages, hk, d, 3, page, w.kind)
+    from oracle.paged import Sequence
+    w.seqs = [Sequence(hk, d, ORACLE_DTYPE[w.kind])]
+    assert int(w.table[0, 11]) * hk * 2 * 35 * d > 1 << 32
+    w.step([300])
+    check_read(w)
+    check_attention(w, [1], 8)
+    check_attention(w, [30], 8)
+
+
+def test_another_formatbook_reaches_the_paged_kernels():
+    book = oracle.formatbook().copy()
+    book[0, 6], book[1, 6] = 13, 9                                  # another member of the first pair
+    try:
+        bd.set_formatbook(book)
+        oracle.set_formatbook(book)
+        w = World(1, 1, 128, 32, torch.bfloat16, seed=43, max_tokens=200)
+        w.step([77])
+        check_read(w)
+        check_attention(w, [1], 4)
+        check_attention(w, [60], 4)
+    finally:
+        bd.set_formatbook(None)
+        oracle.set_formatbook(None)
 
 
 def test_sharp_rows_and_tiny_and_huge_queries():
