@@ -376,7 +376,9 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
  * that type.  Unlike bd_kvcache_attention, which follows the paper's scope "all", queries and probabilities stay
  * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  lse (optional, fp32 [rows][q_heads]) receives
  * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result does not
- * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.
+ * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.  |scale| is
+ * below 1e30; softcap is 0 (none) or between 1e-6 and 1e30.  The workspace belongs to one call at a time: calls (or captured
+ * graphs) that may overlap need one each.  The size asked for serves every window.
  * Accuracy: products exact, fp32 sums; probabilities rounded to 11 bits, or to the cache's type (bf16: 8 bits) in calls of
  * more than 16 rows (tokens of a sequence times query heads per KV head). */
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes);

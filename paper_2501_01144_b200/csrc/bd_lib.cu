@@ -1489,7 +1489,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
                              void *stream) {
     bd_status s = check_paged(c, b);
     if (s) return s;
-    if (q_heads <= 0 || window < 0 || !(scale == scale) || !(softcap >= 0.0f) || softcap > 1e30f) return BD_ERR_INVALID_ARG;
+    if (q_heads <= 0 || window < 0 || !(scale > -1e30f && scale < 1e30f) || !(softcap == 0.0f || (softcap >= 1e-6f && softcap <= 1e30f))) return BD_ERR_INVALID_ARG;
     if (odtype != BD_F32 && odtype != BD_BF16 && odtype != BD_F16) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads) return BD_ERR_SHAPE;
     if ((b->max_q * (q_heads / c->kv_heads) / 256 + 1) * b->n > INT32_MAX / (148 * c->kv_heads)) return BD_ERR_UNSUPPORTED;   // CTAs of a launch

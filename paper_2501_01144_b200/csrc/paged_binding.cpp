@@ -76,10 +76,23 @@ void check(bd_status s) {
     }
     throw Raised();
 }
+// A descriptor as Python keeps it, with the device its buffers are on.
+template <typename T>
+struct Held {
+    T s;
+    int64_t device;
+};
+template <typename T>
+PyObject *hold(const T &s) {
+    const Held<T> h{s, (int64_t)c10::cuda::current_device()};
+    return PyBytes_FromStringAndSize((const char *)&h, sizeof h);
+}
 template <typename T>
 const T &structure(PyObject *o) {
-    if (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof(T)) refuse("not a descriptor of this module");
-    return *(const T *)PyBytes_AS_STRING(o);
+    if (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof(Held<T>)) refuse("not a descriptor of this module");
+    const Held<T> &h = *(const Held<T> *)PyBytes_AS_STRING(o);
+    if (h.device != c10::cuda::current_device()) refuse("cache and batch must be on the current CUDA device");
+    return h.s;
 }
 void need(Py_ssize_t got, Py_ssize_t want) {
     if (got != want) refuse("wrong number of arguments");
@@ -114,7 +127,7 @@ PyObject *cache(PyObject *const *a, Py_ssize_t n) {
     here(pool, "pool");
     here(tail, "tail");
     c.pages = pool.size(0); c.pool = pool.data_ptr(); c.tail = tail.data_ptr();
-    return PyBytes_FromStringAndSize((const char *)&c, sizeof c);
+    return hold(c);
 }
 
 PyObject *batch(PyObject *const *a, Py_ssize_t n) {
@@ -134,7 +147,7 @@ PyObject *batch(PyObject *const *a, Py_ssize_t n) {
     b.ld_table = m > 1 ? table.stride(0) : table.size(1);
     b.n = m; b.max_q = integer(a[4]); b.max_kv = a[5] == Py_None ? -1 : integer(a[5]);
     b.rows = table.size(1);                                       // the table's width until a call's rows are known
-    return PyBytes_FromStringAndSize((const char *)&b, sizeof b);
+    return hold(b);
 }
 // The descriptor of one call: bounds completed from the call's rows and the cache's pages.
 bd_paged_batch batch_for(const bd_paged_batch &b0, const bd_paged_cache &c, int64_t rows) {

@@ -147,7 +147,7 @@ def test_bad_rows_are_refused(args, status):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(q_heads=3), 2), (dict(q_heads=0), 1), (dict(window=-1), 1), (dict(softcap=-1.0), 1), (dict(softcap=float("nan")), 1), (dict(scale=float("nan")), 1),
+    (dict(q_heads=3), 2), (dict(q_heads=0), 1), (dict(window=-1), 1), (dict(softcap=-1.0), 1), (dict(softcap=float("nan")), 1), (dict(softcap=1e-9), 1), (dict(scale=float("inf")), 1), (dict(scale=float("nan")), 1),
     (dict(odtype=9), 1), (dict(odtype=bd.F16), 4), (dict(dtype=bd.F32), 4), (dict(ldo=500), 2), (dict(lse=0x5002), 3), (dict(ws=0, q_heads=4), 8),
     (dict(ws=0x100010, q_heads=4), 3), (dict(wbytes=100), 8),
 ])
