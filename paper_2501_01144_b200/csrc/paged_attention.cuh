@@ -320,49 +320,55 @@ struct RowWork {
         // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
         const int tok0 = c * kChunk + 8 * (g / 2) + g % 2;
         const bool masked = (c + 1) * kChunk > first_pos + 1 || (p.window && c * kChunk <= last_pos - p.window);
+        // The running maximum (the same in the eight lanes of a column) moves only when a score exceeds it by more than 2^8:
+        // probabilities up to 2^8 do no harm in fp16 with fp32 sums, and without a move no lane needs another's scores.
         uint32_t pf[NT][4];
-        float alpha[NT][2];
         bool grew = false;
-        float pv[NT][4][2];
+        float x[NT][4][2], top[NT][2], pv[NT][4][2];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                float x[4];
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    x[j] = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
-                    if (CAP) x[j] = capped(x[j], p.softcap * 1.4426950408889634f);
+                    float &y = x[nt][j][i];
+                    y = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
+                    if (CAP) y = capped(y, p.softcap * 1.4426950408889634f);
                     if (masked) {
                         const int tok = tok0 + 2 * j;
-                        if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) x[j] = -INFINITY;
+                        if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) y = -INFINITY;
                     }
                 }
-                float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                const float m_new = fmaxf(m_run[nt][i], top);
-                const float base = m_new == -INFINITY ? 0.0f : m_new;
-                alpha[nt][i] = fast_exp2(m_run[nt][i] - base);
-                grew |= m_new > m_run[nt][i];
-                m_run[nt][i] = m_new;
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    pv[nt][j][i] = fast_exp2(x[j] - base);
-                    sum += pv[nt][j][i];
-                }
-                l_run[nt][i] = fmaf(l_run[nt][i], alpha[nt][i], sum);
+                top[nt][i] = fmaxf(fmaxf(x[nt][0][i], x[nt][1][i]), fmaxf(x[nt][2][i], x[nt][3][i]));
+                grew |= top[nt][i] > m_run[nt][i] + 8.0f;
             }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                for (int b = 0; b < NB; b++)
+                for (int i = 0; i < 2; i++) {
+                    float m = fmaxf(top[nt][i], m_run[nt][i]);
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                    const float alpha = m == -INFINITY ? 1.0f : fast_exp2(m_run[nt][i] - m);
+                    m_run[nt][i] = m;
+                    l_run[nt][i] *= alpha;
 #pragma unroll
-                    for (int x = 0; x < 8; x++) O[nt][b][x / 4][x % 4] *= alpha[nt][x % 2];
+                    for (int b = 0; b < NB; b++)
+#pragma unroll
+                        for (int y = 0; y < 4; y++) O[nt][b][y / 2][2 * (y % 2) + i] *= alpha;
+                }
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const float base = m_run[nt][i] == -INFINITY ? 0.0f : m_run[nt][i];
+#pragma unroll
+                for (int j = 0; j < 4; j++) pv[nt][j][i] = fast_exp2(x[nt][j][i] - base);
+                l_run[nt][i] += (pv[nt][0][i] + pv[nt][1][i]) + (pv[nt][2][i] + pv[nt][3][i]);
+            }
         if (c < full) {
             // ---- values stored in 4 bits ----
 #pragma unroll
