@@ -583,3 +583,52 @@ def test_two_captured_graphs_with_workspaces_of_their_own_and_another_stream():
     assert torch.equal(o, want[1])
     o = bd.paged_attention(w.cache, b, qs[0], stream=torch.cuda.current_stream())
     assert torch.equal(o, want[0])
+
+
+def test_captured_without_a_workspace_and_two_calls_at_once():
+    """A capture takes its workspace from the graph's own pool; calls on two streams each get their own."""
+    w = World(3, 2, 128, 64, torch.bfloat16, seed=44, max_tokens=3000)
+    w.step([2900, 1500, 40])
+    b = w.batch([1, 2, 1])
+    qs = [to_device(queries(w.rng, 4, 8, 128, w.kind)[0], w.kind) for _ in range(3)]
+    want = [bd.paged_attention(w.cache, b, q) for q in qs]
+    x, out = qs[0].clone(), torch.empty_like(want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bd.paged_attention(w.cache, b, x, out=out)
+    for q, y in zip(qs, want):
+        x.copy_(q)
+        junk = torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")
+        graph.replay()
+        assert torch.equal(out, y)
+        del junk
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for q, s in zip(qs, streams):
+            with torch.cuda.stream(s):
+                got.append(bd.paged_attention(w.cache, b, q))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, y) for g, y in zip(got, want))
+    got = [bd.paged_attention(w.cache, b, q, stream=s) for q, s in zip(qs, streams)]     # the stream as an argument
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, y) for g, y in zip(got, want))
+    bd.poll_status()
+
+
+def test_the_tensor_core_product_and_the_chunk_kernel_back_to_back():
+    """Both keep their accumulators in tensor memory and start under each other's tails."""
+    w = World(1, 2, 128, 64, torch.bfloat16, seed=45, max_tokens=700)
+    w.step([600])
+    b = w.batch([200])
+    q = to_device(queries(w.rng, 200, 8, 128, w.kind)[0], w.kind)
+    rng = np.random.default_rng(1)
+    wq = bd.quantize_weights(torch.from_numpy(rng.standard_normal((1024, 1024)).astype(np.float32)).cuda(), bd.SELECT_TWO_STAGE)
+    want_o = bd.paged_attention(w.cache, b, q)
+    want_y = bd.linear(want_o.view(200, 1024), wq)
+    for _ in range(20):
+        o = bd.paged_attention(w.cache, b, q)
+        y = bd.linear(o.view(200, 1024), wq)
+        assert torch.equal(bd.paged_attention(w.cache, b, q), want_o) and torch.equal(y, want_y) and torch.equal(o, want_o)
+    bd.poll_status()
