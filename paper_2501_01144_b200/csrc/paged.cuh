@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(NB * 32) append_kernel(Pool pool, Batch batch,
     const int seq = blockIdx.z, h = blockIdx.y;
     const Sequence s = sequence_of(batch, seq);
     const int slot = batch.slot[seq];
-    if (!s.ok || s.t > s.kv || slot < 0 || slot >= pool.slots) {
+    if (!s.ok || s.t > s.kv || (s.t > 0 && (slot < 0 || slot >= pool.slots))) {   // (a sequence without rows needs no slot)
         if (threadIdx.x == 0) atomicOr(&g_status_word, kStatusIndex);
         return;
     }

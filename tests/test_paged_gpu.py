@@ -408,6 +408,22 @@ def test_pages_and_slots_out_of_range_are_reported_and_not_followed():
         reported()
 
 
+def test_sequences_without_rows_need_no_slot_and_no_pages():
+    """A padded batch: entries without rows carry -1 for slot and pages."""
+    w = World(2, 2, 64, 32, torch.bfloat16, seed=36, max_tokens=64)
+    w.step([20, 13])
+    table, slots = torch.cat([w.table, torch.full_like(w.table, -1)]), torch.cat([w.slots, torch.full_like(w.slots, -1)])
+    rows = [source_rows(w.rng, 1, 2, 64, w.kind) for _ in range(2)]
+    for s, (k, v) in zip(w.seqs, rows):
+        s.append(k, v)
+    b = bd.PagedBatch(table, slots, i32([21, 14, 0, 0]), i32([0, 1, 2, 2, 2]), 1)
+    bd.paged_append(w.cache, b, *(to_device(np.concatenate([r[j] for r in rows]), w.kind) for j in (0, 1)))
+    bd.paged_read(w.cache, b, 2)
+    bd.paged_attention(w.cache, b, to_device(queries(w.rng, 2, 4, 64, w.kind)[0], w.kind))
+    bd.poll_status()
+    check_read(w)
+
+
 def test_binding_refuses_what_does_not_fit():
     w = World(1, 2, 64, 32, torch.bfloat16, seed=35, max_tokens=64)
     b = w.batch([1], kv_len=[1])
