@@ -371,7 +371,8 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
 /* Causal attention of the step's queries over the cache, the step's own tokens included (append them first):
  *     o_i = sum_j p_ij v_j,   p_i = softmax over the visible j of  s_ij,
  *     s_ij = scale * q_i . k_j,  or  softcap * tanh(scale * q_i . k_j / softcap)  for softcap > 0,
- * where the query of token t sees tokens t - window + 1 .. t (window 0: all up to t).  Query head h reads KV head
+ * where the query of token t sees tokens t - window + 1 .. t (window 0: all up to t); page numbers of chunks in front of every
+ * row's window are not looked at (such pages may have been given away).  Query head h reads KV head
  * h / (q_heads / kv_heads).  Q has the cache's type, BD_BF16 or BD_F16 (fp32 caches: BD_ERR_UNSUPPORTED); O is BD_F32 or
  * that type.  Unlike bd_kvcache_attention, which follows the paper's scope "all", queries and probabilities stay
  * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  lse (optional, fp32 [rows][q_heads]) receives

@@ -139,9 +139,10 @@ __global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ Att
     if (!s.ok || s.t == 0) return;
     if (tile * kTileTokens >= s.kv || (p.window && (tile + 1) * kTileTokens <= s.kv - s.t - p.window + 1)) return;   // nobody sees it
     const int c = 4 * tile + e, full = s.kv / kChunk, n_chunks = (s.kv + kChunk - 1) / kChunk;
-    const int64_t off = c < n_chunks ? record_offset(p.pool, p.batch, seq, h, c) : -1, at = image_index(p, seq, h, tile);
+    const bool seen = c < n_chunks && c >= (p.window ? max(0, s.kv - s.t - p.window + 1) / kChunk : 0);   // pages in front of the window are not looked up
+    const int64_t off = seen ? record_offset(p.pool, p.batch, seq, h, c) : -1, at = image_index(p, seq, h, tile);
     uint8_t *image = p.images + at * (2 * kImage) + (values ? kImage : 0);
-    if (off < 0 && c < n_chunks && lane == 0) atomicOr(&g_status_word, kStatusIndex);
+    if (off < 0 && seen && lane == 0) atomicOr(&g_status_word, kStatusIndex);
     __shared__ uint32_t ok;
     if (threadIdx.x == 0) ok = 0;
     __syncthreads();
@@ -455,9 +456,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         } else {
         // ---- expansion: warp e takes chunk e of every tile; lane = row of the record's tiles ----
         const uint4 *table = (const uint4 *)(sm + S::table);
+        const int first_seen = seen_begin / kChunk;
         auto place = [&](int j) -> int64_t {                      // the chunk's record, -1: none
             const int c = 4 * (t_begin + j) + e;
-            if (c >= n_chunks) return -1;
+            if (c >= n_chunks || c < first_seen) return -1;       // (pages in front of the window are not looked up: they may be gone)
             const int at = (int)fast_div(c, p.by_page), page = p.batch.table[(int64_t)seq * p.batch.ld_table + at];
             if (page < 0 || page >= p.pool.pages) {
                 if (lane == 0) atomicOr(&g_status_word, kStatusIndex);

@@ -336,6 +336,32 @@ def test_sharp_rows_and_tiny_and_huge_queries():
         check_attention(w, [1, 2], 4, spread=spread, scale=1.0 / (spread * 11.0) if spread > 100 else None)
 
 
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d,heads,old,new,window", [
+    (128, 4, 300, 2, 40), (64, 16, 1900, 1, 1100),                  # few rows: a CTA per head, runs
+    (64, 4, 690, 40, 100), (128, 2, 2900, 33, 700),                 # more rows: alone, shared by CTAs
+    (128, 8, 4350, 256, 4000)])                                     # tiles expanded in front
+def test_pages_in_front_of_the_window_may_be_gone(kind, d, heads, old, new, window):
+    n = old + new
+    w = World(1, 1, d, 32, kind, seed=window, max_tokens=n)
+    k, v = (to_device(x, kind) for x in source_rows(w.rng, n, 1, d, kind))
+    bd.paged_append(w.cache, bd.PagedBatch(w.table, w.slots, i32([n]), i32([0, n]), n), k, v)
+    q = to_device(queries(w.rng, new, heads, d, kind)[0], kind)
+    want, lse = (torch.empty(new, heads, d, device="cuda"), torch.empty(new, heads, device="cuda"))
+    bd.paged_attention(w.cache, bd.PagedBatch(w.table, w.slots, i32([n]), i32([0, new]), new), q, window=window, out=want, lse=lse)
+    gone = (old - window + 1) // 32
+    assert gone > 0 and torch.isfinite(want).all()
+    junk = next(p for p in range(w.cache.pages) if p not in w.table[0].tolist())      # a page that nobody wrote
+    for number in (-1, w.cache.pages, junk):
+        table = w.table.clone()
+        table[0, :gone] = number
+        b = bd.PagedBatch(table, w.slots, i32([n]), i32([0, new]), new)
+        got_lse = torch.empty_like(lse)
+        got = bd.paged_attention(w.cache, b, q, window=window, dtype=torch.float32, lse=got_lse)
+        bd.poll_status()
+        assert torch.equal(got, want) and torch.equal(got_lse, lse)
+
+
 def test_rows_that_see_nothing_give_zeros():
     w = World(2, 2, 128, 32, torch.bfloat16, seed=32, max_tokens=64)
     w.step([2, 40])
