@@ -594,7 +594,17 @@ def kvcache_attention(caches, Qs, scale, out=None, dtype=torch.float32, probs=No
     return out
 
 
-class PagedKVCache:
+class _Described:
+    """Base of the objects whose C descriptor is made once, at construction: their members are fixed (the descriptor holds the
+    tensors' addresses), the tensors' contents are not."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed: write into the tensor, or make a new object")
+
+    __delattr__ = lambda self, name: self.__setattr__(name, None)  # noqa: E731
+
+
+class PagedKVCache(_Described):
     """Paged DialectFP4 KV cache shared by many sequences (storage: bd.h).  `pool` uint8 [pages, kv_heads,
     page_tokens / 32, 35 * head_dim], `tail` [slots, kv_heads, 64, head_dim] of `dtype`.  The caller hands out pages
     and slots; nothing has to be initialised."""
@@ -613,8 +623,7 @@ class PagedKVCache:
         return self
 
     def _set(self, pool, tail, page_tokens):
-        self._c = (_paged or _load_paged()).cache(pool, tail, page_tokens)
-        self.pool, self.tail, self.page_tokens = pool, tail, page_tokens
+        self.__dict__.update(_c=(_paged or _load_paged()).cache(pool, tail, page_tokens), pool=pool, tail=tail, page_tokens=page_tokens)
 
     pages = property(lambda self: self.pool.shape[0])
     slots = property(lambda self: self.tail.shape[0])
@@ -623,14 +632,14 @@ class PagedKVCache:
     dtype = property(lambda self: self.tail.dtype)
 
 
-class PagedBatch:
+class PagedBatch(_Described):
     """One step's sequences (int32 CUDA tensors): page_table [n, width], slots [n], kv_len [n] (this step's tokens
-    included), q_start [n + 1].  max_q: host bound of the rows of one sequence; max_kv: of its tokens (default: what
+    included), q_start [n + 1]; their contents may change between calls (and replays).  max_q: host bound of the rows of one sequence; max_kv: of its tokens (default: what
     the page table can hold)."""
 
     def __init__(self, page_table, slots, kv_len, q_start, max_q, max_kv=None):
-        self._c = (_paged or _load_paged()).batch(page_table, slots, kv_len, q_start, max_q, max_kv)
-        self.page_table, self.slots, self.kv_len, self.q_start, self.max_q, self.max_kv = page_table, slots, kv_len, q_start, max_q, max_kv
+        self.__dict__.update(_c=(_paged or _load_paged()).batch(page_table, slots, kv_len, q_start, max_q, max_kv), page_table=page_table,
+                             slots=slots, kv_len=kv_len, q_start=q_start, max_q=max_q, max_kv=max_kv)
 
 
 def paged_append(cache, batch, k, v, stream=None):

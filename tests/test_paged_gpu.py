@@ -475,6 +475,19 @@ def test_binding_refuses_what_does_not_fit():
     bd.poll_status()
 
 
+def test_members_of_caches_and_batches_are_fixed():
+    """Their descriptors hold the tensors' addresses: another tensor in a member's place would not be seen."""
+    w = World(1, 2, 64, 32, torch.bfloat16, seed=37, max_tokens=64)
+    b = w.batch([1], kv_len=[1])
+    for obj, name in ((w.cache, "pool"), (w.cache, "tail"), (w.cache, "page_tokens"), (b, "kv_len"), (b, "page_table"), (b, "max_kv")):
+        with pytest.raises(AttributeError):
+            setattr(obj, name, getattr(obj, name))
+        with pytest.raises(AttributeError):
+            delattr(obj, name)
+    b.kv_len.fill_(0)                                               # contents may change
+    assert (bd.paged_attention(w.cache, b, torch.ones(1, 2, 64, dtype=torch.bfloat16, device="cuda")) == 0).all()
+
+
 # ---- rotation -------------------------------------------------------------------------------------------------------
 
 
