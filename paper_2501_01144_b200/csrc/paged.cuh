@@ -197,7 +197,9 @@ __device__ __forceinline__ void make_base_tables(uint4 *to) {
     for (int i = threadIdx.x; i < (DT == BD_BF16 ? 128 : 64); i += blockDim.x) ((uint32_t *)to)[i] = from[i];
 }
 // TINY: bf16 blocks of scale < 2 (magnitudes below 2^-123) keep their subnormal values; otherwise they count as zeros.
-template <int DT, bool TINY>
+// LOW: fp16 blocks may have scales below kF16Normal.
+constexpr uint32_t kF16Normal = 114;
+template <int DT, bool TINY, bool LOW = true>
 __device__ __forceinline__ uint4 block_table(const uint4 *base, uint32_t id, uint32_t scale) {
     uint4 t = base[DT == BD_BF16 ? 2 * id + (scale & 1u) : id];
     const uint32_t k = DT == BD_BF16 ? (scale >> 1) - 1u : (scale - 113u) * 4u;
@@ -205,7 +207,7 @@ __device__ __forceinline__ uint4 block_table(const uint4 *base, uint32_t id, uin
     t.w += k * 0x01010101u;
     if (DT == BD_BF16 && !TINY) {
         if (scale < 2u) t = make_uint4(0, 0, 0, 0);
-    } else if (scale < (DT == BD_BF16 ? 2u : 114u)) {
+    } else if (LOW && scale < (DT == BD_BF16 ? 2u : kF16Normal)) {
         uint32_t b[4] = {0, 0, 0, 0};
         const uint32_t tlo = c_tables.int_lo[id], thi = c_tables.int_hi[id];
 #pragma unroll
