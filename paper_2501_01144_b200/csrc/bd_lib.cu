@@ -452,10 +452,10 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
         }
         if (window) r.splits = std::min(r.splits, attention_plan(c, b, q_heads, 0).splits);       // the workspace is asked for without a window
         // Tiles expanded once in front pay when many CTAs read each: 32 / 8 heads x 128, expanded by every CTA against in front:
-        // 4096 new of 16384 tokens 1059 / 809 us, 512 of 16384 182 / 170, 768 of 4096 86 / 79, 256 of 16384 103 / 114, 2048 of 2048 57 / 65,
-        // 4096 of 4096 with 32 KV heads 194 / 205.  d = 64 (half the expansion per exponential): 4096 of 8192 358 / 376, never better.
+        // 4096 new of 16384 tokens 932 / 811 us, 1024 of 16384 268 / 253, 512 of 16384 162 / 169, 2048 of 8192 244 / 230, 1024 of 8192 141 / 134,
+        // 512 of 8192 96 / 101, 1024 of 4096 78 / 83; 2 x 2048 of 4096 237 / 240.  d = 64 (half the expansion per exponential): never better.
         const size_t images = (size_t)b->n * (size_t)c->kv_heads * (size_t)((b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens) * (size_t)(2 * 128 * c->head_dim * 2);
-        if (c->head_dim == 128 && r.tiles >= 8 && seen >= 4096 && b->max_kv >= 2 * b->max_q && images <= ((size_t)1 << 30)) r.images = images;
+        if (c->head_dim == 128 && r.tiles >= 16 && seen >= 6144 && b->max_kv >= 2 * b->max_q && images <= ((size_t)1 << 30)) r.images = images;
         return r;
     }
     r.wide = rows > 8;

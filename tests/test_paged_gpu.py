@@ -236,22 +236,23 @@ def test_long_context_is_split_and_joined():
 
 
 @pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("softcap,window", [(0.0, 0), (12.0, 4050)])
+@pytest.mark.parametrize("softcap,window", [(0.0, 0), (12.0, 6200)])
 def test_many_rows_over_a_long_context(kind, softcap, window):
-    """Tiles expanded in front (2048 rows and 4096 tokens or more, head_dim 128), with an unfinished chunk."""
-    w = World(2, 1, 128, 64, kind, seed=36, max_tokens=4300)
-    w.step([3990, 3])
-    assert bd.paged_attention_workspace_size(w.cache, w.batch([256, 1]), 257, 8) > (1 << 20)
-    check_attention(w, [256, 40], 8, softcap=softcap, window=window)
+    """Tiles expanded in front (about 4096 rows and 6144 tokens or more, head_dim 128), with an unfinished chunk."""
+    w = World(2, 1, 128, 64, kind, seed=36, max_tokens=7000)
+    w.step([6390, 3])
+    # the images of two sequences' 55 tiles, 128 keys and values of 256 bytes each
+    assert bd.paged_attention_workspace_size(w.cache, w.batch([512, 1]), 513, 8) >= 2 * 55 * 2 * 128 * 256
+    check_attention(w, [512, 40], 8, softcap=softcap, window=window)
     # a page number outside the pool: its tokens are not seen, by this kernel or the one for few rows
-    bits, _ = queries(w.rng, 257, 8, 128, kind)
+    bits, _ = queries(w.rng, 513, 8, 128, kind)
     q, table = to_device(bits, kind), w.table.clone()
     table[0, 20] = -7
-    many = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([4246, 43]), i32([0, 256, 257]), 256), q, softcap=softcap, window=window, dtype=torch.float32)
-    few = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([4246, 43]), i32([0, 2, 3]), 2), torch.cat([q[254:256], q[256:]]), softcap=softcap, window=window, dtype=torch.float32)
+    many = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([6902, 43]), i32([0, 512, 513]), 512), q, softcap=softcap, window=window, dtype=torch.float32)
+    few = bd.paged_attention(w.cache, bd.PagedBatch(table, w.slots, i32([6902, 43]), i32([0, 2, 3]), 2), torch.cat([q[510:512], q[512:]]), softcap=softcap, window=window, dtype=torch.float32)
     with pytest.raises(bd.BdError):
         bd.poll_status()
-    assert (many[254:] - few).abs().max() <= 2 * (HALF_STEP[kind] + 2.0 ** -11) * w.cache.head_dim ** 0.5 * 4 and torch.isfinite(many).all()
+    assert (many[510:] - few).abs().max() <= 2 * (HALF_STEP[kind] + 2.0 ** -11) * w.cache.head_dim ** 0.5 * 4 and torch.isfinite(many).all()
 
 
 @pytest.mark.parametrize("heads,most", [(4, 1), (8, 4), (16, 4)])
@@ -340,7 +341,7 @@ def test_sharp_rows_and_tiny_and_huge_queries():
 @pytest.mark.parametrize("d,heads,old,new,window", [
     (128, 4, 300, 2, 40), (64, 16, 1900, 1, 1100),                  # few rows: a CTA per head, runs
     (64, 4, 690, 40, 100), (128, 2, 2900, 33, 700),                 # more rows: alone, shared by CTAs
-    (128, 8, 4350, 256, 4000)])                                     # tiles expanded in front
+    (128, 8, 6800, 512, 6200)])                                     # tiles expanded in front
 def test_pages_in_front_of_the_window_may_be_gone(kind, d, heads, old, new, window):
     n = old + new
     w = World(1, 1, d, 32, kind, seed=window, max_tokens=n)
