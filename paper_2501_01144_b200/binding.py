@@ -596,18 +596,30 @@ def kvcache_attention(caches, Qs, scale, out=None, dtype=torch.float32, probs=No
 
 class _Described:
     """Base of the objects whose C descriptor is made once, at construction: their members are fixed (the descriptor holds the
-    tensors' addresses), the tensors' contents are not."""
+    tensors' addresses, so their storage has to stay too: no set_, no .data), the tensors' contents are not."""
 
     def __setattr__(self, name, value):
         raise AttributeError(f"{type(self).__name__}.{name} is fixed: write into the tensor, or make a new object")
 
     __delattr__ = lambda self, name: self.__setattr__(name, None)  # noqa: E731
 
+    def __reduce__(self):
+        """Copies (copy, deepcopy, pickle) are made anew from the copied members: a descriptor of their own tensors."""
+        return _describe, (type(self), *(self.__dict__[name] for name in self._members))
+
+
+def _describe(cls, *members):
+    obj = cls.__new__(cls)
+    obj._set(*members)
+    return obj
+
 
 class PagedKVCache(_Described):
     """Paged DialectFP4 KV cache shared by many sequences (storage: bd.h).  `pool` uint8 [pages, kv_heads,
     page_tokens / 32, 35 * head_dim], `tail` [slots, kv_heads, 64, head_dim] of `dtype`.  The caller hands out pages
-    and slots; nothing has to be initialised."""
+    and slots; nothing has to be initialised.  copy.deepcopy makes a cache with buffers of its own (a fork)."""
+
+    _members = ("pool", "tail", "page_tokens")
 
     def __init__(self, pages, kv_heads, head_dim, slots, page_tokens=64, dtype=torch.bfloat16, device="cuda"):
         if head_dim not in (64, 128) or page_tokens <= 0 or page_tokens % 32:
@@ -618,9 +630,7 @@ class PagedKVCache(_Described):
     @classmethod
     def from_buffers(cls, pool, tail, page_tokens):
         """A cache over the caller's own buffers (contiguous, shapes as above)."""
-        self = cls.__new__(cls)
-        self._set(pool, tail, page_tokens)
-        return self
+        return _describe(cls, pool, tail, page_tokens)
 
     def _set(self, pool, tail, page_tokens):
         self.__dict__.update(_c=(_paged or _load_paged()).cache(pool, tail, page_tokens), pool=pool, tail=tail, page_tokens=page_tokens)
@@ -637,7 +647,12 @@ class PagedBatch(_Described):
     included), q_start [n + 1]; their contents may change between calls (and replays).  max_q: host bound of the rows of one sequence; max_kv: of its tokens (default: what
     the page table can hold)."""
 
+    _members = ("page_table", "slots", "kv_len", "q_start", "max_q", "max_kv")
+
     def __init__(self, page_table, slots, kv_len, q_start, max_q, max_kv=None):
+        self._set(page_table, slots, kv_len, q_start, max_q, max_kv)
+
+    def _set(self, page_table, slots, kv_len, q_start, max_q, max_kv):
         self.__dict__.update(_c=(_paged or _load_paged()).batch(page_table, slots, kv_len, q_start, max_q, max_kv), page_table=page_table,
                              slots=slots, kv_len=kv_len, q_start=q_start, max_q=max_q, max_kv=max_kv)
 

@@ -1,11 +1,15 @@
 """Paged cache without a GPU: the storage's index arithmetic (compiled for the host from the kernels' own header), the
 refusals of the C entry points, and the oracle's pins."""
+import copy
 import ctypes
 import os
+import pickle
 import subprocess
+import types
 
 import numpy as np
 import pytest
+import torch
 
 import oracle
 import paper_2501_01144_b200 as bd
@@ -179,6 +183,27 @@ def test_sizes():
     assert p.value == 10 * 2 * 2 * 35 * 128 and t.value == 4 * 2 * 64 * 128 * 2
     assert lib.bd_paged_sizes(ctypes.byref(cache(head_dim=32)), None, None) == 2
     assert lib.bd_status_string(10) != b"unknown status"
+
+
+# ---- the descriptors that Python keeps ----
+
+
+@pytest.mark.parametrize("duplicate", [copy.deepcopy, lambda x: pickle.loads(pickle.dumps(x)), copy.copy], ids=["deepcopy", "pickle", "copy"])
+def test_a_copied_cache_or_batch_is_described_by_its_own_tensors(monkeypatch, duplicate):
+    """The descriptor holds addresses: a copy that kept it would read and write the original's buffers, or freed ones."""
+    where = lambda *members: tuple(x.data_ptr() if torch.is_tensor(x) else x for x in members)  # noqa: E731
+    monkeypatch.setattr(bd.binding, "_paged", types.SimpleNamespace(cache=where, batch=where))
+    i32 = lambda *s: torch.arange(int(np.prod(s)), dtype=torch.int32).view(*s)  # noqa: E731
+    cache = bd.PagedKVCache.from_buffers(torch.ones(3, 2, 1, 35 * 64, dtype=torch.uint8), torch.ones(2, 2, 64, 64), 32)
+    batch = bd.PagedBatch(i32(2, 3), i32(2), i32(2), i32(3), 4, max_kv=90)
+    for x, names in ((cache, ("pool", "tail", "page_tokens")), (batch, ("page_table", "slots", "kv_len", "q_start", "max_q", "max_kv"))):
+        y = duplicate(x)
+        assert type(y) is type(x) and y._c == where(*(getattr(y, n) for n in names))
+        for n in names:
+            a, b = getattr(x, n), getattr(y, n)
+            assert torch.equal(a, b) and (a.data_ptr() == b.data_ptr()) == (duplicate is copy.copy) if torch.is_tensor(a) else a == b
+        with pytest.raises(AttributeError):
+            setattr(y, names[0], None)
 
 
 # ---- the oracle ----

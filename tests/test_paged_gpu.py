@@ -1,4 +1,6 @@
 """The paged cache on the GPU: append, read back, attention and rotation against the oracle in 64 bits."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -487,6 +489,25 @@ def test_members_of_caches_and_batches_are_fixed():
             delattr(obj, name)
     b.kv_len.fill_(0)                                               # contents may change
     assert (bd.paged_attention(w.cache, b, torch.ones(1, 2, 64, dtype=torch.bfloat16, device="cuda")) == 0).all()
+
+
+def test_a_forked_cache_has_buffers_of_its_own():
+    """deepcopy: what is appended to the copy shows in the copy alone, and it outlives the original."""
+    w = World(1, 2, 64, 32, torch.bfloat16, seed=47, max_tokens=96)
+    w.step([40])
+    fork, batch = copy.deepcopy((w.cache, w.batch([45], kv_len=[45])))
+    before = [x.clone() for x in bd.paged_read(w.cache, w.batch([40]), 40)]
+    pool, tail = w.cache.pool.clone(), w.cache.tail.view(torch.int16).clone()
+    k, v = source_rows(w.rng, 5, 2, 64, w.kind)
+    bd.paged_append(fork, bd.PagedBatch(w.table, w.slots, i32([45]), i32([0, 5]), 5), to_device(k, w.kind), to_device(v, w.kind))
+    assert torch.equal(pool, w.cache.pool) and torch.equal(tail, w.cache.tail.view(torch.int16))
+    w.seqs[0].append(k, v)
+    w.cache.pool.fill_(255), w.cache.tail.view(torch.int16).fill_(-1), w.table.fill_(-1)
+    w.cache = fork
+    got = [x.clone() for x in bd.paged_read(fork, batch, 45)]
+    assert np.array_equal(got[0].double().cpu().numpy(), w.seqs[0].keys().transpose(1, 0, 2)) and torch.equal(got[0][:40], before[0])
+    assert np.array_equal(got[1].double().cpu().numpy(), w.seqs[0].values().transpose(1, 0, 2))
+    bd.poll_status()
 
 
 # ---- rotation -------------------------------------------------------------------------------------------------------
