@@ -518,8 +518,8 @@ bd_status launch_head_kernel(const pg::Attention &a, cudaStream_t st) {
 }
 template <int DT, int NB, int NT>
 bd_status launch_rows(const pg::Attention &a, cudaStream_t st) {
-    if (a.whole) return a.softcap > 0.0f ? launch_head_kernel<DT, NB, NT, true>(a, st) : launch_head_kernel<DT, NB, NT, false>(a, st);
-    return a.softcap > 0.0f ? launch_rows_kernel<DT, NB, NT, true>(a, st) : launch_rows_kernel<DT, NB, NT, false>(a, st);
+    if (a.whole) return a.cap > 0.0f ? launch_head_kernel<DT, NB, NT, true>(a, st) : launch_head_kernel<DT, NB, NT, false>(a, st);
+    return a.cap > 0.0f ? launch_rows_kernel<DT, NB, NT, true>(a, st) : launch_rows_kernel<DT, NB, NT, false>(a, st);
 }
 template <int DT>
 bd_status launch_rows_dtype(const pg::Attention &a, bool wide, cudaStream_t st) {
@@ -538,7 +538,7 @@ bd_status launch_chunk_kernel(const pg::Attention &a, dim3 grid, cudaStream_t st
 }
 template <int DT>
 bd_status launch_chunk(const pg::Attention &a, dim3 grid, cudaStream_t st) {
-    const bool cap = a.softcap > 0.0f;
+    const bool cap = a.cap > 0.0f;
     if (a.images) return cap ? launch_chunk_kernel<DT, 4, true, true>(a, grid, st) : launch_chunk_kernel<DT, 4, false, true>(a, grid, st);
     if (a.pool.head_dim == 128) return cap ? launch_chunk_kernel<DT, 4, true, false>(a, grid, st) : launch_chunk_kernel<DT, 4, false, false>(a, grid, st);
     return cap ? launch_chunk_kernel<DT, 2, true, false>(a, grid, st) : launch_chunk_kernel<DT, 2, false, false>(a, grid, st);
@@ -1509,7 +1509,8 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.o = (uint8_t *)O; a.ldo = ldo; a.hso = head_stride_o;
     a.lse = lse;
     a.part = (float *)workspace;
-    a.scale = scale; a.softcap = softcap;
+    a.scale = scale;
+    if (softcap > 0.0f) { a.cap = softcap * 1.4426950408889634f; a.cap_inv = 1.0f / a.cap; }
     a.q_heads = (int)q_heads; a.group = (int)(q_heads / c->kv_heads); a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
     a.odtype = (int)odtype;
     a.splits = plan.splits; a.row_tiles = plan.tiles; a.workers = plan.workers; a.whole = plan.whole; a.rounds = plan.rounds;

@@ -40,7 +40,8 @@ struct Attention {
     float *lse;                       // [rows][q_heads] or null
     float *part;                      // partial results: of the warps' runs (rows kernel; see Runs), or of the splits
                                       // [splits][rows][q_heads][d + 2] (chunk kernel): output, maximum (log2 units), sum
-    float scale, softcap;
+    float scale;
+    float cap, cap_inv;               // the cap in units of log2 e, and its reciprocal
     int q_heads, group, window, splits, row_tiles, odtype;
     bool whole;                       // rows kernel: a CTA per head (workers: its warps)
     int workers, rounds;              // rows kernel: warps that share the units, runs per warp at most
@@ -97,8 +98,48 @@ __device__ __forceinline__ float fast_exp2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// cap * tanh(x), through exp2; xl = 2 x log2 e.  Absolute error of the tanh about 1e-7.
-__device__ __forceinline__ float capped(float xl, float cap) { return cap - __fdividef(2.0f * cap, fast_exp2(xl) + 1.0f); }
+// cap * tanh(y / cap) = cap * x P(x^2) / Q(x^2), x = y / cap within +-8 (where tanh is 1 - 2^-22).  The quotient was fitted here to
+// tanh(x) / x with the constants 1 kept (iteratively reweighted least squares, relative error 2^-22.6); all coefficients are positive, so
+// nothing cancels and scores keep their bits however large the cap is: within 2^-20 of the result in fp32.  (cap - 2 cap / (e^2x + 1), with an
+// exponential more, is off by 2^-22 caps.)
+constexpr float kCapP1 = 1.29303646e-01f, kCapP2 = 2.95581807e-03f, kCapP3 = 1.14752201e-05f;
+constexpr float kCapQ1 = 4.62636188e-01f, kCapQ2 = 2.38358284e-02f, kCapQ3 = 2.39316360e-04f, kCapQ4 = 2.47326551e-07f;
+__device__ __forceinline__ float cap_range(float x) {
+    asm("min.NaN.f32 %0, %0, 0f41000000;\n\tmax.NaN.f32 %0, %0, 0fC1000000;" : "+f"(x));
+    return x;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Two fp32 numbers of a 64-bit register: one issue slot for both.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_of(float a) { return pair_of(a, a); }
+__device__ __forceinline__ void unpair(uint64_t r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// a = the capped a * mul_a, b likewise.
+__device__ __forceinline__ void cap_pair(float &a, float &b, float mul_a, float mul_b, float inverse, float cap) {
+    unpair(mul_pair(mul_pair(pair_of(a, b), pair_of(mul_a, mul_b)), pair_of(inverse)), a, b);
+    const uint64_t x = pair_of(cap_range(a), cap_range(b)), u = mul_pair(x, x);
+    const uint64_t n = fma_pair(fma_pair(fma_pair(u, pair_of(kCapP3), pair_of(kCapP2)), u, pair_of(kCapP1)), u, pair_of(1.0f));
+    const uint64_t d = fma_pair(fma_pair(fma_pair(fma_pair(u, pair_of(kCapQ4), pair_of(kCapQ3)), u, pair_of(kCapQ2)), u, pair_of(kCapQ1)), u, pair_of(1.0f));
+    unpair(d, a, b);
+    unpair(mul_pair(mul_pair(x, n), mul_pair(pair_of(cap), pair_of(reciprocal(a), reciprocal(b)))), a, b);
+}
 
 // One row's result: 2^23 is what the half-unit subnormals left out (2^-24 per code, 0.5 per half unit).
 __device__ __forceinline__ void store_out(const Attention &p, int64_t row, int head, int ch, float v) {
@@ -250,8 +291,7 @@ struct RowWork {
 #pragma unroll
             for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
                 const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
-                const float k = f * 8388608.0f * p.scale;
-                mul[nt][i] = CAP ? k / p.softcap * (2.0f * 1.4426950408889634f) : k * 1.4426950408889634f;
+                mul[nt][i] = f * 8388608.0f * p.scale * 1.4426950408889634f;
                 const int rc = 8 * nt + 2 * t4 + i;
                 pos[nt][i] = rc < n_rows ? first_pos + p.token(rc) : -1;
                 m_run[nt][i] = -INFINITY;
@@ -328,12 +368,18 @@ struct RowWork {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
+            for (int j = 0; j < 4; j++) {
+#pragma unroll
+                for (int i = 0; i < 2; i++) x[nt][j][i] = CAP ? sc[nt][j / 2][2 * (j % 2) + i] : sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
+                if (CAP) cap_pair(x[nt][j][0], x[nt][j][1], mul[nt][0], mul[nt][1], p.cap_inv, p.cap);
+            }
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
             for (int i = 0; i < 2; i++) {
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     float &y = x[nt][j][i];
-                    y = sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
-                    if (CAP) y = capped(y, p.softcap * 1.4426950408889634f);
                     if (masked) {
                         const int tok = tok0 + 2 * j;
                         if (tok > pos[nt][i] || (p.window && tok <= pos[nt][i] - p.window)) y = -INFINITY;

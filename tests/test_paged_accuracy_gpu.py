@@ -1,0 +1,106 @@
+"""Attention over the paged cache where its arithmetic is at the edge: caps from far below to far above the scores.  Against
+64 bits, on every way a call can take."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2501_01144_b200 as bd
+from paged_util import World, values_of
+from paper_2501_01144_b200 import inputs
+from util import to_device
+
+pytestmark = pytest.mark.gpu
+F16_HALF_STEP = 2.0 ** -11
+
+# (head_dim, query heads, KV heads, tokens there, rows): which kernels serve the call
+WAYS = {
+    "a CTA per head": (128, 4, 2, 300, 1),
+    "a CTA per head, 16 columns": (64, 8, 2, 290, 3),
+    "runs and join": (64, 8, 1, 2900, 1),
+    "runs and join, 16 columns": (128, 4, 1, 2900, 4),
+    "row tiles": (64, 4, 2, 333, 40),
+    "two row tiles": (128, 8, 2, 400, 70),
+    "row tiles, shared tokens": (128, 4, 1, 4100, 33),
+    "tiles expanded in front": (128, 8, 1, 6500, 520),
+}
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x, np.int32)).cuda()
+
+
+def bits_of(x, kind):
+    x = np.asarray(x, np.float32)
+    return inputs.to_bf16_bits(x) if kind == torch.bfloat16 else inputs.to_f16_bits(x)
+
+
+def ask(w, q_bits, t, heads, table=None, **kw):
+    """The last t tokens' rows of sequence 0 alone: fp32 output and log-sum-exp as fp64."""
+    lse = torch.full((t, heads), 7.0, device="cuda")
+    b = bd.PagedBatch(w.table if table is None else table, w.slots, i32([w.seqs[0].length]), i32([0, t]), t)
+    o = bd.paged_attention(w.cache, b, to_device(q_bits, w.kind), dtype=torch.float32, lse=lse, **kw)
+    return o.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+def compare(got, q, k, v, see, scale, kind, softcap=0.0):
+    """got = (o, lse) against softmax(scores of q [t, heads, d] and k [kv_heads, n, d] where see [t, n]) v, all in fp64."""
+    o, lse = got
+    t, heads, d = q.shape
+    group = heads // k.shape[0]
+    # more than 16 rows per KV head: probabilities in the cache's type, values of fp16 caches in fp16 (half of its smallest step)
+    wide = group * t > 16
+    p_half_step = 2.0 ** -8 if wide and kind == torch.bfloat16 else F16_HALF_STEP
+    p_floor = 0.0 if wide and kind == torch.bfloat16 else 2.0 ** -25
+    v_floor = 2.0 ** -25 if wide and kind == torch.float16 else 0.0
+    for h in range(heads):
+        kh, vh = k[h // group], v[h // group]
+        s = scale * (q[:, h] @ kh.T)
+        # exact products, at most 128 + 8 fp32 roundings of sums, each relative to the sum of the products' sizes
+        ds = 136 * 2.0 ** -24 * abs(scale) * (np.abs(q[:, h]) @ np.abs(kh).T)
+        if softcap:
+            # c x P(x^2) / Q(x^2) with x = y / c within +-8, all coefficients positive: the fit 2^-22.6 (tanh(8) itself is 1 - 2^-22), x three
+            # roundings, P and Q two each, the reciprocal and three products seven halves: 13 * 2^-24 + 2^-22.6 < 2^-20 of the result
+            s = softcap * np.tanh(s / softcap)
+            ds = ds + 2.0 ** -20 * np.abs(s)
+        s = np.where(see, s, -np.inf)
+        seen = see.any(1)
+        m = np.where(seen, s.max(1), 0.0)
+        p = np.exp(s - m[:, None])
+        total = np.where(seen, p.sum(1), 1.0)
+        ref = p @ vh / total[:, None]
+        size, flat = p @ np.abs(vh) / total[:, None], see @ np.abs(vh) / total[:, None]
+        # the score in units of log2 e, its difference from the reference: four roundings of the largest score's size
+        dsm = np.where(see, ds, 0).max(1) + 2.0 ** -22 * np.where(see, np.abs(s), 0).max(1)
+        # exp2 2^-22, sums of see.sum() terms in fp32
+        rel = p_half_step + 2 * dsm + 2.0 ** -21 + see.sum(1) * 2.0 ** -24
+        bound = rel[:, None] * size + p_floor * flat + v_floor + 2.0 ** -24 * np.abs(ref)
+        err = np.abs(o[:, h] - ref)
+        assert (err <= bound).all(), f"head {h}: error {np.nanmax(err)}, error / bound {np.nanmax(err / np.maximum(bound, 1e-300))}"
+        want = m + np.log(total)
+        assert (np.isinf(lse[:, h]) == ~seen).all()
+        off = np.abs(np.where(seen, lse[:, h], 0) - np.where(seen, want, 0))
+        assert (off <= dsm + 2.0 ** -20 + see.sum(1) * 2.0 ** -24 + 2.0 ** -23 * np.abs(want)).all(), f"head {h}: log-sum-exp off by {off.max()}"
+
+
+def causal(n, t, window=0):
+    key, pos = np.arange(n)[None], np.arange(n - t, n)[:, None]
+    return (key <= pos) & ((key > pos - window) if window else True)
+
+
+def world(way, kind, seed):
+    d, heads, kv_heads, n, t = WAYS[way]
+    w = World(1, kv_heads, d, 32, kind, seed=seed, max_tokens=n)
+    w.step([n])
+    q = bits_of(w.rng.standard_normal((t, heads, d)), kind)
+    return w, q, t, heads
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("softcap", [3.0, 50.0, 1e3, 1e5, 1e8, 1e30])
+def test_a_cap_costs_no_accuracy_however_far_above_the_scores(kind, way, softcap):
+    w, q, t, heads = world(way, kind, seed=50)
+    s = w.seqs[0]
+    got = ask(w, q, t, heads, softcap=softcap)
+    bd.poll_status()
+    compare(got, values_of(q, kind), s.keys(), s.values(), causal(s.length, t), w.d ** -0.5, kind, softcap)
