@@ -1,11 +1,11 @@
-"""Attention over the paged cache where its arithmetic is at the edge: caps from far below to far above the scores.  Against
+"""Attention over the paged cache at its edges: caps from far below to far above the scores, pages that are not there.  Against
 64 bits, on every way a call can take."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2501_01144_b200 as bd
-from paged_util import World, values_of
+from paged_util import World, source_rows, values_of
 from paper_2501_01144_b200 import inputs
 from util import to_device
 
@@ -104,3 +104,58 @@ def test_a_cap_costs_no_accuracy_however_far_above_the_scores(kind, way, softcap
     got = ask(w, q, t, heads, softcap=softcap)
     bd.poll_status()
     compare(got, values_of(q, kind), s.keys(), s.values(), causal(s.length, t), w.d ** -0.5, kind, softcap)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("window", [0, 270])
+def test_tokens_of_a_bad_page_are_not_seen(kind, way, window):
+    """Page numbers outside the pool inside the visible range: the result is that of the other tokens, although the missing ones
+    have the largest scores (or, a second time, all scores are alike, so that keys left over from other tiles would count)."""
+    d, heads, kv_heads, n, t = WAYS[way]
+    rng = np.random.default_rng(60)
+    common = rng.standard_normal(d)
+    pages = -(-n // 32)
+    near = (n - t - 130) // 32                                      # a page that every row's window of 270 tokens holds
+    bad = {near: -1, pages - 1: 2 ** 31 - 1}                        # the last one: an unfinished chunk
+    if not window:
+        bad |= {0: -7, 5: None, 6: -2 ** 31} | ({k: -1 for k in range(12, 16)} if pages > 16 else {})
+    token = np.arange(n)
+    gone = np.isin(token // 32, list(bad))
+    for loud in (True, False):
+        w = World(1, kv_heads, d, 32, kind, seed=61, max_tokens=n)
+        k, v = source_rows(rng, n, kv_heads, d, torch.float32)
+        if loud:
+            k[gone] = 0.4 * common
+        else:
+            k *= 0.1
+        k, v = bits_of(k, kind), bits_of(v, kind)
+        w.seqs[0].append(k, v)
+        bd.paged_append(w.cache, w.batch([n]), to_device(k, kind), to_device(v, kind))
+        q = bits_of(common + 0.5 * rng.standard_normal((t, heads, d)), kind)
+        table = w.table.clone()
+        for page, number in bad.items():
+            table[0, page] = w.cache.pages if number is None else number
+        s = w.seqs[0]
+        args = values_of(q, kind), s.keys(), s.values()
+        whole = ask(w, q, t, heads, window=window)
+        bd.poll_status()
+        compare(whole, *args, causal(n, t, window), d ** -0.5, kind)
+        got = ask(w, q, t, heads, table=table, window=window)
+        with pytest.raises(bd.BdError) as e:
+            bd.poll_status()
+        assert e.value.status == 10
+        compare(got, *args, causal(n, t, window) & ~gone, d ** -0.5, kind)
+        if loud:
+            with pytest.raises(AssertionError):                     # the missing tokens would show
+                compare(whole, *args, causal(n, t, window) & ~gone, d ** -0.5, kind)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("way", WAYS)
+def test_a_sequence_without_any_good_page_gives_zeros(kind, way):
+    w, q, t, heads = world(way, kind, seed=62)
+    o, lse = ask(w, q, t, heads, table=torch.full_like(w.table, w.cache.pages))
+    with pytest.raises(bd.BdError) as e:
+        bd.poll_status()
+    assert e.value.status == 10 and (o == 0).all() and (lse == -np.inf).all()
