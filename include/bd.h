@@ -375,7 +375,8 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
  * row's window are not looked at (such pages may have been given away).  Query head h reads KV head
  * h / (q_heads / kv_heads).  Q has the cache's type, BD_BF16 or BD_F16 (fp32 caches: BD_ERR_UNSUPPORTED); O is BD_F32 or
  * that type.  Unlike bd_kvcache_attention, which follows the paper's scope "all", queries and probabilities stay
- * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  lse (optional, fp32 [rows][q_heads]) receives
+ * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  After BD_ERR_TIMEOUT (from
+ * bd_poll_status) some of the call's rows were left unwritten; those written are right.  lse (optional, fp32 [rows][q_heads]) receives
  * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result does not
  * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.  |scale| is
  * below 1e30; softcap is 0 (none) or between 1e-6 and 1e30.  The workspace belongs to one call at a time: calls (or captured
@@ -468,7 +469,7 @@ bd_status bd_poll_status(void *stream);
  * return).  poll_limit > 0 replaces the built-in limit (about a second) on the current device, rounded
  * up to 1024 polls; skip_first_code_stage != 0 makes the tensor-core product leave out the first copy
  * of packed weights of every CTA, so that the wait for it runs out: the call then writes no result and
- * bd_poll_status returns BD_ERR_TIMEOUT.  (0, 0) restores normal operation.  Synchronises the device. */
+ * bd_poll_status returns BD_ERR_TIMEOUT; in bd_paged_attention a wait of the first CTA runs out.  (0, 0) restores normal operation.  Synchronises the device. */
 bd_status bd_debug_fault(uint32_t poll_limit, int skip_first_code_stage);
 
 bd_status bd_set_gemm_impl(bd_gemm_impl impl);

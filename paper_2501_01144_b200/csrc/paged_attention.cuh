@@ -549,6 +549,28 @@ __device__ __forceinline__ void store_rows(const Attention &p, const RowWork<DT,
         }
 }
 
+// Waits for a record.  (The loop that polls is not inlined: it would cost the callers registers.)
+__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, volatile uint32_t *flags) { return tc::mbar_wait_warp(bar, parity, flags); }
+__device__ __forceinline__ bool wait_record(uint32_t bar, uint32_t parity, volatile uint32_t *flags) {
+    return __all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity)) || wait_longer(bar, parity, flags);
+}
+// A warp's wait ran out (status word).  Copies that may be in flight arrive first (a stage without one costs the limit); then its run's parts,
+// and those of all the runs it would still take, get a negative sum, by which the join kernel knows that they were not written.
+// (Not inlined: it would cost the main loop registers.)
+__device__ __noinline__ void drain_stages(uint32_t bar0, uint32_t phase) {
+    for (int st = 0; st < kRowStages; st++) tc::mbar_drain(bar0 + 8 * st, phase >> st & 1u);
+}
+template <int NB, int NT>
+__device__ __noinline__ void give_up(float *part, uint32_t count, uint32_t run, uint32_t turn, volatile uint32_t *flags, uint32_t bar0, uint32_t phase, int lane) {
+    drain_stages(bar0, phase);
+    while (run < count) {
+        for (int i = lane; i < 16 * NT; i += 32) part[(int64_t)(2 * run + i % 2) * part_floats<NB, NT>() + NT * NB * 2 * 128 + 2 * (i / 2) + 1] = -1.0f;
+        run = turn * gridDim.x + blockIdx.x;
+        if (lane == 0) turn = atomicAdd((uint32_t *)&flags[3], 1u);
+        turn = __shfl_sync(0xffffffffu, turn, 0);
+    }
+}
+
 template <int DT, int NB, int NT, bool CAP>
 __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(const __grid_constant__ Attention p) {
     using S = RowSmem<NB, NT>;
@@ -563,7 +585,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
     }
     const uint32_t bar0 = tc::smem_u32(smem + S::bars) + warp * kRowStages * 8;
     if (lane == 0)
-        for (int i = 0; i < kRowStages; i++) tc::mbar_init(bar0 + 8 * i, 1);
+        for (int i = 0; i < kRowStages; i++) tc::mbar_init(bar0 + 8 * i, i + warp + blockIdx.x == 0 && g_debug_skip_first_code_stage ? 2 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     pdl_wait();
@@ -663,9 +685,11 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
         }
         const int st = unit % kRowStages;
         if (loaded >> st & 1u) {
-            if (!tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags)) return;   // (status word; this warp's later results stay unwritten)
+            if (!wait_record(bar0 + 8 * st, phase >> st & 1u, flags)) {
+                give_up<NB, NT>(p.part, runs.count, run, turn, flags, bar0, phase, lane);
+                return;
+            }
             phase ^= 1u << st;
-            __syncwarp();
             work.chunk(p, ring + st * S::stage, smem + S::table, at, c, lane);
         }
         __syncwarp();                                             // every lane is done with the stage
@@ -714,7 +738,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
     }
     const uint32_t bar0 = tc::smem_u32(smem + S::bars) + warp * kRowStages * 8;
     if (lane == 0)
-        for (int i = 0; i < kRowStages; i++) tc::mbar_init(bar0 + 8 * i, 1);
+        for (int i = 0; i < kRowStages; i++) tc::mbar_init(bar0 + 8 * i, i + warp + blockIdx.x + blockIdx.y == 0 && g_debug_skip_first_code_stage ? 2 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     pdl_wait();
@@ -748,14 +772,14 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(c
     for (int i = 0; i < kRowStages && i < n; i++) fetch(i);
     RowWork<DT, NB, NT, CAP> work;
     work.begin(p, s, h, (uint4 *)(ring + S::queries), lane);
-    bool alive = true;
     for (int i = 0; i < n; i++) {
         const int st = i % kRowStages;
         if (loaded >> st & 1u) {
-            alive = tc::mbar_wait(bar0 + 8 * st, phase >> st & 1u, flags);
-            if (!alive) break;
+            if (!wait_record(bar0 + 8 * st, phase >> st & 1u, flags)) {
+                drain_stages(bar0, phase);
+                break;
+            }
             phase ^= 1u << st;
-            __syncwarp();
             work.chunk(p, ring + st * S::stage, smem + S::table, seq, v.begin + warp + i * warps, lane);
         }
         __syncwarp();
@@ -822,11 +846,16 @@ __global__ void __launch_bounds__(64 * NB * NT) attention_rows_join_kernel(const
         auto load = [&](int k) { return active && k < n ? *(const float4 *)(part_of(base + k) + (piece * 32 + lane) * 4) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
 #pragma unroll
         for (int k = 0; k < kAhead; k++) ahead[k] = load(k);
+        bool missing = false;
         for (int i = threadIdx.x; i < n * ROWS; i += THREADS) {
             const int r = i % ROWS;
-            if (r < n_rows) ml[i / ROWS][r] = *(const float2 *)(part_of(base + i / ROWS) + NT * NB * 2 * 128 + 2 * r);
+            if (r < n_rows) {
+                const float2 x = *(const float2 *)(part_of(base + i / ROWS) + NT * NB * 2 * 128 + 2 * r);
+                ml[i / ROWS][r] = x;
+                missing |= x.y < 0.0f;
+            }
         }
-        __syncthreads();
+        if (__syncthreads_or(missing)) return;                    // a warp gave up: the head's rows stay unwritten
         for (int r = piece; r < n_rows; r += THREADS / 32) {      // a warp per row
             const float2 a = lane < n ? ml[lane][r] : make_float2(-INFINITY, 0.0f), c = lane + 32 < n ? ml[lane + 32][r] : make_float2(-INFINITY, 0.0f);
             const float old = base == w0 ? -INFINITY : top[r];
@@ -900,7 +929,12 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const __grid_consta
     const int64_t row = s.q0 + i, step = (int64_t)p.batch.rows * p.q_heads * (D + 2);
     const float *src = p.part + (row * p.q_heads + head) * (D + 2);
     float m = -INFINITY;
-    for (int k = 0; k < p.splits; k++) m = fmaxf(m, src[k * step + D]);
+    bool missing = false;
+    for (int k = 0; k < p.splits; k++) {
+        m = fmaxf(m, src[k * step + D]);
+        missing |= src[k * step + D + 1] < 0.0f;
+    }
+    if (missing) return;                                          // a CTA gave up (status word): the row stays unwritten
     const float base = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, o[D / 32] = {};
     for (int k = 0; k < p.splits; k++) {

@@ -18,7 +18,8 @@
 // has in shared memory, and one thread copies the tiles with bulk copies: the softmax then has the SM's issue slots for itself.
 // 4096 new of 16384 tokens, 32 / 8 heads x 128: 812 us = 1185 TFLOP/s.  The tensor pipe and the exponential unit would each need
 // 2048 cycles per pair of tiles; a pair takes 3500, the softmax of one tile about 1700 of them and then a wait for its products.
-// All waits are bounded; a wait that runs out raises the abort word, every role drains and nothing is written.
+// All waits are bounded; a wait that runs out raises the abort word, every role waits for what it has in flight, and the CTA's rows
+// that are not finished stay unwritten (of a shared tile all rows: the join kernel is told).
 #pragma once
 #include <type_traits>
 
@@ -196,14 +197,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         abort_flag[2] = g_debug_spin_limit ? g_debug_spin_limit : tc::kSpinLimit;
         abort_flag[4] = 0;                                        // the final wait's own words
         abort_flag[5] = 1;
-        abort_flag[6] = abort_flag[2];
+        abort_flag[6] = tc::kSpinLimit;
         tc::mbar_init(q_full, 8);
         tc::mbar_init(drained, 1);
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(s_full + 8 * i, 1);
             tc::mbar_init(p_full + 8 * i, 4);
             tc::mbar_init(p_half + 8 * i, 4);
-            tc::mbar_init(k_full + 8 * i, IMAGES ? 1 : 4);
+            tc::mbar_init(k_full + 8 * i, (IMAGES ? 1 : 4) + (i + blockIdx.x == 0 && g_debug_skip_first_code_stage ? 1 : 0));
             tc::mbar_init(k_empty + 8 * i, 1);
             tc::mbar_init(v_full + 8 * i, IMAGES ? 1 : 4);
             tc::mbar_init(v_empty + 8 * i, 1);
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             float m = -INFINITY, l = 0.0f;
             bool alive = true;
             for (int j = 0; j < n_tiles && alive; j++) {
-                alive = tc::mbar_wait(s_full + 8 * wg, j & 1, abort_flag, 0);
+                alive = tc::mbar_wait_warp(s_full + 8 * wg, j & 1, abort_flag, 0);
                 if (!alive) break;
                 tc::tcgen05_fence_after();
                 if (CAP) {
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                 l += l0 + l1;
             }
             // ---- the tile's result ----
-            if (n_tiles > 0 && alive) alive = tc::mbar_wait(s_full + 8 * wg, n_tiles & 1, abort_flag);
+            if (n_tiles > 0 && alive) alive = tc::mbar_wait_warp(s_full + 8 * wg, n_tiles & 1, abort_flag);
             tc::tcgen05_fence_after();
             if (alive) {
                 const int64_t out_row = s.q0 + p.token(r);
@@ -451,6 +452,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                     if (p.splits > 1) { part[D] = m; part[D + 1] = l; }
                     else if (p.lse) p.lse[out_row * p.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
                 }
+            } else if (p.splits > 1 && r < row_end) {
+                p.part[(((int64_t)split * p.batch.rows + s.q0 + p.token(r)) * p.q_heads + h * p.group + (r - p.token(r) * p.group)) * (D + 2) + D + 1] = -1.0f;
             }
         }
     } else if (wg == 2) {
@@ -463,6 +466,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             if (e == 0 && lane == 0) {
                 const uint8_t *src = p.images + image_index(p, seq, h, t_begin) * (2 * S::kv_tile);
                 const uint32_t *ok = p.image_ok + image_index(p, seq, h, t_begin);
+                int keys = 0, values = 0;                         // copies begun
                 for (int j = 0; j < n_tiles && alive; j++, src += 2 * S::kv_tile) {
                     const int st = j & 1;
                     const uint32_t parity = (uint32_t)(j >> 1 & 1) ^ 1u;
@@ -472,11 +476,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                     chunk_ok[j & 7] = there;
                     tc::mbar_expect_tx(k_full + 8 * st, S::kv_tile);
                     tc::bulk_load(base + S::k + st * S::kv_tile, src, S::kv_tile, k_full + 8 * st);
+                    keys++;
                     alive = tc::mbar_wait(v_empty + 8 * st, parity, abort_flag);
                     if (!alive) break;
                     tc::mbar_expect_tx(v_full + 8 * st, S::kv_tile);
                     tc::bulk_load(base + S::v + st * S::kv_tile, src + S::kv_tile, S::kv_tile, v_full + 8 * st);
+                    values++;
                 }
+                // the last copies into each stage have arrived before the CTA ends, also when nobody takes them any more
+                for (int j = max(0, keys - 2); j < keys; j++) tc::mbar_drain(k_full + 8 * (j & 1), j >> 1 & 1);
+                for (int j = max(0, values - 2); j < values; j++) tc::mbar_drain(v_full + 8 * (j & 1), j >> 1 & 1);
             }
             __syncwarp();
         } else {
@@ -507,7 +516,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             const int c = 4 * (t_begin + j) + e;
             const bool stored = c < full && off >= 0;
             if (stored) load_lane<NB>(p.pool, off, true, lane, vx);
-            alive = tc::mbar_wait(k_empty + 8 * st, parity, abort_flag);
+            alive = tc::mbar_wait_warp(k_empty + 8 * st, parity, abort_flag);
             if (!alive) break;
             if (off >= 0) expand_lane<DT, NB>(table, kx, false, sm + S::k + st * S::kv_tile, e, lane);
             // tile j + 8 reuses this flag: eight tiles on, every reader of tile j is done (two tiles in shared memory, one in S)
@@ -521,7 +530,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
             const int64_t next = place(j + 1, page_ahead);
             page_ahead = look_up(j + 2);
             if (next >= 0) load_lane<NB>(p.pool, next, false, lane, kx);
-            alive = tc::mbar_wait(v_empty + 8 * st, parity, abort_flag);
+            alive = tc::mbar_wait_warp(v_empty + 8 * st, parity, abort_flag);
             if (!alive) break;
             uint8_t *vt = sm + S::v + st * S::kv_tile;
             if (stored) {

@@ -11,7 +11,8 @@ namespace bd {
 // Device status word, read and cleared by bd_poll_status (bits: kStatusNonfinite, kStatusTimeout, kStatusIndex).
 __device__ uint32_t g_status_word = 0;
 // Test hooks (bd_debug_fault): a lower poll limit for the bounded waits (0 = the built-in one) and "the code
-// producer of the tensor-core product leaves out its very first stage", which makes a wait run out on purpose.
+// producer of the tensor-core product leaves out its very first stage", which makes a wait run out on purpose (the paged
+// attention kernels: a barrier of the first CTA expects one arrival more than it gets).
 __device__ uint32_t g_debug_spin_limit = 0;
 __device__ uint32_t g_debug_skip_first_code_stage = 0;
 
@@ -70,6 +71,15 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     atomicOr(&g_status_word, kStatusTimeout);
     return false;
+}
+// mbar_wait by a whole warp, with one answer for all its lanes (some may see the phase complete as the others give up).
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t sleep_ns = 32) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, sleep_ns));
+}
+// After a wait ran out: waits for a copy of the caller's own that may still be in flight, whatever the abort word says, since
+// its shared memory must not be used again, or go back with the CTA, under it.  Bounded too (some 16 ms).
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+    for (uint32_t spin = 0; spin < 1u << 18 && !mbar_try_wait(bar, parity); spin++) __nanosleep(32);
 }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile(
