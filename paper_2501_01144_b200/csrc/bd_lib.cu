@@ -1510,6 +1510,7 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     a.lse = lse;
     a.part = (float *)workspace;
     a.scale = scale;
+    a.score = scale * 8388608.0f * 1.4426950408889634f;
     if (softcap > 0.0f) { a.cap = softcap * 1.4426950408889634f; a.cap_inv = 1.0f / a.cap; }
     a.q_heads = (int)q_heads; a.group = (int)(q_heads / c->kv_heads); a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
     a.odtype = (int)odtype;

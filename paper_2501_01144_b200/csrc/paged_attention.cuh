@@ -41,6 +41,7 @@ struct Attention {
     float *part;                      // partial results: of the warps' runs (rows kernel; see Runs), or of the splits
                                       // [splits][rows][q_heads][d + 2] (chunk kernel): output, maximum (log2 units), sum
     float scale;
+    float score;                      // rows kernel: scale * log2 e * 2^23, from block sums to scores in units of log2 e
     float cap, cap_inv;               // the cap in units of log2 e, and its reciprocal
     int q_heads, group, window, splits, row_tiles, odtype;
     bool whole;                       // rows kernel: a CTA per head (workers: its warps)
@@ -131,14 +132,14 @@ __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-// a = the capped a * mul_a, b likewise.
-__device__ __forceinline__ void cap_pair(float &a, float &b, float mul_a, float mul_b, float inverse, float cap) {
-    unpair(mul_pair(mul_pair(pair_of(a, b), pair_of(mul_a, mul_b)), pair_of(inverse)), a, b);
+__device__ __forceinline__ uint64_t cap_pair(uint64_t y, float inverse, float cap) {
+    float a, b;
+    unpair(mul_pair(y, pair_of(inverse)), a, b);
     const uint64_t x = pair_of(cap_range(a), cap_range(b)), u = mul_pair(x, x);
     const uint64_t n = fma_pair(fma_pair(fma_pair(u, pair_of(kCapP3), pair_of(kCapP2)), u, pair_of(kCapP1)), u, pair_of(1.0f));
     const uint64_t d = fma_pair(fma_pair(fma_pair(fma_pair(u, pair_of(kCapQ4), pair_of(kCapQ3)), u, pair_of(kCapQ2)), u, pair_of(kCapQ1)), u, pair_of(1.0f));
     unpair(d, a, b);
-    unpair(mul_pair(mul_pair(x, n), mul_pair(pair_of(cap), pair_of(reciprocal(a), reciprocal(b)))), a, b);
+    return mul_pair(mul_pair(x, n), mul_pair(pair_of(cap), pair_of(reciprocal(a), reciprocal(b))));
 }
 
 // One row's result: 2^23 is what the half-unit subnormals left out (2^-24 per code, 0.5 per half unit).
@@ -241,7 +242,7 @@ template <int DT, int NB, int NT, bool CAP>
 struct RowWork {
     static constexpr int D = 32 * NB;
     uint4 *qf;                                                    // queries: fragments of the 8-column operand in fp16, [NT][NB][32 lanes] (shared memory)
-    float mul[NT][2];                                             // column's factor from block sums to scores
+    float mul[NT][2];                                             // bf16: the power of two that the column's query was divided by
     int pos[NT][2];
     float O[NT][NB][2][4], m_run[NT][2], l_run[NT][2];
     Sequence s;
@@ -273,7 +274,7 @@ struct RowWork {
                 m = max(m & 0x7fffu, m >> 16 & 0x7fffu);
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                const int ex = min(max((int)(m >> 7), 27), 240);      // biased exponent of the row's largest element
+                const int ex = min(max((int)(m >> 7), 27), 254);      // biased exponent of the row's largest element
                 const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - ex) << 23);
                 qs = __uint_as_float((uint32_t)(ex - 14) << 23);
 #pragma unroll
@@ -290,8 +291,7 @@ struct RowWork {
             }
 #pragma unroll
             for (int i = 0; i < 2; i++) {                     // this lane's columns 2 t4 + i of the score fragments
-                const float f = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
-                mul[nt][i] = f * 8388608.0f * p.scale * 1.4426950408889634f;
+                mul[nt][i] = __shfl_sync(0xffffffffu, qs, 4 * (2 * t4 + i));
                 const int rc = 8 * nt + 2 * t4 + i;
                 pos[nt][i] = rc < n_rows ? first_pos + p.token(rc) : -1;
                 m_run[nt][i] = -INFINITY;
@@ -369,9 +369,12 @@ struct RowWork {
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) x[nt][j][i] = CAP ? sc[nt][j / 2][2 * (j % 2) + i] : sc[nt][j / 2][2 * (j % 2) + i] * mul[nt][i];
-                if (CAP) cap_pair(x[nt][j][0], x[nt][j][1], mul[nt][0], mul[nt][1], p.cap_inv, p.cap);
+                // (the power first: with the scale's factors it could pass the range of fp32, where the score does not)
+                uint64_t y = pair_of(sc[nt][j / 2][2 * (j % 2)], sc[nt][j / 2][2 * (j % 2) + 1]);
+                if (DT == BD_BF16) y = mul_pair(y, pair_of(mul[nt][0], mul[nt][1]));
+                y = mul_pair(y, pair_of(p.score));
+                if (CAP) y = cap_pair(y, p.cap_inv, p.cap);
+                unpair(y, x[nt][j][0], x[nt][j][1]);
             }
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)

@@ -314,8 +314,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                         tc::tcgen05_wait_ld();
 #pragma unroll
                         for (int n = 0; n < 32; n += 2) {
-                            float a = __uint_as_float(z[n]), b = __uint_as_float(z[n + 1]);
-                            cap_pair(a, b, mul, mul, p.cap_inv, p.cap);
+                            float a, b;
+                            unpair(cap_pair(mul_pair(pair_of(__uint_as_float(z[n]), __uint_as_float(z[n + 1])), pair_of(mul)), p.cap_inv, p.cap), a, b);
                             z[n] = __float_as_uint(a);
                             z[n + 1] = __float_as_uint(b);
                         }

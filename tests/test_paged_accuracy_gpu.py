@@ -159,3 +159,18 @@ def test_a_sequence_without_any_good_page_gives_zeros(kind, way):
     with pytest.raises(bd.BdError) as e:
         bd.poll_status()
     assert e.value.status == 10 and (o == 0).all() and (lse == -np.inf).all()
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("power", [-100, 90, 116, 119])
+def test_queries_of_any_finite_size_give_what_their_scores_say(way, power):
+    """bf16 queries from 2^-100 to about 2^121, the scale making ordinary scores of them."""
+    kind = torch.bfloat16
+    w, q, t, heads = world(way, kind, seed=71)
+    q = bits_of(np.ldexp(values_of(q, kind), power), kind)
+    scale = w.d ** -0.5 * 2.0 ** -power
+    s = w.seqs[0]
+    for cap in (0.0, 20.0):
+        got = ask(w, q, t, heads, scale=scale, softcap=cap)
+        bd.poll_status()
+        compare(got, values_of(q, kind), s.keys(), s.values(), causal(s.length, t), scale, kind, cap)
