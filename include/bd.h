@@ -381,8 +381,9 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
  * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.  |scale| is
  * below 1e30; softcap is 0 (none) or between 1e-6 and 1e30.  The workspace belongs to one call at a time: calls (or captured
  * graphs) that may overlap need one each.  The size asked for serves every window.
- * Accuracy: products exact, fp32 sums; capped scores within 2^-20 of their value, whatever the cap; probabilities rounded to 11 bits, or to the cache's type (bf16: 8 bits) in calls of
- * more than 16 rows (tokens of a sequence times query heads per KV head). */
+ * Accuracy: products exact, fp32 sums; capped scores within 2^-20 of their value, whatever the cap; probabilities rounded to
+ * 11 bits (those below 2^-21 of the row's largest to a multiple of 2^-31 of it), or on bf16 caches to 8 bits in calls of
+ * more than 16 rows (tokens of a sequence times query heads per KV head), while the sum they are divided by adds them unrounded. */
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes);
 bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, const void *Q, int64_t q_heads, int64_t ldq,
                              int64_t head_stride_q, float scale, float softcap, int64_t window, void *O, bd_dtype odtype,

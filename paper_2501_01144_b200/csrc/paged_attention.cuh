@@ -16,8 +16,8 @@
 // expanded twice.  A code becomes the fp16 number index-value * 2^-24 (a subnormal: the half-unit integer itself in the
 // low byte, the sign on top) without any conversion; the block's power-of-two scale multiplies the fp32 block sum.  bf16
 // queries are first scaled per row by a power of two into the range of fp16 (exact down to 2^-29 of the row's largest
-// element).  Probabilities are rounded to fp16 (2^-11) for the second product, and their fp32 values are what the row sum
-// adds; the unfinished chunk's values meet probabilities split in two bf16 parts (bf16 caches) or the same fp16 ones.
+// element).  Probabilities are rounded to fp16 (2^-11, and an absolute 2^-32 of the row's largest) for the second product, and their
+// fp32 values are what the row sum adds; the unfinished chunk's values meet probabilities split in two bf16 parts (bf16 caches) or the same fp16 ones.
 // What bounds it: the integer (ALU) pipe, which takes two cycles per warp instruction.  A code word costs ten of them, a
 // block two; the left shift of a block's scale goes to the multiply-add pipe.  64 sequences of 6000 to 12000 tokens, 8 KV heads
 // x 128: 207 us = 3.2 TB/s, that pipe 70 % busy, 922 warp instructions per chunk; the copies alone run at 5.5 TB/s (120 us).
@@ -56,6 +56,7 @@ struct Attention {
 };
 
 constexpr int kRowStages = 2;
+constexpr float kPeak = 7.0f;         // log2 of a row's largest probability as it goes into fp16
 constexpr int kRunUnits = 8;          // units that make a further round of runs worth its joins
 __host__ __device__ constexpr int row_warps(int nt) { return nt == 1 ? 16 : 12; }    // warps of a CTA = of an SM, by registers
 
@@ -360,8 +361,9 @@ struct RowWork {
         // ---- softmax: rows of the fragment are tokens (row 8 j + g = token 8 (g / 2) + 2 j + g % 2), columns queries ----
         const int tok0 = c * kChunk + 8 * (g / 2) + g % 2;
         const bool masked = (c + 1) * kChunk > first_pos + 1 || (p.window && c * kChunk <= last_pos - p.window);
-        // The running maximum (the same in the eight lanes of a column) moves only when a score exceeds it by more than 2^8:
-        // probabilities up to 2^8 do no harm in fp16 with fp32 sums, and without a move no lane needs another's scores.
+        // m_run, the same in the eight lanes of a column, is kPeak below the running maximum and moves only when a score exceeds it
+        // by kPeak + 8: probabilities are up to 2^15 (fp16 ends at 2^16, sums are fp32), so that fp16's subnormals begin at 2^-21 of the
+        // row's largest and lose 2^-32 of it; without a move no lane needs another's scores.
         uint32_t pf[NT][4];
         bool grew = false;
         float x[NT][4][2], top[NT][2], pv[NT][4][2];
@@ -389,14 +391,14 @@ struct RowWork {
                     }
                 }
                 top[nt][i] = fmaxf(fmaxf(x[nt][0][i], x[nt][1][i]), fmaxf(x[nt][2][i], x[nt][3][i]));
-                grew |= top[nt][i] > m_run[nt][i] + 8.0f;
+                grew |= top[nt][i] > m_run[nt][i] + (kPeak + 8.0f);
             }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    float m = fmaxf(top[nt][i], m_run[nt][i]);
+                    float m = fmaxf(top[nt][i] - kPeak, m_run[nt][i]);
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -453,8 +455,10 @@ struct RowWork {
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    const float a = pv[nt][j][0], b = pv[nt][j][1];
-                    if (DT == BD_BF16) {
+                    float a = pv[nt][j][0], b = pv[nt][j][1];
+                    if (DT == BD_BF16) {                          // (in the units of O: bf16's values may be as large as fp32's)
+                        a *= 1.0f / 8388608.0f;
+                        b *= 1.0f / 8388608.0f;
                         const uint32_t hi = pack_bf16(a, b);
                         pf[nt][j] = transpose8x8(hi);
                         lo[nt][j] = transpose8x8(pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u)));
@@ -481,18 +485,19 @@ struct RowWork {
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                     for (int x = 0; x < 2; x++) {
-                        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                         if (DT == BD_BF16) {
+                            float (&acc)[4] = O[nt][b][x];
                             mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
                             mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
                             mma_bf16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], lo[nt][0], lo[nt][1]);
                             mma_bf16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], lo[nt][2], lo[nt][3]);
                         } else {
-                            mma_f16(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
+                            float acc[4];
+                            mma_f16_zero(acc, a[2 * x][0], a[2 * x + 1][0], a[2 * x][1], a[2 * x + 1][1], pf[nt][0], pf[nt][1]);
                             mma_f16(acc, a[2 * x][2], a[2 * x + 1][2], a[2 * x][3], a[2 * x + 1][3], pf[nt][2], pf[nt][3]);
-                        }
 #pragma unroll
-                        for (int y = 0; y < 4; y++) O[nt][b][x][y] = fmaf(acc[y], 1.0f / 8388608.0f, O[nt][b][x][y]);
+                            for (int y = 0; y < 4; y++) O[nt][b][x][y] = fmaf(acc[y], 1.0f / 8388608.0f, O[nt][b][x][y]);
+                        }
                     }
             }
         }

@@ -8,7 +8,7 @@
 // Warps: two groups of four run the softmax of a tile each (thread = row, so no exchange between threads), four expand
 // the cache, one issues the MMAs: while one tile's softmax runs, the tensor pipe works on the other tile.  The output
 // stays in tensor memory and is rescaled only when a row's maximum has grown by more than 2^8 since the last time
-// (probabilities up to 2^8 do no harm in 16 bits with fp32 sums).
+// (probabilities up to 2^8, 2^15 in fp16, do no harm in 16 bits with fp32 sums).
 // Expansion: a thread owns a block (row of a key or value tile).  Its dialect's eight magnitudes as 16-bit floats of
 // the block's scale are two eight-byte tables, low and high bytes, read from shared memory with the scale added to the
 // exponent bits; a code word becomes eight values with byte permutes alone.  Keys keep the record's row order in the
@@ -267,6 +267,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
     const uint32_t tmem = *words;
     // tensor memory: S_0, S_1 at columns 0, 128 (P over their first halves), O_0, O_1 at 256, 384
     constexpr uint32_t kFmt = DT == BD_BF16 ? 1u : 0u;
+    // what the reference of a row's exponentials lies below its maximum when it moves: fp16 subnormals then lose 2^-32 of the row's largest
+    // probability (see RowWork::chunk); bf16 has fp32's exponents
+    constexpr float kAbove = DT == BD_BF16 ? 0.0f : kPeak;
 
     if (wg < 2) {
         if (IMAGES) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -370,10 +373,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
                     for (int n = 1; n < 32; n++) top[c] = fmaxf(top[c], __uint_as_float(x[c][n]));
                 }
                 const float m_new = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;       // (k > 0: a scale of zero counts as 1e-37)
-                const bool grew = m_new > m + 8.0f;               // m = -inf: the first visible token; m_new = -inf: none
+                const bool grew = m_new > m + (kAbove + 8.0f);    // m = -inf: the first visible token; m_new = -inf: none
                 if (__any_sync(0xffffffffu, grew)) {
-                    const float alpha = grew ? fast_exp2(m - m_new) : 1.0f;
-                    if (grew) m = m_new;
+                    const float alpha = grew ? fast_exp2(m - (m_new - kAbove)) : 1.0f;
+                    if (grew) m = m_new - kAbove;
                     l *= alpha;
                     if (j > 0) {                                  // S(j) complete implies that the products up to j - 1 are
 #pragma unroll 1

@@ -50,7 +50,8 @@ def compare(got, q, k, v, see, scale, kind, softcap=0.0):
     # more than 16 rows per KV head: probabilities in the cache's type, values of fp16 caches in fp16 (half of its smallest step)
     wide = group * t > 16
     p_half_step = 2.0 ** -8 if wide and kind == torch.bfloat16 else F16_HALF_STEP
-    p_floor = 0.0 if wide and kind == torch.bfloat16 else 2.0 ** -25
+    # fp16 probabilities: half of the smallest step, 2^-25, and the largest of a row is at least 2^7 in the kernels' units
+    p_floor = 0.0 if wide and kind == torch.bfloat16 else 2.0 ** -32
     v_floor = 2.0 ** -25 if wide and kind == torch.float16 else 0.0
     for h in range(heads):
         kh, vh = k[h // group], v[h // group]
@@ -174,3 +175,26 @@ def test_queries_of_any_finite_size_give_what_their_scores_say(way, power):
         got = ask(w, q, t, heads, scale=scale, softcap=cap)
         bd.poll_status()
         compare(got, values_of(q, kind), s.keys(), s.values(), causal(s.length, t), scale, kind, cap)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("first", [True, False])
+def test_a_long_flat_tail_beside_a_dominant_token_keeps_its_weight(kind, way, first):
+    """One token with a score of about 17 and a value of zero, all others with a score of 0 (2^-24.5 of its weight) and values
+    of about 1: the result is the tail's alone."""
+    d, heads, kv_heads, n, t = WAYS[way]
+    rng = np.random.default_rng(80)
+    w = World(1, kv_heads, d, 32, kind, seed=81, max_tokens=n)
+    common = rng.choice([-1.0, 1.0], d)
+    k, v = np.zeros((n, kv_heads, d)), 1.0 + 0.2 * rng.random((n, kv_heads, d))
+    top = 3 if first else n - t - 1
+    k[top], v[top] = 17.0 / d ** 0.5 * common, 0.0
+    k, v = bits_of(k, kind), bits_of(v, kind)
+    w.seqs[0].append(k, v)
+    bd.paged_append(w.cache, w.batch([n]), to_device(k, kind), to_device(v, kind))
+    q = bits_of(np.broadcast_to(common, (t, heads, d)), kind)
+    got = ask(w, q, t, heads)
+    bd.poll_status()
+    s = w.seqs[0]
+    compare(got, values_of(q, kind), s.keys(), s.values(), causal(n, t), d ** -0.5, kind)
