@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
         }
         if (wg < n_q) {
             const int pos = r < n_rows ? s.kv - s.t + p.token(r) : -1;
-            const float mul = fmaxf(fabsf(p.scale), 1e-37f) * 1.4426950408889634f;
+            const float mul = fmaxf(fabsf(p.scale), 1.4e-45f) * 1.4426950408889634f;     // (the smallest number for zero: masked scores stay -inf)
             const uint32_t t_s = tmem + 128u * wg + ((uint32_t)(32 * quad) << 16), t_o = tmem + 256u + 128u * wg + ((uint32_t)(32 * quad) << 16);
             // positions of the warp's 32 rows: the tiles that need a mask
             const int w_first = s.kv - s.t + p.token(r0 + 128 * wg + 32 * quad);
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attention_chunk_kernel(const
 #pragma unroll
                     for (int n = 1; n < 32; n++) top[c] = fmaxf(top[c], __uint_as_float(x[c][n]));
                 }
-                const float m_new = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;       // (k > 0: a scale of zero counts as 1e-37)
+                const float m_new = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;       // (k > 0)
                 const bool grew = m_new > m + (kAbove + 8.0f);    // m = -inf: the first visible token; m_new = -inf: none
                 if (__any_sync(0xffffffffu, grew)) {
                     const float alpha = grew ? fast_exp2(m - (m_new - kAbove)) : 1.0f;

@@ -198,3 +198,23 @@ def test_a_long_flat_tail_beside_a_dominant_token_keeps_its_weight(kind, way, fi
     bd.poll_status()
     s = w.seqs[0]
     compare(got, values_of(q, kind), s.keys(), s.values(), causal(n, t), d ** -0.5, kind)
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -122, -(2.0 ** -122), 2.0 ** -126])
+def test_scales_at_the_bottom_of_the_range(way, scale):
+    """Queries and keys of about 2^58 each, so that scales below 1e-36 matter; a scale of zero weighs all tokens alike."""
+    kind = torch.bfloat16
+    d, heads, kv_heads, n, t = WAYS[way]
+    rng = np.random.default_rng(90)
+    w = World(1, kv_heads, d, 32, kind, seed=91, max_tokens=n)
+    k, v = source_rows(rng, n, kv_heads, d, torch.float32)
+    k, v = bits_of(np.ldexp(k, 58), kind), bits_of(v, kind)
+    w.seqs[0].append(k, v)
+    bd.paged_append(w.cache, w.batch([n]), to_device(k, kind), to_device(v, kind))
+    q = bits_of(np.ldexp(rng.standard_normal((t, heads, d)), 58), kind)
+    s = w.seqs[0]
+    for cap in (0.0, 3.0):
+        got = ask(w, q, t, heads, scale=scale, softcap=cap)
+        bd.poll_status()
+        compare(got, values_of(q, kind), s.keys(), s.values(), causal(n, t), scale, kind, cap)
