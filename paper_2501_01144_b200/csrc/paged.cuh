@@ -19,12 +19,6 @@ __device__ __forceinline__ float load_one(const void *p) {
     if (DT == BD_BF16) return __uint_as_float((uint32_t) * (const uint16_t *)p << 16);
     return __half2float(*(const __half *)p);
 }
-template <int DT>
-__device__ __forceinline__ void store_one(void *p, float v) {
-    if (DT == BD_F32) *(float *)p = v;
-    else if (DT == BD_BF16) *(__nv_bfloat16 *)p = __float2bfloat16_rn(v);
-    else *(__half *)p = __float2half_rn(v);
-}
 // A block in a thread's registers as the quantizers take it, and its quantisation into the record's words.
 template <int DT>
 struct Block {

@@ -56,7 +56,6 @@ struct Sequence {
 };
 
 BD_HD int64_t record_bytes(int d) { return 35 * (int64_t)d; }
-BD_HD int64_t key_codes(int) { return 0; }
 BD_HD int64_t value_codes(int d) { return 16 * (int64_t)d; }
 BD_HD int64_t key_scales(int d) { return 32 * (int64_t)d; }
 BD_HD int64_t value_scales(int d) { return 33 * (int64_t)d; }
