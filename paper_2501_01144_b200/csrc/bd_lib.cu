@@ -400,7 +400,7 @@ bd_status check_paged(const bd_paged_cache *c, const bd_paged_batch *b) {
     if (!aligned16(c->pool) || !aligned16(c->tail)) return BD_ERR_ALIGN;
     if (!b || !b->page_table || !b->slot || !b->kv_len || !b->q_start) return BD_ERR_INVALID_ARG;
     if (b->n <= 0 || b->rows < 0 || b->max_q < 0 || b->max_kv < 0 || b->ld_table <= 0) return BD_ERR_INVALID_ARG;
-    if (b->n > 65535 || b->rows > INT32_MAX || b->max_kv > INT32_MAX - pg::kChunk) return BD_ERR_UNSUPPORTED;
+    if (b->n > 65535 || b->rows > INT32_MAX || b->max_kv > INT32_MAX - 8 * pg::kTileTokens) return BD_ERR_UNSUPPORTED;   // (tiles ahead of the last are numbered too)
     if (b->n * c->kv_heads > INT32_MAX / (b->max_kv / pg::kChunk + 1)) return BD_ERR_UNSUPPORTED;   // chunks are numbered in 32 bits
     if (b->max_q > b->rows || b->max_kv > b->ld_table * c->page_tokens) return BD_ERR_SHAPE;
     if (((uintptr_t)b->page_table | (uintptr_t)b->slot | (uintptr_t)b->kv_len | (uintptr_t)b->q_start) & 3u) return BD_ERR_ALIGN;
@@ -1492,8 +1492,9 @@ bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, c
     if (q_heads <= 0 || window < 0 || !(scale > -1e30f && scale < 1e30f) || !(softcap == 0.0f || (softcap >= 1e-6f && softcap <= 1e30f))) return BD_ERR_INVALID_ARG;
     if (odtype != BD_F32 && odtype != BD_BF16 && odtype != BD_F16) return BD_ERR_INVALID_ARG;
     if (q_heads % c->kv_heads) return BD_ERR_SHAPE;
-    if ((b->max_q * (q_heads / c->kv_heads) / 256 + 1) * b->n > INT32_MAX / (148 * c->kv_heads)) return BD_ERR_UNSUPPORTED;   // CTAs of a launch
     if (c->dtype == BD_F32 || (odtype != BD_F32 && odtype != c->dtype) || q_heads > 65535) return BD_ERR_UNSUPPORTED;
+    if (b->max_q * (q_heads / c->kv_heads) > INT32_MAX - 512) return BD_ERR_UNSUPPORTED;              // a sequence's rows are numbered in 32 bits
+    if ((b->max_q * (q_heads / c->kv_heads) / 256 + 1) * b->n > INT32_MAX / (148 * c->kv_heads)) return BD_ERR_UNSUPPORTED;   // CTAs of a launch
     if ((s = check_rows(Q, b->rows, q_heads, c->head_dim, ldq, head_stride_q, 2))) return s;
     if ((s = check_rows(O, b->rows, q_heads, c->head_dim, ldo, head_stride_o, elem_bytes(odtype)))) return s;
     if ((uintptr_t)lse & 3u) return BD_ERR_ALIGN;

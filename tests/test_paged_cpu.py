@@ -164,6 +164,16 @@ def test_bad_attention_calls_are_refused(kw, status):
                                   a["ldo"], 128, a["lse"], a["ws"], a["wbytes"], None) == status
 
 
+@pytest.mark.parametrize("b,q_heads", [
+    (dict(rows=2 ** 31 - 1, max_q=2 ** 31 - 1), 1), (dict(rows=2 ** 30, max_q=2 ** 30), 2), (dict(rows=2 ** 30, max_q=2 ** 30), 2 ** 62),
+    (dict(max_kv=2 ** 31 - 40, ld_table=2 ** 26), 1)])
+def test_sizes_that_pass_32_bits_are_refused(b, q_heads):
+    lib = bd.load()
+    cc, bb = cache(kv_heads=1), batch(n=1, **b)
+    assert lib.bd_paged_attention(ctypes.byref(cc), ctypes.byref(bb), 0x8000, q_heads, 128 * q_heads if q_heads < 2 ** 40 else 128, 128, 0.1, 0.0, 0, 0x9000, bd.BF16,
+                                  128 * q_heads if q_heads < 2 ** 40 else 128, 128, None, None, 0, None) == 4
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(rot=24), 2), (dict(rot=0), 2), (dict(rot=144), 2), (dict(head_dim=96), 2), (dict(dtype=7), 1), (dict(positions=0), 1), (dict(eps=-1.0), 1),
     (dict(eps=float("nan")), 1), (dict(pos=0), 1), (dict(table=0), 1), (dict(table=0x2004), 3), (dict(heads=0), 1), (dict(x=0x8004), 3), (dict(ldx=128), 2), (dict(w=0x7004), 3),
