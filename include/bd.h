@@ -361,6 +361,8 @@ typedef struct {
 bd_status bd_paged_sizes(const bd_paged_cache *c, size_t *pool_bytes, size_t *tail_bytes);
 /* Stores the step's keys and values: row r, head h at K + r * ldk + h * head_stride_k elements (pointers and strides
  * 16-byte aligned), V alike.  Keys are quantised at once; values when their chunk is full, then once and for all.
+ * Both have to be finite: an Inf or NaN is told (BD_ERR_NONFINITE from bd_poll_status) with the step that brings it, and rows of
+ * attention that share a chunk with it may be NaN whether they see it or not.
  * The calls that touch one sequence (its pages, its slot) have to be ordered; a batch names a sequence once. */
 bd_status bd_paged_append(const bd_paged_cache *c, const bd_paged_batch *b, const void *K, const void *V, int64_t ldk,
                           int64_t head_stride_k, int64_t ldv, int64_t head_stride_v, void *stream);

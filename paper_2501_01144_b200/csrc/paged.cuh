@@ -19,6 +19,13 @@ __device__ __forceinline__ float load_one(const void *p) {
     if (DT == BD_BF16) return __uint_as_float((uint32_t) * (const uint16_t *)p << 16);
     return __half2float(*(const __half *)p);
 }
+// Whether a 32-bit word of elements holds an infinity or a NaN.
+template <int DT>
+__device__ __forceinline__ bool nonfinite(uint32_t w) {
+    if (DT == BD_F32) return (w & 0x7f800000u) == 0x7f800000u;
+    const uint32_t ones = DT == BD_BF16 ? 0x7f80u : 0x7c00u;
+    return (w & ones) == ones || (w >> 16 & ones) == ones;
+}
 // A block in a thread's registers as the quantizers take it, and its quantisation into the record's words.
 template <int DT>
 struct Block {
@@ -170,11 +177,15 @@ __global__ void __launch_bounds__(NB * 32) append_kernel(Pool pool, Batch batch,
     if (blockIdx.x == 0) {
         // (the waiting rows are in shared memory of every thread's copy: it waited, and met the others, above)
         const int from = max(p0, p1 / kChunk * kChunk - kChunk);
+        bool bad = false;
         for (int i = threadIdx.x; i < (p1 - from) * kPieces; i += NB * 32) {
             const int row = from + i / kPieces, piece = i % kPieces;
             const uint8_t *src = V + ((int64_t)(s.q0 + row - p0) * ldv + (int64_t)h * hsv) * EB;
-            *((uint4 *)(tail + tail_offset(pool, slot, h, row) * EB) + piece) = *((const uint4 *)src + piece);
+            const uint4 x = *((const uint4 *)src + piece);
+            *((uint4 *)(tail + tail_offset(pool, slot, h, row) * EB) + piece) = x;
+            bad |= nonfinite<DT>(x.x) || nonfinite<DT>(x.y) || nonfinite<DT>(x.z) || nonfinite<DT>(x.w);
         }
+        if (bad) atomicOr(&g_status_word, kStatusNonfinite);      // (told with the step, not when the chunk is full)
     }
 }
 

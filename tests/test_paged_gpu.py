@@ -161,6 +161,27 @@ def test_nonfinite_keys_are_reported():
     bd.poll_status()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_nonfinite_values_are_reported_with_the_step_that_brings_them(kind, d, value):
+    """Also while their chunk is unfinished and no quantizer has met them; the largest finite value is none of them."""
+    w = World(2, 2, d, 32, kind, seed=48, max_tokens=64)
+    w.step([30, 3])
+    for row, head, ch in ((0, 0, 0), (0, 1, d - 1), (1, 0, 7), (2, 1, 33)):
+        k, v = (torch.zeros(3, 2, d, dtype=kind, device="cuda") for _ in range(2))
+        v[:] = torch.finfo(kind).max
+        b = bd.PagedBatch(w.table, w.slots, i32([31, 5]), i32([0, 1, 3]), 2)
+        bd.paged_append(w.cache, b, k, v)
+        bd.poll_status()
+        v[row, head, ch] = value
+        bd.paged_append(w.cache, b, k, v)
+        with pytest.raises(bd.BdError) as e:
+            bd.poll_status()
+        assert e.value.status == 6
+        bd.poll_status()
+
+
 # ---- attention ------------------------------------------------------------------------------------------------------
 
 
