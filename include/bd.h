@@ -379,13 +379,18 @@ bd_status bd_paged_read(const bd_paged_cache *c, const bd_paged_batch *b, void *
  * that type.  Unlike bd_kvcache_attention, which follows the paper's scope "all", queries and probabilities stay
  * in 16 bits here and only the cache is in 4.  A row that sees nothing gives zeros.  After BD_ERR_TIMEOUT (from
  * bd_poll_status) some of the call's rows were left unwritten; those written are right.  lse (optional, fp32 [rows][q_heads]) receives
- * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result does not
- * depend on the other sequences of the batch beyond how the launch is split, and is the same in every run.  |scale| is
- * below 1e30; softcap is 0 (none) or between 1e-6 and 1e30.  The workspace belongs to one call at a time: calls (or captured
- * graphs) that may overlap need one each.  The size asked for serves every window.
+ * the natural logarithm of the row's sum of exponentials (-inf for a row that sees nothing).  The result is the same in every
+ * run.  The batch decides by its bounds (n, rows, max_q, max_kv, not by the numbers on the device) which kernel serves all of its
+ * sequences and how the work is split: a sequence gives the same bits in every batch of the same bounds and lengths, and may
+ * differ by the roundings below between others.  |scale| is below 1e30; softcap is 0 (none) or between 1e-6 and 1e30.  The
+ * workspace belongs to one call at a time: calls (or captured graphs) that may overlap need one each.  The size asked for serves
+ * every window; it grows with max_kv (up to about 1 GiB for long chunks at head_dim 128, whose cache is expanded in it), so max_kv
+ * is better near the longest sequence than at the table's width.
  * Accuracy: products exact, fp32 sums; capped scores within 2^-20 of their value, whatever the cap; probabilities rounded to
  * 11 bits (those below 2^-21 of the row's largest to a multiple of 2^-31 of it), or on bf16 caches to 8 bits in calls of
- * more than 16 rows (tokens of a sequence times query heads per KV head), while the sum they are divided by adds them unrounded. */
+ * more than 16 rows (max_q times query heads per KV head), while the sum they are divided by adds them unrounded.  Such calls also
+ * hold the cache's values in its type: fp16 rounds what lies below its normal range, bf16 magnitudes below 2^-123 count as zeros.
+ * bf16 queries lose bits that lie more than 2^-29 below the row's largest in calls of at most 16 rows. */
 bd_status bd_paged_attention_workspace_size(const bd_paged_cache *c, const bd_paged_batch *b, int64_t q_heads, size_t *bytes);
 bd_status bd_paged_attention(const bd_paged_cache *c, const bd_paged_batch *b, const void *Q, int64_t q_heads, int64_t ldq,
                              int64_t head_stride_q, float scale, float softcap, int64_t window, void *O, bd_dtype odtype,

@@ -645,7 +645,7 @@ class PagedKVCache(_Described):
 class PagedBatch(_Described):
     """One step's sequences (int32 CUDA tensors): page_table [n, width], slots [n], kv_len [n] (this step's tokens
     included), q_start [n + 1]; their contents may change between calls (and replays).  max_q: host bound of the rows of one sequence; max_kv: of its tokens (default: what
-    the page table can hold)."""
+    the page table can hold, which plans a call and sizes its workspace for tables that full: give it where the table is wider)."""
 
     _members = ("page_table", "slots", "kv_len", "q_start", "max_q", "max_kv")
 
