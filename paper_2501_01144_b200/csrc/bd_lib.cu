@@ -442,8 +442,8 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
         const int64_t ctas = std::max<int64_t>(1, b->n * c->kv_heads * r.tiles);
         const int64_t seen = window ? std::min(b->max_kv, window + b->max_q + pg::kTileTokens) : b->max_kv, tiles = std::max<int64_t>(1, (seen + pg::kTileTokens - 1) / pg::kTileTokens);
         // CTAs that share a tile's tokens, where the batch alone does not fill the SMs: the time of a CTA's tiles (2.6 us each at
-        // d = 128, 1.65 at 64) against the join's (12 us and its traffic).  Measured, 32 / 8 heads x 128, alone against split:
-        // 32 new of 1024 tokens 23.4 / 22.3 us (2), 256 of 1024 28.5 / 33.5 (2), 256 of 4096 83.5 / 44.9 (4), 32 of 16384 268 / 38 (18).
+        // d = 128, 1.65 at 64) against the join's (12 us and its traffic).  Measured, 32 / 8 heads x 128, alone against split, us a call:
+        // 32 new of 1024 tokens 22.2 / 20.3 (8), 256 of 1024 26.9 / 33.0 (2), 256 of 4096 74.3 / 43.4 (4), 32 of 16384 229 / 38 (16).
         double best = 0;
         for (int64_t k = 1; k <= std::max<int64_t>(1, std::min<int64_t>(148 / ctas, tiles)); k++) {
             const double join = k > 1 ? 12.0 + 2.0 * (double)k * (double)b->rows * (double)q_heads * (double)(c->head_dim + 2) * 4.0 / 4e6 : 0.0;
@@ -451,9 +451,10 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
             if (k == 1 || us < best) { best = us; r.splits = (int)k; }
         }
         if (window) r.splits = std::min(r.splits, attention_plan(c, b, q_heads, 0).splits);       // the workspace is asked for without a window
-        // Tiles expanded once in front pay when many CTAs read each: 32 / 8 heads x 128, expanded by every CTA against in front:
-        // 4096 new of 16384 tokens 932 / 811 us, 1024 of 16384 268 / 253, 512 of 16384 162 / 169, 2048 of 8192 244 / 230, 1024 of 8192 141 / 134,
-        // 512 of 8192 96 / 101, 1024 of 4096 78 / 83; 2 x 2048 of 4096 237 / 240.  d = 64 (half the expansion per exponential): never better.
+        // Tiles expanded once in front pay when many CTAs read each: 32 / 8 heads x 128, expanded by every CTA against in front, us a call:
+        // 4096 new of 16384 tokens 978 / 876, 1024 of 16384 288 / 264, 512 of 16384 169 / 168, 2048 of 8192 260 / 239, 1024 of 8192 142 / 139,
+        // 512 of 8192 96 / 102, 1024 of 4096 76 / 81; 2 x 2048 of 4096 258 / 239, which the bound on tokens gives away.  d = 64 (half the
+        // expansion per exponential): 83 / 121 on six ragged chunks.
         const size_t images = (size_t)b->n * (size_t)c->kv_heads * (size_t)((b->max_kv + pg::kTileTokens - 1) / pg::kTileTokens) * (size_t)(2 * 128 * c->head_dim * 2);
         if (c->head_dim == 128 && r.tiles >= 16 && seen >= 6144 && b->max_kv >= 2 * b->max_q && images <= ((size_t)1 << 30)) r.images = images;
         return r;
@@ -462,8 +463,8 @@ AttentionPlan attention_plan(const bd_paged_cache *c, const bd_paged_batch *b, i
     const int warps = pg::row_warps(r.wide ? 2 : 1);
     const int64_t units = b->n * c->kv_heads * std::max<int64_t>(1, (b->max_kv + pg::kChunk - 1) / pg::kChunk);
     // A CTA per head and no join where that is about one wave of short heads: measured at 32 / 8 heads x 128, 1 token, whole
-    // against runs: 1 sequence of 512 tokens 8.6 / 10.1 us, of 2048 17.7 / 14.2; 16 of 1024 12.4 / 19.8; 64 of 256 17.3 / 19.9,
-    // of 512 33.8 / 23.7.  4 tokens (16 rows): 8 of 512 12.1 / 13.9, 1 of 1024 16.2 / 14.2, 64 of 256 35.7 / 29.0.
+    // against runs, us a call: 1 sequence of 512 tokens 7.8 / 9.7, of 513 9.4 / 11.3, of 2048 16.1 / 13.8; 16 of 1024 11.5 / 17.7; 64 of 256
+    // 15.1 / 17.3, of 512 33.3 / 25.2.  4 tokens (16 rows): 8 of 512 11.3 / 13.4, 1 of 1024 14.3 / 13.7, 64 of 256 31.3 / 29.6.
     const int64_t seen = window ? std::min(b->max_kv, window + b->max_q + pg::kChunk) : b->max_kv;   // tokens from the first visible chunk on
     const int64_t chunks = std::max<int64_t>(1, (seen + pg::kChunk - 1) / pg::kChunk);
     const int head_warps = chunks <= 4 ? 4 : chunks <= 8 ? 8 : warps;

@@ -80,8 +80,9 @@ struct Block<BD_BF16> {                                           // two element
 // and of the one before it.
 // A record's part that is new as a whole is assembled in shared memory and leaves as 16-byte pieces; the keys of a partly new
 // chunk go out as the few words that are theirs, since their neighbours belong to other steps.
-// Bound: 2 * 2 d bytes read and 35 / 32 d written per token and head for 16-bit sources; in practice instruction issue, as in the
-// operand quantizer.  7346 bf16 tokens x 8 heads x 128: 13.1 us = 2.9 TB/s; one token of 64 sequences: 3.5 us.
+// Bound: 2 * 2 d bytes read and 35 / 32 d written per token and head for 16-bit sources.  7346 bf16 tokens x 8 heads x 128: 14.0 us =
+// 2.7 TB/s; 58 % of the issue slots while SMs are active, the warps waiting for each other at the chunk's barriers and for shared-memory
+// instructions (a value block is 32 two-byte reads).  One token of 64 sequences: 3.4 us.
 // ---------------------------------------------------------------------------
 template <int DT, int NB>
 __global__ void __launch_bounds__(NB * 32) append_kernel(Pool pool, Batch batch, const uint8_t *__restrict__ K,
@@ -254,7 +255,7 @@ __device__ __forceinline__ void word_values(uint32_t w, uint32_t tlo, uint32_t t
 // a token's result; the value words of a warp are eight tokens of a channel each, which stmatrix turns around on the way to
 // shared memory (pieces exchanged within a row so that its eight rows meet different banks), from where whole tokens leave.
 // fp32 (read_f32_kernel): the record comes to shared memory, values are multiplied out element by element.
-// The tokens of an unfinished chunk come from the tail.  7346 bf16 tokens x 8 heads x 128: 10.3 us, of which writing 30 MB is
+// The tokens of an unfinished chunk come from the tail.  7346 bf16 tokens x 8 heads x 128: 10.2 us, of which writing 30 MB is
 // the larger part (a fill reaches 3.9 TB/s here).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int turned_piece(int token, int piece) { return piece ^ ((token >> 3) << 1 | (token & 1)); }
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(NB * 32) read_f32_kernel(Pool pool, Batch batc
 // D / 8 lanes hold a head, eight elements each as two groups of four: of the rotated part elements 4 l .. and rot / 2 + 4 l ..
 // (pairs that are half the part apart meet in one lane, no exchange), else eight neighbours.  A group of lanes does up to
 // five heads of its row, all loads in front, with the row's cosines and sines in registers.
-// Bound: bytes (every element read and written once).  8192 rows x 40 heads x 128 bf16: 33 us = 5.2 TB/s; 64 rows: 2.1 us.
+// Bound: bytes (every element read and written once).  8192 rows x 40 heads x 128 bf16: 33 us = 5.3 TB/s; 64 rows: 1.9 us.
 // ---------------------------------------------------------------------------
 template <int DT>
 struct Quad { typedef uint2 Type; };                              // four elements

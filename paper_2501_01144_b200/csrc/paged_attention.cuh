@@ -20,7 +20,7 @@
 // fp32 values are what the row sum adds; the unfinished chunk's values meet probabilities split in two bf16 parts (bf16 caches) or the same fp16 ones.
 // What bounds it: the integer (ALU) pipe, which takes two cycles per warp instruction.  A code word costs ten of them, a
 // block two; the left shift of a block's scale goes to the multiply-add pipe.  64 sequences of 6000 to 12000 tokens, 8 KV heads
-// x 128: 207 us = 3.2 TB/s, that pipe 70 % busy, 922 warp instructions per chunk; the copies alone run at 5.5 TB/s (120 us).
+// x 128: 211 us = 3.2 TB/s, that pipe 69 % busy, 924 warp instructions per chunk; the copies alone run at 5.5 TB/s (120 us).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_rows_kernel(c
 }
 
 // Short contexts: a CTA takes a whole head, its warps the head's chunks in turn, and the warps' parts meet in shared memory,
-// so that the call is one launch (one sequence of 513 tokens: 10.6 us against 15.2 through runs and the join kernel).
+// so that the call is one launch (one sequence of 513 tokens: 9.4 us a call against 11.3 through runs and the join kernel).
 template <int DT, int NB, int NT, bool CAP>
 __global__ void __launch_bounds__(32 * row_warps(NT), 1) attention_head_kernel(const __grid_constant__ Attention p) {
     using S = RowSmem<NB, NT>;

@@ -16,8 +16,9 @@
 // P is rounded to the cache's type (8 or 11 bits): the MMA takes both operands of one type.
 // When many CTAs read the same tokens (IMAGES), a kernel in front expands every tile once into the workspace, in the layout it
 // has in shared memory, and one thread copies the tiles with bulk copies: the softmax then has the SM's issue slots for itself.
-// 4096 new of 16384 tokens, 32 / 8 heads x 128: 812 us = 1185 TFLOP/s.  The tensor pipe and the exponential unit would each need
-// 2048 cycles per pair of tiles; a pair takes 3500, the softmax of one tile about 1700 of them and then a wait for its products.
+// 4096 new of 16384 tokens, 32 / 8 heads x 128: 880 us a call = 1090 TFLOP/s (817 back to back before the power cap lowers the clock, 866
+// after).  The tensor pipe and the exponential unit would each need 2048 cycles per pair of tiles; a pair takes about 3500, the softmax of
+// one tile about 1700 of them and then a wait for its products.
 // All waits are bounded; a wait that runs out raises the abort word, every role waits for what it has in flight, and the CTA's rows
 // that are not finished stay unwritten (of a shared tile all rows: the join kernel is told).
 #pragma once
