@@ -42,13 +42,13 @@ def ask(w, q_bits, t, heads, table=None, **kw):
     return o.double().cpu().numpy(), lse.double().cpu().numpy()
 
 
-def compare(got, q, k, v, see, scale, kind, softcap=0.0):
+def compare(got, q, k, v, see, scale, kind, softcap=0.0, wide=None):
     """got = (o, lse) against softmax(scores of q [t, heads, d] and k [kv_heads, n, d] where see [t, n]) v, all in fp64."""
     o, lse = got
     t, heads, d = q.shape
     group = heads // k.shape[0]
     # more than 16 rows per KV head: probabilities in the cache's type, values of fp16 caches in fp16 (half of its smallest step)
-    wide = group * t > 16
+    wide = group * t > 16 if wide is None else wide
     p_half_step = 2.0 ** -8 if wide and kind == torch.bfloat16 else F16_HALF_STEP
     # fp16 probabilities: half of the smallest step, 2^-25, and the largest of a row is at least 2^7 in the kernels' units
     p_floor = 0.0 if wide and kind == torch.bfloat16 else 2.0 ** -32
@@ -218,3 +218,97 @@ def test_scales_at_the_bottom_of_the_range(way, scale):
         got = ask(w, q, t, heads, scale=scale, softcap=cap)
         bd.poll_status()
         compare(got, values_of(q, kind), s.keys(), s.values(), causal(n, t), scale, kind, cap)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("way", WAYS)
+def test_captured_calls_follow_the_numbers_on_the_device(kind, way):
+    """A step captured with the bounds of its longest sequence, replayed with other lengths, row counts, pages and queries."""
+    d, heads, kv_heads, n, t = WAYS[way]
+    w, q0, _, _ = world(way, kind, seed=100)
+    s = w.seqs[0]
+    keys, values = s.keys(), s.values()
+    kv_len, start, table = i32([n]), i32([0, t]), w.table.clone()
+    b = bd.PagedBatch(table, w.slots, kv_len, start, t)
+    q, out, lse = to_device(q0, kind), torch.empty(t, heads, d, device="cuda"), torch.empty(t, heads, device="cuda")
+    workspace = torch.empty(max(256, bd.paged_attention_workspace_size(w.cache, b, t, heads)), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bd.paged_attention(w.cache, b, q, out=out, lse=lse, workspace=workspace)
+    order = torch.from_numpy(w.rng.permutation(w.cache.pages)).cuda()           # the same records in other pages
+    moved = torch.empty_like(w.cache.pool)
+    moved[order] = w.cache.pool
+    for length, rows, other in ((n, t, False), (n // 32 * 32, t, True), (n // 64 * 32, max(1, t // 2), True), (32, 1, False), (n, 1, True), (n // 32 * 32, 0, False), (n, t, False)):
+        bits = bits_of(w.rng.standard_normal((t, heads, d)), kind)
+        q.copy_(to_device(bits, kind))
+        kv_len.fill_(length)
+        start[1] = rows
+        table.copy_(order[w.table.long()].to(torch.int32) if other else w.table)
+        pool = w.cache.pool.clone()
+        if other:
+            w.cache.pool.copy_(moved)
+        workspace.fill_(255), out.fill_(-7), lse.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        bd.poll_status()
+        w.cache.pool.copy_(pool)
+        assert (out[rows:] == -7).all() and (lse[rows:] == -7).all()
+        if rows:
+            # (kernels and roundings go by the bounds)
+            compare((out[:rows].double().cpu().numpy(), lse[:rows].double().cpu().numpy()), values_of(bits, kind)[:rows], keys[:, :length], values_of_prefix(s, length, values),
+                    causal(length, rows), d ** -0.5, kind, wide=heads // kv_heads * t > 16)
+
+
+def values_of_prefix(s, length, values):
+    """The stored values of the first `length` tokens: a whole number of chunks, or all."""
+    assert length % 32 == 0 or length == s.length
+    return values[:, :length]
+
+
+def test_the_largest_batch():
+    """65535 sequences: grids at their limit, unit numbers found by scanning two thousand groups."""
+    n, d, heads, kind = 65535, 64, 4, torch.bfloat16
+    rng = np.random.default_rng(110)
+    cache = bd.PagedKVCache(2 * n, 1, d, n, 32, kind)
+    table = torch.randperm(2 * n, device="cuda").to(torch.int32).view(n, 2)
+    slots = torch.randperm(n, device="cuda").to(torch.int32)
+    length = torch.from_numpy(rng.integers(0, 65, n).astype(np.int32)).cuda()
+    start = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    start[1:] = length.cumsum(0)
+    total = int(start[-1])
+    k, v = (torch.randn(total, 1, d, device="cuda").to(kind) for _ in range(2))
+    whole = bd.PagedBatch(table, slots, length, start, 64)
+    bd.paged_append(cache, whole, k, v)
+    rk, rv = (x.double().cpu().numpy() for x in bd.paged_read(cache, whole, total))
+    for t in (1, 5):                                                # few rows; 20 rows: the tensor-core kernel, more tiles than a CTA orders
+        q = torch.randn(n * t, heads, d, device="cuda").to(kind)
+        lse = torch.empty(n * t, heads, device="cuda")
+        o = bd.paged_attention(cache, bd.PagedBatch(table, slots, length, torch.arange(0, n * t + 1, t, dtype=torch.int32, device="cuda"), t), q, dtype=torch.float32, lse=lse)
+        bd.poll_status()
+        for i in [0, 1, 31, 32, 33, 1023, 1024, 40000, n - 2, n - 1] + [int(x) for x in rng.integers(0, n, 200)]:
+            a, m = int(start[i]), int(length[i])
+            at = slice(i * t, i * t + t)
+            got = o[at].double().cpu().numpy(), lse[at].double().cpu().numpy()
+            compare(got, q[at].double().cpu().numpy(), rk[a:a + m].transpose(1, 0, 2), rv[a:a + m].transpose(1, 0, 2), causal(m, t), d ** -0.5, kind) if m else None
+            assert m or ((got[0] == 0).all() and (got[1] == -np.inf).all())
+        if t == 1:
+            workspace = bd.paged_attention_workspace_size(cache, bd.PagedBatch(table, slots, length, start, 1), n, heads)
+            assert workspace > 0
+
+
+def test_queries_that_do_not_fit_are_refused():
+    w = World(1, 2, 64, 32, torch.bfloat16, seed=120, max_tokens=64)
+    b = w.batch([1], kv_len=[1])
+    x = torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (x.half(), x.float(), x[:, :3], torch.zeros(1, 4, 128, dtype=torch.bfloat16, device="cuda"), x.cpu(), x[0], x[..., None],
+                torch.zeros(1, 64, 4, dtype=torch.bfloat16, device="cuda").transpose(1, 2), None):
+        with pytest.raises(ValueError):
+            bd.paged_attention(w.cache, b, bad)
+    for kw in (dict(out=x[:, :2]), dict(out=x.cpu()), dict(out=x.double()), dict(lse=torch.zeros(1, 2, device="cuda")), dict(lse=torch.zeros(1, 4)), dict(dtype=torch.float64),
+               dict(workspace=torch.zeros(8, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            bd.paged_attention(w.cache, b, x, **kw)
+    for kw in (dict(window=-1), dict(softcap=-1.0), dict(scale=float("nan")), dict(softcap=float("inf"))):
+        with pytest.raises(bd.BdError):
+            bd.paged_attention(w.cache, b, x, **kw)
+    bd.poll_status()
