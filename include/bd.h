@@ -413,6 +413,88 @@ bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd
                           const int32_t *position, const float *cos_sin, int64_t positions, int64_t rot, int interleaved,
                           float eps, void *stream);
 
+/* Routing to experts.  Of each token's logits x [experts] (fp32, bf16 or fp16; row t at logits + t * ld elements):
+ *   score  s = softmax(x) or 1 / (1 + exp(-x));  key = s + bias (fp32 [experts]); without a bias the order of the logits;
+ *   groups of experts / groups neighbours: a group's value is its largest key, or the sum of its two largest (group_top 1 or 2;
+ *          the keys are the scores here when there is no bias); the top_groups groups of largest value stay;
+ *   ids    the top_k largest keys that stay, in descending order; of equal keys (and values) the lower number first;
+ *   weights  scale * s, or with `renormalise` scale * s / (sum of the chosen s), rounded to fp32 once.
+ * Keys and values are compared as 64-bit numbers computed from the logits as they are.  An expert whose logit or key is -Inf is not there: never
+ * chosen; slots that find no expert get id -1 and weight 0.  A NaN counts as -Inf and a logit of +Inf as the largest fp32 number;
+ * both are told (BD_ERR_NONFINITE from bd_poll_status).  `valid` (device, optional): tokens from *valid on are padding and get ids -1, weights 0.
+ * ids and weights are [tokens][top_k].  experts <= 512, top_k <= 32 and <= experts, groups <= 32 and a divisor of experts.
+ *
+ * The plan (optional in bd_route) says where the rows of each expert lie: expert e has rows start[e] .. start[e] + count[e] - 1, in the order of
+ * its tokens; starts are multiples of 128 and follow one another, start[experts] is the end; place[t][j] is the row of token t's j-th
+ * expert, -1 where there is none.  All of it is int32 on the device; `scratch`: bd_expert_plan_scratch bytes, 16-byte aligned, of the call that
+ * makes the plan alone.  bd_make_expert_plan makes it for ids from elsewhere: negative ids are left out, ids of `experts` and more
+ * are left out and told (BD_ERR_INDEX), a token that names an expert twice has one row with it.
+ * At most 64 tokens: one launch, otherwise two. */
+typedef enum { BD_SCORE_SOFTMAX = 0, BD_SCORE_SIGMOID = 1 } bd_score;
+typedef struct {
+    bd_score score;
+    int64_t experts, top_k, groups, top_groups; /* groups 1, top_groups 1: no groups */
+    int group_top, renormalise;
+    float scale;
+} bd_route_rule;
+typedef struct {
+    int32_t *count, *start, *place; /* [experts], [experts + 1], [tokens][top_k] */
+    void *scratch;
+    int64_t tokens, top_k, experts;
+} bd_expert_plan;
+bd_status bd_expert_plan_scratch(int64_t tokens, int64_t experts, size_t *bytes);
+bd_status bd_route(const void *logits, bd_dtype dtype, int64_t tokens, int64_t ld, const float *bias, const bd_route_rule *rule,
+                   const int32_t *valid, int32_t *ids, float *weights, const bd_expert_plan *plan, void *stream);
+bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, void *stream);
+
+/* The weights of `experts` experts: the buffers of that many operands [rows, K] (bd_qtensor_sizes bytes each) one after the other,
+ * so that expert e's operand is a bd_qtensor on its part and bd_quantize_weights and the like work on it.
+ *
+ * The experts' gated feed-forward product of a mixture-of-experts block:
+ *     Y[t] = sum_j weights[t][j] * dq(D_e) q(act(dq(G_e) q(x_t)) * (dq(U_e) q(x_t))),   e = the j-th expert of token t,
+ * q = the online two-stage quantisation (Sec. 3.2; along K as everywhere, the fp32 result of the first product requantised in its
+ * epilogue as in bd_linear_requant), act = silu x / (1 + exp(-x)) or gelu in its tanh form.  up holds G and U, [2 * inter, K] per
+ * expert, their rows alternating in groups of 32: rows 64 i .. 64 i + 31 are gate rows 32 i .. 32 i + 31, the next 32 the up rows of
+ * the same numbers.  down is [N, inter].  K and inter are multiples of 32, N of 8; at most 512 experts.
+ * X [tokens, K] and its pitch, Y [tokens, N] (BD_F32 or BD_BF16) and its pitch are 16-byte aligned.  The plan is bd_route's or bd_make_expert_plan's;
+ * a token without experts gets zeros.  `inner` (optional, for checking; fp32 [tokens][top_k][inter]) receives the values q(...) that the second
+ * product read.  Four launches, of no fixed relation to the plan's numbers, which stay on the device: a call can be captured and replayed
+ * with other tokens and plans.  The result is the same in every run, and a token's does not depend on the other tokens of the call.
+ * Accuracy: the products as BD_GEMM_TCGEN05; act by fast exponentials and division, 2^-19 relative (gelu: of 1 + |x| where x is far below
+ * zero); each expert's part of the sum is rounded to bf16 before it is weighted when Y is BD_BF16, and not rounded for BD_F32.
+ * Device-side conditions (bd_poll_status): an Inf or NaN in X or before the second product (BD_ERR_NONFINITE); a plan whose numbers
+ * lie outside its bounds (BD_ERR_INDEX; nothing is addressed by them).  Workspace: 256-byte aligned, of one call at a time. */
+typedef struct {
+    void *codes, *ids, *scales;
+    int64_t experts, rows, K;
+} bd_experts;
+typedef enum { BD_ACT_SILU = 0, BD_ACT_GELU = 1 } bd_activation;
+bd_status bd_expert_mlp_workspace_size(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype, size_t *bytes);
+bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t ldx, const bd_expert_plan *plan, const float *weights,
+                        const bd_experts *up, const bd_experts *down, bd_activation act, void *Y, bd_dtype ydtype, int64_t ldy, float *inner,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* The norms around a block and the residual sum between them, in one pass over the rows:
+ *     u = norm(y) * (post_weight + weight_offset) + post_bias    (post_weight NULL: u = y)
+ *     h = residual + scale * gate * u                            (residual NULL: 0; gate NULL: 1)
+ *     n = norm(h) * (weight + weight_offset) + bias
+ * norm(x) = x / sqrt(mean(x^2) + eps), or with `layer` (x - mean(x)) / sqrt(var(x) + eps).  fp32 arithmetic; n comes from the unrounded h, and h
+ * and n are rounded to the rows' type once.  h NULL: not stored.  n goes to n [rows, dim], or with q to a quantised operand [rows, dim]
+ * (dim a multiple of 32; the bits that bd_quantize_act would make of the rounded n); with both NULL only h is made.
+ * All of one type (fp32, bf16, fp16); row r of an operand at its pointer + r * ld elements, weights and biases contiguous [dim].  gate: element
+ * (r, c) at gate + r * gate_row + c * gate_col, gate_col 0 or 1, gate_row any (0: one for all rows).  1 <= dim <= 16384, any alignment
+ * and pitch that the type allows (16-byte aligned ones are faster).  h and n may each be y's or residual's memory as a whole, in place. */
+typedef struct {
+    const void *y, *residual, *gate, *post_weight, *post_bias, *weight, *bias;
+    int64_t ldy, ld_residual, gate_row, gate_col;
+    float scale, eps, weight_offset;
+    int layer;
+    void *h, *n;
+    int64_t ldh, ldn;
+    const bd_qtensor *q;
+} bd_norm;
+bd_status bd_residual_norm(const bd_norm *a, bd_dtype dtype, int64_t rows, int64_t dim, void *stream);
+
 /* bd_linear for callers that can neither allocate device memory nor hand in a
  * workspace (the paper has no counterpart; this is a convenience of the library).
  * Think of code that runs where cudaMalloc is off limits: inside a region whose

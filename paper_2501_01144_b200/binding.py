@@ -1,4 +1,5 @@
 """ctypes binding of the C ABI in include/bd.h (same names without the bd_ prefix)."""
+import contextlib
 import ctypes
 import os
 import subprocess
@@ -8,6 +9,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libblockdialect.so")
 _PAGED_PATH = os.path.join(_HERE, "_paged.so")
+_BLOCK_PATH = os.path.join(_HERE, "_block.so")
 _SRC = os.path.join(_HERE, "csrc", "bd_lib.cu")
 
 F32, BF16, F16 = 0, 1, 2
@@ -19,6 +21,7 @@ _TORCH_DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 _lib = None
 _paged = None
+_block = None
 
 
 class BdError(RuntimeError):
@@ -63,31 +66,33 @@ def library_path():
 
 def build(verbose=False):
     """Compile the CUDA library in-tree for sm_100a."""
-    srcs = [os.path.join(_HERE, "csrc", f) for f in os.listdir(os.path.join(_HERE, "csrc")) if not f.endswith(".cpp")]
+    srcs = [os.path.join(_HERE, "csrc", f) for f in os.listdir(os.path.join(_HERE, "csrc")) if f.endswith((".cu", ".cuh"))]
     if os.path.exists(_LIB_PATH) and all(os.path.getmtime(_LIB_PATH) >= os.path.getmtime(s) for s in srcs):
-        _build_paged()
+        _build_bindings()
         return _LIB_PATH
     cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", "-o", _LIB_PATH, _SRC]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     subprocess.run(cmd, check=True)
-    _build_paged()
+    _build_bindings()
     return _LIB_PATH
 
 
-def _build_paged():
-    """Compile the native binding of the paged-cache calls (a CPython module beside the library, linked to it)."""
-    src, header = os.path.join(_HERE, "csrc", "paged_binding.cpp"), os.path.join(os.path.dirname(_HERE), "include", "bd.h")
-    if os.path.exists(_PAGED_PATH) and os.path.getmtime(_PAGED_PATH) >= max(os.path.getmtime(src), os.path.getmtime(header)):
-        return
-    import sysconfig
-    from torch.utils import cpp_extension
-    includes = cpp_extension.include_paths("cuda") + [sysconfig.get_paths()["include"]]
-    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", _PAGED_PATH, src]
-    cmd += [f"-I{i}" for i in includes] + [f"-L{_HERE}", "-l:libblockdialect.so", f"-L{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
-    subprocess.run(cmd, check=True)
+def _build_bindings():
+    """Compile the native bindings of the calls that a decode step makes per layer (CPython modules beside the library, linked to it)."""
+    csrc, header = os.path.join(_HERE, "csrc"), os.path.join(os.path.dirname(_HERE), "include", "bd.h")
+    for path, source in ((_PAGED_PATH, "paged_binding.cpp"), (_BLOCK_PATH, "block_binding.cpp")):
+        src = os.path.join(csrc, source)
+        if os.path.exists(path) and os.path.getmtime(path) >= max(os.path.getmtime(f) for f in (src, header, os.path.join(csrc, "binding_common.h"))):
+            continue
+        import sysconfig
+        from torch.utils import cpp_extension
+        includes = cpp_extension.include_paths("cuda") + [sysconfig.get_paths()["include"]]
+        libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+        cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-o", path, src]
+        cmd += [f"-I{i}" for i in includes] + [f"-L{_HERE}", "-l:libblockdialect.so", f"-L{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+        subprocess.run(cmd, check=True)
 
 
 def load():
@@ -157,20 +162,33 @@ def load():
     return lib
 
 
+def _load_module(path):
+    """A native binding module beside the library."""
+    load()
+    if not os.path.exists(path):
+        raise BdError(-1, f"{path} is missing: run __graft_entry__.build() first")
+    import importlib.util
+    spec = importlib.util.spec_from_file_location(os.path.basename(path)[:-3], path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.set_check(_check)
+    return module
+
+
 def _load_paged():
     """The native binding of the paged-cache calls (once)."""
     global _paged
     if _paged is None:
-        load()
-        if not os.path.exists(_PAGED_PATH):
-            raise BdError(-1, f"{_PAGED_PATH} is missing: run __graft_entry__.build() first")
-        import importlib.util
-        spec = importlib.util.spec_from_file_location("_paged", _PAGED_PATH)
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        module.set_check(_check)
-        _paged = module
+        _paged = _load_module(_PAGED_PATH)
     return _paged
+
+
+def _load_block():
+    """The native binding of the mixture-of-experts and norm calls (once)."""
+    global _block
+    if _block is None:
+        _block = _load_module(_BLOCK_PATH)
+    return _block
 
 
 def _check(status):
@@ -244,6 +262,13 @@ class QTensor:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_c", None)                      # a buffer or a shape changed: the descriptor is rebuilt
+
+    @classmethod
+    def from_buffers(cls, codes, ids, scales, rows, K):
+        """An operand over the caller's own buffers (the sizes that the library asks for)."""
+        q = cls.__new__(cls)
+        q.rows, q.K, q.codes, q.ids, q.scales = rows, K, codes, ids, scales
+        return q
 
     def c_struct(self):
         """The C descriptor (kept until a member changes: a decode step passes dozens of these per call)."""
@@ -684,6 +709,119 @@ def qk_norm_rope(q, k, positions, cos_sin, q_weight=None, k_weight=None, eps=1e-
     and keys [rows, kv_heads, head_dim] (k may be None) in one pass.  positions int32 [rows]; cos_sin fp32
     [positions, rot]: rot / 2 cosines, then rot / 2 sines.  The outputs may be the inputs."""
     return (_paged or _load_paged()).rope(q, k, positions, cos_sin, q_weight, k_weight, eps, interleaved, out_q, out_k, stream)
+
+
+class ExpertWeights(_Described):
+    """The DialectFP4 weights [rows, K] of several experts: uint8 tensors codes, ids, scales [experts, bytes of one operand]."""
+
+    _members = ("codes", "ids", "scales", "rows", "K")
+
+    def __init__(self, experts, rows, K, device="cuda"):
+        sizes = [ctypes.c_size_t() for _ in range(3)]
+        _check(load().bd_qtensor_sizes(rows, K, *[ctypes.byref(b) for b in sizes]))
+        self._set(*[torch.empty(experts, b.value, dtype=torch.uint8, device=device) for b in sizes], rows, K)
+
+    @classmethod
+    def from_buffers(cls, codes, ids, scales, rows, K):
+        """Weights over the caller's own buffers (contiguous, shapes as above)."""
+        return _describe(cls, codes, ids, scales, rows, K)
+
+    def _set(self, codes, ids, scales, rows, K):
+        self.__dict__.update(_c=(_block or _load_block()).experts(codes, ids, scales, rows, K), codes=codes, ids=ids, scales=scales, rows=rows, K=K)
+
+    experts = property(lambda self: self.codes.shape[0])
+
+    def expert(self, e):
+        """Expert e's operand, on its part of the buffers."""
+        return QTensor.from_buffers(self.codes[e], self.ids[e], self.scales[e], self.rows, self.K)
+
+
+def quantize_experts(W, select=SELECT_MSE, gated=False, out=None, stream=None):
+    """Offline quantisation of the experts' weights W [experts, N, K] along K.  gated: W is the first product's, N = 2 * inter with the gate
+    rows before the up rows; they are stored in turns of 32, as expert_mlp reads them (inter a multiple of 32)."""
+    if W.dim() != 3:
+        raise ValueError("W must be [experts, N, K]")
+    experts, N, K = W.shape
+    if gated and N % 64:
+        raise ValueError("gated weights have 2 * inter rows, inter a multiple of 32")
+    out = out or ExpertWeights(experts, N, K, W.device)
+    if (out.experts, out.rows, out.K) != (experts, N, K):
+        raise ValueError("out must have the shape of W")
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        for e in range(experts):
+            w = W[e].unflatten(0, (2, N // 64, 32)).transpose(0, 1).reshape(N, K) if gated else W[e]
+            quantize_weights(w, select, out=out.expert(e))
+    return out
+
+
+class ExpertPlan:
+    """Where the rows of each expert lie (int32 CUDA tensors): count [experts], start [experts + 1], place [tokens, top_k]."""
+
+    __slots__ = ("count", "start", "place", "_scratch")
+
+    def __init__(self, count, start, place, scratch):
+        self.count, self.start, self.place, self._scratch = count, start, place, scratch
+
+    def _tensors(self):
+        return self.count, self.start, self.place, self._scratch
+
+
+_SCORES = {"softmax": False, "sigmoid": True}
+_ACTIVATIONS = {"silu": False, "gelu": True}
+_NORMS = {"rms": False, "layer": True}
+
+
+def _choice(table, name, what):
+    try:
+        return table[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"{what} must be one of {', '.join(table)}") from None
+
+
+def route(logits, top_k, score="softmax", bias=None, groups=1, top_groups=1, group_top=2, renormalise=True, scale=1.0, valid=None, ids=None, weights=None, plan=True, stream=None):
+    """The experts of each token from router logits [tokens, experts], their weights, and the plan of the experts' rows: (ids int32
+    [tokens, top_k], weights fp32 [tokens, top_k], ExpertPlan).  score: "softmax" or "sigmoid"; bias: fp32 [experts], added to the scores for the
+    choice alone; groups > 1: only experts of the top_groups groups with the largest sums of their group_top best; renormalise: weights
+    that sum to `scale`.  valid: int32 on the device, the number of tokens that are no padding.  ids, weights, plan: buffers of an
+    earlier call to be written again; plan=False: none is made (and None returned)."""
+    given = plan._tensors() if isinstance(plan, ExpertPlan) else None
+    ids, weights, count, start, place, scratch = (_block or _load_block()).route(
+        logits, top_k, _choice(_SCORES, score, "score"), bias, groups, top_groups, group_top, renormalise, scale, valid, ids, weights, given, plan is not False, stream)
+    if given is None:
+        plan = None if plan is False else ExpertPlan(count, start, place, scratch)
+    return ids, weights, plan
+
+
+def expert_plan(ids, experts, out=None, stream=None):
+    """The plan for ids [tokens, top_k] (int32) that come from elsewhere; negative ids are left out."""
+    tensors = (_block or _load_block()).plan(ids, experts, out._tensors() if out is not None else None, stream)
+    return out if out is not None else ExpertPlan(*tensors)
+
+
+def expert_mlp_workspace_size(tokens, top_k, up, down, dtype=torch.bfloat16):
+    return (_block or _load_block()).mlp_workspace_size(tokens, top_k, up._c, down._c, dtype)
+
+
+def expert_mlp(x, plan, weights, up, down, activation="silu", out=None, dtype=torch.bfloat16, inner=None, workspace=None, stream=None):
+    """The gated feed-forward product of each token's experts, weighted and added up: Y [tokens, N] for x [tokens, K].  up: ExpertWeights of
+    2 * inter rows (quantize_experts with gated=True), down: of [N, inter].  activation: "silu" or "gelu" (tanh form).  weights fp32
+    [tokens, top_k] as route gives them.  inner: fp32 [tokens, top_k, inter] that receives the requantised values between the products."""
+    return (_block or _load_block()).mlp(x, plan.count, plan.start, plan.place, weights, up._c, down._c, _choice(_ACTIVATIONS, activation, "activation"), out, dtype, inner, workspace, stream)
+
+
+def residual_norm(y, weight, residual=None, bias=None, post_weight=None, post_bias=None, gate=None, scale=1.0, norm="rms", eps=1e-6, weight_offset=0.0, quantise=False, want_h=True, out_h=None,
+                  out_n=None, stream=None):
+    """(h, n): h = residual + scale * gate * u, u = y or norm(y) * (post_weight + weight_offset) + post_bias; n = norm(h) * (weight +
+    weight_offset) + bias, or with quantise a QTensor of it.  y, residual [rows, dim]; gate [rows or 1, dim or 1]; norm: "rms" or
+    "layer".  weight None: n is None; want_h False: h is not stored.  out_h, out_n may be y or residual."""
+    if quantise and out_n is None:
+        if y.dim() != 2:
+            raise ValueError("y must be [rows, dim]")
+        out_n = QTensor(*y.shape, y.device)
+    q = (out_n.codes, out_n.ids, out_n.scales) if quantise else None
+    h, n = (_block or _load_block()).norm(y, weight, residual, bias, post_weight, post_bias, gate, scale, _choice(_NORMS, norm, "norm"), eps, weight_offset, want_h, out_h, None if quantise else out_n, q,
+                                          stream)
+    return h, out_n if quantise else n
 
 
 NOALLOC_SCRATCH_BYTES = 32 << 20

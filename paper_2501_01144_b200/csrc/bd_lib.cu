@@ -13,10 +13,13 @@
 #include "blocksize.cuh"
 #include "kvcache.cuh"
 #include "attention.cuh"
+#include "experts.cuh"
+#include "norm.cuh"
 #include "paged.cuh"
 #include "paged_attention.cuh"
 #include "paged_chunk.cuh"
 #include "quantize.cuh"
+#include "route.cuh"
 
 using namespace bd;
 
@@ -575,6 +578,114 @@ void launch_read(const bd_paged_cache *c, const bd_paged_batch *b, dim3 grid, vo
     else if (c->dtype == BD_BF16) launch_serialized(pg::read_kernel<BD_BF16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
     else launch_serialized(pg::read_kernel<BD_F16, NB>, grid, 32 * NB, 0, st, p, q, k, v, ldk, ldv, hsk, hsv);
 }
+
+// ---- routing, experts, norms --------------------------------------------------------------------------------------------
+template <int NV, bool SIGMOID, bool WIDE>
+bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, unsigned blocks, cudaStream_t st) {
+    static bool configured[64] = {};                              // per instantiation and device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    constexpr size_t most = (size_t)rt::kWarps * (rt::kMaxExperts + 1) * sizeof(double);
+    if (WIDE && dev >= 0 && dev < 64 && !configured[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(rt::route_kernel<NV, SIGMOID, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+        if (e != cudaSuccess) return cuda_result(e);
+        configured[dev] = true;
+    }
+    const size_t smem = WIDE && r.groups > 1 ? (size_t)rt::kWarps * (r.experts + 1) * sizeof(double) : 0;
+    launch_serialized(rt::route_kernel<NV, SIGMOID, WIDE>, blocks, rt::kThreads, smem, st, r, plan);
+    return launch_result();
+}
+template <bool SIGMOID, bool WIDE>
+bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, unsigned blocks, cudaStream_t st) {
+    const int per_lane = (r.experts + 31) / 32;
+    if (per_lane <= 2) return launch_route<2, SIGMOID, WIDE>(r, plan, blocks, st);
+    if (per_lane <= 4) return launch_route<4, SIGMOID, WIDE>(r, plan, blocks, st);
+    if (per_lane <= 8) return launch_route<8, SIGMOID, WIDE>(r, plan, blocks, st);
+    return launch_route<16, SIGMOID, WIDE>(r, plan, blocks, st);
+}
+bd_status check_plan(const bd_expert_plan *p) {
+    if (!p || !p->count || !p->start || !p->place) return BD_ERR_INVALID_ARG;
+    if (p->tokens < 0 || p->top_k < 1 || p->experts < 1) return BD_ERR_INVALID_ARG;
+    if (p->experts > rt::kMaxExperts || p->top_k > rt::kMaxTopK || p->tokens > (1ll << 30) / p->top_k) return BD_ERR_UNSUPPORTED;
+    if (((uintptr_t)p->count | (uintptr_t)p->start | (uintptr_t)p->place) & 3u) return BD_ERR_ALIGN;
+    return BD_OK;
+}
+// Several blocks of tokens: the second launch, at most 256 CTAs.
+bd_status launch_places(const rt::Rule &r, const rt::Plan &plan, int64_t blocks, cudaStream_t st) {
+    const int per = (int)((blocks + 255) / 256);
+    launch_serialized(rt::plan_place_kernel, (unsigned)((blocks + per - 1) / per), rt::kThreads, 0, st, r, plan, (int)blocks, per);
+    return launch_result();
+}
+bd_status check_experts(const bd_experts *w) {
+    if (!w || !w->codes || !w->ids || !w->scales || w->experts <= 0 || w->rows <= 0 || w->K <= 0) return BD_ERR_INVALID_ARG;
+    if (w->K % kBlock) return BD_ERR_SHAPE;
+    if (w->experts > ex::kMaxExperts || w->rows >= (1ll << 31) || w->K >= (1ll << 31) || row_tiles(w->rows) * k_groups(w->K) * w->experts >= (1ll << 31)) return BD_ERR_UNSUPPORTED;
+    if (!aligned16(w->codes) || !aligned16(w->ids) || !aligned16(w->scales)) return BD_ERR_ALIGN;
+    return BD_OK;
+}
+// Parts of an expert call's workspace: the token operand (later the second product's result), its scales, the inner operand and its scales.
+struct ExpertSpace {
+    int64_t rows;
+    size_t x_scales, h, h_scales, total;
+};
+ExpertSpace expert_space(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype) {
+    ExpertSpace s;
+    s.rows = ex::padded_rows(tokens * top_k, up->experts);
+    const size_t x = (size_t)s.rows * (size_t)up->K, y = (size_t)s.rows * (size_t)down->rows * (size_t)elem_bytes(ydtype);
+    s.x_scales = align256(std::max(x, y));
+    s.h = s.x_scales + align256((size_t)(s.rows / kRowTile * k_groups(up->K)) * kScaleAtomBytes);
+    s.h_scales = s.h + align256((size_t)s.rows * (size_t)down->K);
+    s.total = s.h_scales + align256((size_t)(s.rows / kRowTile * k_groups(down->K)) * kScaleAtomBytes);
+    return s;
+}
+bd_status check_expert_pair(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype) {
+    bd_status s = check_experts(up);
+    if (s) return s;
+    if ((s = check_experts(down))) return s;
+    if (tokens < 0 || top_k < 1 || (ydtype != BD_F32 && ydtype != BD_BF16)) return BD_ERR_INVALID_ARG;
+    if (up->experts != down->experts || up->rows != 2 * down->K || down->rows % 8) return BD_ERR_SHAPE;
+    if (top_k > rt::kMaxTopK || tokens > (1ll << 30) / top_k) return BD_ERR_UNSUPPORTED;
+    const int64_t rows = ex::padded_rows(tokens * top_k, up->experts), pairs = (std::max(up->rows, down->rows) + 255) / 256;
+    if (rows / kRowTile * std::max(k_groups(up->K), k_groups(down->K)) >= (1ll << 31) || (rows / 256 + up->experts + 1) * pairs >= (1ll << 30) ||
+        tokens * k_groups(up->K) * kBlocksPerAtom >= (1ll << 31) - 32)
+        return BD_ERR_UNSUPPORTED;
+    return BD_OK;
+}
+template <int DT>
+void launch_spread(const void *X, int64_t ldx, const bd_expert_plan *plan, const bd_experts *up, const ExpertSpace &s, uint8_t *ws, cudaStream_t st) {
+    const int kgs = (int)k_groups(up->K);
+    const unsigned per_row = (unsigned)kgs * kBlocksPerAtom;
+    const unsigned grid = (unsigned)std::min<int64_t>((plan->tokens * per_row + 255) / 256, 148 * 8);
+    launch_serialized(ex::spread_kernel<DT>, grid, 256, 0, st, (const uint8_t *)X, ldx, (int)plan->tokens, (int)plan->top_k, plan->place, (int)(up->K / kBlock), kgs,
+                      (int)s.rows, ws, ws + s.x_scales, make_fast_div(per_row));
+}
+template <int DT, int VPT, bool QUANT, bool VEC>
+bd_status launch_norm(const nm::Args &a, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
+    if (QUANT) {
+        static bool configured[64] = {};
+        int dev = 0;
+        cudaGetDevice(&dev);
+        if (dev >= 0 && dev < 64 && !configured[dev]) {
+            cudaError_t e = cudaFuncSetAttribute(nm::residual_norm_kernel<DT, VPT, QUANT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, nm::kMaxDim * 4);
+            if (e != cudaSuccess) return cuda_result(e);
+            configured[dev] = true;
+        }
+    }
+    launch_serialized(nm::residual_norm_kernel<DT, VPT, QUANT, VEC>, grid, block, smem, st, a);
+    return launch_result();
+}
+template <int DT, int VPT>
+bd_status launch_norm(const nm::Args &a, bool quant, bool vec, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
+    if (quant) return vec ? launch_norm<DT, VPT, true, true>(a, grid, block, smem, st) : launch_norm<DT, VPT, true, false>(a, grid, block, smem, st);
+    return vec ? launch_norm<DT, VPT, false, true>(a, grid, block, smem, st) : launch_norm<DT, VPT, false, false>(a, grid, block, smem, st);
+}
+template <int DT>
+bd_status launch_norm(const nm::Args &a, int vpt, bool quant, bool vec, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
+    if (vpt == 1) return launch_norm<DT, 1>(a, quant, vec, grid, block, smem, st);
+    if (vpt == 2) return launch_norm<DT, 2>(a, quant, vec, grid, block, smem, st);
+    return launch_norm<DT, 4>(a, quant, vec, grid, block, smem, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1577,6 +1688,172 @@ bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd
         else launch_rotate<BD_F16, 64>(r, il, st);
     }
     return launch_result();
+}
+
+bd_status bd_expert_plan_scratch(int64_t tokens, int64_t experts, size_t *bytes) {
+    if (!bytes || tokens < 0 || experts < 1) return BD_ERR_INVALID_ARG;
+    if (experts > rt::kMaxExperts || tokens > (1ll << 30)) return BD_ERR_UNSUPPORTED;
+    *bytes = tokens > rt::kBlockTokens ? (size_t)(rt::blocks_of(tokens) * rt::count_pitch(experts)) : 0;
+    return BD_OK;
+}
+
+bd_status bd_route(const void *logits, bd_dtype dtype, int64_t tokens, int64_t ld, const float *bias, const bd_route_rule *rule,
+                   const int32_t *valid, int32_t *ids, float *weights, const bd_expert_plan *plan, void *stream) {
+    if (!rule || tokens < 0 || (tokens > 0 && (!logits || !ids || !weights))) return BD_ERR_INVALID_ARG;
+    if (dtype != BD_F32 && dtype != BD_BF16 && dtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if (rule->score != BD_SCORE_SOFTMAX && rule->score != BD_SCORE_SIGMOID) return BD_ERR_INVALID_ARG;
+    if (rule->experts < 1 || rule->top_k < 1 || rule->groups < 1 || rule->top_groups < 1 || (rule->group_top != 1 && rule->group_top != 2) ||
+        !(rule->scale > -INFINITY && rule->scale < INFINITY))
+        return BD_ERR_INVALID_ARG;
+    if (rule->top_k > rule->experts || rule->experts % rule->groups || rule->top_groups > rule->groups || ld < rule->experts) return BD_ERR_SHAPE;
+    if (rule->experts > rt::kMaxExperts || rule->top_k > rt::kMaxTopK || rule->groups > rt::kMaxGroups || tokens > (1ll << 30) / rule->top_k) return BD_ERR_UNSUPPORTED;
+    if (((uintptr_t)logits % elem_bytes(dtype)) || (((uintptr_t)bias | (uintptr_t)valid | (uintptr_t)ids | (uintptr_t)weights) & 3u)) return BD_ERR_ALIGN;
+    const int64_t blocks = std::max<int64_t>(1, rt::blocks_of(tokens));
+    if (plan) {
+        bd_status s = check_plan(plan);
+        if (s) return s;
+        if (plan->tokens != tokens || plan->top_k != rule->top_k || plan->experts != rule->experts) return BD_ERR_SHAPE;
+        if (blocks > 1 && !plan->scratch) return BD_ERR_WORKSPACE;
+        if (!aligned16(plan->scratch)) return BD_ERR_ALIGN;
+    } else if (tokens == 0) {
+        return BD_OK;
+    }
+    const rt::Rule r{logits, ld, bias, valid, ids, weights, (int)dtype, (int)tokens, (int)rule->experts, (int)rule->top_k, (int)rule->groups,
+                     (int)rule->top_groups, rule->group_top, rule->scale, rule->renormalise != 0};
+    const rt::Plan p = plan ? rt::Plan{plan->count, plan->start, plan->place, (uint8_t *)plan->scratch} : rt::Plan{};
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool wide = bias || rule->groups > 1;
+    bd_status s;
+    if (rule->score == BD_SCORE_SIGMOID) s = wide ? launch_route<true, true>(r, p, (unsigned)blocks, st) : launch_route<true, false>(r, p, (unsigned)blocks, st);
+    else s = wide ? launch_route<false, true>(r, p, (unsigned)blocks, st) : launch_route<false, false>(r, p, (unsigned)blocks, st);
+    return s || !plan || blocks == 1 ? s : launch_places(r, p, blocks, st);
+}
+
+bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, void *stream) {
+    bd_status s = check_plan(plan);
+    if (s) return s;
+    if (plan->tokens > 0 && !ids) return BD_ERR_INVALID_ARG;
+    if ((uintptr_t)ids & 3u) return BD_ERR_ALIGN;
+    const int64_t blocks = std::max<int64_t>(1, rt::blocks_of(plan->tokens));
+    if (blocks > 1 && !plan->scratch) return BD_ERR_WORKSPACE;
+    if (!aligned16(plan->scratch)) return BD_ERR_ALIGN;
+    const rt::Rule r{nullptr, 0, nullptr, nullptr, (int32_t *)ids, nullptr, 0, (int)plan->tokens, (int)plan->experts, (int)plan->top_k, 1, 1, 1, 1.0f, 0};
+    const rt::Plan p{plan->count, plan->start, plan->place, (uint8_t *)plan->scratch};
+    launch_serialized(rt::plan_count_kernel, (unsigned)blocks, rt::kThreads, 0, (cudaStream_t)stream, r, p);
+    if ((s = launch_result()) || blocks == 1) return s;
+    return launch_places(r, p, blocks, (cudaStream_t)stream);
+}
+
+bd_status bd_expert_mlp_workspace_size(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype, size_t *bytes) {
+    bd_status s = check_expert_pair(tokens, top_k, up, down, ydtype);
+    if (s) return s;
+    if (!bytes) return BD_ERR_INVALID_ARG;
+    *bytes = tokens ? expert_space(tokens, top_k, up, down, ydtype).total : 0;
+    return BD_OK;
+}
+
+bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t ldx, const bd_expert_plan *plan, const float *weights,
+                        const bd_experts *up, const bd_experts *down, bd_activation act, void *Y, bd_dtype ydtype, int64_t ldy, float *inner,
+                        void *workspace, size_t workspace_bytes, void *stream) {
+    bd_status s = check_plan(plan);
+    if (s) return s;
+    if ((s = check_expert_pair(tokens, plan->top_k, up, down, ydtype))) return s;
+    if (xdtype != BD_F32 && xdtype != BD_BF16 && xdtype != BD_F16) return BD_ERR_INVALID_ARG;
+    if (act != BD_ACT_SILU && act != BD_ACT_GELU) return BD_ERR_INVALID_ARG;
+    if (plan->tokens != tokens || plan->experts != up->experts) return BD_ERR_SHAPE;
+    if (tokens == 0) return BD_OK;
+    if (!X || !Y || !weights) return BD_ERR_INVALID_ARG;
+    if (ldx < up->K || ldy < down->rows) return BD_ERR_SHAPE;
+    if (!aligned16(X) || (ldx * elem_bytes(xdtype)) % 16 || !aligned16(Y) || (ldy * elem_bytes(ydtype)) % 16 || ((uintptr_t)weights & 3u) || ((uintptr_t)inner & 3u))
+        return BD_ERR_ALIGN;
+    const ExpertSpace sp = expert_space(tokens, plan->top_k, up, down, ydtype);
+    if (!workspace || workspace_bytes < sp.total) return BD_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 255u) return BD_ERR_ALIGN;
+    cudaStream_t st = (cudaStream_t)stream;
+    uint8_t *ws = (uint8_t *)workspace;
+    if (xdtype == BD_F32) launch_spread<BD_F32>(X, ldx, plan, up, sp, ws, st);
+    else if (xdtype == BD_BF16) launch_spread<BD_BF16>(X, ldx, plan, up, sp, ws, st);
+    else launch_spread<BD_F16>(X, ldx, plan, up, sp, ws, st);
+    if ((s = launch_result())) return s;
+    const int64_t rows = tokens * plan->top_k, most = rows / 256 + std::min(rows, up->experts);   // items of 256 tokens
+    const ex::Experts e{plan->count, plan->start, (int)up->experts, (int)sp.rows};
+    ex::Product p{};
+    p.live_k = (int)(down->K / kBlock);
+    p.h = ws + sp.h;
+    p.h_scales = ws + sp.h_scales;
+    p.inter = down->K;
+    p.gelu = act == BD_ACT_GELU;
+    cudaError_t err = ex::launch_product<true>(ws, ws + sp.x_scales, e, most, up, p, nullptr, false, st);
+    if (err != cudaSuccess) return cuda_result(err);
+    g_launches += 1;
+    if (inner) {
+        launch_serialized(ex::inner_kernel, (unsigned)std::min<int64_t>((rows * (down->K / kBlock) + 255) / 256, 148 * 8), 256, 0, st, (const uint8_t *)p.h,
+                          (const uint8_t *)p.h_scales, plan->place, rows, (int)sp.rows, (int)down->K, inner);
+        if ((s = launch_result())) return s;
+    }
+    err = ex::launch_product<false>(p.h, p.h_scales, e, most, down, p, ws, ydtype == BD_BF16, st);
+    if (err != cudaSuccess) return cuda_result(err);
+    g_launches += 1;
+    const unsigned grid = (unsigned)std::min<int64_t>((tokens * (down->rows / 8) + 255) / 256, 148 * 16);
+    if (ydtype == BD_BF16)
+        launch_serialized(ex::combine_kernel<true>, grid, 256, 0, st, (const uint8_t *)ws, plan->place, weights, (int)tokens, (int)plan->top_k, (int)sp.rows, (int)down->rows, Y, ldy);
+    else
+        launch_serialized(ex::combine_kernel<false>, grid, 256, 0, st, (const uint8_t *)ws, plan->place, weights, (int)tokens, (int)plan->top_k, (int)sp.rows, (int)down->rows, Y, ldy);
+    return launch_result();
+}
+
+bd_status bd_residual_norm(const bd_norm *a, bd_dtype dtype, int64_t rows, int64_t dim, void *stream) {
+    if (!a || rows < 0 || dim < 1 || (dtype != BD_F32 && dtype != BD_BF16 && dtype != BD_F16)) return BD_ERR_INVALID_ARG;
+    const bool next = a->n || a->q;
+    if ((!next && !a->h) || (a->n && a->q) || (next && !a->weight) || (rows > 0 && !a->y) || (!a->post_weight && a->post_bias)) return BD_ERR_INVALID_ARG;
+    if (!(a->eps >= 0.0f && a->eps < INFINITY) || !(a->scale > -INFINITY && a->scale < INFINITY) || !(a->weight_offset > -INFINITY && a->weight_offset < INFINITY)) return BD_ERR_INVALID_ARG;
+    if (a->gate && (a->gate_col < 0 || a->gate_col > 1 || a->gate_row < 0)) return BD_ERR_INVALID_ARG;
+    if (a->h && a->h == a->n) return BD_ERR_INVALID_ARG;
+    if (rows > 1 && (a->ldy < dim || (a->residual && a->ld_residual < dim) || (a->h && a->ldh < dim) || (a->n && a->ldn < dim))) return BD_ERR_SHAPE;
+    if (dim > nm::kMaxDim || rows > INT32_MAX - 128) return BD_ERR_UNSUPPORTED;
+    if (rows == 0) return BD_OK;
+    nm::Args k{};
+    if (a->q) {
+        bd_status s = check_qtensor(a->q);
+        if (s) return s;
+        if (a->q->rows != rows || a->q->K != dim) return BD_ERR_SHAPE;
+        k.q = view_of(a->q);
+    }
+    const int esz = elem_bytes(dtype);
+    // every operand that is read or written in pieces has to allow 16-byte accesses; one that does not takes the call to single elements
+    bool vec = dim % 8 == 0, fits = true;
+    auto operand = [&](const void *p, int64_t ld, bool pieces) {
+        if (!p) return;
+        fits = fits && (uintptr_t)p % esz == 0;
+        if (pieces) vec = vec && aligned16(p) && (rows == 1 || (ld * esz) % 16 == 0);
+    };
+    operand(a->y, a->ldy, true);
+    operand(a->residual, a->ld_residual, true);
+    operand(a->gate, a->gate_row, a->gate_col == 1);
+    for (const void *w : {a->post_weight, a->post_bias, a->weight, a->bias}) operand(w, 0, true);
+    operand(a->h, a->ldh, true);
+    operand(a->n, a->ldn, true);
+    if (!fits) return BD_ERR_ALIGN;
+    k.y = (const uint8_t *)a->y; k.residual = (const uint8_t *)a->residual; k.gate = (const uint8_t *)a->gate;
+    k.post_weight = (const uint8_t *)a->post_weight; k.post_bias = (const uint8_t *)a->post_bias;
+    k.weight = (const uint8_t *)a->weight; k.bias = (const uint8_t *)a->bias;
+    k.h = (uint8_t *)a->h; k.n = (uint8_t *)a->n;
+    k.ldy = a->ldy; k.ldr = a->ld_residual; k.ldh = a->ldh; k.ldn = a->ldn; k.gate_row = a->gate_row; k.gate_col = (int)a->gate_col;
+    k.rows = (int)rows; k.dim = (int)dim; k.layer = a->layer != 0;
+    k.scale = a->scale; k.eps = a->eps; k.offset = a->weight_offset;
+    // threads of a row: as many pieces of eight elements as the row has, up to 512 threads with one, two or four pieces each; short rows share a CTA
+    const int pieces = (int)((dim + 7) / 8);
+    const int vpt = pieces <= nm::kMaxThreads ? 1 : pieces <= 2 * nm::kMaxThreads ? 2 : 4;
+    k.row_threads = ((pieces + vpt - 1) / vpt + 31) / 32 * 32;
+    k.row_groups = std::max(1, 256 / k.row_threads);
+    const int64_t total = a->q ? row_tiles(rows) * kRowTile : rows;
+    const unsigned block = (unsigned)(k.row_threads * k.row_groups);
+    const unsigned grid = (unsigned)std::min<int64_t>((total + k.row_groups - 1) / k.row_groups, 148 * (2048 / block));
+    const size_t smem = a->q ? (size_t)k.row_groups * dim * esz : 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == BD_F32) return launch_norm<BD_F32>(k, vpt, a->q != nullptr, vec, grid, block, smem, st);
+    if (dtype == BD_BF16) return launch_norm<BD_BF16>(k, vpt, a->q != nullptr, vec, grid, block, smem, st);
+    return launch_norm<BD_F16>(k, vpt, a->q != nullptr, vec, grid, block, smem, st);
 }
 
 bd_status bd_export_canonical(const bd_qtensor *q, uint8_t *codes, uint8_t *ids, uint8_t *scales, void *stream) {

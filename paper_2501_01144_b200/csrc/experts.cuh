@@ -1,0 +1,664 @@
+// The experts' gated products of a mixture-of-experts block, in DialectFP4:
+//     y_t = sum_j w_tj * D_e q(act(G_e q(x_t)) * (U_e q(x_t))),   e = the j-th expert of token t,
+// q the online two-stage quantisation, G, U, D stored in DialectFP4.  Four launches:
+//   spread    quantises each token once and writes its operand bytes to the rows of its experts (each expert's rows begin at a multiple of
+//             128, the rows of a scale atom);
+//   product   gate and up rows of all experts against those rows; the epilogue forms act(g) * u and requantises it (GATED);
+//   product   the down rows against the result;
+//   combine   the weighted sum of a token's rows, in the order of its experts (fp32, the same in every run).
+//
+// The products are the tile of gemm_tc.cuh (256 weight rows x up to 256 tokens per pair of CTAs, weights expanded into tensor memory, one
+// block-scaled MMA per block of 32) under a schedule that each CTA works out from the experts' counts, which live on the
+// device: item = (expert, 256 weight rows, up to 256 of its tokens), clusters take items in turn.  The MMA is as wide as the item has
+// tokens (rounded up to 16), so a decode step, where an expert has a few tokens, pays for the weights' way through the SM and
+// little else.  The gate and up rows of 32 channels are neighbours (rows 64 j + i and 64 j + 32 + i): they meet in the warps of
+// one CTA, and 32 channels are one block of the next product's operand.
+#pragma once
+#include "bd_common.cuh"
+#include "gemm_tc.cuh"
+#include "ptx_sm100.cuh"
+#include "quantize.cuh"
+
+namespace bd {
+namespace ex {
+
+using namespace tc;
+
+constexpr int kMaxExperts = 512;
+constexpr int kBoxes = 5;                    // tensor maps of the token operand: 8, 16, 32, 64, 128 rows per CTA
+constexpr int kRowAlign = 128;
+
+// Most rows that the experts' segments can take: every expert's rows are rounded up to 128.
+inline int64_t padded_rows(int64_t assignments, int64_t experts) {
+    const int64_t used = experts < assignments ? experts : assignments;
+    return (assignments + (kRowAlign - 1) * used) / kRowAlign * kRowAlign;
+}
+
+struct Experts {                             // what the kernels know of the plan
+    const int32_t *count, *start;
+    int experts, rows;                       // rows: of the padded operand
+};
+struct Maps {
+    CUtensorMap x[kBoxes], codes, sfw, sfx, y;
+};
+struct Product {
+    const uint8_t *ids;                      // of all experts
+    int64_t ids_stride;                      // bytes between experts
+    int w_pairs, row_tiles, k_tiles, clusters;
+    int live_k;                              // GATED: blocks of the result (inter / 32)
+    uint8_t *h;                              // GATED: operand bytes [rows][inter] and scale atoms of the result
+    uint8_t *h_scales;
+    int64_t inter;
+    int gelu;
+    int y_bf16;
+};
+
+// Shared memory: the rings of gemm_tc.cuh, the schedule, and staging for the epilogue (GATED: 8 KiB a warp).
+template <bool GATED>
+struct Layout {
+    static constexpr int kStage = GATED ? 8192 : 4096;
+    static constexpr int x = 0;
+    static constexpr int codes = x + kXStages * kXTile;
+    static constexpr int sfw = codes + kCodeStages * kCodeTile;
+    static constexpr int sfx = sfw + kXStages * kScaleAtomBytes;
+    static constexpr int ids = sfx + kXStages * 2 * kScaleAtomBytes;
+    static constexpr int bars = ids + kCodeStages * kIdAtomBytes;
+    static constexpr int words = bars + 512;
+    static constexpr int luts = words + 64;
+    static constexpr int qtab = luts + 128;
+    static constexpr int first = (qtab + (int)sizeof(SmemTables) + 15) / 16 * 16;   // first item of each expert
+    static constexpr int count = first + 4 * (kMaxExperts + 4);
+    static constexpr int out = (count + 4 * kMaxExperts + 1023) / 1024 * 1024;
+    static constexpr int total = out + kEpilogueWarps * kStage + 1024 /* alignment slack */;
+};
+static_assert(Layout<true>::total <= 227 * 1024, "shared memory budget");
+
+struct Item {
+    int expert, w_pair;
+    int row0;                                // first row of the token operand, a multiple of 128
+    int live;                                // rows of this item that are tokens
+    int n;                                   // the N of the MMA: live rounded up to 16
+    int box;                                 // tensor map of the token operand: 8 << box rows per CTA
+};
+// Items of cluster c: c, c + clusters, ...; numbered expert by expert, then weight rows, the token tile running fastest.
+struct Walk {
+    const int *first, *count;
+    const int32_t *start;
+    int experts, clusters, c, e;
+    __device__ Walk(const int *first_, const int *count_, const int32_t *start_, int experts_, int clusters_, int c_)
+        : first(first_), count(count_), start(start_), experts(experts_), clusters(clusters_), c(c_), e(0) {}
+    __device__ bool operator()(int i, Item &t) {
+        const int item = i * clusters + c;
+        if (item >= first[experts]) return false;
+        while (item >= first[e + 1]) e++;
+        const int cnt = count[e], tiles = (cnt + 255) / 256, in = item - first[e], tt = in % tiles;
+        t.expert = e;
+        t.w_pair = in / tiles;
+        t.row0 = __ldg(start + e) + tt * 256;
+        t.live = min(256, cnt - tt * 256);
+        t.n = (t.live + 15) / 16 * 16;
+        t.box = t.n <= 16 ? 0 : 28 - __clz(t.n - 1);               // 8 << box >= n / 2
+        return true;
+    }
+};
+
+__device__ __forceinline__ float gated(float g, float u, int gelu) {
+    // act(g) = g / (1 + exp(-a)), a = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (gelu in its tanh form)
+    const float a = gelu ? 1.5957691216057308f * fmaf(0.044715f * g * g, g, g) : g;
+    return __fdividef(g, 1.0f + __expf(-a)) * u;
+}
+
+template <bool GATED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
+    using L = Layout<GATED>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    auto x_tile = [&](int s) { return base + L::x + (uint32_t)s * kXTile; };
+    auto code_tile = [&](int s) { return base + L::codes + (uint32_t)s * kCodeTile; };
+    auto sfw_tile = [&](int s) { return base + L::sfw + (uint32_t)s * kScaleAtomBytes; };
+    auto sfx_tile = [&](int s) { return base + L::sfx + (uint32_t)s * 2 * kScaleAtomBytes; };
+    auto id_tile = [&](int s) { return base + L::ids + (uint32_t)s * kIdAtomBytes; };
+    const uint32_t bars = base + L::bars;
+    auto x_full = [&](int s) { return bars + 8u * s; };                                   // leader: tile + scales of both CTAs
+    auto x_empty = [&](int s) { return bars + 8u * (kXStages + s); };                     // both: stage consumed by the MMA
+    auto c_full = [&](int s) { return bars + 8u * (2 * kXStages + s); };                  // local: codes + ids landed
+    auto c_empty = [&](int s) { return bars + 8u * (2 * kXStages + kCodeStages + s); };   // local: codes read by the decode group
+    auto a_full = [&](int b) { return bars + 8u * (2 * kXStages + 2 * kCodeStages + b); };            // leader: buffer written in both CTAs
+    auto a_empty = [&](int b) { return bars + 8u * (2 * kXStages + 2 * kCodeStages + kABufs + b); };  // both: buffer consumed
+    const uint32_t tmem_full_bar = bars + 8u * (2 * kXStages + 2 * kCodeStages + 2 * kABufs);         // both: accumulator complete
+    const uint32_t tmem_empty_bar = tmem_full_bar + 8u;                                               // leader: accumulator read out
+    volatile uint32_t *const shared_words = (volatile uint32_t *)(base_ptr + L::words);
+    volatile uint32_t *const tmem_slot = shared_words;
+    volatile uint32_t *const abort_flag = shared_words + 1;
+    uint32_t *const luts = (uint32_t *)(base_ptr + L::luts);
+    int *const first = (int *)(base_ptr + L::first), *const count = (int *)(base_ptr + L::count);
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_ctarank();
+    const int cluster = blockIdx.x / 2;
+
+    if (threadIdx.x == 0) {
+        abort_flag[0] = 0;
+        abort_flag[1] = 0;                                        // set once the previous kernel has completed
+        abort_flag[2] = g_debug_spin_limit ? g_debug_spin_limit : kSpinLimit;
+        for (int s = 0; s < kXStages; s++) {
+            mbar_init(x_full(s), 1);
+            mbar_init(x_empty(s), 1);
+        }
+        for (int s = 0; s < kCodeStages; s++) {
+            mbar_init(c_full(s), 1);
+            mbar_init(c_empty(s), 4);                             // one arrival per warp of the decode group
+        }
+        for (int b = 0; b < kABufs; b++) {
+            mbar_init(a_full(b), 2);                              // one arrival per CTA of the pair
+            mbar_init(a_empty(b), 1);
+        }
+        mbar_init(tmem_full_bar, 1);
+        mbar_init(tmem_empty_bar, 2 * kEpilogueWarps);            // the epilogue warps of both CTAs
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 32)
+        luts[threadIdx.x] = threadIdx.x < 16 ? c_tables.e4m3_lo[threadIdx.x] : c_tables.e4m3_hi[threadIdx.x - 16];
+    SmemTables &qtab = *(SmemTables *)(base_ptr + L::qtab);
+    if (GATED) load_tables(qtab);                                 // (ends with __syncthreads())
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32((const void *)tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    // The schedule: items of the experts before each one, by a scan in the first warp.  The plan is older than the kernel in front of
+    // this one (which waited for it before it let this one start), so no wait is needed.  Numbers that cannot be (a plan overwritten by
+    // the caller) leave the expert out and are told: nothing is addressed by them.
+    if (warp == 0) {
+        int before = 0;
+        for (int e0 = 0; e0 < ex.experts; e0 += 32) {
+            const int e = e0 + lane;
+            int cnt = 0;
+            if (e < ex.experts) {
+                cnt = __ldg(ex.count + e);
+                const int start = __ldg(ex.start + e);
+                if (cnt < 0 || start < 0 || start % kRowAlign || cnt > ex.rows || start > ex.rows - cnt) {
+                    cnt = 0;
+                    atomicOr(&g_status_word, kStatusIndex);
+                }
+                count[e] = cnt;
+            }
+            const int items = (cnt + 255) / 256 * p.w_pairs;
+            int incl = items;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            if (e < ex.experts) first[e] = before + incl - items;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) first[ex.experts] = before;
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                           // both CTAs: barriers initialised, TMEM allocated
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    Walk next(first, count, ex.start, ex.experts, p.clusters, cluster);
+    Item t;
+
+    if (warp == 0) {
+        // ---- TMA producer of the token tile and the scale atoms; the one warp that reads what the kernel in front wrote ----
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        if (lane == 0) abort_flag[1] = 1;                         // from here on every bounded wait counts its polls
+        int s = 0;
+        uint32_t ph = 1;
+        const uint32_t x_full_leader = map_to_cta(x_full(0), 0);
+        const int tiles_x = ex.rows / kRowAlign;
+        for (int i = 0; next(i, t); i++) {
+            // each CTA holds half of the MMA's tokens (and, where the box is higher, rows that are not looked at)
+            const int t0 = t.row0 + (int)rank * (t.n / 2);
+            const uint32_t tx_pair = 2u * ((8u << t.box) * BK + 3u * kScaleAtomBytes);
+            const int sf_row = t.expert * p.k_tiles * p.row_tiles + t.w_pair * 2 + (int)rank;
+            for (int kt = 0; kt < p.k_tiles; kt++) {
+                if (!mbar_wait(x_empty(s), ph, abort_flag)) break;
+                const uint32_t fb = x_full_leader + 8u * (uint32_t)s;
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect_tx(x_full(s), tx_pair);
+                    tma_load_2d_pair(x_tile(s), &maps.x[t.box], kt * BK, t0, fb);
+                    tma_load_2d_pair(sfw_tile(s), &maps.sfw, 0, sf_row + kt * p.row_tiles, fb);
+                    tma_load_2d_pair(sfx_tile(s), &maps.sfx, 0, kt * tiles_x + t.row0 / kRowAlign, fb);
+                }
+                __syncwarp();
+                if (++s == kXStages) { s = 0; ph ^= 1u; }
+            }
+            if (*abort_flag) break;
+        }
+    } else if (warp == 2) {
+        // ---- TMA producer of this CTA's packed codes and ids ----
+        int s = 0;
+        uint32_t ph = 1;
+        const bool skip_first = g_debug_skip_first_code_stage != 0;   // test hook: see bd_debug_fault
+        const int rows = p.row_tiles;
+        for (int i = 0; next(i, t); i++) {
+            const int my_row_tile = t.w_pair * 2 + (int)rank;
+            const bool have_ids = my_row_tile < rows;
+            const uint8_t *ids = p.ids + (int64_t)t.expert * p.ids_stride + (int64_t)my_row_tile * kIdAtomBytes;
+            for (int kt = 0; kt < p.k_tiles; kt++) {
+                if (!mbar_wait(c_empty(s), ph, abort_flag)) break;
+                if (elect_one() && !(skip_first && i == 0 && kt == 0)) {
+                    mbar_expect_tx(c_full(s), kCodeTile + (have_ids ? kIdAtomBytes : 0));
+                    tma_load_3d(code_tile(s), &maps.codes, kt * (BK / 2), my_row_tile * 128, t.expert, c_full(s));
+                    if (have_ids) bulk_load(id_tile(s), ids + (int64_t)kt * rows * kIdAtomBytes, kIdAtomBytes, c_full(s));
+                }
+                __syncwarp();
+                if (++s == kCodeStages) { s = 0; ph ^= 1u; }
+            }
+            if (*abort_flag) break;
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            // ---- MMA issuer (leader CTA; whole warp converged, one elected lane issues) ----
+            const uint32_t hi_op = desc_hi(1024, kLayoutSwizzle128), hi_sf = desc_hi(128, kLayoutNone);
+            const uint32_t lo_x0 = (x_tile(0) >> 4) | 1u << 16;
+            const uint32_t lo_sfw0 = sfw_tile(0) >> 4, lo_sfx0 = sfx_tile(0) >> 4;
+            // (instruction descriptor: see gemm_tc.cuh; N >> 3 at bit 17 follows the item)
+            const uint32_t idesc_m = 1u << 23 | (uint32_t)(256 >> 4) << 24;
+            const uint32_t t_d = tmem + kColD, t_sfw = tmem + kColSfW, t_sfx = tmem + kColSfX;
+            int s = 0, b = 0;
+            uint32_t ph_s = 0, ph_b = 0;
+            bool ready = false;
+            for (int i = 0; next(i, t); i++) {
+                const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17;
+                if (i > 0) mbar_wait(tmem_empty_bar, (uint32_t)(i - 1) & 1u, abort_flag);
+                tcgen05_fence_after();
+                for (int kt = 0; kt < p.k_tiles; kt++) {
+                    if (!ready) {
+                        if (!mbar_wait(x_full(s), ph_s, abort_flag) || !mbar_wait(a_full(b), ph_b, abort_flag)) break;
+                    }
+                    tcgen05_fence_after();
+                    const uint32_t lo_sfw = lo_sfw0 + (uint32_t)s * (kScaleAtomBytes >> 4);
+                    const uint32_t lo_sfx = lo_sfx0 + (uint32_t)s * (2 * kScaleAtomBytes >> 4);
+                    const uint32_t lo_x = lo_x0 + (uint32_t)s * (kXTile >> 4);
+                    const uint32_t t_a = tmem + kColA + 32u * (uint32_t)b;
+                    if (elect_one()) {
+                        tcgen05_cp_pair(t_sfw, desc_join(lo_sfw, hi_sf));
+                        tcgen05_cp_pair(t_sfx, desc_join(lo_sfx, hi_sf));
+                        tcgen05_cp_pair(t_sfx + 4, desc_join(lo_sfx + (kScaleAtomBytes >> 4), hi_sf));
+#pragma unroll
+                        for (int k = 0; k < BK / 32; k++)
+                            tcgen05_mma_mxf8_pair_atmem(t_d, t_a + 8u * k, desc_join(lo_x + 2 * k, hi_op),
+                                                        idesc0 | (uint32_t)k << 4 | (uint32_t)k << 29, t_sfw, t_sfx,
+                                                        k == 0 ? (kt > 0 ? 1u : 0u) : 1u);
+                        tcgen05_commit_pair(x_empty(s));
+                        tcgen05_commit_pair(a_empty(b));
+                    }
+                    __syncwarp();
+                    if (++s == kXStages) { s = 0; ph_s ^= 1u; }
+                    if (++b == kABufs) { b = 0; ph_b ^= 1u; }
+                    const bool x_ok = mbar_test_wait(x_full(s), ph_s), a_ok = mbar_test_wait(a_full(b), ph_b);
+                    ready = x_ok && a_ok;
+                }
+                if (*abort_flag && elect_one()) {
+                    // this CTA is aborting: tell the peer before its epilogue warps are woken by the commit below
+                    asm volatile("st.shared::cluster.u32 [%0], %1;\n\tfence.acq_rel.cluster;"
+                                 ::"r"(map_to_cta(smem_u32((const void *)abort_flag), 1)), "r"(1u) : "memory");
+                }
+                __syncwarp();
+                if (elect_one()) tcgen05_commit_pair(tmem_full_bar);
+                __syncwarp();
+                if (*abort_flag) break;
+            }
+        }
+    } else if (warp < kEpilogueWarp0) {
+        // ---- decode warps (as in gemm_tc.cuh): group g takes k-steps g, g + groups, ... counted across items ----
+        const int group = (warp - kDecodeWarp0) / 4, quad = warp % 4;
+        const int j = quad * 32 + lane;
+        const bool group_leader = (warp - kDecodeWarp0) % 4 == 0 && lane == 0;
+        const uint32_t swz64 = (uint32_t)(j >> 1) & 3u;
+        const uint32_t a_full_leader = map_to_cta(a_full(0), 0);
+        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + kColA;
+        const int items = first[ex.experts];
+        const int total_k = cluster < items ? ((items - cluster + p.clusters - 1) / p.clusters) * p.k_tiles : 0;
+        int s = group % kCodeStages, b = group % kABufs;
+        uint32_t s_par = 0, b_par = 1;
+        static_assert(kDecodeGroups <= kCodeStages && kDecodeGroups <= kABufs, "one wrap per step at most");
+        bool dead = false;                                        // (a warp whose wait ran out keeps meeting its group at the barrier)
+        for (int g = group; g < total_k; g += kDecodeGroups) {
+            uint4 w[4];
+            uint32_t ids16 = 0;
+            if (!dead) dead = !mbar_wait(c_full(s), s_par, abort_flag);
+            if (!dead) {
+                const uint8_t *codes = base_ptr + L::codes + s * kCodeTile + j * 64;
+                ids16 = *(const uint16_t *)(base_ptr + L::ids + s * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
+#pragma unroll
+                for (int c = 0; c < 4; c++) w[c] = *(const uint4 *)(codes + 16 * (c ^ swz64));
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(c_empty(s));
+                dead = !mbar_wait(a_empty(b), b_par, abort_flag);
+            }
+            if (!dead) {
+                tcgen05_fence_after();                            // the MMAs that read this buffer have completed
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const uint32_t id = (ids16 >> (4 * c)) & 15u;
+                    const uint32_t lo = luts[id], hi = luts[16 + id];
+                    uint32_t o[8];
+                    decode_word(w[c].x, lo, hi, o[0], o[1]);
+                    decode_word(w[c].y, lo, hi, o[2], o[3]);
+                    decode_word(w[c].z, lo, hi, o[4], o[5]);
+                    decode_word(w[c].w, lo, hi, o[6], o[7]);
+                    tcgen05_st_32x32b_x8(t_row + 32u * (uint32_t)b + 8u * (uint32_t)c, o);
+                }
+                tcgen05_wait_st();
+                tcgen05_fence_before();
+            }
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");   // the four warps of this group are done
+            if (group_leader && !dead) mbar_arrive_cluster(a_full_leader + 8u * b);
+            s += kDecodeGroups;
+            if (s >= kCodeStages) { s -= kCodeStages; s_par ^= 1u; }
+            b += kDecodeGroups;
+            if (b >= kABufs) { b -= kABufs; b_par ^= 1u; }
+        }
+    } else {
+        // ---- epilogue: warp w reads the TMEM lanes 32 * (w % 4) .. + 31 (weight rows) of this CTA's accumulator ----
+        const int quad = warp % 4, half = (warp - kEpilogueWarp0) / 4, slot = half * 4 + quad;   // (the first epilogue warp need not be quadrant 0's)
+        const uint32_t tmem_empty_leader = map_to_cta(tmem_empty_bar, 0);
+        const uint32_t stage_out = base + L::out + (uint32_t)slot * L::kStage;
+        uint8_t *const stage_ptr = base_ptr + L::out + slot * L::kStage;
+        auto release_accumulator = [&]() {
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader);
+        };
+        uint32_t stage_turn = 0;
+        auto staging_free = [&]() -> uint32_t {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+            stage_turn ^= 1u;
+            return stage_turn * kStageOut;
+        };
+        for (int i = 0; next(i, t); i++) {
+            mbar_wait(tmem_full_bar, (uint32_t)i & 1u, abort_flag, 256);
+            tcgen05_fence_after();
+            const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + kColD;
+            if (GATED) {
+                // Tokens 64 at a time; the two epilogue halves take turns.  The warps of quadrants 2 m and 2 m + 1 hold the gate and
+                // the up rows of the same 32 channels (block 2 m of this CTA's): both store two 32 x 32 tiles of sums (element
+                // (token q, row r) at q * 32 + (r ^ q): rows are written and tokens read without bank conflicts), meet, and then the
+                // first finishes the first 32 tokens and the second the others, a token's block per lane.
+                const int groups = (t.n + 63) / 64, pair = quad / 2, which = quad & 1;
+                const int b = t.w_pair * 4 + (int)rank * 2 + pair;                     // block of the result
+                const bool block_ok = b < p.live_k;
+                const uint32_t *const tile_g = (const uint32_t *)(base_ptr + L::out + (slot - which) * L::kStage) + which * 1024;
+                const uint32_t *const tile_u = (const uint32_t *)(base_ptr + L::out + (slot - which + 1) * L::kStage) + which * 1024;
+                const int tiles_h = ex.rows / kRowAlign;
+                if (half >= groups) release_accumulator();
+                for (int g = half; g < groups; g += 2) {
+#pragma unroll
+                    for (int v = 0; v < 2; v++) {
+                        uint32_t r[32];
+                        uint32_t *const tile = (uint32_t *)stage_ptr + v * 1024;
+                        tcgen05_ld_32x32b_x32(t_base + g * 64 + v * 32, r);
+                        tcgen05_wait_ld();
+                        if (v == 1 && g + 2 >= groups) release_accumulator();
+#pragma unroll
+                        for (int q = 0; q < 32; q++) tile[q * 32 + (lane ^ q)] = r[q];
+                    }
+                    asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory");
+                    const int tok = g * 64 + which * 32 + lane, row = t.row0 + tok;
+                    uint32_t bits[32];
+#pragma unroll
+                    for (int k = 0; k < 32; k++)
+                        bits[k] = __float_as_uint(gated(__uint_as_float(tile_g[lane * 32 + (k ^ lane)]), __uint_as_float(tile_u[lane * 32 + (k ^ lane)]), p.gelu));
+                    asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory");   // the tiles may be written again
+                    if (tok < t.live && !*abort_flag) {
+                        BlockResult res;
+                        res.scale = 0;
+                        if (block_ok) {
+                            bool nonfinite;
+                            uint32_t o[8];
+                            quantize_two_stage_f32<true>(bits, qtab, res, o, nonfinite);
+                            if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
+                            uint4 *dst = (uint4 *)(p.h + (int64_t)row * p.inter + (int64_t)b * 32);
+                            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                        }
+                        // (blocks behind the last one, up to the atom's four: zeros)
+                        p.h_scales[((int64_t)(b / kBlocksPerAtom) * tiles_h + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4 + b % kBlocksPerAtom] = (uint8_t)res.scale;
+                    }
+                }
+            } else {
+                // chunks of 32 tokens: the first half's warps take the larger part
+                const int chunks = (t.n + 31) / 32, mine0 = half ? (chunks + 1) / 2 : 0, mine = half ? chunks / 2 : (chunks + 1) / 2;
+                const int n0 = t.w_pair * 256 + (int)rank * 128 + quad * 32, t0 = t.row0 + mine0 * 32;
+                const uint32_t t_mine = t_base + mine0 * 32;
+                if (p.y_bf16) {
+                    switch (mine) {
+                        case 4: epilogue_bf16<4>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
+                        case 3: epilogue_bf16<3>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
+                        case 2: epilogue_bf16<2>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
+                        case 1: epilogue_bf16<1>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
+                        default: release_accumulator();
+                    }
+                } else {
+                    if (mine == 0) release_accumulator();
+                    for (int pass = 0; pass < 2 * mine; pass++) {     // fp32: 16 tokens x 32 columns per pass
+                        uint32_t r[16];
+                        tcgen05_ld_32x32b_x16(t_mine + pass * 16, r);
+                        tcgen05_wait_ld();
+                        if (pass + 1 == 2 * mine) release_accumulator();
+                        const uint32_t sb = staging_free();
+#pragma unroll
+                        for (int q = 0; q < 16; q++) *(uint32_t *)(stage_ptr + sb + q * 128 + lane * 4) = r[q];
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0 && !*abort_flag) {
+                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                         ::"l"(&maps.y), "r"(n0), "r"(t0 + pass * 16), "r"(stage_out + sb) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    }
+                }
+            }
+        }
+        // the staging buffers must outlive the stores' reads of them; the writes themselves complete with the grid
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                           // the peer may still signal our barriers until here
+    if (warp == 1) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// Quantises the tokens and writes each to the rows of its experts: thread = (token, block of 32), four lanes a scale word.
+template <int DT>
+__global__ void __launch_bounds__(256) spread_kernel(const uint8_t *__restrict__ X, int64_t ldx, int tokens, int top_k, const int32_t *__restrict__ place,
+                                                     int nb, int kgroups, int rows, uint8_t *__restrict__ x8, uint8_t *__restrict__ scales, FastDiv div_row) {
+    __shared__ SmemTables tab;
+    load_tables(tab);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t per_row = (uint32_t)kgroups * kBlocksPerAtom, items = (uint32_t)tokens * per_row;
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < (items + 31u) / 32u * 32u; i += gridDim.x * 256u) {   // (whole warps)
+        const uint32_t t = fast_div(i, div_row), b = i - t * per_row;
+        uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        BlockResult res;
+        res.scale = 0;
+        const bool valid = i < items && b < (uint32_t)nb;
+        if (valid) {
+            const uint8_t *src = X + ((int64_t)t * ldx + b * 32u) * Loader<DT>::kElemBytes;
+            if (DT == BD_BF16) {
+                uint32_t pairs[16];
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const uint4 u = __ldg((const uint4 *)src + q);
+                    pairs[4 * q] = u.x; pairs[4 * q + 1] = u.y; pairs[4 * q + 2] = u.z; pairs[4 * q + 3] = u.w;
+                }
+                quantize_bf16_block<true>(pairs, tab, res, o);
+            } else {
+                uint32_t bits[32];
+                bool nonfinite;
+                Loader<DT>::contiguous(src, bits);
+                quantize_two_stage_f32<true>(bits, tab, res, o, nonfinite);
+                if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
+            }
+        }
+        uint32_t sc = res.scale << (8 * (b & 3u));
+        sc |= __shfl_xor_sync(0xffffffffu, sc, 1);
+        sc |= __shfl_xor_sync(0xffffffffu, sc, 2);
+        if (i >= items) continue;
+        for (int j = 0; j < top_k; j++) {
+            const int row = __ldg(place + (int64_t)t * top_k + j);
+            if (row < 0) continue;
+            if (row >= rows) {
+                atomicOr(&g_status_word, kStatusIndex);
+                continue;
+            }
+            if (valid) {
+                uint4 *dst = (uint4 *)(x8 + (int64_t)row * ((int64_t)nb * 32) + b * 32u);
+                dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            }
+            if ((b & 3u) == 0)
+                *(uint32_t *)(scales + ((int64_t)(b / 4) * (rows / kRowTile) + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4) = sc;
+        }
+    }
+}
+
+// y_t = sum_j w_tj * part[place_tj], thread = eight neighbouring outputs of a token.  A token without experts gets zeros.
+template <bool BF16>
+__global__ void __launch_bounds__(256) combine_kernel(const uint8_t *__restrict__ part, const int32_t *__restrict__ place, const float *__restrict__ weights,
+                                                      int tokens, int top_k, int rows, int n, void *__restrict__ Y, int64_t ldy) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int per_row = n / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)tokens * per_row; i += (int64_t)gridDim.x * 256) {
+        const int t = (int)(i / per_row), c = (int)(i - (int64_t)t * per_row) * 8;
+        float acc[8];
+#pragma unroll
+        for (int q = 0; q < 8; q++) acc[q] = 0.0f;
+#pragma unroll 4
+        for (int j = 0; j < top_k; j++) {
+            const int row = __ldg(place + (int64_t)t * top_k + j);
+            if (row < 0 || row >= rows) continue;
+            const float w = __ldg(weights + (int64_t)t * top_k + j);
+            if (BF16) {
+                const uint4 u = __ldcs((const uint4 *)(part + ((int64_t)row * n + c) * 2));
+                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    acc[2 * q] = fmaf(w, __uint_as_float(x[q] << 16), acc[2 * q]);
+                    acc[2 * q + 1] = fmaf(w, __uint_as_float(x[q] & 0xffff0000u), acc[2 * q + 1]);
+                }
+            } else {
+                const float4 u = __ldcs((const float4 *)(part + ((int64_t)row * n + c) * 4)), v = __ldcs((const float4 *)(part + ((int64_t)row * n + c) * 4) + 1);
+                const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int q = 0; q < 8; q++) acc[q] = fmaf(w, x[q], acc[q]);
+            }
+        }
+        if (BF16) {
+            uint32_t o[4];
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(acc[2 * q], acc[2 * q + 1]);
+                o[q] = *(const uint32_t *)&h;
+            }
+            *(uint4 *)((uint16_t *)Y + (int64_t)t * ldy + c) = make_uint4(o[0], o[1], o[2], o[3]);
+        } else {
+            float4 *dst = (float4 *)((float *)Y + (int64_t)t * ldy + c);
+            dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        }
+    }
+}
+
+// The values that the second product reads, for checking: out[token][slot][inter] in fp32 (zeros where no expert serves).
+__global__ void __launch_bounds__(256) inner_kernel(const uint8_t *__restrict__ h, const uint8_t *__restrict__ scales, const int32_t *__restrict__ place,
+                                                    int64_t assignments, int rows, int inter, float *__restrict__ out) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int nb = inter / 32;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < assignments * nb; i += (int64_t)gridDim.x * 256) {
+        const int64_t a = i / nb;
+        const int b = (int)(i - a * nb), row = __ldg(place + a);
+        float *dst = out + a * inter + b * 32;
+        const bool there = row >= 0 && row < rows;
+        const int e = there ? (int)scales[((int64_t)(b / 4) * (rows / kRowTile) + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4 + b % 4] - 127 : 0;
+        for (int k = 0; k < 32; k++) {
+            float v = 0.0f;
+            if (there) {
+                const uint32_t x = h[(int64_t)row * inter + b * 32 + k];              // E4M3: no magnitude here is subnormal
+                const uint32_t f = x >> 3 & 15u;
+                if (f) v = scalbnf(1.0f + (float)(x & 7u) * 0.125f, (int)f - 7 + e);
+                if (x & 0x80u) v = -v;
+            }
+            dst[k] = v;
+        }
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------
+inline bool make_map_3d(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, uint64_t inner, uint64_t rows, uint64_t outer, uint64_t row_bytes,
+                        uint64_t outer_bytes, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {inner, rows, outer}, strides[2] = {row_bytes, outer_bytes};
+    cuuint32_t box[3] = {box_inner, box_rows, 1}, elem[3] = {1, 1, 1};
+    return fn(map, type, 3, (void *)ptr, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool GATED>
+inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t items_most, const bd_experts *W, Product p, void *Y, bool y_bf16, cudaStream_t st) {
+    Maps m;
+    const int64_t N = W->rows, K = W->K, rtw = row_tiles(N), kg = k_groups(K);
+    for (int b = 0; b < kBoxes; b++)
+        if (!make_map_2d(&m.x[b], CU_TENSOR_MAP_DATA_TYPE_UINT8, x8, K, ex.rows, K, BK, 8u << b, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
+    if (!make_map_3d(&m.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, W->codes, K / 2, N, W->experts, K / 2, (uint64_t)N * (K / 2), 64, 128, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !make_map_2d(&m.sfw, CU_TENSOR_MAP_DATA_TYPE_UINT32, W->scales, 128, (uint64_t)rtw * kg * W->experts, kScaleAtomBytes, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_map_2d(&m.sfx, CU_TENSOR_MAP_DATA_TYPE_UINT32, sfx, 128, (uint64_t)(ex.rows / kRowAlign) * kg, kScaleAtomBytes, 128, 2, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cudaErrorInvalidValue;
+    if (!GATED) {
+        if (!make_map_2d(&m.y, y_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, Y, N, ex.rows, (uint64_t)N * (y_bf16 ? 2 : 4), 32,
+                         y_bf16 ? 32 : 16, CU_TENSOR_MAP_SWIZZLE_NONE))
+            return cudaErrorInvalidValue;
+    } else {
+        m.y = m.sfx;                                                  // unused, but must be a valid object
+    }
+    static bool configured[tc::kMaxDevices] = {};
+    const int dev = current_device();
+    if (!configured[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<GATED>::total);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    p.ids = (const uint8_t *)W->ids;
+    p.ids_stride = rtw * kg * kIdAtomBytes;
+    p.w_pairs = (int)((N + 255) / 256);
+    p.row_tiles = (int)rtw;
+    p.k_tiles = (int)kg;
+    p.y_bf16 = y_bf16;
+    const int resident = max_resident_clusters();
+    const int64_t most = items_most * p.w_pairs;
+    p.clusters = most < resident ? (int)most : resident;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * p.clusters);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Layout<GATED>::total;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, expert_product_kernel<GATED>, m, ex, p);
+}
+
+}  // namespace ex
+}  // namespace bd

@@ -1,0 +1,316 @@
+// The norms around a block, fused with the residual sum between them:
+//     u = norm(y) * (post_weight + offset) + post_bias     (or y itself)
+//     h = residual + scale * gate * u
+//     n = norm(h) * (weight + offset) + bias               (of the unrounded h; rounded to the rows' type once)
+// with norm(x) = x / sqrt(mean(x^2) + eps), or (x - mean x) / sqrt(var x + eps); n may leave as a DialectFP4 operand, quantised from
+// the rounded value by the two-stage rule, so that it has the bits that storing n and quantising it would give.
+//
+// A row lives in the registers of its threads (VPT pieces of eight elements each) from the first load to the last store: every
+// input is read once, every output written once, and what stays are the reductions.  Sums, means and variances are fp32; the
+// variance comes from the centred values in registers, not from a difference of squares.  For the quantised result the row
+// passes through shared memory, where a thread picks up a whole block of 32.
+// Bound: memory; a row's latency (two to four reductions) where there are few rows.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "bd_common.cuh"
+#include "quantize.cuh"
+
+namespace bd {
+namespace nm {
+
+constexpr int kMaxDim = 16384, kMaxThreads = 512;
+
+struct Args {
+    const uint8_t *y, *residual, *gate, *post_weight, *post_bias, *weight, *bias;
+    uint8_t *h, *n;
+    int64_t ldy, ldr, ldh, ldn, gate_row;
+    QView q;                                 // the quantised result (QUANT)
+    int rows, dim, gate_col, layer, row_threads, row_groups;   // threads of a row, rows a CTA has at a time
+    float scale, eps, offset;
+};
+
+// Eight elements in fp32.  VEC: neighbours, in one or two 16-byte accesses; else elements `step` apart, those behind `dim` zeros.
+template <int DT, bool VEC>
+__device__ __forceinline__ void load8(const uint8_t *p, int e, int step, int dim, float (&v)[8]) {
+    constexpr int EB = Loader<DT>::kElemBytes;
+    if (VEC) {
+        if (e >= dim) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) v[q] = 0.0f;
+            return;
+        }
+        const uint4 *src = (const uint4 *)(p + (int64_t)e * EB);
+        const uint4 a = src[0];
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        if (DT == BD_F32) {
+            const uint4 b = src[1];
+            const uint32_t z[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int q = 0; q < 4; q++) { v[q] = __uint_as_float(w[q]); v[4 + q] = __uint_as_float(z[q]); }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                if (DT == BD_BF16) {
+                    v[2 * q] = __uint_as_float(w[q] << 16);
+                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                } else {
+                    const float2 f = __half22float2(*(const __half2 *)&w[q]);
+                    v[2 * q] = f.x;
+                    v[2 * q + 1] = f.y;
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            const int at = e + q * step;
+            v[q] = 0.0f;
+            if (at < dim) {
+                const uint8_t *src = p + (int64_t)at * EB;
+                if (DT == BD_F32) v[q] = *(const float *)src;
+                else if (DT == BD_BF16) v[q] = __uint_as_float((uint32_t) * (const uint16_t *)src << 16);
+                else v[q] = __half2float(*(const __half *)src);
+            }
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ uint32_t pair_of(float a, float b) {
+    if (DT == BD_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *(const uint32_t *)&h;
+    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *(const uint32_t *)&h;
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ void store8(uint8_t *p, int e, int step, int dim, const float (&v)[8]) {
+    constexpr int EB = Loader<DT>::kElemBytes;
+    if (VEC) {
+        if (e >= dim) return;
+        uint4 *dst = (uint4 *)(p + (int64_t)e * EB);
+        if (DT == BD_F32) {
+            dst[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            dst[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        } else {
+            dst[0] = make_uint4(pair_of<DT>(v[0], v[1]), pair_of<DT>(v[2], v[3]), pair_of<DT>(v[4], v[5]), pair_of<DT>(v[6], v[7]));
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            const int at = e + q * step;
+            if (at >= dim) continue;
+            uint8_t *dst = p + (int64_t)at * EB;
+            if (DT == BD_F32) *(float *)dst = v[q];
+            else *(uint16_t *)dst = (uint16_t)pair_of<DT>(v[q], 0.0f);
+        }
+    }
+}
+
+// Where element e of the row lies in the shared row buffer: 16-byte pieces, those of a block permuted so that eight threads that
+// read the same piece of neighbouring blocks meet eight different groups of banks.
+template <int DT>
+__device__ __forceinline__ int place(int e) {
+    constexpr int EB = Loader<DT>::kElemBytes, kPieces = 2 * EB, kPer = 16 / EB;   // pieces of a block, elements of a piece
+    const int b = e / kBlock, p = e % kBlock / kPer;
+    const int s = EB == 4 ? p ^ (b & 7) : p ^ ((b >> 1) & 3);
+    return (b * kPieces + s) * 16 + e % kPer * EB;
+}
+
+template <int DT, int VPT, bool QUANT, bool VEC>
+__global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid_constant__ Args a) {
+    __shared__ float part[2][kMaxThreads / 32];
+    __shared__ SmemTables tab;
+    extern __shared__ __align__(16) uint8_t row_buffer[];         // QUANT: [row groups] rows of dim elements
+    if (QUANT) load_tables(tab);
+    const int rt = a.row_threads, group = threadIdx.x / rt, t = threadIdx.x % rt, lane = threadIdx.x % 32;
+    const int warps = rt / 32, warp0 = group * warps;
+    const float inv = 1.0f / (float)a.dim;
+    int turn = 0;
+    // sum over the row's threads; the two halves of `part` take turns, so one barrier a sum is enough
+    auto row_sum = [&](float v) {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (warps == 1) return v;
+        turn ^= 1;
+        if (lane == 0) part[turn][threadIdx.x / 32] = v;
+        __syncthreads();
+        float s = lane < warps ? part[turn][warp0 + lane] : 0.0f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        return s;
+    };
+    auto elem = [&](int v) { return VEC ? (v * rt + t) * 8 : v * 8 * rt + t; };   // first element of piece v; the others follow, or are rt apart
+    auto normalise = [&](float (&x)[VPT][8], const uint8_t *w, const uint8_t *b) {
+        if (a.layer) {
+            float s = 0.0f;
+#pragma unroll
+            for (int v = 0; v < VPT; v++)
+#pragma unroll
+                for (int q = 0; q < 8; q++) s += x[v][q];         // (elements behind the row are zeros)
+            const float mean = row_sum(s) * inv;
+#pragma unroll
+            for (int v = 0; v < VPT; v++)
+#pragma unroll
+                for (int q = 0; q < 8; q++) x[v][q] = (VEC ? elem(v) : elem(v) + q * rt) < a.dim ? x[v][q] - mean : 0.0f;
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < VPT; v++)
+#pragma unroll
+            for (int q = 0; q < 8; q++) s = fmaf(x[v][q], x[v][q], s);
+        const float f = rsqrtf(fmaf(row_sum(s), inv, a.eps));
+#pragma unroll
+        for (int v = 0; v < VPT; v++) {
+            float g[8];
+            load8<DT, VEC>(w, elem(v), rt, a.dim, g);
+#pragma unroll
+            for (int q = 0; q < 8; q++) x[v][q] = x[v][q] * f * (g[q] + a.offset);
+            if (b) {
+                load8<DT, VEC>(b, elem(v), rt, a.dim, g);
+#pragma unroll
+                for (int q = 0; q < 8; q++) x[v][q] += g[q];
+            }
+        }
+    };
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    constexpr int EB = Loader<DT>::kElemBytes;
+    const int kgs = QUANT ? (int)k_groups(a.q.K) : 0, total = QUANT ? (int)row_tiles(a.q.rows) * kRowTile : a.rows;
+    // every thread of the CTA goes through the same number of rounds (barriers inside); a group behind the last row only keeps step
+    for (int base = blockIdx.x * a.row_groups; base < total; base += gridDim.x * a.row_groups) {
+        const int r = base + group;
+        const bool there = r < a.rows;
+        float x[VPT][8], g[8];
+#pragma unroll
+        for (int v = 0; v < VPT; v++) {
+            if (there) {
+                load8<DT, VEC>(a.y + (int64_t)r * a.ldy * EB, elem(v), rt, a.dim, x[v]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; q++) x[v][q] = 0.0f;
+            }
+        }
+        if (a.post_weight) normalise(x, a.post_weight, a.post_bias);
+        if (there) {
+            if (a.gate || a.residual) {
+                const float one = a.gate && a.gate_col == 0 ? 1.0f : 0.0f;
+                float row_gate = a.scale;
+                if (one != 0.0f) {
+                    const uint8_t *p = a.gate + (int64_t)r * a.gate_row * EB;
+                    row_gate *= __uint_as_float(Loader<DT>::one(p));
+                }
+#pragma unroll
+                for (int v = 0; v < VPT; v++) {
+                    if (a.gate && a.gate_col) {
+                        load8<DT, VEC>(a.gate + (int64_t)r * a.gate_row * EB, elem(v), rt, a.dim, g);
+#pragma unroll
+                        for (int q = 0; q < 8; q++) x[v][q] *= g[q];
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; q++) g[q] = 0.0f;
+                    if (a.residual) load8<DT, VEC>(a.residual + (int64_t)r * a.ldr * EB, elem(v), rt, a.dim, g);
+#pragma unroll
+                    for (int q = 0; q < 8; q++) x[v][q] = fmaf(row_gate, x[v][q], g[q]);
+                }
+            } else if (a.scale != 1.0f) {
+#pragma unroll
+                for (int v = 0; v < VPT; v++)
+#pragma unroll
+                    for (int q = 0; q < 8; q++) x[v][q] *= a.scale;
+            }
+            if (a.h) {
+#pragma unroll
+                for (int v = 0; v < VPT; v++) store8<DT, VEC>(a.h + (int64_t)r * a.ldh * EB, elem(v), rt, a.dim, x[v]);
+            }
+        }
+        if (!QUANT && !a.n) continue;
+        normalise(x, a.weight, a.bias);
+        if (!QUANT) {
+            if (there) {
+#pragma unroll
+                for (int v = 0; v < VPT; v++) store8<DT, VEC>(a.n + (int64_t)r * a.ldn * EB, elem(v), rt, a.dim, x[v]);
+            }
+            continue;
+        }
+        uint8_t *row = row_buffer + group * a.dim * EB;
+#pragma unroll
+        for (int v = 0; v < VPT; v++) {
+            if (VEC) {                                            // eight neighbours: one piece of 16 bytes, fp32 two
+                if (elem(v) < a.dim) {
+                    if (DT == BD_F32) {
+                        *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(__float_as_uint(x[v][0]), __float_as_uint(x[v][1]), __float_as_uint(x[v][2]), __float_as_uint(x[v][3]));
+                        *(uint4 *)(row + place<DT>(elem(v) + 4)) = make_uint4(__float_as_uint(x[v][4]), __float_as_uint(x[v][5]), __float_as_uint(x[v][6]), __float_as_uint(x[v][7]));
+                    } else {
+                        *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(pair_of<DT>(x[v][0], x[v][1]), pair_of<DT>(x[v][2], x[v][3]), pair_of<DT>(x[v][4], x[v][5]), pair_of<DT>(x[v][6], x[v][7]));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; q++)
+                    if (elem(v) + q * rt < a.dim) {
+                        if (DT == BD_F32) *(float *)(row + place<DT>(elem(v) + q * rt)) = x[v][q];
+                        else *(uint16_t *)(row + place<DT>(elem(v) + q * rt)) = (uint16_t)pair_of<DT>(x[v][q], 0.0f);
+                    }
+            }
+        }
+        if (warps == 1) __syncwarp();
+        else __syncthreads();
+        const int nb = a.dim / kBlock;
+        for (int b0 = 0; b0 < kgs * kBlocksPerAtom; b0 += rt) {   // (whole quads of lanes: rt is a multiple of 32)
+            const int b = b0 + t;
+            BlockResult res;
+            res.id = 0; res.scale = 0;
+            if (there && b < nb) {
+                uint32_t unused[8];
+                if (DT == BD_BF16) {
+                    uint32_t pairs[16];
+#pragma unroll
+                    for (int p = 0; p < 4; p++) {
+                        const uint4 u = *(const uint4 *)(row + place<DT>(b * kBlock + 8 * p));
+                        pairs[4 * p] = u.x; pairs[4 * p + 1] = u.y; pairs[4 * p + 2] = u.z; pairs[4 * p + 3] = u.w;
+                    }
+                    quantize_bf16_block<false>(pairs, tab, res, unused);
+                } else {
+                    uint32_t bits[32];
+#pragma unroll
+                    for (int p = 0; p < 2 * EB; p++) {
+                        const uint4 u = *(const uint4 *)(row + place<DT>(b * kBlock + 16 / EB * p));
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            if (DT == BD_F32) {
+                                bits[4 * p + q] = w[q];
+                            } else {
+                                const float2 f = __half22float2(*(const __half2 *)&w[q]);
+                                bits[(8 * p + 2 * q) % 32] = __float_as_uint(f.x);
+                                bits[(8 * p + 2 * q + 1) % 32] = __float_as_uint(f.y);
+                            }
+                        }
+                    }
+                    bool nonfinite;
+                    quantize_two_stage_f32<false>(bits, tab, res, unused, nonfinite);
+                    if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
+                }
+                *(uint4 *)(a.q.codes + (int64_t)r * a.q.ldc + (int64_t)b * 16) = make_uint4(res.words[0], res.words[1], res.words[2], res.words[3]);
+            }
+            // four neighbouring lanes' scale bytes and id nibbles go out together; padding of the atoms as zeros
+            uint32_t sc = res.scale << (8 * (t & 3)), idn = res.id << (4 * (t & 3));
+            sc |= __shfl_xor_sync(0xffffffffu, sc, 1);
+            idn |= __shfl_xor_sync(0xffffffffu, idn, 1);
+            sc |= __shfl_xor_sync(0xffffffffu, sc, 2);
+            idn |= __shfl_xor_sync(0xffffffffu, idn, 2);
+            if ((t & 3) == 0 && b < kgs * kBlocksPerAtom && r < total) {
+                *(uint32_t *)(a.q.scales + scale_offset(a.q.rows, r, b)) = sc;
+                *(uint16_t *)(a.q.ids + id_byte_offset(a.q.rows, r, b)) = (uint16_t)idn;
+            }
+        }
+        if (warps == 1) __syncwarp();
+        else __syncthreads();                                     // the buffer is the next round's
+    }
+}
+
+}  // namespace nm
+}  // namespace bd
