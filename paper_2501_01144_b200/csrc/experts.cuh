@@ -220,7 +220,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             const uint32_t tx_pair = 2u * ((8u << t.box) * BK + 3u * kScaleAtomBytes);
             const int sf_row = t.expert * p.k_tiles * p.row_tiles + t.w_pair * 2 + (int)rank;
             for (int kt = 0; kt < p.k_tiles; kt++) {
-                if (!mbar_wait(x_empty(s), ph, abort_flag)) break;
+                if (!mbar_wait_warp(x_empty(s), ph, abort_flag)) break;
                 const uint32_t fb = x_full_leader + 8u * (uint32_t)s;
                 if (elect_one()) {
                     if (rank == 0) mbar_expect_tx(x_full(s), tx_pair);
@@ -244,7 +244,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             const bool have_ids = my_row_tile < rows;
             const uint8_t *ids = p.ids + (int64_t)t.expert * p.ids_stride + (int64_t)my_row_tile * kIdAtomBytes;
             for (int kt = 0; kt < p.k_tiles; kt++) {
-                if (!mbar_wait(c_empty(s), ph, abort_flag)) break;
+                if (!mbar_wait_warp(c_empty(s), ph, abort_flag)) break;
                 if (elect_one() && !(skip_first && i == 0 && kt == 0)) {
                     mbar_expect_tx(c_full(s), kCodeTile + (have_ids ? kIdAtomBytes : 0));
                     tma_load_3d(code_tile(s), &maps.codes, kt * (BK / 2), my_row_tile * 128, t.expert, c_full(s));
@@ -269,11 +269,11 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             bool ready = false;
             for (int i = 0; next(i, t); i++) {
                 const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17;
-                if (i > 0) mbar_wait(tmem_empty_bar, (uint32_t)(i - 1) & 1u, abort_flag);
+                if (i > 0) mbar_wait_warp(tmem_empty_bar, (uint32_t)(i - 1) & 1u, abort_flag);
                 tcgen05_fence_after();
                 for (int kt = 0; kt < p.k_tiles; kt++) {
                     if (!ready) {
-                        if (!mbar_wait(x_full(s), ph_s, abort_flag) || !mbar_wait(a_full(b), ph_b, abort_flag)) break;
+                        if (!mbar_wait_warp(x_full(s), ph_s, abort_flag) || !mbar_wait_warp(a_full(b), ph_b, abort_flag)) break;
                     }
                     tcgen05_fence_after();
                     const uint32_t lo_sfw = lo_sfw0 + (uint32_t)s * (kScaleAtomBytes >> 4);
@@ -326,15 +326,13 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         for (int g = group; g < total_k; g += kDecodeGroups) {
             uint4 w[4];
             uint32_t ids16 = 0;
-            if (!dead) dead = !mbar_wait(c_full(s), s_par, abort_flag);
+            if (!dead) dead = !mbar_wait_warp(c_full(s), s_par, abort_flag);
             if (!dead) {
                 const uint8_t *codes = base_ptr + L::codes + s * kCodeTile + j * 64;
                 ids16 = *(const uint16_t *)(base_ptr + L::ids + s * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
 #pragma unroll
                 for (int c = 0; c < 4; c++) w[c] = *(const uint4 *)(codes + 16 * (c ^ swz64));
-                __syncwarp();
-                if (lane == 0) mbar_arrive_local(c_empty(s));
-                dead = !mbar_wait(a_empty(b), b_par, abort_flag);
+                dead = !mbar_wait_warp(a_empty(b), b_par, abort_flag);
             }
             if (!dead) {
                 tcgen05_fence_after();                            // the MMAs that read this buffer have completed
@@ -351,6 +349,10 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 }
                 tcgen05_wait_st();
                 tcgen05_fence_before();
+                // The codes' stage goes back only here, after what was read from it has been used: handed back right behind the loads, a
+                // warp that then waits long for its operand buffer has been seen to decode the stage's next contents.
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(c_empty(s));
             }
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");   // the four warps of this group are done
             if (group_leader && !dead) mbar_arrive_cluster(a_full_leader + 8u * b);
@@ -378,7 +380,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             return stage_turn * kStageOut;
         };
         for (int i = 0; next(i, t); i++) {
-            mbar_wait(tmem_full_bar, (uint32_t)i & 1u, abort_flag, 256);
+            mbar_wait_warp(tmem_full_bar, (uint32_t)i & 1u, abort_flag, 256);
             tcgen05_fence_after();
             const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + kColD;
             if (GATED) {
@@ -411,6 +413,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                     for (int k = 0; k < 32; k++)
                         bits[k] = __float_as_uint(gated(__uint_as_float(tile_g[lane * 32 + (k ^ lane)]), __uint_as_float(tile_u[lane * 32 + (k ^ lane)]), p.gelu));
                     asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory");   // the tiles may be written again
+                    __syncwarp();
                     if (tok < t.live && !*abort_flag) {
                         BlockResult res;
                         res.scale = 0;
@@ -426,6 +429,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                         // (blocks behind the last one, up to the atom's four: zeros)
                         p.h_scales[((int64_t)(b / kBlocksPerAtom) * tiles_h + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4 + b % kBlocksPerAtom] = (uint8_t)res.scale;
                     }
+                    __syncwarp();                                 // (the whole warp loads from tensor memory again)
                 }
             } else {
                 // chunks of 32 tokens: the first half's warps take the larger part

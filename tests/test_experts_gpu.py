@@ -109,6 +109,18 @@ def test_tokens_of_every_number_per_expert(counts):
     check(tokens_of(tokens, 256, torch.bfloat16), ids, w, up, down, dtype=torch.bfloat16)
 
 
+@pytest.mark.parametrize("tokens,hidden,inter,n", [(700, 1024, 4096, 1024), (300, 256, 8192, 4096)])
+def test_many_items_for_every_cluster(tokens, hidden, inter, n):
+    up, down = weights(2, hidden, inter, n)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ids = torch.randint(0, 2, (tokens, 1), generator=g, device="cuda", dtype=torch.int32)
+    x, w = tokens_of(tokens, hidden, torch.bfloat16), torch.rand(tokens, 1, generator=g, device="cuda")
+    y = check(x, ids, w, up, down)
+    plan = bd.expert_plan(ids, 2)
+    for _ in range(8):
+        assert torch.equal(bd.expert_mlp(x, plan, w, up, down, dtype=torch.float32), y)
+
+
 def test_sizes_of_a_model():
     up, down = weights(8, 2048, 1408, 2048)
     g = torch.Generator(device="cuda").manual_seed(3)
