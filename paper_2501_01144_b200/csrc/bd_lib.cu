@@ -631,10 +631,10 @@ struct ExpertSpace {
 ExpertSpace expert_space(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype) {
     ExpertSpace s;
     s.rows = ex::padded_rows(tokens * top_k, up->experts);
-    const size_t x = (size_t)s.rows * (size_t)up->K, y = (size_t)s.rows * (size_t)down->rows * (size_t)elem_bytes(ydtype);
+    const size_t x = (size_t)s.rows * (size_t)ex::row_pitch(up->K), y = (size_t)s.rows * (size_t)down->rows * (size_t)elem_bytes(ydtype);
     s.x_scales = align256(std::max(x, y));
     s.h = s.x_scales + align256((size_t)(s.rows / kRowTile * k_groups(up->K)) * kScaleAtomBytes);
-    s.h_scales = s.h + align256((size_t)s.rows * (size_t)down->K);
+    s.h_scales = s.h + align256((size_t)s.rows * (size_t)ex::row_pitch(down->K));
     s.total = s.h_scales + align256((size_t)(s.rows / kRowTile * k_groups(down->K)) * kScaleAtomBytes);
     return s;
 }
@@ -646,7 +646,7 @@ bd_status check_expert_pair(int64_t tokens, int64_t top_k, const bd_experts *up,
     if (up->experts != down->experts || up->rows != 2 * down->K || down->rows % 8) return BD_ERR_SHAPE;
     if (top_k > rt::kMaxTopK || tokens > (1ll << 30) / top_k) return BD_ERR_UNSUPPORTED;
     const int64_t rows = ex::padded_rows(tokens * top_k, up->experts), pairs = (std::max(up->rows, down->rows) + 255) / 256;
-    if (rows / kRowTile * std::max(k_groups(up->K), k_groups(down->K)) >= (1ll << 31) || (rows / 256 + up->experts + 1) * pairs >= (1ll << 30) ||
+    if (rows / kRowTile * std::max(k_groups(up->K), k_groups(down->K)) >= (1ll << 31) || (rows / 128 + up->experts + 1) * pairs >= (1ll << 30) ||
         tokens * k_groups(up->K) * kBlocksPerAtom >= (1ll << 31) - 32)
         return BD_ERR_UNSUPPORTED;
     return BD_OK;
@@ -1775,23 +1775,27 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     else if (xdtype == BD_BF16) launch_spread<BD_BF16>(X, ldx, plan, up, sp, ws, st);
     else launch_spread<BD_F16>(X, ldx, plan, up, sp, ws, st);
     if ((s = launch_result())) return s;
-    const int64_t rows = tokens * plan->top_k, most = rows / 256 + std::min(rows, up->experts);   // items of 256 tokens
+    // Few rows per expert: items of at most 128 tokens (two accumulators, more stages for the codes); else of 256, so that an expert's weights
+    // are expanded once for as many tokens as possible.
+    const int64_t rows = tokens * plan->top_k, used = std::min(rows, up->experts);
+    const bool narrow = rows <= 64 * used;
+    const int64_t most = rows / (narrow ? 128 : 256) + used;      // items per 256 weight rows
     const ex::Experts e{plan->count, plan->start, (int)up->experts, (int)sp.rows};
     ex::Product p{};
     p.live_k = (int)(down->K / kBlock);
     p.h = ws + sp.h;
     p.h_scales = ws + sp.h_scales;
-    p.inter = down->K;
+    p.h_pitch = ex::row_pitch(down->K);
     p.gelu = act == BD_ACT_GELU;
-    cudaError_t err = ex::launch_product<true>(ws, ws + sp.x_scales, e, most, up, p, nullptr, false, st);
+    cudaError_t err = (narrow ? ex::launch_product<true, 128> : ex::launch_product<true, 256>)(ws, ws + sp.x_scales, e, most, up, p, nullptr, false, st);
     if (err != cudaSuccess) return cuda_result(err);
     g_launches += 1;
     if (inner) {
         launch_serialized(ex::inner_kernel, (unsigned)std::min<int64_t>((rows * (down->K / kBlock) + 255) / 256, 148 * 8), 256, 0, st, (const uint8_t *)p.h,
-                          (const uint8_t *)p.h_scales, plan->place, rows, (int)sp.rows, (int)down->K, inner);
+                          (const uint8_t *)p.h_scales, plan->place, rows, (int)sp.rows, (int)down->K, p.h_pitch, inner);
         if ((s = launch_result())) return s;
     }
-    err = ex::launch_product<false>(p.h, p.h_scales, e, most, down, p, ws, ydtype == BD_BF16, st);
+    err = (narrow ? ex::launch_product<false, 128> : ex::launch_product<false, 256>)(p.h, p.h_scales, e, most, down, p, ws, ydtype == BD_BF16, st);
     if (err != cudaSuccess) return cuda_result(err);
     g_launches += 1;
     const unsigned grid = (unsigned)std::min<int64_t>((tokens * (down->rows / 8) + 255) / 256, 148 * 16);

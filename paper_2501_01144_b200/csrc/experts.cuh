@@ -33,45 +33,70 @@ inline int64_t padded_rows(int64_t assignments, int64_t experts) {
     const int64_t used = experts < assignments ? experts : assignments;
     return (assignments + (kRowAlign - 1) * used) / kRowAlign * kRowAlign;
 }
+// Bytes between the rows of an operand that a product reads: whole k-groups (the part behind K holds zeros).
+__host__ __device__ inline int64_t row_pitch(int64_t K) { return (K + 127) / 128 * 128; }
 
 struct Experts {                             // what the kernels know of the plan
     const int32_t *count, *start;
     int experts, rows;                       // rows: of the padded operand
 };
 struct Maps {
-    CUtensorMap x[kBoxes], codes, sfw, sfx, y;
+    CUtensorMap x[kBoxes], codes, ids, sfw, sfx, y;
 };
 struct Product {
-    const uint8_t *ids;                      // of all experts
-    int64_t ids_stride;                      // bytes between experts
-    int w_pairs, row_tiles, k_tiles, clusters;
+    int w_pairs, row_tiles, k_groups, clusters;
     int live_k;                              // GATED: blocks of the result (inter / 32)
-    uint8_t *h;                              // GATED: operand bytes [rows][inter] and scale atoms of the result
+    uint8_t *h;                              // GATED: operand bytes [rows][row_pitch(inter)] and scale atoms of the result
     uint8_t *h_scales;
-    int64_t inter;
+    int64_t h_pitch;
     int gelu;
     int y_bf16;
 };
 
-// Shared memory: the rings of gemm_tc.cuh, the schedule, and staging for the epilogue (GATED: 8 KiB a warp).
-template <bool GATED>
+// A k-step is 256 elements of K, two k-groups.  The hand-overs of a k-step (a barrier wait, an election, a copy instruction: some 70 ns
+// each for the one thread that does it) set the pace of the narrow items and much of the wide ones', whatever a step holds; with
+// steps of 128 they took 0.33 to 0.4 us each.
+constexpr int kStep = 2;                     // k-groups of a k-step
+constexpr int kGroupBytes = 128;             // operand bytes of a row and k-group
+constexpr int kCodeBytes = 128 * kStep * 64; // packed codes of 128 weight rows
+constexpr int kBufs = 3;                     // decoded k-steps in tensor memory (64 columns each)
+
+// Warps: four for control (token producer, MMA issuer, code producer, one idle), three decode groups, two epilogue halves.  Each is a
+// warpgroup, since registers are handed from one to the other: at launch every thread has kLaunchRegs.
+constexpr int kDecode0 = 4, kGroups = 3, kEpilogue0 = kDecode0 + 4 * kGroups, kBlockThreads = 32 * (kEpilogue0 + kEpilogueWarps);
+constexpr int kLaunchRegs = 80, kControlRegs = 40, kDecodeRegs = 56, kEpilogueRegs = 136;
+static_assert(128 * kControlRegs + 128 * kGroups * kDecodeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kLaunchRegs * kBlockThreads, "more registers than the launch brings");
+
+// TOK: most tokens of an item.  256: one accumulator of 256 columns.  128, where experts have few tokens: two accumulators, so that
+// the next item's products run while one is read out, smaller token stages and more stages for the codes.
+template <bool GATED, int TOK>
 struct Layout {
-    static constexpr int kStage = GATED ? 8192 : 4096;
+    static constexpr int kSlots = 256 / TOK;                     // accumulators
+    static constexpr int kXS = TOK == 256 ? 3 : 4, kCS = TOK == 256 ? 3 : 5;
+    static constexpr int kXBytes = kStep * (TOK / 2) * kGroupBytes;
+    static constexpr int kSfxBytes = kStep * (TOK / 128) * kScaleAtomBytes;
+    static constexpr int kStage = GATED ? 8192 : 4096;           // epilogue staging of a warp
     static constexpr int x = 0;
-    static constexpr int codes = x + kXStages * kXTile;
-    static constexpr int sfw = codes + kCodeStages * kCodeTile;
-    static constexpr int sfx = sfw + kXStages * kScaleAtomBytes;
-    static constexpr int ids = sfx + kXStages * 2 * kScaleAtomBytes;
-    static constexpr int bars = ids + kCodeStages * kIdAtomBytes;
-    static constexpr int words = bars + 512;
+    static constexpr int codes = x + kXS * kXBytes;
+    static constexpr int sfw = codes + kCS * kCodeBytes;
+    static constexpr int sfx = sfw + kXS * kStep * kScaleAtomBytes;
+    static constexpr int ids = sfx + kXS * kSfxBytes;
+    static constexpr int bars = ids + kCS * kStep * kIdAtomBytes;
+    static constexpr int words = bars + 256;
+    static constexpr int seen = words + 16;                      // a word per decode warp
     static constexpr int luts = words + 64;
+    static_assert(16 + 4 * 4 * kGroups <= 64, "words");
     static constexpr int qtab = luts + 128;
     static constexpr int first = (qtab + (int)sizeof(SmemTables) + 15) / 16 * 16;   // first item of each expert
     static constexpr int count = first + 4 * (kMaxExperts + 4);
     static constexpr int out = (count + 4 * kMaxExperts + 1023) / 1024 * 1024;
     static constexpr int total = out + kEpilogueWarps * kStage + 1024 /* alignment slack */;
+    static_assert((2 * kXS + 2 * kCS + 2 * kBufs + 2 * kSlots) * 8 <= 256, "barrier area too small");
+    static_assert(total <= 227 * 1024, "shared memory budget");
+    // tensor memory columns: accumulators, decoded weights, scales of the weights and of the tokens (per k-group 4, and 4 per 128 tokens)
+    static constexpr int kColA = 256, kColSfW = kColA + 64 * kBufs, kColSfX = kColSfW + 4 * kStep;
+    static_assert(kColSfX + kStep * 4 * (TOK / 128) <= 512, "tensor memory budget");
 };
-static_assert(Layout<true>::total <= 227 * 1024, "shared memory budget");
 
 struct Item {
     int expert, w_pair;
@@ -81,6 +106,7 @@ struct Item {
     int box;                                 // tensor map of the token operand: 8 << box rows per CTA
 };
 // Items of cluster c: c, c + clusters, ...; numbered expert by expert, then weight rows, the token tile running fastest.
+template <int TOK>
 struct Walk {
     const int *first, *count;
     const int32_t *start;
@@ -91,11 +117,11 @@ struct Walk {
         const int item = i * clusters + c;
         if (item >= first[experts]) return false;
         while (item >= first[e + 1]) e++;
-        const int cnt = count[e], tiles = (cnt + 255) / 256, in = item - first[e], tt = in % tiles;
+        const int cnt = count[e], tiles = (cnt + TOK - 1) / TOK, in = item - first[e], tt = in % tiles;
         t.expert = e;
         t.w_pair = in / tiles;
-        t.row0 = __ldg(start + e) + tt * 256;
-        t.live = min(256, cnt - tt * 256);
+        t.row0 = __ldg(start + e) + tt * TOK;
+        t.live = min(TOK, cnt - tt * TOK);
         t.n = (t.live + 15) / 16 * 16;
         t.box = t.n <= 16 ? 0 : 28 - __clz(t.n - 1);               // 8 << box >= n / 2
         return true;
@@ -108,27 +134,39 @@ __device__ __forceinline__ float gated(float g, float u, int gelu) {
     return __fdividef(g, 1.0f + __expf(-a)) * u;
 }
 
-template <bool GATED>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+template <int N>
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// TMA load whose completion is counted on a barrier of the pair's leader CTA.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+template <bool GATED, int TOK>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
-    using L = Layout<GATED>;
+    using L = Layout<GATED, TOK>;
+    constexpr int kXS = L::kXS, kCS = L::kCS, kSlots = L::kSlots;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    auto x_tile = [&](int s) { return base + L::x + (uint32_t)s * kXTile; };
-    auto code_tile = [&](int s) { return base + L::codes + (uint32_t)s * kCodeTile; };
-    auto sfw_tile = [&](int s) { return base + L::sfw + (uint32_t)s * kScaleAtomBytes; };
-    auto sfx_tile = [&](int s) { return base + L::sfx + (uint32_t)s * 2 * kScaleAtomBytes; };
-    auto id_tile = [&](int s) { return base + L::ids + (uint32_t)s * kIdAtomBytes; };
+    auto x_tile = [&](int s) { return base + L::x + (uint32_t)s * L::kXBytes; };
+    auto code_tile = [&](int s) { return base + L::codes + (uint32_t)s * kCodeBytes; };
+    auto sfw_tile = [&](int s) { return base + L::sfw + (uint32_t)s * (kStep * kScaleAtomBytes); };
+    auto sfx_tile = [&](int s) { return base + L::sfx + (uint32_t)s * L::kSfxBytes; };
+    auto id_tile = [&](int s) { return base + L::ids + (uint32_t)s * (kStep * kIdAtomBytes); };
     const uint32_t bars = base + L::bars;
-    auto x_full = [&](int s) { return bars + 8u * s; };                                   // leader: tile + scales of both CTAs
-    auto x_empty = [&](int s) { return bars + 8u * (kXStages + s); };                     // both: stage consumed by the MMA
-    auto c_full = [&](int s) { return bars + 8u * (2 * kXStages + s); };                  // local: codes + ids landed
-    auto c_empty = [&](int s) { return bars + 8u * (2 * kXStages + kCodeStages + s); };   // local: codes read by the decode group
-    auto a_full = [&](int b) { return bars + 8u * (2 * kXStages + 2 * kCodeStages + b); };            // leader: buffer written in both CTAs
-    auto a_empty = [&](int b) { return bars + 8u * (2 * kXStages + 2 * kCodeStages + kABufs + b); };  // both: buffer consumed
-    const uint32_t tmem_full_bar = bars + 8u * (2 * kXStages + 2 * kCodeStages + 2 * kABufs);         // both: accumulator complete
-    const uint32_t tmem_empty_bar = tmem_full_bar + 8u;                                               // leader: accumulator read out
+    auto x_full = [&](int s) { return bars + 8u * s; };                           // leader: tile + scales of both CTAs
+    auto x_empty = [&](int s) { return bars + 8u * (kXS + s); };                  // both: stage consumed by the MMA
+    auto c_full = [&](int s) { return bars + 8u * (2 * kXS + s); };               // local: codes + ids landed
+    auto c_empty = [&](int s) { return bars + 8u * (2 * kXS + kCS + s); };        // local: codes read by the decode group
+    auto a_full = [&](int b) { return bars + 8u * (2 * kXS + 2 * kCS + b); };             // leader: buffer written in both CTAs
+    auto a_empty = [&](int b) { return bars + 8u * (2 * kXS + 2 * kCS + kBufs + b); };    // both: buffer consumed
+    auto d_full = [&](int d) { return bars + 8u * (2 * kXS + 2 * kCS + 2 * kBufs + d); };            // both: accumulator complete
+    auto d_empty = [&](int d) { return bars + 8u * (2 * kXS + 2 * kCS + 2 * kBufs + kSlots + d); };  // leader: accumulator read out
     volatile uint32_t *const shared_words = (volatile uint32_t *)(base_ptr + L::words);
     volatile uint32_t *const tmem_slot = shared_words;
     volatile uint32_t *const abort_flag = shared_words + 1;
@@ -143,20 +181,22 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         abort_flag[0] = 0;
         abort_flag[1] = 0;                                        // set once the previous kernel has completed
         abort_flag[2] = g_debug_spin_limit ? g_debug_spin_limit : kSpinLimit;
-        for (int s = 0; s < kXStages; s++) {
+        for (int s = 0; s < kXS; s++) {
             mbar_init(x_full(s), 1);
             mbar_init(x_empty(s), 1);
         }
-        for (int s = 0; s < kCodeStages; s++) {
+        for (int s = 0; s < kCS; s++) {
             mbar_init(c_full(s), 1);
             mbar_init(c_empty(s), 4);                             // one arrival per warp of the decode group
         }
-        for (int b = 0; b < kABufs; b++) {
+        for (int b = 0; b < kBufs; b++) {
             mbar_init(a_full(b), 2);                              // one arrival per CTA of the pair
             mbar_init(a_empty(b), 1);
         }
-        mbar_init(tmem_full_bar, 1);
-        mbar_init(tmem_empty_bar, 2 * kEpilogueWarps);            // the epilogue warps of both CTAs
+        for (int d = 0; d < kSlots; d++) {
+            mbar_init(d_full(d), 1);
+            mbar_init(d_empty(d), 2 * kEpilogueWarps);            // the epilogue warps of both CTAs
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x < 32)
@@ -185,7 +225,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 }
                 count[e] = cnt;
             }
-            const int items = (cnt + 255) / 256 * p.w_pairs;
+            const int items = (cnt + TOK - 1) / TOK * p.w_pairs;
             int incl = items;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -202,101 +242,108 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     cluster_sync_all();                                           // both CTAs: barriers initialised, TMEM allocated
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
-    Walk next(first, count, ex.start, ex.experts, p.clusters, cluster);
+    const int steps = (p.k_groups + kStep - 1) / kStep;
+    Walk<TOK> next(first, count, ex.start, ex.experts, p.clusters, cluster);
     Item t;
 
-    if (warp == 0) {
-        // ---- TMA producer of the token tile and the scale atoms; the one warp that reads what the kernel in front wrote ----
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        if (lane == 0) abort_flag[1] = 1;                         // from here on every bounded wait counts its polls
-        int s = 0;
-        uint32_t ph = 1;
-        const uint32_t x_full_leader = map_to_cta(x_full(0), 0);
-        const int tiles_x = ex.rows / kRowAlign;
-        for (int i = 0; next(i, t); i++) {
-            // each CTA holds half of the MMA's tokens (and, where the box is higher, rows that are not looked at)
-            const int t0 = t.row0 + (int)rank * (t.n / 2);
-            const uint32_t tx_pair = 2u * ((8u << t.box) * BK + 3u * kScaleAtomBytes);
-            const int sf_row = t.expert * p.k_tiles * p.row_tiles + t.w_pair * 2 + (int)rank;
-            for (int kt = 0; kt < p.k_tiles; kt++) {
-                if (!mbar_wait_warp(x_empty(s), ph, abort_flag)) break;
-                const uint32_t fb = x_full_leader + 8u * (uint32_t)s;
-                if (elect_one()) {
-                    if (rank == 0) mbar_expect_tx(x_full(s), tx_pair);
-                    tma_load_2d_pair(x_tile(s), &maps.x[t.box], kt * BK, t0, fb);
-                    tma_load_2d_pair(sfw_tile(s), &maps.sfw, 0, sf_row + kt * p.row_tiles, fb);
-                    tma_load_2d_pair(sfx_tile(s), &maps.sfx, 0, kt * tiles_x + t.row0 / kRowAlign, fb);
+    if (warp < kDecode0) {
+        registers_down<kControlRegs>();
+        if (warp == 0) {
+            // ---- TMA producer of the token tile and the scale atoms; the one warp that reads what the kernel in front wrote ----
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            if (lane == 0) abort_flag[1] = 1;                     // from here on every bounded wait counts its polls
+            int s = 0;
+            uint32_t ph = 1;
+            const uint32_t x_full_leader = map_to_cta(x_full(0), 0);
+            for (int i = 0; next(i, t); i++) {
+                // each CTA holds half of the MMA's tokens (and, where the box is higher, rows that are not looked at)
+                const int t0 = t.row0 + (int)rank * (t.n / 2), sf_z = t.expert * p.k_groups;
+                const uint32_t tx_pair = 2u * (kStep * (8u << t.box) * kGroupBytes + kStep * kScaleAtomBytes + L::kSfxBytes);
+                for (int k = 0; k < steps; k++) {
+                    if (!mbar_wait_warp(x_empty(s), ph, abort_flag)) break;
+                    const uint32_t fb = x_full_leader + 8u * (uint32_t)s;
+                    if (elect_one()) {
+                        if (rank == 0) mbar_expect_tx(x_full(s), tx_pair);
+                        tma_load_3d_pair(x_tile(s), &maps.x[t.box], 0, t0, kStep * k, fb);
+                        tma_load_3d_pair(sfw_tile(s), &maps.sfw, 0, t.w_pair * 2 + (int)rank, sf_z + kStep * k, fb);
+                        tma_load_3d_pair(sfx_tile(s), &maps.sfx, 0, t.row0 / kRowAlign, kStep * k, fb);
+                    }
+                    __syncwarp();
+                    if (++s == kXS) { s = 0; ph ^= 1u; }
                 }
-                __syncwarp();
-                if (++s == kXStages) { s = 0; ph ^= 1u; }
+                if (*abort_flag) break;
             }
-            if (*abort_flag) break;
-        }
-    } else if (warp == 2) {
-        // ---- TMA producer of this CTA's packed codes and ids ----
-        int s = 0;
-        uint32_t ph = 1;
-        const bool skip_first = g_debug_skip_first_code_stage != 0;   // test hook: see bd_debug_fault
-        const int rows = p.row_tiles;
-        for (int i = 0; next(i, t); i++) {
-            const int my_row_tile = t.w_pair * 2 + (int)rank;
-            const bool have_ids = my_row_tile < rows;
-            const uint8_t *ids = p.ids + (int64_t)t.expert * p.ids_stride + (int64_t)my_row_tile * kIdAtomBytes;
-            for (int kt = 0; kt < p.k_tiles; kt++) {
-                if (!mbar_wait_warp(c_empty(s), ph, abort_flag)) break;
-                if (elect_one() && !(skip_first && i == 0 && kt == 0)) {
-                    mbar_expect_tx(c_full(s), kCodeTile + (have_ids ? kIdAtomBytes : 0));
-                    tma_load_3d(code_tile(s), &maps.codes, kt * (BK / 2), my_row_tile * 128, t.expert, c_full(s));
-                    if (have_ids) bulk_load(id_tile(s), ids + (int64_t)kt * rows * kIdAtomBytes, kIdAtomBytes, c_full(s));
+        } else if (warp == 2) {
+            // ---- TMA producer of this CTA's packed codes and ids ----
+            int s = 0;
+            uint32_t ph = 1;
+            const bool skip_first = g_debug_skip_first_code_stage != 0;   // test hook: see bd_debug_fault
+            for (int i = 0; next(i, t); i++) {
+                const int my_tile = t.w_pair * 2 + (int)rank, id_z = t.expert * p.k_groups;
+                for (int k = 0; k < steps; k++) {
+                    if (!mbar_wait_warp(c_empty(s), ph, abort_flag)) break;
+                    if (elect_one() && !(skip_first && i == 0 && k == 0)) {
+                        mbar_expect_tx(c_full(s), kCodeBytes + kStep * kIdAtomBytes);
+                        tma_load_3d(code_tile(s), &maps.codes, k * (kStep * 64), my_tile * 128, t.expert, c_full(s));
+                        tma_load_3d(id_tile(s), &maps.ids, 0, my_tile, id_z + kStep * k, c_full(s));
+                    }
+                    __syncwarp();
+                    if (++s == kCS) { s = 0; ph ^= 1u; }
                 }
-                __syncwarp();
-                if (++s == kCodeStages) { s = 0; ph ^= 1u; }
+                if (*abort_flag) break;
             }
-            if (*abort_flag) break;
-        }
-    } else if (warp == 1) {
-        if (rank == 0) {
+        } else if (warp == 1 && rank == 0) {
             // ---- MMA issuer (leader CTA; whole warp converged, one elected lane issues) ----
             const uint32_t hi_op = desc_hi(1024, kLayoutSwizzle128), hi_sf = desc_hi(128, kLayoutNone);
             const uint32_t lo_x0 = (x_tile(0) >> 4) | 1u << 16;
             const uint32_t lo_sfw0 = sfw_tile(0) >> 4, lo_sfx0 = sfx_tile(0) >> 4;
             // (instruction descriptor: see gemm_tc.cuh; N >> 3 at bit 17 follows the item)
             const uint32_t idesc_m = 1u << 23 | (uint32_t)(256 >> 4) << 24;
-            const uint32_t t_d = tmem + kColD, t_sfw = tmem + kColSfW, t_sfx = tmem + kColSfX;
+            const uint32_t t_sfw = tmem + L::kColSfW, t_sfx = tmem + L::kColSfX;
             int s = 0, b = 0;
             uint32_t ph_s = 0, ph_b = 0;
             bool ready = false;
             for (int i = 0; next(i, t); i++) {
-                const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17;
-                if (i > 0) mbar_wait_warp(tmem_empty_bar, (uint32_t)(i - 1) & 1u, abort_flag);
+                const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17, x_half = (8u << t.box) * kGroupBytes >> 4;
+                const int slot = i % kSlots;
+                const uint32_t t_d = tmem + (uint32_t)slot * TOK;
+                if (i >= kSlots) mbar_wait_warp(d_empty(slot), (uint32_t)(i / kSlots - 1) & 1u, abort_flag);
                 tcgen05_fence_after();
-                for (int kt = 0; kt < p.k_tiles; kt++) {
+                for (int k = 0; k < steps; k++) {
                     if (!ready) {
+                        // slow path: the probe at the end of the previous k-step found a barrier open
                         if (!mbar_wait_warp(x_full(s), ph_s, abort_flag) || !mbar_wait_warp(a_full(b), ph_b, abort_flag)) break;
                     }
                     tcgen05_fence_after();
-                    const uint32_t lo_sfw = lo_sfw0 + (uint32_t)s * (kScaleAtomBytes >> 4);
-                    const uint32_t lo_sfx = lo_sfx0 + (uint32_t)s * (2 * kScaleAtomBytes >> 4);
-                    const uint32_t lo_x = lo_x0 + (uint32_t)s * (kXTile >> 4);
-                    const uint32_t t_a = tmem + kColA + 32u * (uint32_t)b;
+                    const uint32_t lo_sfw = lo_sfw0 + (uint32_t)s * (kStep * kScaleAtomBytes >> 4);
+                    const uint32_t lo_sfx = lo_sfx0 + (uint32_t)s * (L::kSfxBytes >> 4);
+                    const uint32_t lo_x = lo_x0 + (uint32_t)s * (L::kXBytes >> 4);
+                    const uint32_t t_a = tmem + L::kColA + 64u * (uint32_t)b;
+                    const bool both = kStep * k + 1 < p.k_groups;     // (K may end with the step's first k-group)
                     if (elect_one()) {
-                        tcgen05_cp_pair(t_sfw, desc_join(lo_sfw, hi_sf));
-                        tcgen05_cp_pair(t_sfx, desc_join(lo_sfx, hi_sf));
-                        tcgen05_cp_pair(t_sfx + 4, desc_join(lo_sfx + (kScaleAtomBytes >> 4), hi_sf));
 #pragma unroll
-                        for (int k = 0; k < BK / 32; k++)
-                            tcgen05_mma_mxf8_pair_atmem(t_d, t_a + 8u * k, desc_join(lo_x + 2 * k, hi_op),
-                                                        idesc0 | (uint32_t)k << 4 | (uint32_t)k << 29, t_sfw, t_sfx,
-                                                        k == 0 ? (kt > 0 ? 1u : 0u) : 1u);
+                        for (int h = 0; h < kStep; h++) {
+                            if (h > 0 && !both) break;
+                            tcgen05_cp_pair(t_sfw + 4 * h, desc_join(lo_sfw + h * (kScaleAtomBytes >> 4), hi_sf));
+#pragma unroll
+                            for (int q = 0; q < TOK / 128; q++)
+                                tcgen05_cp_pair(t_sfx + 4 * (h * (TOK / 128) + q), desc_join(lo_sfx + (h * (TOK / 128) + q) * (kScaleAtomBytes >> 4), hi_sf));
+#pragma unroll
+                            for (int j = 0; j < 4; j++)
+                                tcgen05_mma_mxf8_pair_atmem(t_d, t_a + 32u * h + 8u * j, desc_join(lo_x + h * x_half + 2 * j, hi_op),
+                                                            idesc0 | (uint32_t)j << 4 | (uint32_t)j << 29, t_sfw + 4 * h, t_sfx + 4 * h * (TOK / 128),
+                                                            h == 0 && j == 0 ? (k > 0 ? 1u : 0u) : 1u);
+                        }
                         tcgen05_commit_pair(x_empty(s));
                         tcgen05_commit_pair(a_empty(b));
                     }
                     __syncwarp();
-                    if (++s == kXStages) { s = 0; ph_s ^= 1u; }
-                    if (++b == kABufs) { b = 0; ph_b ^= 1u; }
+                    if (++s == kXS) { s = 0; ph_s ^= 1u; }
+                    if (++b == kBufs) { b = 0; ph_b ^= 1u; }
+                    // probe the next k-step's barriers now (the rings run across items): the round trip overlaps the issue above
                     const bool x_ok = mbar_test_wait(x_full(s), ph_s), a_ok = mbar_test_wait(a_full(b), ph_b);
-                    ready = x_ok && a_ok;
+                    ready = __all_sync(0xffffffffu, x_ok && a_ok);
                 }
                 if (*abort_flag && elect_one()) {
                     // this CTA is aborting: tell the peer before its epilogue warps are woken by the commit below
@@ -304,74 +351,79 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                                  ::"r"(map_to_cta(smem_u32((const void *)abort_flag), 1)), "r"(1u) : "memory");
                 }
                 __syncwarp();
-                if (elect_one()) tcgen05_commit_pair(tmem_full_bar);
+                if (elect_one()) tcgen05_commit_pair(d_full(slot));
                 __syncwarp();
                 if (*abort_flag) break;
             }
         }
-    } else if (warp < kEpilogueWarp0) {
-        // ---- decode warps (as in gemm_tc.cuh): group g takes k-steps g, g + groups, ... counted across items ----
-        const int group = (warp - kDecodeWarp0) / 4, quad = warp % 4;
+    } else if (warp < kEpilogue0) {
+        // ---- decode warps: group g takes this CTA's k-steps g, g + groups, ... (counted across items); a warp may only touch the TMEM
+        // lanes 32 * (warp % 4) .. + 31, so thread `lane` of warp w owns weight row (and TMEM lane) j = 32 * (w % 4) + lane ----
+        registers_down<kDecodeRegs>();
+        const int group = (warp - kDecode0) / 4, quad = warp % 4;
         const int j = quad * 32 + lane;
-        const bool group_leader = (warp - kDecodeWarp0) % 4 == 0 && lane == 0;
-        const uint32_t swz64 = (uint32_t)(j >> 1) & 3u;
+        const bool group_leader = quad == 0 && lane == 0;
+        const uint32_t swz = (uint32_t)j & 7u;
         const uint32_t a_full_leader = map_to_cta(a_full(0), 0);
-        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + kColA;
+        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + L::kColA;
         const int items = first[ex.experts];
-        const int total_k = cluster < items ? ((items - cluster + p.clusters - 1) / p.clusters) * p.k_tiles : 0;
-        int s = group % kCodeStages, b = group % kABufs;
+        const int total = cluster < items ? ((items - cluster + p.clusters - 1) / p.clusters) * steps : 0;
+        int s = group % kCS, b = group % kBufs;
         uint32_t s_par = 0, b_par = 1;
-        static_assert(kDecodeGroups <= kCodeStages && kDecodeGroups <= kABufs, "one wrap per step at most");
+        static_assert(kGroups <= kCS && kGroups <= kBufs, "one wrap per step at most");
         bool dead = false;                                        // (a warp whose wait ran out keeps meeting its group at the barrier)
-        for (int g = group; g < total_k; g += kDecodeGroups) {
-            uint4 w[4];
-            uint32_t ids16 = 0;
+        for (int g = group; g < total; g += kGroups) {
+            uint4 w[8];
+            uint32_t ids[kStep] = {0, 0};
             if (!dead) dead = !mbar_wait_warp(c_full(s), s_par, abort_flag);
             if (!dead) {
-                const uint8_t *codes = base_ptr + L::codes + s * kCodeTile + j * 64;
-                ids16 = *(const uint16_t *)(base_ptr + L::ids + s * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
+                const uint8_t *codes = base_ptr + L::codes + s * kCodeBytes + j * 128;
 #pragma unroll
-                for (int c = 0; c < 4; c++) w[c] = *(const uint4 *)(codes + 16 * (c ^ swz64));
+                for (int h = 0; h < kStep; h++)
+                    ids[h] = *(const uint16_t *)(base_ptr + L::ids + (s * kStep + h) * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
+#pragma unroll
+                for (int c = 0; c < 8; c++) w[c] = *(const uint4 *)(codes + 16 * ((uint32_t)c ^ swz));
+                // The stage goes back to its producer once the loads have arrived, not only been issued: the epilogue's stores can hold them
+                // up for longer than a refill takes, and then rows were seen to be decoded from the stage's next contents.  A store of
+                // something made of all of them cannot leave before them, nor the hand-over before the store.
+                uint32_t seen = ids[0] ^ ids[1];
+#pragma unroll
+                for (int c = 0; c < 8; c++) seen ^= w[c].x;
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)L::seen + 4u * (uint32_t)(warp - kDecode0)), "r"(seen) : "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(c_empty(s));
                 dead = !mbar_wait_warp(a_empty(b), b_par, abort_flag);
             }
             if (!dead) {
                 tcgen05_fence_after();                            // the MMAs that read this buffer have completed
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    const uint32_t id = (ids16 >> (4 * c)) & 15u;
+                for (int c = 0; c < 8; c++) {
+                    const uint32_t id = (ids[c / 4] >> (4 * (c % 4))) & 15u;
                     const uint32_t lo = luts[id], hi = luts[16 + id];
                     uint32_t o[8];
                     decode_word(w[c].x, lo, hi, o[0], o[1]);
                     decode_word(w[c].y, lo, hi, o[2], o[3]);
                     decode_word(w[c].z, lo, hi, o[4], o[5]);
                     decode_word(w[c].w, lo, hi, o[6], o[7]);
-                    tcgen05_st_32x32b_x8(t_row + 32u * (uint32_t)b + 8u * (uint32_t)c, o);
+                    tcgen05_st_32x32b_x8(t_row + 64u * (uint32_t)b + 8u * (uint32_t)c, o);
                 }
                 tcgen05_wait_st();
                 tcgen05_fence_before();
-                // The codes' stage goes back only here, after what was read from it has been used: handed back right behind the loads, a
-                // warp that then waits long for its operand buffer has been seen to decode the stage's next contents.
-                __syncwarp();
-                if (lane == 0) mbar_arrive_local(c_empty(s));
             }
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");   // the four warps of this group are done
             if (group_leader && !dead) mbar_arrive_cluster(a_full_leader + 8u * b);
-            s += kDecodeGroups;
-            if (s >= kCodeStages) { s -= kCodeStages; s_par ^= 1u; }
-            b += kDecodeGroups;
-            if (b >= kABufs) { b -= kABufs; b_par ^= 1u; }
+            s += kGroups;
+            if (s >= kCS) { s -= kCS; s_par ^= 1u; }
+            b += kGroups;
+            if (b >= kBufs) { b -= kBufs; b_par ^= 1u; }
         }
     } else {
         // ---- epilogue: warp w reads the TMEM lanes 32 * (w % 4) .. + 31 (weight rows) of this CTA's accumulator ----
-        const int quad = warp % 4, half = (warp - kEpilogueWarp0) / 4, slot = half * 4 + quad;   // (the first epilogue warp need not be quadrant 0's)
-        const uint32_t tmem_empty_leader = map_to_cta(tmem_empty_bar, 0);
-        const uint32_t stage_out = base + L::out + (uint32_t)slot * L::kStage;
-        uint8_t *const stage_ptr = base_ptr + L::out + slot * L::kStage;
-        auto release_accumulator = [&]() {
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader);
-        };
+        registers_up<kEpilogueRegs>();
+        const int quad = warp % 4, half = (warp - kEpilogue0) / 4, slot_of_warp = warp - kEpilogue0;
+        const uint32_t d_empty_leader = map_to_cta(d_empty(0), 0);
+        const uint32_t stage_out = base + L::out + (uint32_t)slot_of_warp * L::kStage;
+        uint8_t *const stage_ptr = base_ptr + L::out + slot_of_warp * L::kStage;
         uint32_t stage_turn = 0;
         auto staging_free = [&]() -> uint32_t {
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
@@ -380,56 +432,88 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             return stage_turn * kStageOut;
         };
         for (int i = 0; next(i, t); i++) {
-            mbar_wait_warp(tmem_full_bar, (uint32_t)i & 1u, abort_flag, 256);
+            const int slot = i % kSlots;
+            auto release_accumulator = [&]() {
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(d_empty_leader + 8u * (uint32_t)slot);
+            };
+            mbar_wait_warp(d_full(slot), (uint32_t)(i / kSlots) & 1u, abort_flag, 256);
             tcgen05_fence_after();
-            const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + kColD;
+            const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)slot * TOK;
             if (GATED) {
                 // Tokens 64 at a time; the two epilogue halves take turns.  The warps of quadrants 2 m and 2 m + 1 hold the gate and
                 // the up rows of the same 32 channels (block 2 m of this CTA's): both store two 32 x 32 tiles of sums (element
                 // (token q, row r) at q * 32 + (r ^ q): rows are written and tokens read without bank conflicts), meet, and then the
-                // first finishes the first 32 tokens and the second the others, a token's block per lane.
+                // first finishes the first 32 tokens and the second the others, a token's block per lane.  A half's second 64 tokens
+                // wait in registers meanwhile, so that the accumulator is free before the arithmetic begins.
                 const int groups = (t.n + 63) / 64, pair = quad / 2, which = quad & 1;
                 const int b = t.w_pair * 4 + (int)rank * 2 + pair;                     // block of the result
                 const bool block_ok = b < p.live_k;
-                const uint32_t *const tile_g = (const uint32_t *)(base_ptr + L::out + (slot - which) * L::kStage) + which * 1024;
-                const uint32_t *const tile_u = (const uint32_t *)(base_ptr + L::out + (slot - which + 1) * L::kStage) + which * 1024;
-                const int tiles_h = ex.rows / kRowAlign;
-                if (half >= groups) release_accumulator();
-                for (int g = half; g < groups; g += 2) {
+                const uint32_t *const tile_g = (const uint32_t *)(base_ptr + L::out + (slot_of_warp - which) * L::kStage) + which * 1024;
+                const uint32_t *const tile_u = (const uint32_t *)(base_ptr + L::out + (slot_of_warp - which + 1) * L::kStage) + which * 1024;
+                uint32_t *const tile = (uint32_t *)stage_ptr;
+                auto put = [&](const uint32_t (&r)[32], int v) {
 #pragma unroll
-                    for (int v = 0; v < 2; v++) {
-                        uint32_t r[32];
-                        uint32_t *const tile = (uint32_t *)stage_ptr + v * 1024;
-                        tcgen05_ld_32x32b_x32(t_base + g * 64 + v * 32, r);
-                        tcgen05_wait_ld();
-                        if (v == 1 && g + 2 >= groups) release_accumulator();
+                    for (int q = 0; q < 32; q++) tile[v * 1024 + q * 32 + (lane ^ q)] = r[q];
+                };
+                auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory"); };
+                uint32_t bits[32];
+                auto activate = [&]() {
+                    meet();
 #pragma unroll
-                        for (int q = 0; q < 32; q++) tile[q * 32 + (lane ^ q)] = r[q];
-                    }
-                    asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory");
-                    const int tok = g * 64 + which * 32 + lane, row = t.row0 + tok;
-                    uint32_t bits[32];
-#pragma unroll
-                    for (int k = 0; k < 32; k++)
+                    for (int k = 0; k < 32; k++) {
                         bits[k] = __float_as_uint(gated(__uint_as_float(tile_g[lane * 32 + (k ^ lane)]), __uint_as_float(tile_u[lane * 32 + (k ^ lane)]), p.gelu));
-                    asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory");   // the tiles may be written again
-                    __syncwarp();
-                    if (tok < t.live && !*abort_flag) {
+                        if (k % 8 == 7) asm volatile("" ::: "memory");   // (no more than eight pairs on the way at a time: registers)
+                    }
+                    meet();                                       // the tiles may be written again
+                };
+                auto store = [&](int g) {
+                    const int tok = g * 64 + which * 32 + lane, row = t.row0 + tok;
+                    if (tok < t.live && b < (p.live_k + 3) / 4 * 4 && !*abort_flag) {
                         BlockResult res;
+                        uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
                         res.scale = 0;
                         if (block_ok) {
                             bool nonfinite;
-                            uint32_t o[8];
                             quantize_two_stage_f32<true>(bits, qtab, res, o, nonfinite);
                             if (nonfinite) atomicOr(&g_status_word, kStatusNonfinite);
-                            uint4 *dst = (uint4 *)(p.h + (int64_t)row * p.inter + (int64_t)b * 32);
-                            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
                         }
-                        // (blocks behind the last one, up to the atom's four: zeros)
-                        p.h_scales[((int64_t)(b / kBlocksPerAtom) * tiles_h + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4 + b % kBlocksPerAtom] = (uint8_t)res.scale;
+                        // (blocks behind the last one, up to the k-group's four: zeros)
+                        uint4 *dst = (uint4 *)(p.h + (int64_t)row * p.h_pitch + (int64_t)b * 32);
+                        dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                        dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+                        p.h_scales[((int64_t)(b / kBlocksPerAtom) * (ex.rows / kRowAlign) + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4 + b % kBlocksPerAtom] = (uint8_t)res.scale;
                     }
-                    __syncwarp();                                 // (the whole warp loads from tensor memory again)
+                    __syncwarp();                                 // (the whole warp works on tensor memory again)
+                };
+                if (half >= groups) {
+                    release_accumulator();
+                } else {
+                    const bool more = TOK == 256 && half + 2 < groups;
+                    uint32_t r[32], later[2][32];
+#pragma unroll
+                    for (int v = 0; v < 2; v++) {
+                        tcgen05_ld_32x32b_x32(t_base + half * 64 + v * 32, r);
+                        tcgen05_wait_ld();
+                        put(r, v);
+                    }
+                    if (more) {
+                        tcgen05_ld_32x32b_x32(t_base + (half + 2) * 64, later[0]);
+                        tcgen05_ld_32x32b_x32(t_base + (half + 2) * 64 + 32, later[1]);
+                        tcgen05_wait_ld();
+                    }
+                    release_accumulator();
+                    activate();
+                    if (more) {
+                        put(later[0], 0);
+                        put(later[1], 1);
+                    }
+                    store(half);
+                    if (more) {
+                        activate();
+                        store(half + 2);
+                    }
                 }
             } else {
                 // chunks of 32 tokens: the first half's warps take the larger part
@@ -463,6 +547,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                         }
                     }
                 }
+                __syncwarp();
             }
         }
         // the staging buffers must outlive the stores' reads of them; the writes themselves complete with the grid
@@ -523,11 +608,9 @@ __global__ void __launch_bounds__(256) spread_kernel(const uint8_t *__restrict__
                 atomicOr(&g_status_word, kStatusIndex);
                 continue;
             }
-            if (valid) {
-                uint4 *dst = (uint4 *)(x8 + (int64_t)row * ((int64_t)nb * 32) + b * 32u);
-                dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-                dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
-            }
+            uint4 *dst = (uint4 *)(x8 + (int64_t)row * ((int64_t)kgroups * 128) + b * 32u);   // (zeros up to the k-group's end)
+            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
             if ((b & 3u) == 0)
                 *(uint32_t *)(scales + ((int64_t)(b / 4) * (rows / kRowTile) + row / kRowTile) * kScaleAtomBytes + (row % 32) * 16 + (row % kRowTile / 32) * 4) = sc;
         }
@@ -584,7 +667,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const uint8_t *__restrict_
 
 // The values that the second product reads, for checking: out[token][slot][inter] in fp32 (zeros where no expert serves).
 __global__ void __launch_bounds__(256) inner_kernel(const uint8_t *__restrict__ h, const uint8_t *__restrict__ scales, const int32_t *__restrict__ place,
-                                                    int64_t assignments, int rows, int inter, float *__restrict__ out) {
+                                                    int64_t assignments, int rows, int inter, int64_t pitch, float *__restrict__ out) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int nb = inter / 32;
@@ -597,7 +680,7 @@ __global__ void __launch_bounds__(256) inner_kernel(const uint8_t *__restrict__ 
         for (int k = 0; k < 32; k++) {
             float v = 0.0f;
             if (there) {
-                const uint32_t x = h[(int64_t)row * inter + b * 32 + k];              // E4M3: no magnitude here is subnormal
+                const uint32_t x = h[(int64_t)row * pitch + b * 32 + k];              // E4M3: no magnitude here is subnormal
                 const uint32_t f = x >> 3 & 15u;
                 if (f) v = scalbnf(1.0f + (float)(x & 7u) * 0.125f, (int)f - 7 + e);
                 if (x & 0x80u) v = -v;
@@ -609,24 +692,27 @@ __global__ void __launch_bounds__(256) inner_kernel(const uint8_t *__restrict__ 
 
 // ---- host side ----------------------------------------------------------------------------------------------------
 inline bool make_map_3d(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, uint64_t inner, uint64_t rows, uint64_t outer, uint64_t row_bytes,
-                        uint64_t outer_bytes, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+                        uint64_t outer_bytes, uint32_t box_inner, uint32_t box_rows, uint32_t box_outer, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     cuuint64_t dims[3] = {inner, rows, outer}, strides[2] = {row_bytes, outer_bytes};
-    cuuint32_t box[3] = {box_inner, box_rows, 1}, elem[3] = {1, 1, 1};
+    cuuint32_t box[3] = {box_inner, box_rows, box_outer}, elem[3] = {1, 1, 1};
     return fn(map, type, 3, (void *)ptr, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool GATED>
+template <bool GATED, int TOK>
 inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t items_most, const bd_experts *W, Product p, void *Y, bool y_bf16, cudaStream_t st) {
+    using L = Layout<GATED, TOK>;
     Maps m;
-    const int64_t N = W->rows, K = W->K, rtw = row_tiles(N), kg = k_groups(K);
+    const int64_t N = W->rows, K = W->K, rtw = row_tiles(N), kg = k_groups(K), pitch = row_pitch(K), tiles_x = ex.rows / kRowAlign;
+    constexpr CUtensorMapDataType kBytes = CU_TENSOR_MAP_DATA_TYPE_UINT8, kWords = CU_TENSOR_MAP_DATA_TYPE_UINT32;
     for (int b = 0; b < kBoxes; b++)
-        if (!make_map_2d(&m.x[b], CU_TENSOR_MAP_DATA_TYPE_UINT8, x8, K, ex.rows, K, BK, 8u << b, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
-    if (!make_map_3d(&m.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, W->codes, K / 2, N, W->experts, K / 2, (uint64_t)N * (K / 2), 64, 128, CU_TENSOR_MAP_SWIZZLE_64B) ||
-        !make_map_2d(&m.sfw, CU_TENSOR_MAP_DATA_TYPE_UINT32, W->scales, 128, (uint64_t)rtw * kg * W->experts, kScaleAtomBytes, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
-        !make_map_2d(&m.sfx, CU_TENSOR_MAP_DATA_TYPE_UINT32, sfx, 128, (uint64_t)(ex.rows / kRowAlign) * kg, kScaleAtomBytes, 128, 2, CU_TENSOR_MAP_SWIZZLE_NONE))
+        if (!make_map_3d(&m.x[b], kBytes, x8, kGroupBytes, ex.rows, kg, pitch, kGroupBytes, kGroupBytes, 8u << b, kStep, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
+    if (!make_map_3d(&m.codes, kBytes, W->codes, K / 2, N, W->experts, K / 2, (uint64_t)N * (K / 2), kStep * 64, 128, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_3d(&m.ids, kWords, W->ids, kIdAtomBytes / 4, rtw, (uint64_t)kg * W->experts, kIdAtomBytes, (uint64_t)rtw * kIdAtomBytes, kIdAtomBytes / 4, 1, kStep, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_map_3d(&m.sfw, kWords, W->scales, kScaleAtomBytes / 4, rtw, (uint64_t)kg * W->experts, kScaleAtomBytes, (uint64_t)rtw * kScaleAtomBytes, kScaleAtomBytes / 4, 1, kStep, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_map_3d(&m.sfx, kWords, sfx, kScaleAtomBytes / 4, tiles_x, kg, kScaleAtomBytes, (uint64_t)tiles_x * kScaleAtomBytes, kScaleAtomBytes / 4, TOK / 128, kStep, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorInvalidValue;
     if (!GATED) {
         if (!make_map_2d(&m.y, y_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, Y, N, ex.rows, (uint64_t)N * (y_bf16 ? 2 : 4), 32,
@@ -638,30 +724,32 @@ inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const E
     static bool configured[tc::kMaxDevices] = {};
     const int dev = current_device();
     if (!configured[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<GATED>::total);
+        cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<GATED, TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::total);
         if (e != cudaSuccess) return e;
+        // the warpgroups trade the registers that the launch brings: with fewer, the ones that ask for more would wait for good
+        cudaFuncAttributes a;
+        if ((e = cudaFuncGetAttributes(&a, expert_product_kernel<GATED, TOK>)) != cudaSuccess) return e;
+        if (a.numRegs < kLaunchRegs) return cudaErrorLaunchOutOfResources;
         configured[dev] = true;
     }
-    p.ids = (const uint8_t *)W->ids;
-    p.ids_stride = rtw * kg * kIdAtomBytes;
     p.w_pairs = (int)((N + 255) / 256);
     p.row_tiles = (int)rtw;
-    p.k_tiles = (int)kg;
+    p.k_groups = (int)kg;
     p.y_bf16 = y_bf16;
     const int resident = max_resident_clusters();
     const int64_t most = items_most * p.w_pairs;
     p.clusters = most < resident ? (int)most : resident;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * p.clusters);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Layout<GATED>::total;
+    cfg.blockDim = dim3(kBlockThreads);
+    cfg.dynamicSmemBytes = L::total;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, expert_product_kernel<GATED>, m, ex, p);
+    return cudaLaunchKernelEx(&cfg, expert_product_kernel<GATED, TOK>, m, ex, p);
 }
 
 }  // namespace ex
