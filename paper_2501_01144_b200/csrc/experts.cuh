@@ -59,7 +59,6 @@ struct Product {
 constexpr int kStep = 2;                     // k-groups of a k-step
 constexpr int kGroupBytes = 128;             // operand bytes of a row and k-group
 constexpr int kCodeBytes = 128 * kStep * 64; // packed codes of 128 weight rows
-constexpr int kBufs = 3;                     // decoded k-steps in tensor memory (64 columns each)
 
 // Warps: four for control (token producer, MMA issuer, code producer, one idle), three decode groups, two epilogue halves.  Each is a
 // warpgroup, since registers are handed from one to the other: at launch every thread has kLaunchRegs.
@@ -67,11 +66,14 @@ constexpr int kDecode0 = 4, kGroups = 3, kEpilogue0 = kDecode0 + 4 * kGroups, kB
 constexpr int kLaunchRegs = 80, kControlRegs = 40, kDecodeRegs = 56, kEpilogueRegs = 136;
 static_assert(128 * kControlRegs + 128 * kGroups * kDecodeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kLaunchRegs * kBlockThreads, "more registers than the launch brings");
 
-// TOK: most tokens of an item.  256: one accumulator of 256 columns.  128, where experts have few tokens: two accumulators, so that
-// the next item's products run while one is read out, smaller token stages and more stages for the codes.
+// TOK: most tokens of an item.  256: an accumulator of 256 columns, room for three decoded k-steps behind it.  128, where experts have few
+// tokens: an accumulator of 128 columns, which items of up to 64 tokens use half by half in turn, so that the next item's products run
+// while one is read out; five decoded k-steps, so that a decode group does not wait for the products of its last one (with three:
+// 1190 cycles a k-step for a few tokens, 970 of 3490 of a group's waiting); smaller token stages and more stages for the codes.
 template <bool GATED, int TOK>
 struct Layout {
-    static constexpr int kSlots = 256 / TOK;                     // accumulators
+    static constexpr int kSlots = TOK == 256 ? 1 : 2;            // accumulators in turn
+    static constexpr int kBufs = TOK == 256 ? 3 : 5;             // decoded k-steps in tensor memory, 64 columns each
     static constexpr int kXS = TOK == 256 ? 3 : 4, kCS = TOK == 256 ? 3 : 5;
     static constexpr int kXBytes = kStep * (TOK / 2) * kGroupBytes;
     static constexpr int kSfxBytes = kStep * (TOK / 128) * kScaleAtomBytes;
@@ -94,7 +96,7 @@ struct Layout {
     static_assert((2 * kXS + 2 * kCS + 2 * kBufs + 2 * kSlots) * 8 <= 256, "barrier area too small");
     static_assert(total <= 227 * 1024, "shared memory budget");
     // tensor memory columns: accumulators, decoded weights, scales of the weights and of the tokens (per k-group 4, and 4 per 128 tokens)
-    static constexpr int kColA = 256, kColSfW = kColA + 64 * kBufs, kColSfX = kColSfW + 4 * kStep;
+    static constexpr int kColA = TOK, kColSfW = kColA + 64 * kBufs, kColSfX = kColSfW + 4 * kStep;
     static_assert(kColSfX + kStep * 4 * (TOK / 128) <= 512, "tensor memory budget");
 };
 
@@ -149,7 +151,7 @@ template <bool GATED, int TOK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
     using L = Layout<GATED, TOK>;
-    constexpr int kXS = L::kXS, kCS = L::kCS, kSlots = L::kSlots;
+    constexpr int kXS = L::kXS, kCS = L::kCS, kSlots = L::kSlots, kBufs = L::kBufs;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -243,6 +245,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int steps = (p.k_groups + kStep - 1) / kStep;
+    auto accumulator = [](const Item &t, int slot) { return kSlots == 2 && t.n <= 64 ? 64u * (uint32_t)slot : 0u; };
     Walk<TOK> next(first, count, ex.start, ex.experts, p.clusters, cluster);
     Item t;
 
@@ -303,12 +306,14 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             const uint32_t t_sfw = tmem + L::kColSfW, t_sfx = tmem + L::kColSfX;
             int s = 0, b = 0;
             uint32_t ph_s = 0, ph_b = 0;
-            bool ready = false;
+            bool ready = false, wide = false;                     // wide: the item before had both halves of the accumulator
             for (int i = 0; next(i, t); i++) {
                 const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17, x_half = (8u << t.box) * kGroupBytes >> 4;
                 const int slot = i % kSlots;
-                const uint32_t t_d = tmem + (uint32_t)slot * TOK;
+                const uint32_t t_d = tmem + accumulator(t, slot);
                 if (i >= kSlots) mbar_wait_warp(d_empty(slot), (uint32_t)(i / kSlots - 1) & 1u, abort_flag);
+                if (kSlots == 2 && i > 0 && (wide || t.n > 64)) mbar_wait_warp(d_empty(slot ^ 1), (uint32_t)((i - 1) / kSlots) & 1u, abort_flag);
+                wide = t.n > 64;
                 tcgen05_fence_after();
                 for (int k = 0; k < steps; k++) {
                     if (!ready) {
@@ -440,7 +445,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             };
             mbar_wait_warp(d_full(slot), (uint32_t)(i / kSlots) & 1u, abort_flag, 256);
             tcgen05_fence_after();
-            const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)slot * TOK;
+            const uint32_t t_base = tmem + ((uint32_t)(quad * 32) << 16) + accumulator(t, slot);
             if (GATED) {
                 // Tokens 64 at a time; the two epilogue halves take turns.  The warps of quadrants 2 m and 2 m + 1 hold the gate and
                 // the up rows of the same 32 channels (block 2 m of this CTA's): both store two 32 x 32 tiles of sums (element
