@@ -73,16 +73,17 @@ static_assert(128 * kControlRegs + 128 * kGroups * kDecodeRegs + 32 * kEpilogueW
 template <bool GATED, int TOK>
 struct Layout {
     static constexpr int kSlots = TOK == 256 ? 1 : 2;            // accumulators in turn
-    static constexpr int kBufs = TOK == 256 ? 3 : 5;             // decoded k-steps in tensor memory, 64 columns each
-    static constexpr int kXS = TOK == 256 ? 3 : 4, kCS = TOK == 256 ? 3 : 5;
+    // k-steps on the way to the MMA: the token tile and scales of one in shared memory, its decoded weights in tensor memory (64 columns)
+    static constexpr int kBufs = TOK == 256 ? 3 : 5;
+    static constexpr int kCS = TOK == 256 ? 3 : 4;               // stages of packed codes
     static constexpr int kXBytes = kStep * (TOK / 2) * kGroupBytes;
     static constexpr int kSfxBytes = kStep * (TOK / 128) * kScaleAtomBytes;
     static constexpr int kStage = GATED ? 8192 : 4096;           // epilogue staging of a warp
     static constexpr int x = 0;
-    static constexpr int codes = x + kXS * kXBytes;
+    static constexpr int codes = x + kBufs * kXBytes;
     static constexpr int sfw = codes + kCS * kCodeBytes;
-    static constexpr int sfx = sfw + kXS * kStep * kScaleAtomBytes;
-    static constexpr int ids = sfx + kXS * kSfxBytes;
+    static constexpr int sfx = sfw + kBufs * kStep * kScaleAtomBytes;
+    static constexpr int ids = sfx + kBufs * kSfxBytes;
     static constexpr int bars = ids + kCS * kStep * kIdAtomBytes;
     static constexpr int words = bars + 256;
     static constexpr int seen = words + 16;                      // a word per decode warp
@@ -93,7 +94,7 @@ struct Layout {
     static constexpr int count = first + 4 * (kMaxExperts + 4);
     static constexpr int out = (count + 4 * kMaxExperts + 1023) / 1024 * 1024;
     static constexpr int total = out + kEpilogueWarps * kStage + 1024 /* alignment slack */;
-    static_assert((2 * kXS + 2 * kCS + 2 * kBufs + 2 * kSlots) * 8 <= 256, "barrier area too small");
+    static_assert((2 * kBufs + 2 * kCS + 2 * kSlots) * 8 <= 256, "barrier area too small");
     static_assert(total <= 227 * 1024, "shared memory budget");
     // tensor memory columns: accumulators, decoded weights, scales of the weights and of the tokens (per k-group 4, and 4 per 128 tokens)
     static constexpr int kColA = TOK, kColSfW = kColA + 64 * kBufs, kColSfX = kColSfW + 4 * kStep;
@@ -151,7 +152,7 @@ template <bool GATED, int TOK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
 expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
     using L = Layout<GATED, TOK>;
-    constexpr int kXS = L::kXS, kCS = L::kCS, kSlots = L::kSlots, kBufs = L::kBufs;
+    constexpr int kCS = L::kCS, kSlots = L::kSlots, kBufs = L::kBufs;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -161,14 +162,14 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     auto sfx_tile = [&](int s) { return base + L::sfx + (uint32_t)s * L::kSfxBytes; };
     auto id_tile = [&](int s) { return base + L::ids + (uint32_t)s * (kStep * kIdAtomBytes); };
     const uint32_t bars = base + L::bars;
-    auto x_full = [&](int s) { return bars + 8u * s; };                           // leader: tile + scales of both CTAs
-    auto x_empty = [&](int s) { return bars + 8u * (kXS + s); };                  // both: stage consumed by the MMA
-    auto c_full = [&](int s) { return bars + 8u * (2 * kXS + s); };               // local: codes + ids landed
-    auto c_empty = [&](int s) { return bars + 8u * (2 * kXS + kCS + s); };        // local: codes read by the decode group
-    auto a_full = [&](int b) { return bars + 8u * (2 * kXS + 2 * kCS + b); };             // leader: buffer written in both CTAs
-    auto a_empty = [&](int b) { return bars + 8u * (2 * kXS + 2 * kCS + kBufs + b); };    // both: buffer consumed
-    auto d_full = [&](int d) { return bars + 8u * (2 * kXS + 2 * kCS + 2 * kBufs + d); };            // both: accumulator complete
-    auto d_empty = [&](int d) { return bars + 8u * (2 * kXS + 2 * kCS + 2 * kBufs + kSlots + d); };  // leader: accumulator read out
+    // One pair of barriers per k-step, for the token tile and the decoded weights together: the issuing warp's waits, probes and commits are
+    // what a narrow k-step takes longest for.
+    auto full = [&](int s) { return bars + 8u * s; };                             // leader: tile + scales landed, weights written, both CTAs
+    auto empty = [&](int s) { return bars + 8u * (kBufs + s); };                  // both: the MMAs of the k-step have completed
+    auto c_full = [&](int s) { return bars + 8u * (2 * kBufs + s); };             // local: codes + ids landed
+    auto c_empty = [&](int s) { return bars + 8u * (2 * kBufs + kCS + s); };      // local: codes read by the decode group
+    auto d_full = [&](int d) { return bars + 8u * (2 * kBufs + 2 * kCS + d); };             // both: accumulator complete
+    auto d_empty = [&](int d) { return bars + 8u * (2 * kBufs + 2 * kCS + kSlots + d); };   // leader: accumulator read out
     volatile uint32_t *const shared_words = (volatile uint32_t *)(base_ptr + L::words);
     volatile uint32_t *const tmem_slot = shared_words;
     volatile uint32_t *const abort_flag = shared_words + 1;
@@ -183,17 +184,13 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         abort_flag[0] = 0;
         abort_flag[1] = 0;                                        // set once the previous kernel has completed
         abort_flag[2] = g_debug_spin_limit ? g_debug_spin_limit : kSpinLimit;
-        for (int s = 0; s < kXS; s++) {
-            mbar_init(x_full(s), 1);
-            mbar_init(x_empty(s), 1);
+        for (int s = 0; s < kBufs; s++) {
+            mbar_init(full(s), 3);                                // the leader's token producer, and a decode group of each CTA
+            mbar_init(empty(s), 1);
         }
         for (int s = 0; s < kCS; s++) {
             mbar_init(c_full(s), 1);
             mbar_init(c_empty(s), 4);                             // one arrival per warp of the decode group
-        }
-        for (int b = 0; b < kBufs; b++) {
-            mbar_init(a_full(b), 2);                              // one arrival per CTA of the pair
-            mbar_init(a_empty(b), 1);
         }
         for (int d = 0; d < kSlots; d++) {
             mbar_init(d_full(d), 1);
@@ -258,22 +255,22 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             if (lane == 0) abort_flag[1] = 1;                     // from here on every bounded wait counts its polls
             int s = 0;
             uint32_t ph = 1;
-            const uint32_t x_full_leader = map_to_cta(x_full(0), 0);
+            const uint32_t full_leader = map_to_cta(full(0), 0);
             for (int i = 0; next(i, t); i++) {
                 // each CTA holds half of the MMA's tokens (and, where the box is higher, rows that are not looked at)
                 const int t0 = t.row0 + (int)rank * (t.n / 2), sf_z = t.expert * p.k_groups;
                 const uint32_t tx_pair = 2u * (kStep * (8u << t.box) * kGroupBytes + kStep * kScaleAtomBytes + L::kSfxBytes);
                 for (int k = 0; k < steps; k++) {
-                    if (!mbar_wait_warp(x_empty(s), ph, abort_flag)) break;
-                    const uint32_t fb = x_full_leader + 8u * (uint32_t)s;
+                    if (!mbar_wait_warp(empty(s), ph, abort_flag)) break;
+                    const uint32_t fb = full_leader + 8u * (uint32_t)s;
                     if (elect_one()) {
-                        if (rank == 0) mbar_expect_tx(x_full(s), tx_pair);
+                        if (rank == 0) mbar_expect_tx(full(s), tx_pair);
                         tma_load_3d_pair(x_tile(s), &maps.x[t.box], 0, t0, kStep * k, fb);
                         tma_load_3d_pair(sfw_tile(s), &maps.sfw, 0, t.w_pair * 2 + (int)rank, sf_z + kStep * k, fb);
                         tma_load_3d_pair(sfx_tile(s), &maps.sfx, 0, t.row0 / kRowAlign, kStep * k, fb);
                     }
                     __syncwarp();
-                    if (++s == kXS) { s = 0; ph ^= 1u; }
+                    if (++s == kBufs) { s = 0; ph ^= 1u; }
                 }
                 if (*abort_flag) break;
             }
@@ -304,8 +301,8 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             // (instruction descriptor: see gemm_tc.cuh; N >> 3 at bit 17 follows the item)
             const uint32_t idesc_m = 1u << 23 | (uint32_t)(256 >> 4) << 24;
             const uint32_t t_sfw = tmem + L::kColSfW, t_sfx = tmem + L::kColSfX;
-            int s = 0, b = 0;
-            uint32_t ph_s = 0, ph_b = 0;
+            int s = 0;
+            uint32_t ph = 0;
             bool ready = false, wide = false;                     // wide: the item before had both halves of the accumulator
             for (int i = 0; next(i, t); i++) {
                 const uint32_t idesc0 = idesc_m | (uint32_t)(t.n >> 3) << 17, x_half = (8u << t.box) * kGroupBytes >> 4;
@@ -316,15 +313,13 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 wide = t.n > 64;
                 tcgen05_fence_after();
                 for (int k = 0; k < steps; k++) {
-                    if (!ready) {
-                        // slow path: the probe at the end of the previous k-step found a barrier open
-                        if (!mbar_wait_warp(x_full(s), ph_s, abort_flag) || !mbar_wait_warp(a_full(b), ph_b, abort_flag)) break;
-                    }
+                    // (slow path: the probe at the end of the previous k-step found the barrier open)
+                    if (!ready && !mbar_wait_warp(full(s), ph, abort_flag)) break;
                     tcgen05_fence_after();
                     const uint32_t lo_sfw = lo_sfw0 + (uint32_t)s * (kStep * kScaleAtomBytes >> 4);
                     const uint32_t lo_sfx = lo_sfx0 + (uint32_t)s * (L::kSfxBytes >> 4);
                     const uint32_t lo_x = lo_x0 + (uint32_t)s * (L::kXBytes >> 4);
-                    const uint32_t t_a = tmem + L::kColA + 64u * (uint32_t)b;
+                    const uint32_t t_a = tmem + L::kColA + 64u * (uint32_t)s;
                     const bool both = kStep * k + 1 < p.k_groups;     // (K may end with the step's first k-group)
                     if (elect_one()) {
 #pragma unroll
@@ -340,15 +335,12 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                                                             idesc0 | (uint32_t)j << 4 | (uint32_t)j << 29, t_sfw + 4 * h, t_sfx + 4 * h * (TOK / 128),
                                                             h == 0 && j == 0 ? (k > 0 ? 1u : 0u) : 1u);
                         }
-                        tcgen05_commit_pair(x_empty(s));
-                        tcgen05_commit_pair(a_empty(b));
+                        tcgen05_commit_pair(empty(s));
                     }
                     __syncwarp();
-                    if (++s == kXS) { s = 0; ph_s ^= 1u; }
-                    if (++b == kBufs) { b = 0; ph_b ^= 1u; }
-                    // probe the next k-step's barriers now (the rings run across items): the round trip overlaps the issue above
-                    const bool x_ok = mbar_test_wait(x_full(s), ph_s), a_ok = mbar_test_wait(a_full(b), ph_b);
-                    ready = __all_sync(0xffffffffu, x_ok && a_ok);
+                    if (++s == kBufs) { s = 0; ph ^= 1u; }
+                    // probe the next k-step's barrier now (the ring runs across items): the round trip overlaps the issue above
+                    ready = __all_sync(0xffffffffu, mbar_test_wait(full(s), ph));
                 }
                 if (*abort_flag && elect_one()) {
                     // this CTA is aborting: tell the peer before its epilogue warps are woken by the commit below
@@ -369,7 +361,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         const int j = quad * 32 + lane;
         const bool group_leader = quad == 0 && lane == 0;
         const uint32_t swz = (uint32_t)j & 7u;
-        const uint32_t a_full_leader = map_to_cta(a_full(0), 0);
+        const uint32_t full_leader = map_to_cta(full(0), 0);
         const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + L::kColA;
         const int items = first[ex.experts];
         const int total = cluster < items ? ((items - cluster + p.clusters - 1) / p.clusters) * steps : 0;
@@ -397,7 +389,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)L::seen + 4u * (uint32_t)(warp - kDecode0)), "r"(seen) : "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(c_empty(s));
-                dead = !mbar_wait_warp(a_empty(b), b_par, abort_flag);
+                dead = !mbar_wait_warp(empty(b), b_par, abort_flag);
             }
             if (!dead) {
                 tcgen05_fence_after();                            // the MMAs that read this buffer have completed
@@ -416,7 +408,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 tcgen05_fence_before();
             }
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");   // the four warps of this group are done
-            if (group_leader && !dead) mbar_arrive_cluster(a_full_leader + 8u * b);
+            if (group_leader && !dead) mbar_arrive_cluster(full_leader + 8u * b);
             s += kGroups;
             if (s >= kCS) { s -= kCS; s_par ^= 1u; }
             b += kGroups;
