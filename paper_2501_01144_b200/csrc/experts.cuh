@@ -60,12 +60,6 @@ constexpr int kStep = 2;                     // k-groups of a k-step
 constexpr int kGroupBytes = 128;             // operand bytes of a row and k-group
 constexpr int kCodeBytes = 128 * kStep * 64; // packed codes of 128 weight rows
 
-// Warps: four for control (token producer, MMA issuer, code producer, one idle), three decode groups, two epilogue halves.  Each is a
-// warpgroup, since registers are handed from one to the other: at launch every thread has kLaunchRegs.
-constexpr int kDecode0 = 4, kGroups = 3, kEpilogue0 = kDecode0 + 4 * kGroups, kBlockThreads = 32 * (kEpilogue0 + kEpilogueWarps);
-constexpr int kLaunchRegs = 80, kControlRegs = 40, kDecodeRegs = 56, kEpilogueRegs = 136;
-static_assert(128 * kControlRegs + 128 * kGroups * kDecodeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kLaunchRegs * kBlockThreads, "more registers than the launch brings");
-
 // TOK: most tokens of an item.  256: an accumulator of 256 columns, room for three decoded k-steps behind it.  128, where experts have few
 // tokens: an accumulator of 128 columns, which items of up to 64 tokens use half by half in turn, so that the next item's products run
 // while one is read out; five decoded k-steps, so that a decode group does not wait for the products of its last one (with three:
@@ -75,7 +69,17 @@ struct Layout {
     static constexpr int kSlots = TOK == 256 ? 1 : 2;            // accumulators in turn
     // k-steps on the way to the MMA: the token tile and scales of one in shared memory, its decoded weights in tensor memory (64 columns)
     static constexpr int kBufs = TOK == 256 ? 3 : 5;
-    static constexpr int kCS = TOK == 256 ? 3 : 4;               // stages of packed codes
+    // Warps: four for control (token producer, MMA issuer, code producer, one idle), the decode groups, two epilogue halves.  Each is a
+    // warpgroup, since registers are handed from one to the other: at launch every thread has kLaunchRegs.
+    static constexpr int kGroups = TOK == 256 ? 3 : 4;
+    static constexpr int kDecode0 = 4, kEpilogue0 = kDecode0 + 4 * kGroups, kThreads = 32 * (kEpilogue0 + kEpilogueWarps);
+    static constexpr int kLaunchRegs = TOK == 256 ? 80 : 72, kControlRegs = 40, kDecodeRegs = 56, kEpilogueRegs = TOK == 256 ? 136 : 120;
+    static_assert(128 * kControlRegs + 128 * kGroups * kDecodeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kLaunchRegs * kThreads, "more registers than the launch brings");
+    // Stages of packed codes, each always used by the same decode group: copies land out of order, and a group that came to a stage before
+    // the contents in front of its own had landed would take the barrier's last-but-one phase for its own (a barrier tells a phase from the
+    // next, not from the one after that).  The ring of k-steps above needs no such rule, since its MMAs complete in order.
+    static constexpr int kCS = kGroups;
+    static_assert(kCS % kGroups == 0, "a stage belongs to one group");
     static constexpr int kXBytes = kStep * (TOK / 2) * kGroupBytes;
     static constexpr int kSfxBytes = kStep * (TOK / 128) * kScaleAtomBytes;
     static constexpr int kStage = GATED ? 8192 : 4096;           // epilogue staging of a warp
@@ -87,12 +91,12 @@ struct Layout {
     static constexpr int bars = ids + kCS * kStep * kIdAtomBytes;
     static constexpr int words = bars + 256;
     static constexpr int seen = words + 16;                      // a word per decode warp
-    static constexpr int luts = words + 64;
-    static_assert(16 + 4 * 4 * kGroups <= 64, "words");
+    static constexpr int luts = words + 80;
+    static_assert(16 + 4 * 4 * kGroups <= 80, "words");
     static constexpr int qtab = luts + 128;
     static constexpr int first = (qtab + (int)sizeof(SmemTables) + 15) / 16 * 16;   // first item of each expert
-    static constexpr int count = first + 4 * (kMaxExperts + 4);
-    static constexpr int out = (count + 4 * kMaxExperts + 1023) / 1024 * 1024;
+    static constexpr int where = first + 4 * (kMaxExperts + 4);
+    static constexpr int out = (where + 4 * kMaxExperts + 1023) / 1024 * 1024;
     static constexpr int total = out + kEpilogueWarps * kStage + 1024 /* alignment slack */;
     static_assert((2 * kBufs + 2 * kCS + 2 * kSlots) * 8 <= 256, "barrier area too small");
     static_assert(total <= 227 * 1024, "shared memory budget");
@@ -111,20 +115,19 @@ struct Item {
 // Items of cluster c: c, c + clusters, ...; numbered expert by expert, then weight rows, the token tile running fastest.
 template <int TOK>
 struct Walk {
-    const int *first, *count;
-    const int32_t *start;
-    int experts, clusters, c, e;
-    __device__ Walk(const int *first_, const int *count_, const int32_t *start_, int experts_, int clusters_, int c_)
-        : first(first_), count(count_), start(start_), experts(experts_), clusters(clusters_), c(c_), e(0) {}
+    const int *first;                        // items before each expert's, [experts + 1]
+    const uint32_t *where;                   // an expert's first row / 128, and (low byte) the tokens of its last tile - 1
+    int w_pairs, experts, clusters, c, e;
     __device__ bool operator()(int i, Item &t) {
         const int item = i * clusters + c;
         if (item >= first[experts]) return false;
         while (item >= first[e + 1]) e++;
-        const int cnt = count[e], tiles = (cnt + TOK - 1) / TOK, in = item - first[e], tt = in % tiles;
+        const int tiles = (first[e + 1] - first[e]) / w_pairs, in = item - first[e], tt = in % tiles;
+        const uint32_t w = where[e];
         t.expert = e;
         t.w_pair = in / tiles;
-        t.row0 = __ldg(start + e) + tt * TOK;
-        t.live = min(TOK, cnt - tt * TOK);
+        t.row0 = (int)(w >> 8) * kRowAlign + tt * TOK;
+        t.live = tt + 1 < tiles ? TOK : (int)(w & 255u) + 1;
         t.n = (t.live + 15) / 16 * 16;
         t.box = t.n <= 16 ? 0 : 28 - __clz(t.n - 1);               // 8 << box >= n / 2
         return true;
@@ -149,10 +152,10 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
 }
 
 template <bool GATED, int TOK>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBlockThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((Layout<GATED, TOK>::kThreads), 1)
 expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
     using L = Layout<GATED, TOK>;
-    constexpr int kCS = L::kCS, kSlots = L::kSlots, kBufs = L::kBufs;
+    constexpr int kCS = L::kCS, kSlots = L::kSlots, kBufs = L::kBufs, kDecode0 = L::kDecode0, kEpilogue0 = L::kEpilogue0, kGroups = L::kGroups;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -174,7 +177,8 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     volatile uint32_t *const tmem_slot = shared_words;
     volatile uint32_t *const abort_flag = shared_words + 1;
     uint32_t *const luts = (uint32_t *)(base_ptr + L::luts);
-    int *const first = (int *)(base_ptr + L::first), *const count = (int *)(base_ptr + L::count);
+    int *const first = (int *)(base_ptr + L::first);
+    uint32_t *const where = (uint32_t *)(base_ptr + L::where);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_ctarank();
@@ -207,22 +211,29 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                      ::"r"(smem_u32((const void *)tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    // The schedule: items of the experts before each one, by a scan in the first warp.  The plan is older than the kernel in front of
-    // this one (which waited for it before it let this one start), so no wait is needed.  Numbers that cannot be (a plan overwritten by
-    // the caller) leave the expert out and are told: nothing is addressed by them.
-    if (warp == 0) {
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                           // both CTAs: running, barriers initialised, TMEM allocated
+    tcgen05_fence_after();
+    // The schedule: items of the experts before each one, by a scan in the leader's first warp, which writes it to both CTAs: they hand
+    // over to one another item by item, so they must go by the same numbers whatever happens to the plan meanwhile.  Only behind the wait: in
+    // front of it a load may still meet what the caches held before the plan was written (the first-level cache's lines, for one).
+    // Numbers that cannot be (a plan overwritten by the caller) leave the expert out and are told: nothing is addressed by them.
+    if (warp == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0 && rank == 0) {
+        const uint32_t to_first = map_to_cta(smem_u32(first), 1), to_where = map_to_cta(smem_u32(where), 1);
+        auto share = [](uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); };
         int before = 0;
         for (int e0 = 0; e0 < ex.experts; e0 += 32) {
             const int e = e0 + lane;
-            int cnt = 0;
+            int cnt = 0, start = 0;
             if (e < ex.experts) {
-                cnt = __ldg(ex.count + e);
-                const int start = __ldg(ex.start + e);
+                cnt = ex.count[e];
+                start = ex.start[e];
                 if (cnt < 0 || start < 0 || start % kRowAlign || cnt > ex.rows || start > ex.rows - cnt) {
-                    cnt = 0;
+                    cnt = start = 0;
                     atomicOr(&g_status_word, kStatusIndex);
                 }
-                count[e] = cnt;
             }
             const int items = (cnt + TOK - 1) / TOK * p.w_pairs;
             int incl = items;
@@ -231,27 +242,34 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 const int up = __shfl_up_sync(0xffffffffu, incl, d);
                 if (lane >= d) incl += up;
             }
-            if (e < ex.experts) first[e] = before + incl - items;
+            if (e < ex.experts) {
+                const uint32_t w = (uint32_t)(start / kRowAlign) << 8 | (uint32_t)((cnt + TOK - 1) % TOK);
+                first[e] = before + incl - items;
+                where[e] = w;
+                share(to_first + 4u * e, (uint32_t)(before + incl - items));
+                share(to_where + 4u * e, w);
+            }
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
-        if (lane == 0) first[ex.experts] = before;
+        if (lane == 0) {
+            first[ex.experts] = before;
+            share(to_first + 4u * (uint32_t)ex.experts, (uint32_t)before);
+        }
+        __syncwarp();
     }
-    tcgen05_fence_before();
     __syncthreads();
-    cluster_sync_all();                                           // both CTAs: barriers initialised, TMEM allocated
-    tcgen05_fence_after();
+    cluster_sync_all();
     const uint32_t tmem = *tmem_slot;
     const int steps = (p.k_groups + kStep - 1) / kStep;
     auto accumulator = [](const Item &t, int slot) { return kSlots == 2 && t.n <= 64 ? 64u * (uint32_t)slot : 0u; };
-    Walk<TOK> next(first, count, ex.start, ex.experts, p.clusters, cluster);
+    Walk<TOK> next{first, where, p.w_pairs, ex.experts, p.clusters, cluster, 0};
     Item t;
 
     if (warp < kDecode0) {
-        registers_down<kControlRegs>();
+        registers_down<L::kControlRegs>();
         if (warp == 0) {
             // ---- TMA producer of the token tile and the scale atoms; the one warp that reads what the kernel in front wrote ----
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the wait is behind this warp)
             if (lane == 0) abort_flag[1] = 1;                     // from here on every bounded wait counts its polls
             int s = 0;
             uint32_t ph = 1;
@@ -356,7 +374,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     } else if (warp < kEpilogue0) {
         // ---- decode warps: group g takes this CTA's k-steps g, g + groups, ... (counted across items); a warp may only touch the TMEM
         // lanes 32 * (warp % 4) .. + 31, so thread `lane` of warp w owns weight row (and TMEM lane) j = 32 * (w % 4) + lane ----
-        registers_down<kDecodeRegs>();
+        registers_down<L::kDecodeRegs>();
         const int group = (warp - kDecode0) / 4, quad = warp % 4;
         const int j = quad * 32 + lane;
         const bool group_leader = quad == 0 && lane == 0;
@@ -409,6 +427,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             }
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");   // the four warps of this group are done
             if (group_leader && !dead) mbar_arrive_cluster(full_leader + 8u * b);
+            __syncwarp();
             s += kGroups;
             if (s >= kCS) { s -= kCS; s_par ^= 1u; }
             b += kGroups;
@@ -416,7 +435,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         }
     } else {
         // ---- epilogue: warp w reads the TMEM lanes 32 * (w % 4) .. + 31 (weight rows) of this CTA's accumulator ----
-        registers_up<kEpilogueRegs>();
+        registers_up<L::kEpilogueRegs>();
         const int quad = warp % 4, half = (warp - kEpilogue0) / 4, slot_of_warp = warp - kEpilogue0;
         const uint32_t d_empty_leader = map_to_cta(d_empty(0), 0);
         const uint32_t stage_out = base + L::out + (uint32_t)slot_of_warp * L::kStage;
@@ -434,6 +453,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(d_empty_leader + 8u * (uint32_t)slot);
+                __syncwarp();
             };
             mbar_wait_warp(d_full(slot), (uint32_t)(i / kSlots) & 1u, abort_flag, 256);
             tcgen05_fence_after();
@@ -443,18 +463,15 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                 // the up rows of the same 32 channels (block 2 m of this CTA's): both store two 32 x 32 tiles of sums (element
                 // (token q, row r) at q * 32 + (r ^ q): rows are written and tokens read without bank conflicts), meet, and then the
                 // first finishes the first 32 tokens and the second the others, a token's block per lane.  A half's second 64 tokens
-                // wait in registers meanwhile, so that the accumulator is free before the arithmetic begins.
+                // are fetched before the first ones are quantised: the accumulator is free while that goes on.  (Fetched at once, into
+                // registers, they spilled: local memory does not fit beside this much shared memory, and the epilogue took twice as long.)
                 const int groups = (t.n + 63) / 64, pair = quad / 2, which = quad & 1;
                 const int b = t.w_pair * 4 + (int)rank * 2 + pair;                     // block of the result
                 const bool block_ok = b < p.live_k;
                 const uint32_t *const tile_g = (const uint32_t *)(base_ptr + L::out + (slot_of_warp - which) * L::kStage) + which * 1024;
                 const uint32_t *const tile_u = (const uint32_t *)(base_ptr + L::out + (slot_of_warp - which + 1) * L::kStage) + which * 1024;
                 uint32_t *const tile = (uint32_t *)stage_ptr;
-                auto put = [&](const uint32_t (&r)[32], int v) {
-#pragma unroll
-                    for (int q = 0; q < 32; q++) tile[v * 1024 + q * 32 + (lane ^ q)] = r[q];
-                };
-                auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(4 + half * 2 + pair) : "memory"); };
+                auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + kGroups + half * 2 + pair) : "memory"); };
                 uint32_t bits[32];
                 auto activate = [&]() {
                     meet();
@@ -488,23 +505,22 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                     release_accumulator();
                 } else {
                     const bool more = TOK == 256 && half + 2 < groups;
-                    uint32_t r[32], later[2][32];
+                    auto fetch = [&](int g) {
+                        uint32_t r[32];
 #pragma unroll
-                    for (int v = 0; v < 2; v++) {
-                        tcgen05_ld_32x32b_x32(t_base + half * 64 + v * 32, r);
-                        tcgen05_wait_ld();
-                        put(r, v);
-                    }
-                    if (more) {
-                        tcgen05_ld_32x32b_x32(t_base + (half + 2) * 64, later[0]);
-                        tcgen05_ld_32x32b_x32(t_base + (half + 2) * 64 + 32, later[1]);
-                        tcgen05_wait_ld();
-                    }
-                    release_accumulator();
+                        for (int v = 0; v < 2; v++) {
+                            tcgen05_ld_32x32b_x32(t_base + g * 64 + v * 32, r);
+                            tcgen05_wait_ld();
+#pragma unroll
+                            for (int q = 0; q < 32; q++) tile[v * 1024 + q * 32 + (lane ^ q)] = r[q];
+                        }
+                    };
+                    fetch(half);
+                    if (!more) release_accumulator();
                     activate();
                     if (more) {
-                        put(later[0], 0);
-                        put(later[1], 1);
+                        fetch(half + 2);
+                        release_accumulator();
                     }
                     store(half);
                     if (more) {
@@ -726,7 +742,7 @@ inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const E
         // the warpgroups trade the registers that the launch brings: with fewer, the ones that ask for more would wait for good
         cudaFuncAttributes a;
         if ((e = cudaFuncGetAttributes(&a, expert_product_kernel<GATED, TOK>)) != cudaSuccess) return e;
-        if (a.numRegs < kLaunchRegs) return cudaErrorLaunchOutOfResources;
+        if (a.numRegs < L::kLaunchRegs) return cudaErrorLaunchOutOfResources;
         configured[dev] = true;
     }
     p.w_pairs = (int)((N + 255) / 256);
@@ -738,7 +754,7 @@ inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const E
     p.clusters = most < resident ? (int)most : resident;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * p.clusters);
-    cfg.blockDim = dim3(kBlockThreads);
+    cfg.blockDim = dim3(L::kThreads);
     cfg.dynamicSmemBytes = L::total;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];

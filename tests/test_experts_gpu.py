@@ -203,6 +203,25 @@ def test_captured_calls_follow_their_inputs():
     bd.poll_status()
 
 
+def test_plans_change_from_call_to_call_in_the_same_memory():
+    up, down = weights(24, 512, 256, 512)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x, w = tokens_of(64, 512, torch.bfloat16), torch.rand(64, 4, generator=g, device="cuda")
+    every = [torch.topk(torch.rand(64, 24, generator=g, device="cuda") + 3 * (torch.arange(24, device="cuda") % (k + 2) == 0), 4)[1].to(torch.int32) for k in range(6)]
+    plan = bd.expert_plan(every[0], 24)
+    want = []
+    for ids in every:
+        torch.cuda.synchronize()
+        want.append(bd.expert_mlp(x, bd.expert_plan(ids, 24), w, up, down))
+        torch.cuda.synchronize()
+    got = []
+    for _ in range(20):                                           # one plan's memory, written again right before each call
+        for ids in every:
+            got.append(bd.expert_mlp(x, bd.expert_plan(ids, 24, out=plan), w, up, down))
+    bd.poll_status()
+    assert all(torch.equal(y, want[k % 6]) for k, y in enumerate(got))
+
+
 def test_calls_on_two_streams():
     up, down = weights(6, 512, 256, 512)
     g = torch.Generator(device="cuda").manual_seed(9)
