@@ -267,7 +267,7 @@ class QTensor:
     def from_buffers(cls, codes, ids, scales, rows, K):
         """An operand over the caller's own buffers (the sizes that the library asks for)."""
         q = cls.__new__(cls)
-        q.rows, q.K, q.codes, q.ids, q.scales = rows, K, codes, ids, scales
+        q.__dict__.update(rows=rows, K=K, codes=codes, ids=ids, scales=scales, _c=None)
         return q
 
     def c_struct(self):
@@ -814,14 +814,14 @@ def residual_norm(y, weight, residual=None, bias=None, post_weight=None, post_bi
     """(h, n): h = residual + scale * gate * u, u = y or norm(y) * (post_weight + weight_offset) + post_bias; n = norm(h) * (weight +
     weight_offset) + bias, or with quantise a QTensor of it.  y, residual [rows, dim]; gate [rows or 1, dim or 1]; norm: "rms" or
     "layer".  weight None: n is None; want_h False: h is not stored.  out_h, out_n may be y or residual."""
-    if quantise and out_n is None:
-        if y.dim() != 2:
-            raise ValueError("y must be [rows, dim]")
-        out_n = QTensor(*y.shape, y.device)
-    q = (out_n.codes, out_n.ids, out_n.scales) if quantise else None
-    h, n = (_block or _load_block()).norm(y, weight, residual, bias, post_weight, post_bias, gate, scale, _choice(_NORMS, norm, "norm"), eps, weight_offset, want_h, out_h, None if quantise else out_n, q,
-                                          stream)
-    return h, out_n if quantise else n
+    q = None
+    if quantise:
+        q = True if out_n is None else (out_n.codes, out_n.ids, out_n.scales)
+    h, n, *operand = (_block or _load_block()).norm(y, weight, residual, bias, post_weight, post_bias, gate, scale, _choice(_NORMS, norm, "norm"), eps, weight_offset, want_h, out_h,
+                                                    None if quantise else out_n, q, stream)
+    if quantise:
+        return h, QTensor.from_buffers(*operand, y.shape[0], y.shape[1]) if out_n is None else out_n
+    return h, n
 
 
 NOALLOC_SCRATCH_BYTES = 32 << 20

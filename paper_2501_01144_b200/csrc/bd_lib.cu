@@ -1787,7 +1787,7 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     p.h_scales = ws + sp.h_scales;
     p.h_pitch = ex::row_pitch(down->K);
     p.gelu = act == BD_ACT_GELU;
-    cudaError_t err = (narrow ? ex::launch_product<true, 128> : ex::launch_product<true, 256>)(ws, ws + sp.x_scales, e, most, up, p, nullptr, false, st);
+    cudaError_t err = (narrow ? ex::launch_product<true, 128> : ex::launch_product<true, 256>)(ws, ws + sp.x_scales, e, tokens, most, up, p, nullptr, false, st);
     if (err != cudaSuccess) return cuda_result(err);
     g_launches += 1;
     if (inner) {
@@ -1795,7 +1795,7 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
                           (const uint8_t *)p.h_scales, plan->place, rows, (int)sp.rows, (int)down->K, p.h_pitch, inner);
         if ((s = launch_result())) return s;
     }
-    err = (narrow ? ex::launch_product<false, 128> : ex::launch_product<false, 256>)(p.h, p.h_scales, e, most, down, p, ws, ydtype == BD_BF16, st);
+    err = (narrow ? ex::launch_product<false, 128> : ex::launch_product<false, 256>)(p.h, p.h_scales, e, tokens, most, down, p, ws, ydtype == BD_BF16, st);
     if (err != cudaSuccess) return cuda_result(err);
     g_launches += 1;
     const unsigned grid = (unsigned)std::min<int64_t>((tokens * (down->rows / 8) + 255) / 256, 148 * 16);
@@ -1847,13 +1847,20 @@ bd_status bd_residual_norm(const bd_norm *a, bd_dtype dtype, int64_t rows, int64
     k.scale = a->scale; k.eps = a->eps; k.offset = a->weight_offset;
     // threads of a row: as many pieces of eight elements as the row has, up to 512 threads with one, two or four pieces each; short rows share a CTA
     const int pieces = (int)((dim + 7) / 8);
-    const int vpt = pieces <= nm::kMaxThreads ? 1 : pieces <= 2 * nm::kMaxThreads ? 2 : 4;
+    // Threads of a row, with one, two or four pieces of eight elements each.  Up to two rows an SM: as many threads as the row has pieces, up
+    // to 512 (64 rows of 4096 bf16: 2.7 us, with 256 threads 3.2).  More rows: up to 256 for rows of up to 8 KiB, so that more of them are on
+    // their way at once (8192 rows of 4096: 48 us, with 512 threads 54; but 4096 rows of 8192: 53 us, with 512 threads 50); a thread per block where the
+    // result is quantised from registers (8192 rows of 4096: 58 us, through shared memory 68); a warp a row up to 512 elements (30000 rows of
+    // 512: 23 us, with two warps 26).
+    const bool many = rows > 2 * 148, own = a->q && vec && many;
+    const int most = !many ? 512 : dim <= 512 ? 32 : dim * esz <= 8192 ? 256 : 512;
+    const int vpt = own ? 4 : pieces <= most ? 1 : pieces <= 2 * most ? 2 : 4;
     k.row_threads = ((pieces + vpt - 1) / vpt + 31) / 32 * 32;
-    k.row_groups = std::max(1, 256 / k.row_threads);
+    k.row_groups = std::max(1, (k.row_threads == 32 ? 256 : 64) / k.row_threads);   // short rows share a CTA
     const int64_t total = a->q ? row_tiles(rows) * kRowTile : rows;
     const unsigned block = (unsigned)(k.row_threads * k.row_groups);
     const unsigned grid = (unsigned)std::min<int64_t>((total + k.row_groups - 1) / k.row_groups, 148 * (2048 / block));
-    const size_t smem = a->q ? (size_t)k.row_groups * dim * esz : 0;
+    const size_t smem = a->q && !(vec && vpt == 4) ? (size_t)k.row_groups * dim * esz : 0;
     cudaStream_t st = (cudaStream_t)stream;
     if (dtype == BD_F32) return launch_norm<BD_F32>(k, vpt, a->q != nullptr, vec, grid, block, smem, st);
     if (dtype == BD_BF16) return launch_norm<BD_BF16>(k, vpt, a->q != nullptr, vec, grid, block, smem, st);

@@ -31,6 +31,15 @@ bool truth(PyObject *o) {
     return v != 0;
 }
 
+// A tensor on a part of another one's storage, `at` bytes in (as a view would be, without the dispatcher's share of its cost).
+at::Tensor part(const at::Tensor &whole, int64_t at, at::ScalarType dt, at::IntArrayRef shape) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(dt));
+    impl->set_storage_offset(at / (int64_t)c10::elementSize(dt));
+    impl->set_sizes_contiguous(shape);
+    return at::Tensor(std::move(impl));
+}
+int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
 bd_expert_plan plan_of(const at::Tensor &count, const at::Tensor &start, const at::Tensor &place, const at::Tensor &scratch) {
     bd_expert_plan p{};
     p.count = count.data_ptr<int32_t>(); p.start = start.data_ptr<int32_t>(); p.place = place.data_ptr<int32_t>();
@@ -38,20 +47,17 @@ bd_expert_plan plan_of(const at::Tensor &count, const at::Tensor &start, const a
     p.tokens = place.size(0); p.top_k = place.size(1); p.experts = count.size(0);
     return p;
 }
-// The tensors of a plan: (count, start, place, scratch), new.  The index tensors are parts of one allocation.
 struct PlanTensors {
     at::Tensor count, start, place, scratch;
 };
-PlanTensors new_plan(int64_t tokens, int64_t top_k, int64_t experts) {
+// The tensors of a new plan, and `more` bytes in front of them, in one allocation.
+PlanTensors new_plan(int64_t tokens, int64_t top_k, int64_t experts, int64_t more, at::Tensor *all) {
     size_t bytes = 0;
     check(bd_expert_plan_scratch(tokens, experts, &bytes));
-    PlanTensors t;
-    const at::Tensor all = at::empty({2 * experts + 1 + tokens * top_k}, on_device(at::kInt));
-    t.count = all.narrow(0, 0, experts);
-    t.start = all.narrow(0, experts, experts + 1);
-    t.place = all.narrow(0, 2 * experts + 1, tokens * top_k).view({tokens, top_k});
-    t.scratch = at::empty({(int64_t)bytes}, on_device(at::kByte));
-    return t;
+    const int64_t index = padded(more), scratch = index + padded(4 * (2 * experts + 1 + tokens * top_k));
+    *all = at::empty({scratch + (int64_t)bytes}, on_device(at::kByte));
+    return {part(*all, index, at::kInt, {experts}), part(*all, index + 4 * experts, at::kInt, {experts + 1}), part(*all, index + 4 * (2 * experts + 1), at::kInt, {tokens, top_k}),
+            part(*all, scratch, at::kByte, {(int64_t)bytes})};
 }
 PlanTensors given_plan(PyObject *o, int64_t tokens, int64_t top_k, int64_t experts) {
     if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) refuse("plan must be an ExpertPlan");
@@ -101,19 +107,17 @@ PyObject *route(PyObject *const *a, Py_ssize_t n) {
         valid = v.data_ptr<int32_t>();
     }
     const StreamScope stream(a[14]);
-    const at::Tensor ids = a[10] == Py_None ? at::empty({tokens, k}, on_device(at::kInt)) : whole(a[10], "ids", at::kInt, {tokens, k});
-    const at::Tensor w = a[11] == Py_None ? at::empty({tokens, k}, on_device(at::kFloat)) : whole(a[11], "weights", at::kFloat, {tokens, k});
+    const bool wants = truth(a[13]), fresh = wants && a[12] == Py_None;
+    const int64_t ids_bytes = a[10] == Py_None ? padded(4 * tokens * k) : 0, w_bytes = a[11] == Py_None ? padded(4 * tokens * k) : 0;
     PlanTensors t;
+    at::Tensor all;
+    if (fresh) t = new_plan(tokens, k, experts, ids_bytes + w_bytes, &all);
+    else if (ids_bytes + w_bytes || tokens == 0) all = at::empty({ids_bytes + w_bytes}, on_device(at::kByte));
+    if (wants && !fresh) t = given_plan(a[12], tokens, k, experts);
+    const at::Tensor ids = a[10] == Py_None ? part(all, 0, at::kInt, {tokens, k}) : whole(a[10], "ids", at::kInt, {tokens, k});
+    const at::Tensor w = a[11] == Py_None ? part(all, ids_bytes, at::kFloat, {tokens, k}) : whole(a[11], "weights", at::kFloat, {tokens, k});
     bd_expert_plan p{};
-    const bool wants = truth(a[13]);
-    if (wants) {
-        if (a[12] == Py_None) {
-            t = new_plan(tokens, k, experts);
-        } else {
-            t = given_plan(a[12], tokens, k, experts);
-        }
-        p = plan_of(t.count, t.start, t.place, t.scratch);
-    }
+    if (wants) p = plan_of(t.count, t.start, t.place, t.scratch);
     check(bd_route(m.p, dt, tokens, m.ld, bias, &r, valid, ids.data_ptr<int32_t>(), w.data_ptr<float>(), wants ? &p : nullptr, stream.raw));
     return tuple_of({ids, w, t.count, t.start, t.place, t.scratch});
 }
@@ -129,7 +133,8 @@ PyObject *plan(PyObject *const *a, Py_ssize_t n) {
     const StreamScope stream(a[3]);
     PlanTensors t;
     if (a[2] == Py_None) {
-        t = new_plan(tokens, k, experts);
+        at::Tensor all;
+        t = new_plan(tokens, k, experts, 0, &all);
     } else {
         t = given_plan(a[2], tokens, k, experts);
     }
@@ -218,7 +223,7 @@ PyObject *mlp(PyObject *const *a, Py_ssize_t n) {
     return THPVariable_Wrap(out);
 }
 
-// y, weight, residual, bias, post_weight, post_bias, gate, scale, layer, eps, offset, want_h, out_h, out_n, (codes, ids, scales) or None, stream
+// y, weight, residual, bias, post_weight, post_bias, gate, scale, layer, eps, offset, want_h, out_h, out_n, (codes, ids, scales) or True (new ones) or None, stream
 PyObject *norm(PyObject *const *a, Py_ssize_t n) {
     need(n, 16);
     const at::Tensor &y = tensor(a[0], "y");
@@ -253,12 +258,24 @@ PyObject *norm(PyObject *const *a, Py_ssize_t n) {
         k.h = rows_of(h, "out_h", &k.ldh);
     }
     bd_qtensor q{};
+    at::Tensor operand[3];
     if (a[14] != Py_None) {
-        if (!PyTuple_Check(a[14]) || PyTuple_GET_SIZE(a[14]) != 3) refuse("out_n must be a QTensor");
         size_t bytes[3] = {0, 0, 0};
-        if (rows) check(bd_qtensor_sizes(rows, dim, &bytes[0], &bytes[1], &bytes[2]));
-        void **part[3] = {&q.codes, &q.ids, &q.scales};
-        for (int i = 0; i < 3; i++) *part[i] = whole(PyTuple_GET_ITEM(a[14], i), "a buffer of out_n", at::kByte, {(int64_t)bytes[i]}).data_ptr();
+        check(bd_qtensor_sizes(rows, dim, &bytes[0], &bytes[1], &bytes[2]));
+        if (a[14] == Py_True) {
+            int64_t at[3], total = 0;
+            for (int i = 0; i < 3; i++) {
+                at[i] = total;
+                total += padded((int64_t)bytes[i]);
+            }
+            const at::Tensor all = at::empty({total}, on_device(at::kByte));
+            for (int i = 0; i < 3; i++) operand[i] = part(all, at[i], at::kByte, {(int64_t)bytes[i]});
+        } else {
+            if (!PyTuple_Check(a[14]) || PyTuple_GET_SIZE(a[14]) != 3) refuse("out_n must be a QTensor");
+            for (int i = 0; i < 3; i++) operand[i] = whole(PyTuple_GET_ITEM(a[14], i), "a buffer of out_n", at::kByte, {(int64_t)bytes[i]});
+        }
+        void **slot[3] = {&q.codes, &q.ids, &q.scales};
+        for (int i = 0; i < 3; i++) *slot[i] = operand[i].data_ptr();
         q.rows = rows; q.K = dim;
         k.q = &q;
     } else if (k.weight) {
@@ -266,7 +283,7 @@ PyObject *norm(PyObject *const *a, Py_ssize_t n) {
         k.n = rows_of(out, "out_n", &k.ldn);
     }
     if (rows) check(bd_residual_norm(&k, dt, rows, dim, stream.raw));
-    return tuple_of({h, out});
+    return tuple_of({h, out, operand[0], operand[1], operand[2]});
 }
 
 PyMethodDef methods[] = {BD_ENTRY(route), BD_ENTRY(plan), BD_ENTRY(experts), BD_ENTRY(mlp_workspace_size), BD_ENTRY(mlp), BD_ENTRY(norm), BD_ENTRY(set_check),

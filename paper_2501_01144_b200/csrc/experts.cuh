@@ -715,13 +715,16 @@ inline bool make_map_3d(CUtensorMap *map, CUtensorMapDataType type, const void *
 }
 
 template <bool GATED, int TOK>
-inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t items_most, const bd_experts *W, Product p, void *Y, bool y_bf16, cudaStream_t st) {
+inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t tokens, int64_t items_most, const bd_experts *W, Product p, void *Y, bool y_bf16, cudaStream_t st) {
     using L = Layout<GATED, TOK>;
     Maps m;
     const int64_t N = W->rows, K = W->K, rtw = row_tiles(N), kg = k_groups(K), pitch = row_pitch(K), tiles_x = ex.rows / kRowAlign;
     constexpr CUtensorMapDataType kBytes = CU_TENSOR_MAP_DATA_TYPE_UINT8, kWords = CU_TENSOR_MAP_DATA_TYPE_UINT32;
+    // (an item has no more tokens than the call: a small call's maps are the few that it can need)
     for (int b = 0; b < kBoxes; b++)
-        if (!make_map_3d(&m.x[b], kBytes, x8, kGroupBytes, ex.rows, kg, pitch, kGroupBytes, kGroupBytes, 8u << b, kStep, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
+        if (b > 0 && (8 << b) > TOK / 2) m.x[b] = m.x[b - 1];
+        else if (b > 0 && (8 << b) >= 2 * tokens) m.x[b] = m.x[b - 1];
+        else if (!make_map_3d(&m.x[b], kBytes, x8, kGroupBytes, ex.rows, kg, pitch, kGroupBytes, kGroupBytes, 8u << b, kStep, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
     if (!make_map_3d(&m.codes, kBytes, W->codes, K / 2, N, W->experts, K / 2, (uint64_t)N * (K / 2), kStep * 64, 128, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_3d(&m.ids, kWords, W->ids, kIdAtomBytes / 4, rtw, (uint64_t)kg * W->experts, kIdAtomBytes, (uint64_t)rtw * kIdAtomBytes, kIdAtomBytes / 4, 1, kStep, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !make_map_3d(&m.sfw, kWords, W->scales, kScaleAtomBytes / 4, rtw, (uint64_t)kg * W->experts, kScaleAtomBytes, (uint64_t)rtw * kScaleAtomBytes, kScaleAtomBytes / 4, 1, kStep, CU_TENSOR_MAP_SWIZZLE_NONE) ||

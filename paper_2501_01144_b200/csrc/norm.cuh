@@ -31,25 +31,44 @@ struct Args {
     float scale, eps, offset;
 };
 
-// Eight elements in fp32.  VEC: neighbours, in one or two 16-byte accesses; else elements `step` apart, those behind `dim` zeros.
+// A piece of eight elements as it comes from memory.  VEC: neighbours, in one or two 16-byte accesses; else elements `step` apart.  Those
+// behind `dim` are zeros.
 template <int DT, bool VEC>
-__device__ __forceinline__ void load8(const uint8_t *p, int e, int step, int dim, float (&v)[8]) {
-    constexpr int EB = Loader<DT>::kElemBytes;
-    if (VEC) {
-        if (e >= dim) {
+struct Piece {
+    static constexpr int EB = Loader<DT>::kElemBytes, W = VEC ? EB / 2 : 1;
+    uint4 raw[W];
+    float one[VEC ? 1 : 8];
+    __device__ __forceinline__ void load(const uint8_t *p, int e, int step, int dim) {
+        if (VEC) {
 #pragma unroll
-            for (int q = 0; q < 8; q++) v[q] = 0.0f;
-            return;
-        }
-        const uint4 *src = (const uint4 *)(p + (int64_t)e * EB);
-        const uint4 a = src[0];
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-        if (DT == BD_F32) {
-            const uint4 b = src[1];
-            const uint32_t z[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int q = 0; q < 4; q++) { v[q] = __uint_as_float(w[q]); v[4 + q] = __uint_as_float(z[q]); }
+            for (int i = 0; i < W; i++) raw[i] = e < dim ? *((const uint4 *)(p + (int64_t)e * EB) + i) : make_uint4(0, 0, 0, 0);
         } else {
+#pragma unroll
+            for (int q = 0; q < 8; q++) {
+                const int at = e + q * step;
+                float v = 0.0f;
+                if (at < dim) {
+                    const uint8_t *src = p + (int64_t)at * EB;
+                    if (DT == BD_F32) v = *(const float *)src;
+                    else if (DT == BD_BF16) v = __uint_as_float((uint32_t) * (const uint16_t *)src << 16);
+                    else v = __half2float(*(const __half *)src);
+                }
+                one[VEC ? 0 : q] = v;
+            }
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        if (!VEC) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) v[q] = one[VEC ? 0 : q];
+        } else if (DT == BD_F32) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const uint4 u = raw[W == 2 ? i : 0];
+                v[4 * i] = __uint_as_float(u.x); v[4 * i + 1] = __uint_as_float(u.y); v[4 * i + 2] = __uint_as_float(u.z); v[4 * i + 3] = __uint_as_float(u.w);
+            }
+        } else {
+            const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
 #pragma unroll
             for (int q = 0; q < 4; q++) {
                 if (DT == BD_BF16) {
@@ -62,19 +81,13 @@ __device__ __forceinline__ void load8(const uint8_t *p, int e, int step, int dim
                 }
             }
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; q++) {
-            const int at = e + q * step;
-            v[q] = 0.0f;
-            if (at < dim) {
-                const uint8_t *src = p + (int64_t)at * EB;
-                if (DT == BD_F32) v[q] = *(const float *)src;
-                else if (DT == BD_BF16) v[q] = __uint_as_float((uint32_t) * (const uint16_t *)src << 16);
-                else v[q] = __half2float(*(const __half *)src);
-            }
-        }
     }
+};
+template <int DT, bool VEC>
+__device__ __forceinline__ void load8(const uint8_t *p, int e, int step, int dim, float (&v)[8]) {
+    Piece<DT, VEC> t;
+    t.load(p, e, step, dim);
+    t.values(v);
 }
 template <int DT>
 __device__ __forceinline__ uint32_t pair_of(float a, float b) {
@@ -120,7 +133,7 @@ __device__ __forceinline__ int place(int e) {
 }
 
 template <int DT, int VPT, bool QUANT, bool VEC>
-__global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kMaxThreads, QUANT && DT == BD_BF16 ? 2 : VPT == 4 || QUANT ? 1 : VPT == 2 ? 2 : 3) residual_norm_kernel(const __grid_constant__ Args a) {
     __shared__ float part[2][kMaxThreads / 32];
     __shared__ SmemTables tab;
     extern __shared__ __align__(16) uint8_t row_buffer[];         // QUANT: [row groups] rows of dim elements
@@ -142,7 +155,10 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
         for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
         return s;
     };
-    auto elem = [&](int v) { return VEC ? (v * rt + t) * 8 : v * 8 * rt + t; };   // first element of piece v; the others follow, or are rt apart
+    // OWN: a thread has the 32 neighbours of one block and quantises them from its registers; otherwise the row goes through shared memory first
+    constexpr bool OWN = QUANT && VEC && VPT == 4;
+    // first element of piece v; the others follow, or are rt apart
+    auto elem = [&](int v) { return OWN ? (t * 4 + v) * 8 : VEC ? (v * rt + t) * 8 : v * 8 * rt + t; };
     auto normalise = [&](float (&x)[VPT][8], const uint8_t *w, const uint8_t *b) {
         if (a.layer) {
             float s = 0.0f;
@@ -179,20 +195,39 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int EB = Loader<DT>::kElemBytes;
     const int kgs = QUANT ? (int)k_groups(a.q.K) : 0, total = QUANT ? (int)row_tiles(a.q.rows) * kRowTile : a.rows;
+    // The next round's rows are on their way while this one's are worked on (AHEAD: whole pieces; single elements would cost too many
+    // registers): with the loads of a row in front of its own reductions, memory idles while a CTA reduces.
+    constexpr bool AHEAD = VEC && !QUANT;
+    Piece<DT, VEC> ny[AHEAD ? VPT : 1], nr[AHEAD ? VPT : 1];
+    auto fetch = [&](int r) {
+        if (AHEAD && r < a.rows) {
+#pragma unroll
+            for (int v = 0; v < (AHEAD ? VPT : 1); v++) {
+                ny[v].load(a.y + (int64_t)r * a.ldy * EB, elem(v), rt, a.dim);
+                if (a.residual) nr[v].load(a.residual + (int64_t)r * a.ldr * EB, elem(v), rt, a.dim);
+            }
+        }
+    };
+    const int step = gridDim.x * a.row_groups;
+    fetch(blockIdx.x * a.row_groups + group);
     // every thread of the CTA goes through the same number of rounds (barriers inside); a group behind the last row only keeps step
-    for (int base = blockIdx.x * a.row_groups; base < total; base += gridDim.x * a.row_groups) {
+    for (int base = blockIdx.x * a.row_groups; base < total; base += step) {
         const int r = base + group;
         const bool there = r < a.rows;
         float x[VPT][8], g[8];
+        Piece<DT, VEC> res[AHEAD ? VPT : 1];
 #pragma unroll
         for (int v = 0; v < VPT; v++) {
             if (there) {
-                load8<DT, VEC>(a.y + (int64_t)r * a.ldy * EB, elem(v), rt, a.dim, x[v]);
+                if (AHEAD) ny[AHEAD ? v : 0].values(x[v]);
+                else load8<DT, VEC>(a.y + (int64_t)r * a.ldy * EB, elem(v), rt, a.dim, x[v]);
+                if (AHEAD) res[AHEAD ? v : 0] = nr[AHEAD ? v : 0];
             } else {
 #pragma unroll
                 for (int q = 0; q < 8; q++) x[v][q] = 0.0f;
             }
         }
+        if (base + step < total) fetch(r + step);
         if (a.post_weight) normalise(x, a.post_weight, a.post_bias);
         if (there) {
             if (a.gate || a.residual) {
@@ -211,7 +246,10 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
                     }
 #pragma unroll
                     for (int q = 0; q < 8; q++) g[q] = 0.0f;
-                    if (a.residual) load8<DT, VEC>(a.residual + (int64_t)r * a.ldr * EB, elem(v), rt, a.dim, g);
+                    if (a.residual) {
+                        if (AHEAD) res[AHEAD ? v : 0].values(g);
+                        else load8<DT, VEC>(a.residual + (int64_t)r * a.ldr * EB, elem(v), rt, a.dim, g);
+                    }
 #pragma unroll
                     for (int q = 0; q < 8; q++) x[v][q] = fmaf(row_gate, x[v][q], g[q]);
                 }
@@ -236,28 +274,30 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
             continue;
         }
         uint8_t *row = row_buffer + group * a.dim * EB;
+        if (!OWN) {
 #pragma unroll
-        for (int v = 0; v < VPT; v++) {
-            if (VEC) {                                            // eight neighbours: one piece of 16 bytes, fp32 two
-                if (elem(v) < a.dim) {
-                    if (DT == BD_F32) {
-                        *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(__float_as_uint(x[v][0]), __float_as_uint(x[v][1]), __float_as_uint(x[v][2]), __float_as_uint(x[v][3]));
-                        *(uint4 *)(row + place<DT>(elem(v) + 4)) = make_uint4(__float_as_uint(x[v][4]), __float_as_uint(x[v][5]), __float_as_uint(x[v][6]), __float_as_uint(x[v][7]));
-                    } else {
-                        *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(pair_of<DT>(x[v][0], x[v][1]), pair_of<DT>(x[v][2], x[v][3]), pair_of<DT>(x[v][4], x[v][5]), pair_of<DT>(x[v][6], x[v][7]));
+            for (int v = 0; v < VPT; v++) {
+                if (VEC) {                                            // eight neighbours: one piece of 16 bytes, fp32 two
+                    if (elem(v) < a.dim) {
+                        if (DT == BD_F32) {
+                            *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(__float_as_uint(x[v][0]), __float_as_uint(x[v][1]), __float_as_uint(x[v][2]), __float_as_uint(x[v][3]));
+                            *(uint4 *)(row + place<DT>(elem(v) + 4)) = make_uint4(__float_as_uint(x[v][4]), __float_as_uint(x[v][5]), __float_as_uint(x[v][6]), __float_as_uint(x[v][7]));
+                        } else {
+                            *(uint4 *)(row + place<DT>(elem(v))) = make_uint4(pair_of<DT>(x[v][0], x[v][1]), pair_of<DT>(x[v][2], x[v][3]), pair_of<DT>(x[v][4], x[v][5]), pair_of<DT>(x[v][6], x[v][7]));
+                        }
                     }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; q++)
+                        if (elem(v) + q * rt < a.dim) {
+                            if (DT == BD_F32) *(float *)(row + place<DT>(elem(v) + q * rt)) = x[v][q];
+                            else *(uint16_t *)(row + place<DT>(elem(v) + q * rt)) = (uint16_t)pair_of<DT>(x[v][q], 0.0f);
+                        }
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; q++)
-                    if (elem(v) + q * rt < a.dim) {
-                        if (DT == BD_F32) *(float *)(row + place<DT>(elem(v) + q * rt)) = x[v][q];
-                        else *(uint16_t *)(row + place<DT>(elem(v) + q * rt)) = (uint16_t)pair_of<DT>(x[v][q], 0.0f);
-                    }
             }
+            if (warps == 1) __syncwarp();
+            else __syncthreads();
         }
-        if (warps == 1) __syncwarp();
-        else __syncthreads();
         const int nb = a.dim / kBlock;
         for (int b0 = 0; b0 < kgs * kBlocksPerAtom; b0 += rt) {   // (whole quads of lanes: rt is a multiple of 32)
             const int b = b0 + t;
@@ -269,14 +309,26 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
                     uint32_t pairs[16];
 #pragma unroll
                     for (int p = 0; p < 4; p++) {
-                        const uint4 u = *(const uint4 *)(row + place<DT>(b * kBlock + 8 * p));
-                        pairs[4 * p] = u.x; pairs[4 * p + 1] = u.y; pairs[4 * p + 2] = u.z; pairs[4 * p + 3] = u.w;
+                        if (OWN) {
+#pragma unroll
+                            for (int q = 0; q < 4; q++) pairs[4 * p + q] = pair_of<DT>(x[OWN ? p : 0][2 * q], x[OWN ? p : 0][2 * q + 1]);
+                        } else {
+                            const uint4 u = *(const uint4 *)(row + place<DT>(b * kBlock + 8 * p));
+                            pairs[4 * p] = u.x; pairs[4 * p + 1] = u.y; pairs[4 * p + 2] = u.z; pairs[4 * p + 3] = u.w;
+                        }
                     }
                     quantize_bf16_block<false>(pairs, tab, res, unused);
                 } else {
                     uint32_t bits[32];
+                    if (OWN) {
 #pragma unroll
-                    for (int p = 0; p < 2 * EB; p++) {
+                        for (int k = 0; k < 32; k++) {
+                            const float v = x[OWN ? k / 8 : 0][k % 8];
+                            bits[k] = __float_as_uint(DT == BD_F16 ? __half2float(__float2half_rn(v)) : v);
+                        }
+                    }
+#pragma unroll
+                    for (int p = 0; p < (OWN ? 0 : 2 * EB); p++) {
                         const uint4 u = *(const uint4 *)(row + place<DT>(b * kBlock + 16 / EB * p));
                         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -307,7 +359,7 @@ __global__ void __launch_bounds__(kMaxThreads) residual_norm_kernel(const __grid
                 *(uint16_t *)(a.q.ids + id_byte_offset(a.q.rows, r, b)) = (uint16_t)idn;
             }
         }
-        if (warps == 1) __syncwarp();
+        if (OWN || warps == 1) __syncwarp();
         else __syncthreads();                                     // the buffer is the next round's
     }
 }
