@@ -429,7 +429,7 @@ bd_status bd_qk_norm_rope(const bd_rope_operand *q, const bd_rope_operand *k, bd
  * expert, -1 where there is none.  All of it is int32 on the device; `scratch`: bd_expert_plan_scratch bytes, 16-byte aligned, of the call that
  * makes the plan alone.  bd_make_expert_plan makes it for ids from elsewhere: negative ids are left out, ids of `experts` and more
  * are left out and told (BD_ERR_INDEX), a token that names an expert twice has one row with it.
- * At most 64 tokens: one launch, otherwise two. */
+ * At most 64 tokens: one launch; otherwise the plan takes two more, or two for given ids. */
 typedef enum { BD_SCORE_SOFTMAX = 0, BD_SCORE_SIGMOID = 1 } bd_score;
 typedef struct {
     bd_score score;

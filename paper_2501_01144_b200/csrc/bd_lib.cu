@@ -581,7 +581,7 @@ void launch_read(const bd_paged_cache *c, const bd_paged_batch *b, dim3 grid, vo
 
 // ---- routing, experts, norms --------------------------------------------------------------------------------------------
 template <int NV, bool SIGMOID, bool WIDE>
-bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, unsigned blocks, cudaStream_t st) {
+bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, cudaStream_t st) {
     static bool configured[64] = {};                              // per instantiation and device
     int dev = 0;
     cudaGetDevice(&dev);
@@ -592,16 +592,33 @@ bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, unsigned blocks,
         configured[dev] = true;
     }
     const size_t smem = WIDE && r.groups > 1 ? (size_t)rt::kWarps * (r.experts + 1) * sizeof(double) : 0;
-    launch_serialized(rt::route_kernel<NV, SIGMOID, WIDE>, blocks, rt::kThreads, smem, st, r, plan);
+    // with a plan the CTAs are one cluster: up to eight, a power of two
+    const int64_t ctas = std::max<int64_t>(1, (r.tokens + rt::kWarps - 1) / rt::kWarps);
+    unsigned cluster = 1;
+    while (plan.place && (int64_t)cluster < ctas) cluster *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((ctas + cluster - 1) / cluster) * cluster);
+    cfg.blockDim = dim3(rt::kRouteThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaLaunchKernelEx(&cfg, rt::route_kernel<NV, SIGMOID, WIDE>, r, plan);
     return launch_result();
 }
 template <bool SIGMOID, bool WIDE>
-bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, unsigned blocks, cudaStream_t st) {
+bd_status launch_route(const rt::Rule &r, const rt::Plan &plan, cudaStream_t st) {
     const int per_lane = (r.experts + 31) / 32;
-    if (per_lane <= 2) return launch_route<2, SIGMOID, WIDE>(r, plan, blocks, st);
-    if (per_lane <= 4) return launch_route<4, SIGMOID, WIDE>(r, plan, blocks, st);
-    if (per_lane <= 8) return launch_route<8, SIGMOID, WIDE>(r, plan, blocks, st);
-    return launch_route<16, SIGMOID, WIDE>(r, plan, blocks, st);
+    if (per_lane <= 2) return launch_route<2, SIGMOID, WIDE>(r, plan, st);
+    if (per_lane <= 4) return launch_route<4, SIGMOID, WIDE>(r, plan, st);
+    if (per_lane <= 8) return launch_route<8, SIGMOID, WIDE>(r, plan, st);
+    return launch_route<16, SIGMOID, WIDE>(r, plan, st);
 }
 bd_status check_plan(const bd_expert_plan *p) {
     if (!p || !p->count || !p->start || !p->place) return BD_ERR_INVALID_ARG;
@@ -610,10 +627,13 @@ bd_status check_plan(const bd_expert_plan *p) {
     if (((uintptr_t)p->count | (uintptr_t)p->start | (uintptr_t)p->place) & 3u) return BD_ERR_ALIGN;
     return BD_OK;
 }
-// Several blocks of tokens: the second launch, at most 256 CTAs.
-bd_status launch_places(const rt::Rule &r, const rt::Plan &plan, int64_t blocks, cudaStream_t st) {
+// The plan of ids in memory: one launch for one block of tokens, else a second one of at most 256 CTAs.
+bd_status plan_of_ids(const rt::Rule &r, const rt::Plan &plan, int64_t blocks, cudaStream_t st) {
+    launch_serialized(rt::plan_count_kernel, (unsigned)blocks, rt::kPlanThreads, 0, st, r, plan);
+    bd_status s = launch_result();
+    if (s || blocks == 1) return s;
     const int per = (int)((blocks + 255) / 256);
-    launch_serialized(rt::plan_place_kernel, (unsigned)((blocks + per - 1) / per), rt::kThreads, 0, st, r, plan, (int)blocks, per);
+    launch_serialized(rt::plan_place_kernel, (unsigned)((blocks + per - 1) / per), rt::kPlanThreads, 0, st, r, plan, (int)blocks, per);
     return launch_result();
 }
 bd_status check_experts(const bd_experts *w) {
@@ -1719,14 +1739,16 @@ bd_status bd_route(const void *logits, bd_dtype dtype, int64_t tokens, int64_t l
         return BD_OK;
     }
     const rt::Rule r{logits, ld, bias, valid, ids, weights, (int)dtype, (int)tokens, (int)rule->experts, (int)rule->top_k, (int)rule->groups,
-                     (int)rule->top_groups, rule->group_top, rule->scale, rule->renormalise != 0};
+                     (int)rule->top_groups, rule->group_top, rule->scale, rule->renormalise != 0, make_fast_div((uint32_t)(rule->experts / rule->groups))};
     const rt::Plan p = plan ? rt::Plan{plan->count, plan->start, plan->place, (uint8_t *)plan->scratch} : rt::Plan{};
     cudaStream_t st = (cudaStream_t)stream;
     const bool wide = bias || rule->groups > 1;
-    bd_status s;
-    if (rule->score == BD_SCORE_SIGMOID) s = wide ? launch_route<true, true>(r, p, (unsigned)blocks, st) : launch_route<true, false>(r, p, (unsigned)blocks, st);
-    else s = wide ? launch_route<false, true>(r, p, (unsigned)blocks, st) : launch_route<false, false>(r, p, (unsigned)blocks, st);
-    return s || !plan || blocks == 1 ? s : launch_places(r, p, blocks, st);
+    const rt::Plan with = blocks == 1 ? p : rt::Plan{};
+    bd_status s = BD_OK;
+    if (tokens == 0) return plan_of_ids(r, p, blocks, st);
+    if (rule->score == BD_SCORE_SIGMOID) s = wide ? launch_route<true, true>(r, with, st) : launch_route<true, false>(r, with, st);
+    else s = wide ? launch_route<false, true>(r, with, st) : launch_route<false, false>(r, with, st);
+    return s || !plan || blocks == 1 ? s : plan_of_ids(r, p, blocks, st);
 }
 
 bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, void *stream) {
@@ -1737,11 +1759,9 @@ bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, vo
     const int64_t blocks = std::max<int64_t>(1, rt::blocks_of(plan->tokens));
     if (blocks > 1 && !plan->scratch) return BD_ERR_WORKSPACE;
     if (!aligned16(plan->scratch)) return BD_ERR_ALIGN;
-    const rt::Rule r{nullptr, 0, nullptr, nullptr, (int32_t *)ids, nullptr, 0, (int)plan->tokens, (int)plan->experts, (int)plan->top_k, 1, 1, 1, 1.0f, 0};
+    const rt::Rule r{nullptr, 0, nullptr, nullptr, (int32_t *)ids, nullptr, 0, (int)plan->tokens, (int)plan->experts, (int)plan->top_k, 1, 1, 1, 1.0f, 0, FastDiv{}};
     const rt::Plan p{plan->count, plan->start, plan->place, (uint8_t *)plan->scratch};
-    launch_serialized(rt::plan_count_kernel, (unsigned)blocks, rt::kThreads, 0, (cudaStream_t)stream, r, p);
-    if ((s = launch_result()) || blocks == 1) return s;
-    return launch_places(r, p, blocks, (cudaStream_t)stream);
+    return plan_of_ids(r, p, blocks, (cudaStream_t)stream);
 }
 
 bd_status bd_expert_mlp_workspace_size(int64_t tokens, int64_t top_k, const bd_experts *up, const bd_experts *down, bd_dtype ydtype, size_t *bytes) {
