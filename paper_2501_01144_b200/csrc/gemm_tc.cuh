@@ -177,6 +177,7 @@ struct Smem {
 };
 static_assert((2 * kXStages + 2 * kCodeStages + 2 * kABufs + 2) * 8 <= 512, "barrier area too small");
 static_assert(Smem::total <= 227 * 1024, "shared memory budget");
+static_assert(16 + 4 * kDecodeWarps <= Smem::luts - Smem::words, "a word per decode warp behind the CTA's own");
 
 // Work items of a launch, identical for every cluster: cluster c takes items c, c + clusters, ...
 // Tiles are numbered with the token tile running fastest (token tile = tile % t_tiles, weight-row pair =
@@ -520,7 +521,12 @@ gemm_wtmem_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 ids16 = *(const uint16_t *)(base_ptr + Smem::ids + s * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
 #pragma unroll
                 for (int c = 0; c < 4; c++) w[c] = *(const uint4 *)(codes + 16 * (c ^ swz64));
-                // the codes are in registers: hand the stage back to its producer
+                // The codes are in registers: hand the stage back to its producer.  With the requantising epilogue's scattered stores on the
+                // way the loads may have been issued and not have arrived for longer than a refill takes (seen in the experts' products,
+                // whose epilogue stores alike): a store of something made of all of them cannot leave before them.
+                if (REQUANT)
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)Smem::words + 16u + 4u * (uint32_t)(warp - kDecodeWarp0)),
+                                 "r"(ids16 ^ w[0].x ^ w[1].x ^ w[2].x ^ w[3].x) : "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(c_empty(s));
                 dead = !mbar_wait(a_empty(b), b_par, abort_flag);
