@@ -568,6 +568,11 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         __syncwarp();
     }
 
+    // After a wait ran out copies and products may be in flight still, to barriers that will not complete: they arrive within some
+    // microseconds, and nothing of the pair's memory goes back before (about a millisecond).
+    if (*abort_flag)
+        for (int i = 0; i < 64; i++) __nanosleep(16384);
+    __syncwarp();
     tcgen05_fence_before();
     __syncthreads();
     cluster_sync_all();                                           // the peer may still signal our barriers until here

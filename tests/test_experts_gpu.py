@@ -288,3 +288,64 @@ def test_experts_are_operands_of_their_own():
         assert all(torch.equal(a, b) for a, b in zip((q.codes, q.ids, q.scales), (e.codes[k], e.ids[k], e.scales[k])))
     x = tokens_of(5, 96, torch.bfloat16)
     assert torch.equal(bd.linear(x, e.expert(1)), bd.linear(x, bd.quantize_weights(w[1][order].contiguous())))
+
+
+@pytest.mark.parametrize("tokens", [4, 600])                      # narrow items, and items of 256 tokens
+def test_a_wait_that_runs_out_is_told_and_the_next_call_is_served(tokens):
+    up, down = weights(2, 512, 256, 256)
+    ids = torch.randint(0, 2, (tokens, 1), generator=torch.Generator().manual_seed(1), dtype=torch.int32).cuda()
+    x, w, plan = tokens_of(tokens, 512, torch.bfloat16), torch.ones(tokens, 1, device="cuda"), bd.expert_plan(ids, 2)
+    good = bd.expert_mlp(x, plan, w, up, down)
+    bd.poll_status()
+    try:
+        # the first copy of packed weights of every CTA is never started: nothing is in flight for it, and the wait for it ends
+        bd.debug_fault(poll_limit=10 * 1024, skip_first_code_stage=True)
+        bd.expert_mlp(x, plan, w, up, down)
+        with pytest.raises(bd.BdError) as e:
+            bd.poll_status()
+        assert e.value.status == 7
+    finally:
+        bd.debug_fault(0, False)
+    for _ in range(3):
+        assert torch.equal(bd.expert_mlp(x, plan, w, up, down), good)
+    bd.poll_status()
+
+
+def test_two_plans_and_two_workspaces_in_two_graphs():
+    up, down = weights(6, 256, 128, 256)
+    g = torch.Generator(device="cuda").manual_seed(21)
+    jobs = []
+    for n in (48, 200):
+        x, logits = tokens_of(n, 256, torch.bfloat16, n), torch.randn(n, 6, generator=g, device="cuda")
+        ws = torch.empty(bd.expert_mlp_workspace_size(n, 2, up, down), dtype=torch.uint8, device="cuda")
+
+        def step(x=x, logits=logits, ws=ws):
+            ids, w, plan = bd.route(logits, 2)
+            return bd.expert_mlp(x, plan, w, up, down, workspace=ws)
+
+        want = step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = step()
+        jobs.append((graph, y, want))
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (graph, _, _) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    bd.poll_status()
+    for _, y, want in jobs:
+        assert torch.equal(y, want)
+
+
+def test_experts_of_large_and_tiny_scales():
+    g = torch.Generator(device="cuda").manual_seed(22)
+    for gain in (2.0 ** -40, 2.0 ** 20):
+        W = torch.randn(2, 128, 128, generator=g, device="cuda") * 128 ** -0.5
+        up = bd.quantize_experts(W, bd.SELECT_TWO_STAGE, gated=True)
+        down = bd.quantize_experts(torch.randn(2, 72, 64, generator=g, device="cuda") * gain, bd.SELECT_TWO_STAGE)
+        ids = torch.arange(30, device="cuda").remainder(2).to(torch.int32)[:, None].contiguous()
+        check(tokens_of(30, 128, torch.float32), ids, torch.ones(30, 1, device="cuda"), up, down)
