@@ -328,16 +328,16 @@ def test_two_plans_and_two_workspaces_in_two_graphs():
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             y = step()
-        jobs.append((graph, y, want))
+        jobs.append((graph, y, want, x, logits, ws))                  # a graph does not keep its inputs alive
     streams = [torch.cuda.Stream() for _ in jobs]
     torch.cuda.synchronize()
     for _ in range(20):
-        for s, (graph, _, _) in zip(streams, jobs):
+        for s, (graph, *_) in zip(streams, jobs):
             with torch.cuda.stream(s):
                 graph.replay()
     torch.cuda.synchronize()
     bd.poll_status()
-    for _, y, want in jobs:
+    for _, y, want, *_ in jobs:
         assert torch.equal(y, want)
 
 
