@@ -463,7 +463,9 @@ bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, vo
  * Accuracy: the products as BD_GEMM_TCGEN05; act by fast exponentials and division, 2^-19 relative (gelu: of 1 + |x| where x is far below
  * zero); each expert's part of the sum is rounded to bf16 before it is weighted when Y is BD_BF16, and not rounded for BD_F32.
  * Device-side conditions (bd_poll_status): an Inf or NaN in X or before the second product (BD_ERR_NONFINITE); a plan whose numbers
- * lie outside its bounds (BD_ERR_INDEX; nothing is addressed by them).  Workspace: 256-byte aligned, of one call at a time. */
+ * lie outside its bounds (BD_ERR_INDEX; nothing is addressed by them); a wait that ran out (BD_ERR_TIMEOUT: what Y holds then means
+ * nothing).  Workspace: 256-byte aligned, of one call at a time, like the plan while the call runs.  After one call per device, shape class
+ * (few or many tokens per expert) and type further calls can be captured. */
 typedef struct {
     void *codes, *ids, *scales;
     int64_t experts, rows, K;

@@ -866,6 +866,9 @@ def import_canonical(codes, ids, scales, stream=None):
 
 def dequantize(q, stream=None):
     """fp32 [rows, K] values of a quantised operand (Sec. 3.3, Fig. 6)."""
+    out = (_block or _load_block()).dequantize(q.codes, q.ids, q.scales, q.rows, q.K, stream)
+    if out is not None:
+        return out
     out = torch.empty(q.rows, q.K, dtype=torch.float32, device=q.codes.device)
     cq = q.c_struct()
     _check(load().bd_dequantize(ctypes.byref(cq), ctypes.c_void_p(out.data_ptr()), out.stride(0), _stream(stream)))

@@ -286,7 +286,27 @@ PyObject *norm(PyObject *const *a, Py_ssize_t n) {
     return tuple_of({h, out, operand[0], operand[1], operand[2]});
 }
 
-PyMethodDef methods[] = {BD_ENTRY(route), BD_ENTRY(plan), BD_ENTRY(experts), BD_ENTRY(mlp_workspace_size), BD_ENTRY(mlp), BD_ENTRY(norm), BD_ENTRY(set_check),
+// codes, ids, scales, rows, K, stream -> fp32 [rows, K]; None where the operand's buffers are not exactly its own on the current device
+PyObject *dequantize(PyObject *const *a, Py_ssize_t n) {
+    need(n, 6);
+    bd_qtensor q{};
+    q.rows = integer(a[3]); q.K = integer(a[4]);
+    size_t bytes[3];
+    check(bd_qtensor_sizes(q.rows, q.K, &bytes[0], &bytes[1], &bytes[2]));
+    void **slot[3] = {&q.codes, &q.ids, &q.scales};
+    for (int i = 0; i < 3; i++) {
+        if (!THPVariable_Check(a[i])) Py_RETURN_NONE;
+        const at::Tensor &x = THPVariable_Unpack(a[i]);
+        if (x.scalar_type() != at::kByte || x.numel() != (int64_t)bytes[i] || !x.is_contiguous() || !x.is_cuda() || x.get_device() != c10::cuda::current_device()) Py_RETURN_NONE;
+        *slot[i] = x.data_ptr();
+    }
+    const StreamScope stream(a[5]);
+    const at::Tensor out = at::empty({q.rows, q.K}, on_device(at::kFloat));
+    check(bd_dequantize(&q, out.data_ptr<float>(), q.K, stream.raw));
+    return THPVariable_Wrap(out);
+}
+
+PyMethodDef methods[] = {BD_ENTRY(route), BD_ENTRY(plan), BD_ENTRY(experts), BD_ENTRY(mlp_workspace_size), BD_ENTRY(mlp), BD_ENTRY(norm), BD_ENTRY(dequantize), BD_ENTRY(set_check),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods};
 
