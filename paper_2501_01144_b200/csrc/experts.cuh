@@ -13,6 +13,14 @@
 // tokens (rounded up to 16), so a decode step, where an expert has a few tokens, pays for the weights' way through the SM and
 // little else.  The gate and up rows of 32 channels are neighbours (rows 64 j + i and 64 j + 32 + i): they meet in the warps of
 // one CTA, and 32 channels are one block of the next product's operand.
+//
+// Bound: few tokens per expert, the weights' expansion (decode groups: 35/64 byte read and 1 byte written to tensor memory per element,
+// integer instructions beside a half-full issue) under the weights' bytes; many tokens, the block-scaled MMA at the clock that the power cap
+// leaves.  Measured (B200; first + second product, us, cold):
+//     1 token, 64 experts, 8 a token, 2048 -> 1024          17.5 + 13.5    27.5 MB: latency of 8 and 4 k-steps behind a launch
+//     64 tokens, 128 experts, 8, 2048 -> 1024               63 + 39        434 MB: 4.6 and 3.7 TB/s
+//     1500 tokens, 64 experts, 6, 2048 -> 1408 (f16)        85 + 42        156 GFLOP
+//     8192 tokens, 8 experts, 2, 4096 -> 14336              1461 + 620     5.77 TFLOP: 2.6 and 3.1 PFLOP/s
 #pragma once
 #include "bd_common.cuh"
 #include "gemm_tc.cuh"
@@ -63,7 +71,7 @@ constexpr int kCodeBytes = 128 * kStep * 64; // packed codes of 128 weight rows
 // TOK: most tokens of an item.  256: an accumulator of 256 columns, room for three decoded k-steps behind it.  128, where experts have few
 // tokens: an accumulator of 128 columns, which items of up to 64 tokens use half by half in turn, so that the next item's products run
 // while one is read out; five decoded k-steps, so that a decode group does not wait for the products of its last one (with three:
-// 1190 cycles a k-step for a few tokens, 970 of 3490 of a group's waiting); smaller token stages and more stages for the codes.
+// 1190 cycles a k-step for a few tokens, 970 of 3490 of a group's waiting; now 1120); smaller token stages and a fourth decode group.
 template <bool GATED, int TOK>
 struct Layout {
     static constexpr int kSlots = TOK == 256 ? 1 : 2;            // accumulators in turn
@@ -583,6 +591,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
 }
 
 // Quantises the tokens and writes each to the rows of its experts: thread = (token, block of 32), four lanes a scale word.
+// Bound: a launch where tokens are few (6 us for 1 token, cold), else reading x and the operand's k copies (8192 x 4096, 2 each: 29.5 us).
 template <int DT>
 __global__ void __launch_bounds__(256) spread_kernel(const uint8_t *__restrict__ X, int64_t ldx, int tokens, int top_k, const int32_t *__restrict__ place,
                                                      int nb, int kgroups, int rows, uint8_t *__restrict__ x8, uint8_t *__restrict__ scales, FastDiv div_row) {
@@ -636,6 +645,7 @@ __global__ void __launch_bounds__(256) spread_kernel(const uint8_t *__restrict__
 }
 
 // y_t = sum_j w_tj * part[place_tj], thread = eight neighbouring outputs of a token.  A token without experts gets zeros.
+// Bound: memory (8192 tokens, 2 rows of 4096 in bf16 each: 40 us for 201 MB), a launch where tokens are few (7.2 us for 1 token, cold).
 template <bool BF16>
 __global__ void __launch_bounds__(256) combine_kernel(const uint8_t *__restrict__ part, const int32_t *__restrict__ place, const float *__restrict__ weights,
                                                       int tokens, int top_k, int rows, int n, void *__restrict__ Y, int64_t ldy) {

@@ -13,7 +13,8 @@
 // At most 64 tokens: all in one launch; else two launches behind the routing, counts and places.
 //
 // Bound: T E logits read and 12 T k bytes written, 9 MB for 8192 x 256 x 8, are a microsecond or two: what counts is the latency of a
-// token's chain of steps, and for many tokens the instructions it takes.
+// token's chain of steps, and for many tokens the instructions it takes.  Measured (B200, from a graph, plan and all): 64 of 128 experts 5.4 us
+// (one launch); 8192 of 256 with a bias and groups 32 us, of 512 53 us; 1001 of 8 6.9 us (three launches).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
