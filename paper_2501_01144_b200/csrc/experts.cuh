@@ -159,6 +159,12 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
+__device__ __forceinline__ int load_relaxed(const int32_t *p) {
+    int v;
+    asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 template <bool GATED, int TOK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((Layout<GATED, TOK>::kThreads), 1)
 expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const Product p) {
@@ -224,10 +230,10 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     cluster_sync_all();                                           // both CTAs: running, barriers initialised, TMEM allocated
     tcgen05_fence_after();
     // The schedule: items of the experts before each one, by a scan in the leader's first warp, which writes it to both CTAs: they hand
-    // over to one another item by item, so they must go by the same numbers whatever happens to the plan meanwhile.  Only behind the wait: in
-    // front of it a load may still meet what the caches held before the plan was written (the first-level cache's lines, for one).
+    // over to one another item by item, so they must go by the same numbers whatever happens to the plan meanwhile.  The plan and the weights
+    // are older than the kernel in front, which starts this one only behind its own wait for all that came before: they are read without
+    // waiting for it (the plan past the first-level cache, whose lines may be older), and codes are loaded and expanded while it ends.
     // Numbers that cannot be (a plan overwritten by the caller) leave the expert out and are told: nothing is addressed by them.
-    if (warp == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 0 && rank == 0) {
         const uint32_t to_first = map_to_cta(smem_u32(first), 1), to_where = map_to_cta(smem_u32(where), 1);
         auto share = [](uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); };
@@ -236,8 +242,8 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             const int e = e0 + lane;
             int cnt = 0, start = 0;
             if (e < ex.experts) {
-                cnt = ex.count[e];
-                start = ex.start[e];
+                cnt = load_relaxed(ex.count + e);
+                start = load_relaxed(ex.start + e);
                 if (cnt < 0 || start < 0 || start % kRowAlign || cnt > ex.rows || start > ex.rows - cnt) {
                     cnt = start = 0;
                     atomicOr(&g_status_word, kStatusIndex);
@@ -277,7 +283,8 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
         registers_down<L::kControlRegs>();
         if (warp == 0) {
             // ---- TMA producer of the token tile and the scale atoms; the one warp that reads what the kernel in front wrote ----
-            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the wait is behind this warp)
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: the next kernel takes it that all before this one is done)
             if (lane == 0) abort_flag[1] = 1;                     // from here on every bounded wait counts its polls
             int s = 0;
             uint32_t ph = 1;
