@@ -1738,8 +1738,11 @@ bd_status bd_route(const void *logits, bd_dtype dtype, int64_t tokens, int64_t l
     } else if (tokens == 0) {
         return BD_OK;
     }
+    int lane_shift = 5;
+    while ((rule->groups << lane_shift) > 32) lane_shift--;
     const rt::Rule r{logits, ld, bias, valid, ids, weights, (int)dtype, (int)tokens, (int)rule->experts, (int)rule->top_k, (int)rule->groups,
-                     (int)rule->top_groups, rule->group_top, rule->scale, rule->renormalise != 0, make_fast_div((uint32_t)(rule->experts / rule->groups))};
+                     (int)rule->top_groups, rule->group_top, rule->scale, rule->renormalise != 0, make_fast_div((uint32_t)(rule->experts / rule->groups)),
+                     (int)(rule->experts / rule->groups), lane_shift};
     const rt::Plan p = plan ? rt::Plan{plan->count, plan->start, plan->place, (uint8_t *)plan->scratch} : rt::Plan{};
     cudaStream_t st = (cudaStream_t)stream;
     const bool wide = bias || rule->groups > 1;

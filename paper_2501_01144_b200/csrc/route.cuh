@@ -13,8 +13,8 @@
 // At most 64 tokens: all in one launch; else two launches behind the routing, counts and places.
 //
 // Bound: T E logits read and 12 T k bytes written, 9 MB for 8192 x 256 x 8, are a microsecond or two: what counts is the latency of a
-// token's chain of steps, and for many tokens the instructions it takes.  Measured (B200, from a graph, plan and all): 64 of 128 experts 5.4 us
-// (one launch); 8192 of 256 with a bias and groups 32 us, of 512 53 us; 1001 of 8 6.9 us (three launches).
+// token's chain of steps, and for many tokens the instructions it takes.  Measured (B200, from a graph, plan and all): 64 of 128 experts 5.5 us
+// (one launch), 64 of 256 with a bias and groups 9.5; 8192 of 256 with a bias and groups 30.5 us, of 512 49; 1001 of 8 6.9 us (three launches).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -52,7 +52,8 @@ struct Rule {
     int dt, tokens, experts, top_k, groups, top_groups, group_top;
     float scale;
     int renormalise;
-    FastDiv group_of;                        // expert -> group
+    FastDiv group_of;                        // expert -> group, and the lanes that a group has in `kept_groups`, as a power of two
+    int group_size, lane_shift;
 };
 
 // Order-preserving integers of floating-point numbers; 0 is below every number's.
@@ -145,12 +146,12 @@ __device__ __forceinline__ double smallest(double a, double b) { return fmin(a, 
 template <typename F>
 __device__ __forceinline__ uint32_t kept_groups(const Rule &r, const F *scratch, F &gap) {
     using Key = typename std::conditional<sizeof(F) == 8, uint64_t, uint32_t>::type;
-    const int lane = threadIdx.x % 32, size = r.experts / r.groups;
-    int lanes = 32;
-    while (lanes * r.groups > 32) lanes >>= 1;
-    const int g = lane / lanes, sub = lane % lanes, turn = g * lanes % size;   // (each group begins elsewhere: other banks)
+    const int lane = threadIdx.x % 32, size = r.group_size, lanes = 1 << r.lane_shift;
+    const int g = lane >> r.lane_shift, sub = lane & (lanes - 1);
+    const int turn = g * lanes - size * (int)fast_div((uint32_t)(g * lanes), r.group_of);   // (each group begins elsewhere: other banks)
     F a = -INFINITY, b = -INFINITY;                               // its two largest keys
     if (g < r.groups)
+#pragma unroll 4
         for (int j = sub; j < size; j += lanes) {
             const int k = j + turn < size ? j + turn : j + turn - size;
             const F v = scratch[g * size + k];
@@ -170,7 +171,7 @@ __device__ __forceinline__ uint32_t kept_groups(const Rule &r, const F *scratch,
         const Key best = warp_max(mine);
         if (best == 0) break;
         const int owner = __ffs(__ballot_sync(0xffffffffu, mine == best)) - 1;   // equal values: the lower group
-        kept |= 1u << (owner / lanes);
+        kept |= 1u << (owner >> r.lane_shift);
         last = best;
         if (lane == owner) mine = 0;
     }
@@ -212,14 +213,19 @@ __device__ __forceinline__ void select_largest(Key (&key)[NV], int count, int &m
 // One token by one warp.  NV: experts per lane.  WIDE: keys that are computed (a bias or groups).  Those are compared in 64 bits, but a
 // 64-bit exponential per expert, 64-bit comparisons and maxima are ten times the work: keys in 32 bits come first, and only where
 // two that decide lie closer together than 32 bits can be off does the token go through 64 bits (some in a thousand of random
-// ones).  How far a 32-bit key can be off: an exponential by 2^-22 of itself and by its argument's rounding, a sum of up to 16 + 5
-// additions by 2^-19, the rest by 2^-23: together below 2^-19 of the largest score, and 2^-24 of the key by the bias' addition.
+// ones).  How far a 32-bit key can be off.  Softmax: an exponential by 2^-22 of itself and by its argument's rounding, a sum of up to
+// 16 + 5 additions by 2^-19, the rest by 2^-23: together below 2^-19 of the largest score.  Sigmoid: the exponential's 2^-22 counts with
+// s (1 - s) <= 1/4, the sum and the quotient are rounded by 2^-24 each: together below 2^-22.  2^-24 of the key by the bias' addition.
 template <int NV, bool SIGMOID, bool WIDE>
 __device__ __forceinline__ void route_token(const Rule &r, int t, double *scratch, uint32_t *mask) {
     const int lane = threadIdx.x % 32;
     const char *row = (const char *)r.logits + (int64_t)t * r.ld * (r.dt == BD_F32 ? 4 : 2);
-    float x[NV];
+    float x[NV], b[WIDE ? NV : 1];
     bool odd = false;
+    if (WIDE) {                                                   // (on their way together with the logits)
+#pragma unroll
+        for (int i = 0; i < NV; i++) b[i] = r.bias && 32 * i + lane < r.experts ? r.bias[32 * i + lane] : 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
         const int e = 32 * i + lane;
@@ -269,14 +275,14 @@ __device__ __forceinline__ void route_token(const Rule &r, int t, double *scratc
             const int e = 32 * i + lane;
             float k = s[i] * inv;
             if (r.bias && e < r.experts) {
-                k += r.bias[e];
+                k += b[i];
                 odd = odd || k != k;
             }
             const bool there = x[i] != -INFINITY && k == k && k != -INFINITY;
             key[i] = there ? ordered(r.bias ? k + 0.0f : x[i]) : 0;   // (without a bias experts compare by the logits, groups by the scores)
             if (r.groups > 1 && e < r.experts) mine[e] = there ? k : -INFINITY;
         }
-        const float off = 3.8147e-6f * inv;                       // 2^-18: of two keys, without the bias' part
+        const float off = SIGMOID ? 4.7684e-7f : 3.8147e-6f * inv;   // 2^-21, 2^-18: of two keys, without the bias' part
         bool close = false;
         if (r.groups > 1) {
             __syncwarp();
