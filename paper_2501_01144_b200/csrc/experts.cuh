@@ -14,9 +14,9 @@
 // little else.  The gate and up rows of 32 channels are neighbours (rows 64 j + i and 64 j + 32 + i): they meet in the warps of
 // one CTA, and 32 channels are one block of the next product's operand.
 //
-// Bound: few tokens per expert, the weights' expansion (decode groups: 35/64 byte read and 1 byte written to tensor memory per element,
-// integer instructions beside a half-full issue) under the weights' bytes; many tokens, the block-scaled MMA at the clock that the power cap
-// leaves.  Measured (B200; first + second product, us, cold):
+// Bound: few tokens per expert, some 20 us of launches and first k-steps, the weights' bytes (5.9 TB/s with 1/8 of the MMAs and of the
+// expansion) and the part of the expansion that does not hide under them (a tenth); many tokens, the block-scaled MMA at the clock that the
+// power cap leaves.  Whole calls from a graph, us: 30, 104, 148 and 2200 for the cases below.  Measured (B200; first + second product, us, cold):
 //     1 token, 64 experts, 8 a token, 2048 -> 1024          17.5 + 13.5    27.5 MB: latency of 8 and 4 k-steps behind a launch
 //     64 tokens, 128 experts, 8, 2048 -> 1024               63 + 39        434 MB: 4.6 and 3.7 TB/s
 //     1500 tokens, 64 experts, 6, 2048 -> 1408 (f16)        85 + 42        156 GFLOP
