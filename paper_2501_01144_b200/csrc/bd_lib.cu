@@ -1803,7 +1803,7 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     const int64_t rows = tokens * plan->top_k, used = std::min(rows, up->experts);
     const bool narrow = rows <= 64 * used;
     const int64_t most = rows / (narrow ? 128 : 256) + used;      // items per 256 weight rows
-    const ex::Experts e{plan->count, plan->start, (int)up->experts, (int)sp.rows};
+    const ex::Experts e{plan->count, plan->start, (int)up->experts, (int)sp.rows, (int)tokens};
     ex::Product p{};
     p.live_k = (int)(down->K / kBlock);
     p.h = ws + sp.h;

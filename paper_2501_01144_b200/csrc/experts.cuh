@@ -46,7 +46,7 @@ __host__ __device__ inline int64_t row_pitch(int64_t K) { return (K + 127) / 128
 
 struct Experts {                             // what the kernels know of the plan
     const int32_t *count, *start;
-    int experts, rows;                       // rows: of the padded operand
+    int experts, rows, tokens;               // rows: of the padded operand; tokens: of the call, more than which no expert has
 };
 struct Maps {
     CUtensorMap x[kBoxes], codes, ids, sfw, sfx, y;
@@ -244,7 +244,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             if (e < ex.experts) {
                 cnt = load_relaxed(ex.count + e);
                 start = load_relaxed(ex.start + e);
-                if (cnt < 0 || start < 0 || start % kRowAlign || cnt > ex.rows || start > ex.rows - cnt) {
+                if (cnt < 0 || start < 0 || start % kRowAlign || cnt > ex.tokens || cnt > ex.rows || start > ex.rows - cnt) {
                     cnt = start = 0;
                     atomicOr(&g_status_word, kStatusIndex);
                 }

@@ -279,6 +279,22 @@ def test_a_plan_out_of_its_bounds_is_told_and_addresses_nothing():
     assert torch.equal(y[keep], want[keep]) and (y[5] == 0).all()
 
 
+@pytest.mark.parametrize("tokens, count", [(20, 21), (20, 100), (3, 128), (200, 201), (200, 256)])
+def test_a_plan_with_more_rows_than_tokens_is_told(tokens, count):
+    # inside the padded operand, but more than an expert can have: the copies of a call's tokens are sized by their number
+    up, down = weights(2, 128, 64, 128)
+    x, ids = tokens_of(tokens, 128, torch.bfloat16), torch.arange(tokens, device="cuda").remainder(2).to(torch.int32)[:, None].contiguous()
+    w = torch.ones(tokens, 1, device="cuda")
+    want = bd.expert_mlp(x, bd.expert_plan(ids, 2), w, up, down)
+    plan = bd.expert_plan(ids, 2)
+    plan.count[0] = count
+    y = bd.expert_mlp(x, plan, w, up, down)
+    with pytest.raises(bd.BdError) as e:
+        bd.poll_status()
+    assert e.value.status == 10
+    assert torch.equal(y[1::2], want[1::2])
+
+
 def test_experts_are_operands_of_their_own():
     w = torch.randn(3, 128, 96, generator=torch.Generator().manual_seed(1)).cuda()
     e = bd.quantize_experts(w, gated=True)
