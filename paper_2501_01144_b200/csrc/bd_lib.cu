@@ -1798,10 +1798,11 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     else if (xdtype == BD_BF16) launch_spread<BD_BF16>(X, ldx, plan, up, sp, ws, st);
     else launch_spread<BD_F16>(X, ldx, plan, up, sp, ws, st);
     if ((s = launch_result())) return s;
-    // Few rows per expert: items of at most 128 tokens (two accumulators, more stages for the codes); else of 256, so that an expert's weights
-    // are expanded once for as many tokens as possible.
+    // Few rows per expert: items of at most 128 tokens (two accumulators, a fourth decode group); else of 256, so that an expert's weights
+    // are expanded once for as many tokens as possible.  Measured, 64 experts, 6 a token, 2048 -> 1408, even loads, us a call, 128 / 256: 24 rows
+    // an expert 86 / 91, 64 98 / 104, 96 113 / 114, 128 135 / 129, 192 186 / 167; 8 experts, 2 a token, 4096 -> 4096: 64 rows 67 / 70, 96 75 / 76, 128 87 / 83.
     const int64_t rows = tokens * plan->top_k, used = std::min(rows, up->experts);
-    const bool narrow = rows <= 64 * used;
+    const bool narrow = rows <= 96 * used;
     const int64_t most = rows / (narrow ? 128 : 256) + used;      // items per 256 weight rows
     const ex::Experts e{plan->count, plan->start, (int)up->experts, (int)sp.rows, (int)tokens};
     ex::Product p{};
