@@ -458,10 +458,12 @@ bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, vo
  * the same numbers.  down is [N, inter].  K and inter are multiples of 32, N of 8; at most 512 experts.
  * X [tokens, K] and its pitch, Y [tokens, N] (BD_F32 or BD_BF16) and its pitch are 16-byte aligned.  The plan is bd_route's or bd_make_expert_plan's;
  * a token without experts gets zeros.  `inner` (optional, for checking; fp32 [tokens][top_k][inter]) receives the values q(...) that the second
- * product read.  Four launches, of no fixed relation to the plan's numbers, which stay on the device: a call can be captured and replayed
+ * product read.  Four launches with the workspace that bd_expert_mlp_workspace_size gives for BD_F32; with that for BD_BF16, the least for such a Y,
+ * the second product and the sum are made for half of the columns or more at a time, two launches each time, with the same result.  The launches
+ * have no fixed relation to the plan's numbers, which stay on the device: a call can be captured and replayed
  * with other tokens and plans.  The result is the same in every run, and a token's does not depend on the other tokens of the call.
  * Accuracy: the products as BD_GEMM_TCGEN05; act by fast exponentials and division, 2^-19 relative (gelu: of 1 + |x| where x is far below
- * zero); each expert's part of the sum is rounded to bf16 before it is weighted when Y is BD_BF16, and not rounded for BD_F32.
+ * zero); the experts' parts are weighted and added in fp32, in the order of a token's experts, and their sum is rounded once.
  * Device-side conditions (bd_poll_status): an Inf or NaN in X or before the second product (BD_ERR_NONFINITE); a plan whose numbers
  * lie outside its bounds (BD_ERR_INDEX; nothing is addressed by them); a wait that ran out (BD_ERR_TIMEOUT: what Y holds then means
  * nothing).  Workspace: 256-byte aligned, of one call at a time, like the plan while the call runs.  After one call per device, shape class

@@ -643,7 +643,8 @@ bd_status check_experts(const bd_experts *w) {
     if (!aligned16(w->codes) || !aligned16(w->ids) || !aligned16(w->scales)) return BD_ERR_ALIGN;
     return BD_OK;
 }
-// Parts of an expert call's workspace: the token operand (later the second product's result), its scales, the inner operand and its scales.
+// Parts of an expert call's workspace: the token operand (later the experts' parts, fp32), its scales, the inner operand and its scales.  The size for a
+// BD_BF16 result holds the parts of half of the columns, or more, at a time.
 struct ExpertSpace {
     int64_t rows;
     size_t x_scales, h, h_scales, total;
@@ -678,6 +679,12 @@ void launch_spread(const void *X, int64_t ldx, const bd_expert_plan *plan, const
     const unsigned grid = (unsigned)std::min<int64_t>((plan->tokens * per_row + 255) / 256, 148 * 8);
     launch_serialized(ex::spread_kernel<DT>, grid, 256, 0, st, (const uint8_t *)X, ldx, (int)plan->tokens, (int)plan->top_k, plan->place, (int)(up->K / kBlock), kgs,
                       (int)s.rows, ws, ws + s.x_scales, make_fast_div(per_row));
+}
+template <bool BF16>
+void launch_combine(const float *parts, const bd_expert_plan *plan, const float *weights, int64_t rows, int cols, void *Y, int64_t ldy, cudaStream_t st) {
+    const bool few = plan->tokens * cols <= 2ll * 148 * 256 * 4;
+    const unsigned grid = (unsigned)std::min<int64_t>((plan->tokens * (cols / (few ? 4 : 8)) + 255) / 256, 148 * 16);
+    launch_serialized(few ? ex::combine_kernel<BF16, 4> : ex::combine_kernel<BF16, 8>, grid, 256, 0, st, parts, plan->place, weights, (int)plan->tokens, (int)plan->top_k, (int)rows, cols, Y, ldy);
 }
 template <int DT, int VPT, bool QUANT, bool VEC>
 bd_status launch_norm(const nm::Args &a, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
@@ -1789,9 +1796,11 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     if (ldx < up->K || ldy < down->rows) return BD_ERR_SHAPE;
     if (!aligned16(X) || (ldx * elem_bytes(xdtype)) % 16 || !aligned16(Y) || (ldy * elem_bytes(ydtype)) % 16 || ((uintptr_t)weights & 3u) || ((uintptr_t)inner & 3u))
         return BD_ERR_ALIGN;
-    const ExpertSpace sp = expert_space(tokens, plan->top_k, up, down, ydtype);
+    ExpertSpace sp = expert_space(tokens, plan->top_k, up, down, ydtype);
     if (!workspace || workspace_bytes < sp.total) return BD_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return BD_ERR_ALIGN;
+    const ExpertSpace whole = expert_space(tokens, plan->top_k, up, down, BD_F32);
+    if (workspace_bytes >= whole.total) sp = whole;
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t *ws = (uint8_t *)workspace;
     if (xdtype == BD_F32) launch_spread<BD_F32>(X, ldx, plan, up, sp, ws, st);
@@ -1811,7 +1820,7 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     p.h_scales = ws + sp.h_scales;
     p.h_pitch = ex::row_pitch(down->K);
     p.gelu = act == BD_ACT_GELU;
-    cudaError_t err = (narrow ? ex::launch_product<true, 128> : ex::launch_product<true, 256>)(ws, ws + sp.x_scales, e, tokens, most, up, p, nullptr, false, st);
+    cudaError_t err = (narrow ? ex::launch_product<true, 128> : ex::launch_product<true, 256>)(ws, ws + sp.x_scales, e, tokens, most, up, p, nullptr, st);
     if (err != cudaSuccess) return cuda_result(err);
     g_launches += 1;
     if (inner) {
@@ -1819,15 +1828,20 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
                           (const uint8_t *)p.h_scales, plan->place, rows, (int)sp.rows, (int)down->K, p.h_pitch, inner);
         if ((s = launch_result())) return s;
     }
-    err = (narrow ? ex::launch_product<false, 128> : ex::launch_product<false, 256>)(p.h, p.h_scales, e, tokens, most, down, p, ws, ydtype == BD_BF16, st);
-    if (err != cudaSuccess) return cuda_result(err);
-    g_launches += 1;
-    const unsigned grid = (unsigned)std::min<int64_t>((tokens * (down->rows / 8) + 255) / 256, 148 * 16);
-    if (ydtype == BD_BF16)
-        launch_serialized(ex::combine_kernel<true>, grid, 256, 0, st, (const uint8_t *)ws, plan->place, weights, (int)tokens, (int)plan->top_k, (int)sp.rows, (int)down->rows, Y, ldy);
-    else
-        launch_serialized(ex::combine_kernel<false>, grid, 256, 0, st, (const uint8_t *)ws, plan->place, weights, (int)tokens, (int)plan->top_k, (int)sp.rows, (int)down->rows, Y, ldy);
-    return launch_result();
+    // The experts' parts are fp32 whatever type Y has.  Where the workspace has room for fewer than all of their columns, the second product and the sum
+    // are made for as many columns at a time as it has (at least 32: a row of the token operand has 128 bytes or more).
+    const int64_t fit = (int64_t)(sp.x_scales / ((size_t)sp.rows * 4)), room = fit >= down->rows ? down->rows : fit / 32 * 32;
+    for (int64_t c = 0; c < down->rows; c += room) {
+        p.col0 = (int)c;
+        p.cols = (int)std::min(room, down->rows - c);
+        err = (narrow ? ex::launch_product<false, 128> : ex::launch_product<false, 256>)(p.h, p.h_scales, e, tokens, most, down, p, (float *)ws, st);
+        if (err != cudaSuccess) return cuda_result(err);
+        g_launches += 1;
+        if (ydtype == BD_BF16) launch_combine<true>((const float *)ws, plan, weights, sp.rows, p.cols, (uint16_t *)Y + c, ldy, st);
+        else launch_combine<false>((const float *)ws, plan, weights, sp.rows, p.cols, (float *)Y + c, ldy, st);
+        if ((s = launch_result())) return s;
+    }
+    return BD_OK;
 }
 
 bd_status bd_residual_norm(const bd_norm *a, bd_dtype dtype, int64_t rows, int64_t dim, void *stream) {

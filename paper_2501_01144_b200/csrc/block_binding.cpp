@@ -214,7 +214,7 @@ PyObject *mlp(PyObject *const *a, Py_ssize_t n) {
             if (!ws.is_contiguous()) refuse("workspace must be contiguous");
         } else {
             size_t bytes = 0;
-            check(bd_expert_mlp_workspace_size(tokens, k, &up, &down, ydt, &bytes));
+            check(bd_expert_mlp_workspace_size(tokens, k, &up, &down, BD_F32, &bytes));   // (room for the parts of all columns at once)
             ws = at::empty({(int64_t)bytes}, on_device(at::kByte));
         }
         check(bd_expert_mlp(mx.p, xdt, tokens, mx.ld, &p, w, &up, &down, gelu ? BD_ACT_GELU : BD_ACT_SILU, my.p, ydt, my.ld, inner, ws.data_ptr(), (size_t)ws.nbytes(),

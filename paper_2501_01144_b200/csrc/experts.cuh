@@ -4,7 +4,9 @@
 //   spread    quantises each token once and writes its operand bytes to the rows of its experts (each expert's rows begin at a multiple of
 //             128, the rows of a scale atom);
 //   product   gate and up rows of all experts against those rows; the epilogue forms act(g) * u and requantises it (GATED);
-//   product   the down rows against the result;
+//   product   the down rows against the result: the experts' parts, in fp32 whatever type their sum is rounded to (rounded to bf16 they
+//             take the result's error from 0.0017 to 0.0024; they cost 60 -> 60, 104 -> 104, 148 -> 160 and 2240 -> 2250 us a call for 16
+//             tokens of 64 experts and the last three cases below);
 //   combine   the weighted sum of a token's rows, in the order of its experts (fp32, the same in every run).
 //
 // The products are the tile of gemm_tc.cuh (256 weight rows x up to 256 tokens per pair of CTAs, weights expanded into tensor memory, one
@@ -49,16 +51,16 @@ struct Experts {                             // what the kernels know of the pla
     int experts, rows, tokens;               // rows: of the padded operand; tokens: of the call, more than which no expert has
 };
 struct Maps {
-    CUtensorMap x[kBoxes], codes, ids, sfw, sfx, y;
+    CUtensorMap x[kBoxes], codes, ids, sfw, sfx, y, y_rest;           // y: boxes of 32 rows, y_rest: of 8
 };
 struct Product {
     int w_pairs, row_tiles, k_groups, clusters;
+    int w_first, col0, cols;                 // down product: the first of the pass's 256-row tiles, its first column and number of columns
     int live_k;                              // GATED: blocks of the result (inter / 32)
     uint8_t *h;                              // GATED: operand bytes [rows][row_pitch(inter)] and scale atoms of the result
     uint8_t *h_scales;
     int64_t h_pitch;
     int gelu;
-    int y_bf16;
 };
 
 // A k-step is 256 elements of K, two k-groups.  The hand-overs of a k-step (a barrier wait, an election, a copy instruction: some 70 ns
@@ -90,7 +92,7 @@ struct Layout {
     static_assert(kCS % kGroups == 0, "a stage belongs to one group");
     static constexpr int kXBytes = kStep * (TOK / 2) * kGroupBytes;
     static constexpr int kSfxBytes = kStep * (TOK / 128) * kScaleAtomBytes;
-    static constexpr int kStage = GATED ? 8192 : 4096;           // epilogue staging of a warp
+    static constexpr int kStage = 8192;                          // epilogue staging of a warp: two 32 x 32 tiles of fp32
     static constexpr int x = 0;
     static constexpr int codes = x + kBufs * kXBytes;
     static constexpr int sfw = codes + kCS * kCodeBytes;
@@ -125,7 +127,7 @@ template <int TOK>
 struct Walk {
     const int *first;                        // items before each expert's, [experts + 1]
     const uint32_t *where;                   // an expert's first row / 128, and (low byte) the tokens of its last tile - 1
-    int w_pairs, experts, clusters, c, e;
+    int w_first, w_pairs, experts, clusters, c, e;
     __device__ bool operator()(int i, Item &t) {
         const int item = i * clusters + c;
         if (item >= first[experts]) return false;
@@ -133,7 +135,7 @@ struct Walk {
         const int tiles = (first[e + 1] - first[e]) / w_pairs, in = item - first[e], tt = in % tiles;
         const uint32_t w = where[e];
         t.expert = e;
-        t.w_pair = in / tiles;
+        t.w_pair = w_first + in / tiles;
         t.row0 = (int)(w >> 8) * kRowAlign + tt * TOK;
         t.live = tt + 1 < tiles ? TOK : (int)(w & 255u) + 1;
         t.n = (t.live + 15) / 16 * 16;
@@ -157,6 +159,10 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
     asm volatile(
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
 }
 
 __device__ __forceinline__ int load_relaxed(const int32_t *p) {
@@ -276,7 +282,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
     const uint32_t tmem = *tmem_slot;
     const int steps = (p.k_groups + kStep - 1) / kStep;
     auto accumulator = [](const Item &t, int slot) { return kSlots == 2 && t.n <= 64 ? 64u * (uint32_t)slot : 0u; };
-    Walk<TOK> next{first, where, p.w_pairs, ex.experts, p.clusters, cluster, 0};
+    Walk<TOK> next{first, where, GATED ? 0 : p.w_first, p.w_pairs, ex.experts, p.clusters, cluster, 0};
     Item t;
 
     if (warp < kDecode0) {
@@ -460,7 +466,7 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
             __syncwarp();
             stage_turn ^= 1u;
-            return stage_turn * kStageOut;
+            return stage_turn * (L::kStage / 2);
         };
         for (int i = 0; next(i, t); i++) {
             const int slot = i % kSlots;
@@ -544,33 +550,32 @@ expert_product_kernel(const __grid_constant__ Maps maps, const Experts ex, const
                     }
                 }
             } else {
-                // chunks of 32 tokens: the first half's warps take the larger part
-                const int chunks = (t.n + 31) / 32, mine0 = half ? (chunks + 1) / 2 : 0, mine = half ? chunks / 2 : (chunks + 1) / 2;
-                const int n0 = t.w_pair * 256 + (int)rank * 128 + quad * 32, t0 = t.row0 + mine0 * 32;
+                // Chunks of 32 tokens, fetched two at a time: the first half's warps take the larger part.  The experts' parts stay fp32 whatever
+                // type the sum is rounded to; warps whose 32 weight rows are not among the pass's columns only release the accumulator.
+                const int chunks = (t.n + 31) / 32, mine0 = half ? (chunks + 1) / 2 : 0;
+                const int n0 = t.w_pair * 256 + (int)rank * 128 + quad * 32 - p.col0;
+                const int mine = n0 < 0 || n0 >= p.cols ? 0 : half ? chunks / 2 : (chunks + 1) / 2;
                 const uint32_t t_mine = t_base + mine0 * 32;
-                if (p.y_bf16) {
-                    switch (mine) {
-                        case 4: epilogue_bf16<4>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
-                        case 3: epilogue_bf16<3>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
-                        case 2: epilogue_bf16<2>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
-                        case 1: epilogue_bf16<1>(t_mine, stage_ptr, stage_out, &maps.y, n0, t0, lane, abort_flag, release_accumulator, staging_free); break;
-                        default: release_accumulator();
-                    }
-                } else {
-                    if (mine == 0) release_accumulator();
-                    for (int pass = 0; pass < 2 * mine; pass++) {     // fp32: 16 tokens x 32 columns per pass
-                        uint32_t r[16];
-                        tcgen05_ld_32x32b_x16(t_mine + pass * 16, r);
-                        tcgen05_wait_ld();
-                        if (pass + 1 == 2 * mine) release_accumulator();
+                if (mine == 0) release_accumulator();
+                for (int c = 0; c < mine; c += 2) {
+                    uint32_t r[2][32];
+                    const bool two = c + 1 < mine;
+                    tcgen05_ld_32x32b_x32(t_mine + c * 32, r[0]);
+                    if (two) tcgen05_ld_32x32b_x32(t_mine + c * 32 + 32, r[1]);
+                    tcgen05_wait_ld();
+                    if (c + 2 >= mine) release_accumulator();
+#pragma unroll
+                    for (int v = 0; v < 2; v++) {
+                        if (v == 1 && !two) break;
                         const uint32_t sb = staging_free();
 #pragma unroll
-                        for (int q = 0; q < 16; q++) *(uint32_t *)(stage_ptr + sb + q * 128 + lane * 4) = r[q];
+                        for (int q = 0; q < 32; q++) *(uint32_t *)(stage_ptr + sb + q * 128 + lane * 4) = r[v][q];
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0 && !*abort_flag) {
-                            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                                         ::"l"(&maps.y), "r"(n0), "r"(t0 + pass * 16), "r"(stage_out + sb) : "memory");
+                            const int row = (mine0 + c + v) * 32, rest = t.live - row;
+                            if (rest > 24) store_box(&maps.y, n0, t.row0 + row, stage_out + sb);
+                            else for (int q = 0; q < rest; q += 8) store_box(&maps.y_rest, n0, t.row0 + row + q, stage_out + sb + q * 128);
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
                     }
@@ -651,51 +656,47 @@ __global__ void __launch_bounds__(256) spread_kernel(const uint8_t *__restrict__
     }
 }
 
-// y_t = sum_j w_tj * part[place_tj], thread = eight neighbouring outputs of a token.  A token without experts gets zeros.
-// Bound: memory (8192 tokens, 2 rows of 4096 in bf16 each: 40 us for 201 MB), a launch where tokens are few (7.2 us for 1 token, cold).
-template <bool BF16>
-__global__ void __launch_bounds__(256) combine_kernel(const uint8_t *__restrict__ part, const int32_t *__restrict__ place, const float *__restrict__ weights,
+// y_t = sum_j w_tj * part[place_tj] in fp32, rounded once; thread = V neighbouring outputs of a token.  A token without experts gets zeros.
+// Bound: memory, a launch where tokens are few.  Four outputs a thread up to two CTAs per SM (64 tokens of 128 experts: the whole call 104 us,
+// with eight 106), eight beyond (512 of 64: 97 us, with four 103).
+template <bool BF16, int V>
+__global__ void __launch_bounds__(256) combine_kernel(const float *__restrict__ part, const int32_t *__restrict__ place, const float *__restrict__ weights,
                                                       int tokens, int top_k, int rows, int n, void *__restrict__ Y, int64_t ldy) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int per_row = n / 8;
+    const int per_row = n / V;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)tokens * per_row; i += (int64_t)gridDim.x * 256) {
-        const int t = (int)(i / per_row), c = (int)(i - (int64_t)t * per_row) * 8;
-        float acc[8];
+        const int t = (int)(i / per_row), c = (int)(i - (int64_t)t * per_row) * V;
+        float acc[V];
 #pragma unroll
-        for (int q = 0; q < 8; q++) acc[q] = 0.0f;
+        for (int q = 0; q < V; q++) acc[q] = 0.0f;
 #pragma unroll 4
         for (int j = 0; j < top_k; j++) {
             const int row = __ldg(place + (int64_t)t * top_k + j);
             if (row < 0 || row >= rows) continue;
             const float w = __ldg(weights + (int64_t)t * top_k + j);
-            if (BF16) {
-                const uint4 u = __ldcs((const uint4 *)(part + ((int64_t)row * n + c) * 2));
-                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    acc[2 * q] = fmaf(w, __uint_as_float(x[q] << 16), acc[2 * q]);
-                    acc[2 * q + 1] = fmaf(w, __uint_as_float(x[q] & 0xffff0000u), acc[2 * q + 1]);
-                }
-            } else {
-                const float4 u = __ldcs((const float4 *)(part + ((int64_t)row * n + c) * 4)), v = __ldcs((const float4 *)(part + ((int64_t)row * n + c) * 4) + 1);
-                const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int q = 0; q < 8; q++) acc[q] = fmaf(w, x[q], acc[q]);
+            for (int q = 0; q < V; q += 4) {
+                const float4 u = __ldcs((const float4 *)(part + (int64_t)row * n + c + q));
+                acc[q] = fmaf(w, u.x, acc[q]);
+                acc[q + 1] = fmaf(w, u.y, acc[q + 1]);
+                acc[q + 2] = fmaf(w, u.z, acc[q + 2]);
+                acc[q + 3] = fmaf(w, u.w, acc[q + 3]);
             }
         }
         if (BF16) {
-            uint32_t o[4];
+            uint32_t o[V / 2];
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
+            for (int q = 0; q < V / 2; q++) {
                 const __nv_bfloat162 h = __floats2bfloat162_rn(acc[2 * q], acc[2 * q + 1]);
                 o[q] = *(const uint32_t *)&h;
             }
-            *(uint4 *)((uint16_t *)Y + (int64_t)t * ldy + c) = make_uint4(o[0], o[1], o[2], o[3]);
+            uint16_t *dst = (uint16_t *)Y + (int64_t)t * ldy + c;
+            if (V == 8) *(uint4 *)dst = make_uint4(o[0], o[1], o[V / 2 - 2], o[V / 2 - 1]);
+            else *(uint2 *)dst = make_uint2(o[0], o[1]);
         } else {
-            float4 *dst = (float4 *)((float *)Y + (int64_t)t * ldy + c);
-            dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+#pragma unroll
+            for (int q = 0; q < V; q += 4) *(float4 *)((float *)Y + (int64_t)t * ldy + c + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
         }
     }
 }
@@ -737,7 +738,7 @@ inline bool make_map_3d(CUtensorMap *map, CUtensorMapDataType type, const void *
 }
 
 template <bool GATED, int TOK>
-inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t tokens, int64_t items_most, const bd_experts *W, Product p, void *Y, bool y_bf16, cudaStream_t st) {
+inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const Experts &ex, int64_t tokens, int64_t pair_items, const bd_experts *W, Product p, float *parts, cudaStream_t st) {
     using L = Layout<GATED, TOK>;
     Maps m;
     const int64_t N = W->rows, K = W->K, rtw = row_tiles(N), kg = k_groups(K), pitch = row_pitch(K), tiles_x = ex.rows / kRowAlign;
@@ -753,11 +754,11 @@ inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const E
         !make_map_3d(&m.sfx, kWords, sfx, kScaleAtomBytes / 4, tiles_x, kg, kScaleAtomBytes, (uint64_t)tiles_x * kScaleAtomBytes, kScaleAtomBytes / 4, TOK / 128, kStep, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorInvalidValue;
     if (!GATED) {
-        if (!make_map_2d(&m.y, y_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, Y, N, ex.rows, (uint64_t)N * (y_bf16 ? 2 : 4), 32,
-                         y_bf16 ? 32 : 16, CU_TENSOR_MAP_SWIZZLE_NONE))
+        if (!make_map_2d(&m.y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, parts, p.cols, ex.rows, (uint64_t)p.cols * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+            !make_map_2d(&m.y_rest, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, parts, p.cols, ex.rows, (uint64_t)p.cols * 4, 32, 8, CU_TENSOR_MAP_SWIZZLE_NONE))
             return cudaErrorInvalidValue;
     } else {
-        m.y = m.sfx;                                                  // unused, but must be a valid object
+        m.y = m.y_rest = m.sfx;                                       // unused, but must be valid objects
     }
     static bool configured[tc::kMaxDevices] = {};
     const int dev = current_device();
@@ -770,12 +771,12 @@ inline cudaError_t launch_product(const uint8_t *x8, const uint8_t *sfx, const E
         if (a.numRegs < L::kLaunchRegs) return cudaErrorLaunchOutOfResources;
         configured[dev] = true;
     }
-    p.w_pairs = (int)((N + 255) / 256);
+    p.w_first = GATED ? 0 : p.col0 / 256;
+    p.w_pairs = (int)(((GATED ? N : (int64_t)p.col0 + p.cols) + 255) / 256) - p.w_first;
     p.row_tiles = (int)rtw;
     p.k_groups = (int)kg;
-    p.y_bf16 = y_bf16;
     const int resident = max_resident_clusters();
-    const int64_t most = items_most * p.w_pairs;
+    const int64_t most = pair_items * p.w_pairs;
     p.clusters = most < resident ? (int)most : resident;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * p.clusters);
