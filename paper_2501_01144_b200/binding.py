@@ -1,6 +1,7 @@
 """ctypes binding of the C ABI in include/bd.h (same names without the bd_ prefix)."""
-import contextlib
 import ctypes
+import functools
+import inspect
 import os
 import subprocess
 
@@ -200,10 +201,27 @@ def _check(status):
         raise BdError(status, text)
 
 
+def _current_stream():
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _stream(stream=None):
-    if stream is None:
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
-    return ctypes.c_void_p(stream.cuda_stream)
+    return ctypes.c_void_p(_current_stream() if stream is None else stream.cuda_stream)
+
+
+def _on_stream(f):
+    """What a call with `stream` allocates belongs to that stream: memory of the current one could still be written by its pending work, or
+    be handed out again while the call's kernels use it."""
+    at = list(inspect.signature(f).parameters).index("stream")
+
+    @functools.wraps(f)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None or stream.cuda_stream == _current_stream():
+            return f(*args, **kw)
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)):
+            return f(*args, **kw)
+    return call
 
 
 def version():
@@ -736,6 +754,7 @@ class ExpertWeights(_Described):
         return QTensor.from_buffers(self.codes[e], self.ids[e], self.scales[e], self.rows, self.K)
 
 
+@_on_stream
 def quantize_experts(W, select=SELECT_MSE, gated=False, out=None, stream=None):
     """Offline quantisation of the experts' weights W [experts, N, K] along K.  gated: W is the first product's, N = 2 * inter with the gate
     rows before the up rows; they are stored in turns of 32, as expert_mlp reads them (inter a multiple of 32)."""
@@ -747,10 +766,9 @@ def quantize_experts(W, select=SELECT_MSE, gated=False, out=None, stream=None):
     out = out or ExpertWeights(experts, N, K, W.device)
     if (out.experts, out.rows, out.K) != (experts, N, K):
         raise ValueError("out must have the shape of W")
-    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-        for e in range(experts):
-            w = W[e].unflatten(0, (2, N // 64, 32)).transpose(0, 1).reshape(N, K) if gated else W[e]
-            quantize_weights(w, select, out=out.expert(e))
+    for e in range(experts):
+        w = W[e].unflatten(0, (2, N // 64, 32)).transpose(0, 1).reshape(N, K) if gated else W[e]
+        quantize_weights(w, select, out=out.expert(e))
     return out
 
 
