@@ -304,6 +304,7 @@ def _src(x):
     return ctypes.c_void_p(x.data_ptr()), _TORCH_DTYPE[x.dtype], x.stride(0)
 
 
+@_on_stream
 def quantize_weights(W, select=SELECT_MSE, out=None, stream=None):
     """Offline weight quantisation of W [N, K] along K (Sec. 3.3)."""
     ptr, dt, ld = _src(W)
@@ -314,6 +315,7 @@ def quantize_weights(W, select=SELECT_MSE, out=None, stream=None):
     return out
 
 
+@_on_stream
 def quantize_act(X, axis=AXIS_CONTIG, out=None, stream=None):
     """Online two-stage quantisation (Sec. 3.2).  AXIS_CONTIG: X [M, K]; AXIS_STRIDED: X [K, M]."""
     ptr, dt, ld = _src(X)
@@ -352,6 +354,7 @@ def _ws(workspace, need, device):
     return workspace, ptr, (workspace.numel() if workspace is not None else 0)
 
 
+@_on_stream
 def gemm(A, B, out=None, dtype=torch.float32, workspace=None, stream=None):
     """Y [M, N] = dq(A) dq(B)^T (Sec. 3.3, Fig. 6)."""
     if out is None:
@@ -369,6 +372,7 @@ def gemm_batched_workspace_size(M, N, K, b_group):
     return b.value
 
 
+@_on_stream
 def gemm_batched(As, Bs, b_group=1, out=None, dtype=torch.float32, workspace=None, stream=None):
     """Batched product; A[b] pairs with B[b // b_group] (grouped-query attention)."""
     batch = len(As)
@@ -383,6 +387,7 @@ def gemm_batched(As, Bs, b_group=1, out=None, dtype=torch.float32, workspace=Non
     return out
 
 
+@_on_stream
 def linear(X, Wq, out=None, dtype=torch.bfloat16, workspace=None, stream=None):
     """The quantised linear layer: two-stage quantisation of X [M, K], then the product with Wq [N, K]."""
     ptr, dt, ld = _src(X)
@@ -408,6 +413,7 @@ def gemm_requant_workspace_size(M, N, K):
     return b.value
 
 
+@_on_stream
 def linear_requant(X, Wq, out=None, workspace=None, stream=None):
     """The quantised linear layer with its result requantised for the next product (Sec. 3.3, last
     paragraph): returns the QTensor [M, N] instead of Y."""
@@ -420,6 +426,7 @@ def linear_requant(X, Wq, out=None, workspace=None, stream=None):
     return out
 
 
+@_on_stream
 def gemm_requant(A, B, out=None, workspace=None, stream=None):
     """dq(A) dq(B)^T requantised along N for the next product (Sec. 3.3, last paragraph)."""
     out = out or QTensor(A.rows, B.rows, A.codes.device)
@@ -434,6 +441,7 @@ def physical_k(K, block):
     return 2 * K if block == 16 else K
 
 
+@_on_stream
 def quantize_bs(X, block, select=SELECT_TWO_STAGE, out=None, stream=None):
     """Quantise X [rows, K] along K in blocks of 16, 32 or 64 elements (Sec. 4.2, Table 3).  The result is an
     ordinary QTensor with K' = physical_k(K, block) that every product takes as it is."""
@@ -445,6 +453,7 @@ def quantize_bs(X, block, select=SELECT_TWO_STAGE, out=None, stream=None):
     return out
 
 
+@_on_stream
 def export_canonical_bs(q, block, stream=None):
     """(codes [rows, K/2], ids [rows, K/block], scales [rows, K/block]) of an operand stored for `block`."""
     dev = q.codes.device
@@ -464,6 +473,7 @@ def linear_bs_workspace_size(M, N, K, block):
     return b.value
 
 
+@_on_stream
 def linear_bs(X, Wq, block, out=None, dtype=torch.bfloat16, workspace=None, stream=None):
     """The quantised linear layer with blocks of 16, 32 or 64 elements; Wq from quantize_bs with the same block."""
     ptr, dt, ld = _src(X)
@@ -483,6 +493,7 @@ def attention_workspace_size(heads, group, sk, head_dim):
     return b.value
 
 
+@_on_stream
 def attention(Qs, Ks, Vs, group=1, scale=None, out=None, dtype=torch.bfloat16, dump=False, workspace=True, stream=None):
     """Full-path attention in one kernel (Sec. 4.1 scope "all"; Sec. 3.3 softmax in high precision): Qs are `heads`
     operands [Sq, d], Ks heads / group operands [Sk, d], Vs heads / group operands [d, Sk] (quantize_act with
@@ -547,6 +558,7 @@ class KVCache:
             self._ws = torch.empty(max(b.value, 256), dtype=torch.uint8, device=self.k.codes.device)
         return ctypes.c_void_p(self._ws.data_ptr()), self._ws.numel()
 
+    @_on_stream
     def scores(self, Q, out=None, dtype=torch.float32, stream=None):
         """S [q, length] = dq(Q) dq(K)^T for a quantised query operand Q [q, head_dim]."""
         if out is None:
@@ -557,6 +569,7 @@ class KVCache:
                                         out.stride(0), wptr, wbytes, _stream(stream)))
         return out
 
+    @_on_stream
     def pv(self, P, out=None, dtype=torch.float32, stream=None):
         """O [q, head_dim] = P V for fp32 probabilities P [q, length]."""
         if P.dtype != torch.float32 or P.dim() != 2 or P.stride(1) != 1 or P.shape[1] != self.length:
@@ -593,6 +606,7 @@ def kvcache_append_batched(caches, k_new, v_new, stream=None):
         c._c.length = done.length
 
 
+@_on_stream
 def kvcache_scores_batched(caches, Qs, out=None, dtype=torch.float32, stream=None):
     """S [n, q, length]: the scores of n KV heads (same length) in one call; Qs[i] is head i's quantised query operand."""
     n, q, length = len(caches), Qs[0].rows, caches[0].length
@@ -605,6 +619,7 @@ def kvcache_scores_batched(caches, Qs, out=None, dtype=torch.float32, stream=Non
     return out
 
 
+@_on_stream
 def kvcache_pv_batched(caches, P, out=None, dtype=torch.float32, stream=None):
     """O [n, q, head_dim] = P[i] V[i] for fp32 probabilities P [n, q, length] of n KV heads (same length) in one call."""
     n = len(caches)
@@ -619,6 +634,7 @@ def kvcache_pv_batched(caches, P, out=None, dtype=torch.float32, stream=None):
     return out
 
 
+@_on_stream
 def kvcache_attention(caches, Qs, scale, out=None, dtype=torch.float32, probs=None, stream=None):
     """O [n, q, head_dim] of one decode step over n cached heads: scores, fp32 softmax of scale * S, P V.  `probs`
     (fp32 [n, q, pitch >= length], pitch a multiple of 4) receives the probabilities when given."""
@@ -860,6 +876,7 @@ def linear_noalloc(X, Wq, out, stream=None):
     return out
 
 
+@_on_stream
 def export_canonical(q, stream=None):
     """(codes [rows, K/2], ids [rows, K/32], scales [rows, K/32]) as uint8 CUDA tensors."""
     dev = q.codes.device
@@ -873,6 +890,7 @@ def export_canonical(q, stream=None):
     return codes, ids, scales
 
 
+@_on_stream
 def import_canonical(codes, ids, scales, stream=None):
     """Build a QTensor from canonical uint8 CUDA tensors."""
     rows, K = codes.shape[0], codes.shape[1] * 2
@@ -884,6 +902,7 @@ def import_canonical(codes, ids, scales, stream=None):
     return q
 
 
+@_on_stream
 def dequantize(q, stream=None):
     """fp32 [rows, K] values of a quantised operand (Sec. 3.3, Fig. 6)."""
     out = (_block or _load_block()).dequantize(q.codes, q.ids, q.scales, q.rows, q.K, stream)
