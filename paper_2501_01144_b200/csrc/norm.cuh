@@ -197,13 +197,15 @@ __global__ void __launch_bounds__(kMaxThreads, QUANT && DT == BD_BF16 ? 2 : VPT 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int EB = Loader<DT>::kElemBytes;
-    const int kgs = QUANT ? (int)k_groups(a.q.K) : 0, total = QUANT ? (int)row_tiles(a.q.rows) * kRowTile : a.rows;
+    // Row numbers are unsigned: the last round's first row may lie a step (up to 9472 rows) behind the last of 2^31 - 1.
+    const uint32_t rows = (uint32_t)a.rows, total = QUANT ? (uint32_t)row_tiles(a.q.rows) * kRowTile : rows;
+    const int kgs = QUANT ? (int)k_groups(a.q.K) : 0;
     // The next round's rows are on their way while this one's are worked on (AHEAD: whole pieces; single elements would cost too many
     // registers): with the loads of a row in front of its own reductions, memory idles while a CTA reduces.
     constexpr bool AHEAD = VEC && !QUANT;
     Piece<DT, VEC> ny[AHEAD ? VPT : 1], nr[AHEAD ? VPT : 1];
-    auto fetch = [&](int r) {
-        if (AHEAD && r < a.rows) {
+    auto fetch = [&](uint32_t r) {
+        if (AHEAD && r < rows) {
 #pragma unroll
             for (int v = 0; v < (AHEAD ? VPT : 1); v++) {
                 ny[v].load(a.y + (int64_t)r * a.ldy * EB, elem(v), rt, a.dim);
@@ -211,12 +213,12 @@ __global__ void __launch_bounds__(kMaxThreads, QUANT && DT == BD_BF16 ? 2 : VPT 
             }
         }
     };
-    const int step = gridDim.x * a.row_groups;
+    const uint32_t step = gridDim.x * (uint32_t)a.row_groups;
     fetch(blockIdx.x * a.row_groups + group);
     // every thread of the CTA goes through the same number of rounds (barriers inside); a group behind the last row only keeps step
-    for (int base = blockIdx.x * a.row_groups; base < total; base += step) {
-        const int r = base + group;
-        const bool there = r < a.rows;
+    for (uint32_t base = blockIdx.x * (uint32_t)a.row_groups; base < total; base += step) {
+        const uint32_t r = base + (uint32_t)group;
+        const bool there = r < rows;
         float x[VPT][8], g[8];
         Piece<DT, VEC> res[AHEAD ? VPT : 1];
 #pragma unroll
