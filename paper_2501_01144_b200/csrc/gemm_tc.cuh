@@ -507,6 +507,9 @@ gemm_wtmem_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
         int s = group % kCodeStages, b = group % kABufs;
         uint32_t s_par = 0, b_par = 1;
         static_assert(kDecodeGroups <= kCodeStages && kDecodeGroups <= kABufs, "one wrap per step at most");
+        // (copies land out of order, and a barrier tells a phase only from the next one: a stage that two groups shared could be taken with the
+        // phase before its own; products complete in order, so the ring of decoded k-steps needs no such rule)
+        static_assert(kCodeStages % kDecodeGroups == 0, "a code stage belongs to one decode group");
         // A warp whose wait ran out (or that saw the abort word) is `dead`: it stops waiting and working but keeps
         // meeting its group at the named barrier of every remaining k-step.  The four warps wait on the same
         // barriers, yet one may see the abort word where another still sees its barrier complete; a warp that left
@@ -521,12 +524,11 @@ gemm_wtmem_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 ids16 = *(const uint16_t *)(base_ptr + Smem::ids + s * kIdAtomBytes + (j % 32) * 8 + (j / 32) * 2);
 #pragma unroll
                 for (int c = 0; c < 4; c++) w[c] = *(const uint4 *)(codes + 16 * (c ^ swz64));
-                // The codes are in registers: hand the stage back to its producer.  With the requantising epilogue's scattered stores on the
-                // way the loads may have been issued and not have arrived for longer than a refill takes (seen in the experts' products,
-                // whose epilogue stores alike): a store of something made of all of them cannot leave before them.
-                if (REQUANT)
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)Smem::words + 16u + 4u * (uint32_t)(warp - kDecodeWarp0)),
-                                 "r"(ids16 ^ w[0].x ^ w[1].x ^ w[2].x ^ w[3].x) : "memory");
+                // The stage goes back to its producer once the loads have arrived, not only been issued: with an epilogue's stores on the way
+                // they may take longer than a refill does (seen in the experts' products).  A store of something made of all of them cannot
+                // leave before them, nor the hand-over before the store.
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + (uint32_t)Smem::words + 16u + 4u * (uint32_t)(warp - kDecodeWarp0)),
+                             "r"(ids16 ^ w[0].x ^ w[1].x ^ w[2].x ^ w[3].x) : "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(c_empty(s));
                 dead = !mbar_wait(a_empty(b), b_par, abort_flag);
