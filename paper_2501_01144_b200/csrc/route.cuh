@@ -353,18 +353,10 @@ __device__ __forceinline__ void route_token(const Rule &r, int t, double *scratc
         const float ref = number(warp_max(my_id >= 0 ? ordered(my_x) : 0u));   // relative to the largest chosen one: no underflow of all
         w = my_id >= 0 ? exp((double)my_x - (double)ref) : 0.0;
     } else {
-        double sum;
-        if (WIDE) {
-            sum = 0.0;
+        double sum = 0.0;
 #pragma unroll
-            for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0.0 : exp((double)x[i] - (double)top);
-            sum = warp_sum(sum);
-        } else {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; i++) s += x[i] == -INFINITY ? 0.0f : expf(x[i] - top);
-            sum = (double)warp_sum(s);
-        }
+        for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0.0 : exp((double)x[i] - (double)top);
+        sum = warp_sum(sum);
         w = my_id >= 0 && sum > 0.0 ? exp((double)my_x - (double)top) / sum : 0.0;
     }
     if (r.renormalise) {
