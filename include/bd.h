@@ -462,8 +462,9 @@ bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, vo
  * the second product and the sum are made for half of the columns or more at a time, two launches each time, with the same result.  The launches
  * have no fixed relation to the plan's numbers, which stay on the device: a call can be captured and replayed
  * with other tokens and plans.  The result is the same in every run, and a token's does not depend on the other tokens of the call.
- * Accuracy: the products as BD_GEMM_TCGEN05; act by fast exponentials and division, 2^-19 relative (gelu: of 1 + |x| where x is far below
- * zero); the experts' parts are weighted and added in fp32, in the order of a token's experts, and their sum is rounded once.
+ * Accuracy: the products as BD_GEMM_TCGEN05; act(x) = x / (1 + exp(-a)), a = x or, for gelu, 2 sqrt(2 / pi) (x + 0.044715 x^3), by fast
+ * exponentials and division: off by (6 + 1.2 |a|) 2^-23 of itself, gelu (6 + 3 |a|) 2^-23, as long as exp(a) is a normal number (a > -87.3); below,
+ * exp(a) is a multiple of 2^-149.  The experts' parts are weighted and added in fp32, in the order of a token's experts, and their sum is rounded once.
  * Device-side conditions (bd_poll_status): an Inf or NaN in X or before the second product (BD_ERR_NONFINITE); a plan whose numbers
  * lie outside its bounds (BD_ERR_INDEX; nothing is addressed by them); a wait that ran out (BD_ERR_TIMEOUT: what Y holds then means
  * nothing).  Workspace: 256-byte aligned, of one call at a time, like the plan while the call runs.  After one call per device, shape class

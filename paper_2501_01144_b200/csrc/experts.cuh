@@ -145,9 +145,12 @@ struct Walk {
 };
 
 __device__ __forceinline__ float gated(float g, float u, int gelu) {
-    // act(g) = g / (1 + exp(-a)), a = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (gelu in its tanh form)
+    // act(g) = g / (1 + exp(-a)), a = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (gelu in its tanh form), with e = exp(-|a|) <= 1: the
+    // divisor lies between 1 and 2, where the fast division is within two steps (it gives 0 for divisors above 2^126).  The fast exponential is
+    // off by up to 2 + 1.2 |a| steps, which counts where a < 0; expf costs 2 to 5 % of a call (1500 tokens of 64 experts: 160 -> 168 us).
     const float a = gelu ? 1.5957691216057308f * fmaf(0.044715f * g * g, g, g) : g;
-    return __fdividef(g, 1.0f + __expf(-a)) * u;
+    const float e = __expf(-fabsf(a));
+    return g * __fdividef(a < 0.0f ? e : 1.0f, 1.0f + e) * u;
 }
 
 template <int N>
