@@ -849,9 +849,12 @@ def residual_norm(y, weight, residual=None, bias=None, post_weight=None, post_bi
                   out_n=None, stream=None):
     """(h, n): h = residual + scale * gate * u, u = y or norm(y) * (post_weight + weight_offset) + post_bias; n = norm(h) * (weight +
     weight_offset) + bias, or with quantise a QTensor of it.  y, residual [rows, dim]; gate [rows or 1, dim or 1]; norm: "rms" or
-    "layer".  weight None: n is None; want_h False: h is not stored.  out_h, out_n may be y or residual."""
+    "layer".  weight None: n is None; want_h False: h is not stored.  out_h, out_n may be y or residual.  With quantise out_n is a QTensor of
+    y's shape, and there has to be a row (a QTensor has at least one)."""
     q = None
     if quantise:
+        if out_n is not None and (out_n.rows, out_n.K) != tuple(getattr(y, "shape", ())):
+            raise ValueError(f"out_n must be a QTensor of y's shape, not of [{out_n.rows}, {out_n.K}]")
         q = True if out_n is None else (out_n.codes, out_n.ids, out_n.scales)
     h, n, *operand = (_block or _load_block()).norm(y, weight, residual, bias, post_weight, post_bias, gate, scale, _choice(_NORMS, norm, "norm"), eps, weight_offset, want_h, out_h,
                                                     None if quantise else out_n, q, stream)
