@@ -908,9 +908,11 @@ def import_canonical(codes, ids, scales, stream=None):
 @_on_stream
 def dequantize(q, stream=None):
     """fp32 [rows, K] values of a quantised operand (Sec. 3.3, Fig. 6)."""
-    out = (_block or _load_block()).dequantize(q.codes, q.ids, q.scales, q.rows, q.K, stream)
-    if out is not None:
-        return out
+    block = _block or (_load_block() if os.path.exists(_BLOCK_PATH) else None)   # (the library alone does too, at more host time)
+    if block is not None:
+        out = block.dequantize(q.codes, q.ids, q.scales, q.rows, q.K, stream)
+        if out is not None:
+            return out
     out = torch.empty(q.rows, q.K, dtype=torch.float32, device=q.codes.device)
     cq = q.c_struct()
     _check(load().bd_dequantize(ctypes.byref(cq), ctypes.c_void_p(out.data_ptr()), out.stride(0), _stream(stream)))

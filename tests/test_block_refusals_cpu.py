@@ -19,3 +19,13 @@ def test_a_quantised_norm_refuses_an_operand_of_another_shape(rows, K, monkeypat
     assert not got
     same = binding.QTensor.from_buffers(q.codes, q.ids, q.scales, 4096, 256)
     assert binding.residual_norm(y, torch.ones(256), quantise=True, out_n=same)[1] is same and got == [(q.codes, q.ids, q.scales)]
+
+
+def test_dequantize_needs_the_library_alone(monkeypatch, tmp_path):
+    calls = []
+    monkeypatch.setattr(binding, "_block", None)
+    monkeypatch.setattr(binding, "_BLOCK_PATH", str(tmp_path / "_block.so"))
+    monkeypatch.setattr(binding, "load", lambda: types.SimpleNamespace(bd_dequantize=lambda *a: calls.append(a) or 0))
+    monkeypatch.setattr(binding, "_stream", lambda stream=None: 0)
+    q = binding.QTensor.from_buffers(*(torch.zeros(64, dtype=torch.uint8) for _ in range(3)), 2, 64)
+    assert binding.dequantize(q).shape == (2, 64) and len(calls) == 1
