@@ -488,7 +488,8 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
  * (dim a multiple of 32; the bits that bd_quantize_act would make of the rounded n); with both NULL only h is made.
  * All of one type (fp32, bf16, fp16); row r of an operand at its pointer + r * ld elements, weights and biases contiguous [dim].  gate: element
  * (r, c) at gate + r * gate_row + c * gate_col, gate_col 0 or 1, gate_row any (0: one for all rows).  1 <= dim <= 16384, any alignment
- * and pitch that the type allows (16-byte aligned ones are faster).  h and n may each be y's or residual's memory as a whole, in place. */
+ * and pitch that the type allows (16-byte aligned ones are faster).  Where all are aligned a row's results depend neither on the other rows nor on
+ * whether n is stored or quantised; rows off a boundary add their sums in another order.  h and n may each be y's or residual's memory as a whole, in place. */
 typedef struct {
     const void *y, *residual, *gate, *post_weight, *post_bias, *weight, *bias;
     int64_t ldy, ld_residual, gate_row, gate_col;

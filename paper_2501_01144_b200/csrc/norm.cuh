@@ -137,56 +137,81 @@ __device__ __forceinline__ int place(int e) {
 
 template <int DT, int VPT, bool QUANT, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads, QUANT && DT == BD_BF16 ? 2 : VPT == 4 || QUANT ? 1 : VPT == 2 ? 2 : 3) residual_norm_kernel(const __grid_constant__ Args a) {
-    __shared__ float part[2][kMaxThreads / 32];
+    __shared__ __align__(8) float part[2][64];                    // sums of 32 pieces
     __shared__ SmemTables tab;
     extern __shared__ __align__(16) uint8_t row_buffer[];         // QUANT: [row groups] rows of dim elements
     if (QUANT) load_tables(tab);
     const int rt = a.row_threads, group = threadIdx.x / rt, t = threadIdx.x % rt, lane = threadIdx.x % 32;
-    const int warps = rt / 32, warp0 = group * warps;
+    const int warps = rt / 32;
     const float inv = 1.0f / (float)a.dim;
     int turn = 0;
-    // sum over the row's threads; the two halves of `part` take turns, so one barrier a sum is enough
-    auto row_sum = [&](float v) {
-#pragma unroll
-        for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        if (warps == 1) return v;
-        turn ^= 1;
-        if (lane == 0) part[turn][threadIdx.x / 32] = v;
-        __syncthreads();
-        float s = lane < warps ? part[turn][warp0 + lane] : 0.0f;
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        return s;
-    };
     // OWN: a thread has the 32 neighbours of one block and quantises them from its registers; otherwise the row goes through shared memory first
     constexpr bool OWN = QUANT && VEC && VPT == 4;
+    // Sum over the row of the pieces' sums: a binary tree over the pieces' numbers, lowest bit first, whichever threads have them, so that a row of
+    // aligned operands has the same sums in every layout, stored or quantised, and among any number of rows.  The warps' sums of 32 pieces
+    // meet in `part`, whose two halves take turns, so one barrier a sum is enough.  (Rows that share a CTA have one warp each.)
+    auto row_sum = [&](float (&s)[VPT]) {
+        if (OWN) {                                                // pieces 4 t .. 4 t + 3: eight lanes have 32 of them
+            float v = __fadd_rn(__fadd_rn(s[0], s[VPT > 1 ? 1 : 0]), __fadd_rn(s[VPT > 2 ? 2 : 0], s[VPT > 3 ? 3 : 0]));
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+            if (warps == 1) {
+                v += __shfl_xor_sync(0xffffffffu, v, 8);
+                return v + __shfl_xor_sync(0xffffffffu, v, 16);
+            }
+            turn ^= 1;
+            if (lane % 8 == 0) part[turn][t / 8] = v;
+        } else {                                                  // piece v rt + t: a warp has 32 neighbouring ones
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1)
+#pragma unroll
+                for (int v = 0; v < VPT; v++) s[v] += __shfl_xor_sync(0xffffffffu, s[v], d);
+            if (warps == 1) return VPT == 4 ? (s[0] + s[VPT > 1 ? 1 : 0]) + (s[VPT > 2 ? 2 : 0] + s[VPT > 3 ? 3 : 0]) : VPT == 2 ? s[0] + s[VPT > 1 ? 1 : 0] : s[0];
+            turn ^= 1;
+            if (lane == 0) {
+#pragma unroll
+                for (int v = 0; v < VPT; v++) part[turn][v * warps + t / 32] = s[v];
+            }
+        }
+        __syncthreads();
+        const int sums = OWN ? 4 * warps : VPT * warps;
+        const float2 two = *(const float2 *)&part[turn][2 * lane];
+        float v = (2 * lane < sums ? two.x : 0.0f) + (2 * lane + 1 < sums ? two.y : 0.0f);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        return v;
+    };
     // first element of piece v; the others follow, or are rt apart
     auto elem = [&](int v) { return OWN ? (t * 4 + v) * 8 : VEC ? (v * rt + t) * 8 : v * 8 * rt + t; };
     auto normalise = [&](float (&x)[VPT][8], const uint8_t *w, const uint8_t *b) {
+        // (products that a sum follows are rounded by themselves: no layout's code has them in one operation where another's has two)
+        float s[VPT];
         if (a.layer) {
-            float s = 0.0f;
 #pragma unroll
-            for (int v = 0; v < VPT; v++)
+            for (int v = 0; v < VPT; v++) {
+                s[v] = x[v][0];
 #pragma unroll
-                for (int q = 0; q < 8; q++) s += x[v][q];         // (elements behind the row are zeros)
-            const float mean = row_sum(s) * inv;
+                for (int q = 1; q < 8; q++) s[v] += x[v][q];      // (elements behind the row are zeros)
+            }
+            const float mean = __fmul_rn(row_sum(s), inv);
 #pragma unroll
             for (int v = 0; v < VPT; v++)
 #pragma unroll
                 for (int q = 0; q < 8; q++) x[v][q] = (VEC ? elem(v) : elem(v) + q * rt) < a.dim ? x[v][q] - mean : 0.0f;
         }
-        float s = 0.0f;
 #pragma unroll
-        for (int v = 0; v < VPT; v++)
+        for (int v = 0; v < VPT; v++) {
+            s[v] = 0.0f;
 #pragma unroll
-            for (int q = 0; q < 8; q++) s = fmaf(x[v][q], x[v][q], s);
+            for (int q = 0; q < 8; q++) s[v] = fmaf(x[v][q], x[v][q], s[v]);
+        }
         const float f = rsqrtf(fmaf(row_sum(s), inv, a.eps));
 #pragma unroll
         for (int v = 0; v < VPT; v++) {
             float g[8];
             load8<DT, VEC>(w, elem(v), rt, a.dim, g);
 #pragma unroll
-            for (int q = 0; q < 8; q++) x[v][q] = x[v][q] * f * (g[q] + a.offset);
+            for (int q = 0; q < 8; q++) x[v][q] = __fmul_rn(x[v][q] * f, g[q] + a.offset);
             if (b) {
                 load8<DT, VEC>(b, elem(v), rt, a.dim, g);
 #pragma unroll

@@ -118,3 +118,22 @@ def test_a_quantised_result_needs_a_row():
     with pytest.raises(bd.BdError) as e:
         bd.residual_norm(torch.empty(0, 64, device="cuda"), w, quantise=True)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,dim", [(297, 4096), (700, 96), (2000, 4096), (1000, 1024), (1000, 2080), (20000, 512), (3000, 8192), (1000, 16384)])
+def test_stored_and_quantised_rows_have_the_same_sums(rows, dim, dtype):
+    # any numbers, two norms: the quantised result is that of the stored one, and a row's does not depend on the other rows
+    g = torch.Generator(device="cuda").manual_seed(rows + dim)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    y, residual, w, post, gate, bias = r(rows, dim), r(rows, dim), r(dim), r(dim), r(rows, dim), r(dim)
+    for kw in (dict(post_weight=post, gate=gate), dict(post_weight=post, post_bias=bias, bias=bias, norm="layer", weight_offset=1.0)):
+        h, n = bd.residual_norm(y, w, residual, **kw)
+        h2, q = bd.residual_norm(y, w, residual, quantise=True, **kw)
+        want = bd.quantize_act(n)
+        assert torch.equal(h, h2) and torch.equal(q.codes, want.codes) and torch.equal(q.ids, want.ids) and torch.equal(q.scales, want.scales)
+        for at, to in ((0, 1), (rows // 2, rows // 2 + 3), (rows - 296, rows)):
+            some = {**kw, **({"gate": gate[at:to]} if "gate" in kw else {})}
+            h3, n3 = bd.residual_norm(y[at:to], w, residual[at:to], **some)
+            assert torch.equal(h3, h[at:to]) and torch.equal(n3, n[at:to])
+    bd.poll_status()
