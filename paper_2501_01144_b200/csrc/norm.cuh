@@ -161,17 +161,23 @@ __global__ void __launch_bounds__(kMaxThreads, QUANT && DT == BD_BF16 ? 2 : VPT 
             }
             turn ^= 1;
             if (lane % 8 == 0) part[turn][t / 8] = v;
-        } else {                                                  // piece v rt + t: a warp has 32 neighbouring ones
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1)
-#pragma unroll
-                for (int v = 0; v < VPT; v++) s[v] += __shfl_xor_sync(0xffffffffu, s[v], d);
-            if (warps == 1) return VPT == 4 ? (s[0] + s[VPT > 1 ? 1 : 0]) + (s[VPT > 2 ? 2 : 0] + s[VPT > 3 ? 3 : 0]) : VPT == 2 ? s[0] + s[VPT > 1 ? 1 : 0] : s[0];
-            turn ^= 1;
-            if (lane == 0) {
-#pragma unroll
-                for (int v = 0; v < VPT; v++) part[turn][v * warps + t / 32] = s[v];
+        } else {                                                  // piece v rt + t: a warp has 32 neighbouring ones of each v
+            // (lanes of one bit go on with one v, those of the other bit with the other: in the end lane v has that v's sum)
+            float v = s[0];
+            if (VPT > 1) v = (lane & 1 ? s[VPT > 1 ? 1 : 0] : s[0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? s[0] : s[VPT > 1 ? 1 : 0], 1);
+            if (VPT > 2) {
+                const float hi = (lane & 1 ? s[VPT > 2 ? 3 : 0] : s[VPT > 2 ? 2 : 0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? s[VPT > 2 ? 2 : 0] : s[VPT > 2 ? 3 : 0], 1);
+                v = (lane & 2 ? hi : v) + __shfl_xor_sync(0xffffffffu, lane & 2 ? v : hi, 2);
             }
+#pragma unroll
+            for (int d = VPT; d < 32; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+            if (warps == 1) {
+#pragma unroll
+                for (int d = 1; d < VPT; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+                return v;
+            }
+            turn ^= 1;
+            if (lane < VPT) part[turn][lane * warps + t / 32] = v;
         }
         __syncthreads();
         const int sums = OWN ? 4 * warps : VPT * warps;
