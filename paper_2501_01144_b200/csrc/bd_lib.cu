@@ -1809,7 +1809,7 @@ bd_status bd_expert_mlp(const void *X, bd_dtype xdtype, int64_t tokens, int64_t 
     if ((s = launch_result())) return s;
     // Few rows per expert: items of at most 128 tokens (two accumulators, a fourth decode group); else of 256, so that an expert's weights
     // are expanded once for as many tokens as possible.  Measured, 64 experts, 6 a token, 2048 -> 1408, even loads, us a call, 128 / 256: 24 rows
-    // an expert 86 / 91, 64 98 / 104, 96 113 / 114, 128 135 / 129, 192 186 / 167; 8 experts, 2 a token, 4096 -> 4096: 64 rows 67 / 70, 96 75 / 76, 128 87 / 83.
+    // an expert 88 / 93, 64 102 / 108, 96 118 / 121, 128 142 / 139, 192 196 / 182; 8 experts, 2 a token, 4096 -> 4096: 64 rows 68 / 72, 96 77 / 78, 128 88 / 85.
     const int64_t rows = tokens * plan->top_k, used = std::min(rows, up->experts);
     const bool narrow = rows <= 96 * used;
     const int64_t most = rows / (narrow ? 128 : 256) + used;      // items per 256 weight rows
@@ -1888,7 +1888,7 @@ bd_status bd_residual_norm(const bd_norm *a, bd_dtype dtype, int64_t rows, int64
     // Threads of a row, with one, two or four pieces of eight elements each.  Up to two rows an SM: as many threads as the row has pieces, up
     // to 512 (64 rows of 4096 bf16: 2.7 us, with 256 threads 3.2).  More rows: up to 256 for rows of up to 8 KiB, so that more of them are on
     // their way at once (8192 rows of 4096: 48 us, with 512 threads 54; but 4096 rows of 8192: 53 us, with 512 threads 50); a thread per block where the
-    // result is quantised from registers (8192 rows of 4096: 58 us, through shared memory 68); a warp a row up to 512 elements (30000 rows of
+    // result is quantised from registers (8192 rows of 4096: 56 us, through shared memory 68); a warp a row up to 512 elements (30000 rows of
     // 512: 23 us, with two warps 26).
     const bool many = rows > 2 * 148, own = a->q && vec && many;
     const int most = !many ? 512 : dim <= 512 ? 32 : dim * esz <= 8192 ? 256 : 512;

@@ -18,11 +18,11 @@
 //
 // Bound: few tokens per expert, some 20 us of launches and first k-steps, the weights' bytes (5.9 TB/s with 1/8 of the MMAs and of the
 // expansion) and the part of the expansion that does not hide under them (a tenth); many tokens, the block-scaled MMA at the clock that the
-// power cap leaves.  Whole calls from a graph, us: 30, 104, 148 and 2200 for the cases below.  Measured (B200; first + second product, us, cold):
-//     1 token, 64 experts, 8 a token, 2048 -> 1024          17.5 + 13.5    27.5 MB: latency of 8 and 4 k-steps behind a launch
-//     64 tokens, 128 experts, 8, 2048 -> 1024               63 + 39        434 MB: 4.6 and 3.7 TB/s
-//     1500 tokens, 64 experts, 6, 2048 -> 1408 (f16)        85 + 42        156 GFLOP
-//     8192 tokens, 8 experts, 2, 4096 -> 14336              1461 + 620     5.77 TFLOP: 2.6 and 3.1 PFLOP/s
+// power cap leaves.  Whole calls from a graph, us: 29, 105, 162 and 2280 for the cases below.  Measured (B200; first + second product, us, cold):
+//     1 token, 64 experts, 8 a token, 2048 -> 1024          17.9 + 13.3    27.5 MB: latency of 8 and 4 k-steps behind a launch
+//     64 tokens, 128 experts, 8, 2048 -> 1024               67 + 40        434 MB: 4.3 and 3.6 TB/s
+//     1500 tokens, 64 experts, 6, 2048 -> 1408 (f16)        93 + 51        156 GFLOP
+//     8192 tokens, 8 experts, 2, 4096 -> 14336              1535 + 667     5.77 TFLOP: 2.5 and 2.9 PFLOP/s
 #pragma once
 #include "bd_common.cuh"
 #include "gemm_tc.cuh"

@@ -11,8 +11,8 @@
 // owns a whole block of 32 (rows that such blocks cover with aligned 16-byte accesses), or the row passes through shared memory, where a
 // thread picks up a block.
 // Bound: memory; a row's latency (two to four reductions) where there are few rows.  Measured (B200, from a graph): 8192 x 4096 bf16 with a
-// residual and two norms, both results 48 us (268 MB, 5.6 TB/s; issue slots 74 %), quantised 58 us (the quantiser's instructions); 1001 x 2559 fp32 (two layer norms) 12.8 us
-// (rows of odd length: 4-byte accesses); 3000 x 768 fp16 4.8 us; 64 x 4096 quantised 3.2 us (one row's latency).
+// residual and two norms, both results 48 us (268 MB, 5.6 TB/s), quantised 56 us (the quantiser's instructions); 1001 x 2559 fp32 (two layer norms) 13.0 us
+// (rows of odd length: 4-byte accesses); 3000 x 768 fp16 4.7 us; 64 x 4096 quantised 3.2 us (one row's latency).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -14,7 +14,8 @@
 //
 // Bound: T E logits read and 12 T k bytes written, 9 MB for 8192 x 256 x 8, are a microsecond or two: what counts is the latency of a
 // token's chain of steps, and for many tokens the instructions it takes.  Measured (B200, from a graph, plan and all): 64 of 128 experts 5.5 us
-// (one launch), 64 of 256 with a bias and groups 9.5; 8192 of 256 with a bias and groups 30.5 us, of 512 49; 1001 of 8 6.9 us (three launches).
+// (one launch), 64 of 256 with a bias and groups 9.5; 8192 of 256 with a bias and groups 30.5 us, of 512 49; 8192 of 256 by softmax alone 20.3 us,
+// not renormalised 23.1 (its sum in 64 bits); 1001 of 8 7.0 us (three launches).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
