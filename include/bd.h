@@ -459,7 +459,7 @@ bd_status bd_make_expert_plan(const int32_t *ids, const bd_expert_plan *plan, vo
  * X [tokens, K] and its pitch, Y [tokens, N] (BD_F32 or BD_BF16) and its pitch are 16-byte aligned.  The plan is bd_route's or bd_make_expert_plan's;
  * a token without experts gets zeros.  `inner` (optional, for checking; fp32 [tokens][top_k][inter]) receives the values q(...) that the second
  * product read.  Four launches with the workspace that bd_expert_mlp_workspace_size gives for BD_F32; with that for BD_BF16, the least for such a Y,
- * the second product and the sum are made for half of the columns or more at a time, two launches each time, with the same result.  The launches
+ * the second product and the sum are made for about half of the columns at a time, two launches each time, with the same result.  The launches
  * have no fixed relation to the plan's numbers, which stay on the device: a call can be captured and replayed
  * with other tokens and plans.  The result is the same in every run, and a token's does not depend on the other tokens of the call.
  * Accuracy: the products as BD_GEMM_TCGEN05; act(x) = x / (1 + exp(-a)), a = x or, for gelu, 2 sqrt(2 / pi) (x + 0.044715 x^3), by fast

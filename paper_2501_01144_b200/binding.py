@@ -833,8 +833,8 @@ def expert_plan(ids, experts, out=None, stream=None):
 
 
 def expert_mlp_workspace_size(tokens, top_k, up, down, dtype=torch.bfloat16):
-    """Bytes of a workspace for expert_mlp.  For a bfloat16 result the least there is; with that for float32 (which a call without a given one
-    takes) the second product is made for all columns at once."""
+    """Bytes of a workspace for expert_mlp: with as many the second product is made for all columns at once, for a result of either dtype (a
+    bfloat16 result is also made in less, column by column: bd_expert_mlp in bd.h)."""
     return (_block or _load_block()).mlp_workspace_size(tokens, top_k, up._c, down._c, dtype)
 
 

@@ -644,7 +644,7 @@ bd_status check_experts(const bd_experts *w) {
     return BD_OK;
 }
 // Parts of an expert call's workspace: the token operand (later the experts' parts, fp32), its scales, the inner operand and its scales.  The size for a
-// BD_BF16 result holds the parts of half of the columns, or more, at a time.
+// BD_BF16 result holds the parts of about half of the columns at a time.
 struct ExpertSpace {
     int64_t rows;
     size_t x_scales, h, h_scales, total;

@@ -172,7 +172,8 @@ PyObject *mlp_workspace_size(PyObject *const *a, Py_ssize_t n) {
     need(n, 5);
     at::ScalarType s;
     size_t bytes = 0;
-    check(bd_expert_mlp_workspace_size(integer(a[0]), integer(a[1]), &weights_of(a[2]), &weights_of(a[3]), output_type(a[4], &s), &bytes));
+    output_type(a[4], &s);                                         // (either type: room for the fp32 parts of all columns at once)
+    check(bd_expert_mlp_workspace_size(integer(a[0]), integer(a[1]), &weights_of(a[2]), &weights_of(a[3]), BD_F32, &bytes));
     return PyLong_FromSize_t(bytes);
 }
 

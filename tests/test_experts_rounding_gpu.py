@@ -1,4 +1,6 @@
 """The experts' parts are added up in fp32: a bf16 result is the fp32 one rounded once, whatever the workspace has room for."""
+import ctypes
+
 import pytest
 import torch
 
@@ -23,7 +25,10 @@ def test_a_bf16_result_is_the_fp32_one_rounded_once(tokens, experts, top_k, hidd
     want = bd.expert_mlp(*args, dtype=torch.float32)
     assert torch.equal(bd.expert_mlp(*args), want.bfloat16())
     # the least workspace (fewer columns at a time), its contents of no account, and one between the two sizes
-    least, full = (bd.expert_mlp_workspace_size(tokens, top_k, *args[3:], dtype) for dtype in (torch.bfloat16, torch.float32))
+    n_bytes, full = ctypes.c_size_t(), bd.expert_mlp_workspace_size(tokens, top_k, *args[3:])
+    assert bd.load().bd_expert_mlp_workspace_size(ctypes.c_int64(tokens), ctypes.c_int64(top_k), *(ctypes.c_char_p(w._c) for w in args[3:]), bd.BF16, ctypes.byref(n_bytes)) == 0
+    least = n_bytes.value
+    assert least <= full == bd.expert_mlp_workspace_size(tokens, top_k, *args[3:], torch.float32)
     for size in (least, (least + full) // 2, full):
         ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
         wide = torch.full((tokens, n + 16), 3.0, dtype=torch.bfloat16, device="cuda")
